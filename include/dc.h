@@ -28,6 +28,14 @@
  *   dc_balance_group_advantage, dc_balance_plan_group_advantage
  *                       the calls above that depend on nothing but the lengths and the rewards, issued
  *                       as one and as one or two launches (same results).
+ *   dc_token_logprob, dc_token_logprob_backward
+ *                       the stage behind the transition (actor log-prob, App. B Table 2): log-probabilities of
+ *                       the packed token ids under the head's logits, with entropy and top alternatives, and
+ *                       the gradient of the logits.
+ *   dc_embedding, dc_embedding_backward
+ *                       the rows of the packed token ids, scaled, and the table's gradient.
+ *   dc_adamw_table, dc_adamw
+ *                       the actor's optimizer step over all its tensors in one launch.
  *   dc_repack_noalloc, dc_gather_timed
  *                       dc_repack without a workspace argument, for callers that cannot allocate;
  *                       dc_gather whose dispatch carries the caller's timing events.
@@ -87,6 +95,11 @@ extern "C" {
 #define DC_MAX_FIELDS     8
 #define DC_MAX_SRC_SHARDS 16
 #define DC_MAX_SEQ_LEN    (1 << 24)
+#define DC_MAX_VOCAB      (1 << 24) /* columns of logits, rows of an embedding table   */
+#define DC_MAX_TOP        64        /* alternatives of dc_token_logprob                */
+#define DC_MAX_TENSORS    65536     /* of one dc_adamw                                 */
+#define DC_STATE_BLOCK    256       /* elements that share a scale of an 8-bit state   */
+#define DC_NO_TOKEN       (-1)      /* a place that holds no token (padding)           */
 #define DC_REPACK_NOALLOC_WS_BYTES (8u << 20)   /* the device array dc_repack_noalloc plans in */
 
 typedef enum dc_status {
@@ -99,8 +112,9 @@ typedef enum dc_status {
     DC_ERR_SEQ_EXCEEDS_BUDGET = 6, /* device: a sequence is longer than token_budget             */
     DC_ERR_ZERO_LENGTH_SEQ = 7,    /* device: a sequence length is <= 0 (or > DC_MAX_SEQ_LEN)    */
     DC_ERR_OVERFLOW = 8,           /* device: packed layout does not fit dst_capacity_tokens     */
-    DC_ERR_BAD_LAYOUT = 9          /* device: rollout offsets out of range / overlapping, group
+    DC_ERR_BAD_LAYOUT = 9,         /* device: rollout offsets out of range / overlapping, group
                                       offsets not monotone, perm not a permutation               */
+    DC_ERR_TOKEN_RANGE = 10        /* device: a token id outside the vocabulary                  */
 } dc_status;
 
 typedef struct dc_params {
@@ -365,6 +379,136 @@ size_t dc_scatter_workspace_bytes(const dc_params* prm, const dc_source* src);
 dc_status dc_scatter(const dc_params* prm, const dc_source* src, const int32_t* d_seq_len, const int32_t* d_perm,
                      const dc_field* fields, int32_t n_fields, int64_t dst_capacity_tokens,
                      const int64_t* d_dst_tok_off, void* d_ws, size_t ws_bytes, int32_t* d_status, void* hip_stream);
+
+/* ---- the actor's update on the packed training layout ---- */
+
+/* Number formats.  DC_E4M3: 8 bits as in the OCP format of that name (a sign, 4 bits of exponent, 3 of fraction; no
+ * infinities, largest 448); only the optimizer's states have it. */
+typedef enum dc_type { DC_F32 = 0, DC_BF16 = 1, DC_F16 = 2, DC_E4M3 = 3 } dc_type;
+
+/* A matrix in device memory, rows of n_cols neighbouring elements, row r at element r * row_stride.  d_data is aligned to
+ * the element size; rows that start on multiples of 16 bytes are moved faster.  row_stride may be anything from n_cols up. */
+typedef struct dc_matrix {
+    void*   d_data;
+    int64_t n_rows;
+    int64_t n_cols;
+    int64_t row_stride;     /* elements, >= n_cols                                            */
+    int32_t type;           /* dc_type                                                        */
+    int32_t reserved;       /* must be 0                                                      */
+} dc_matrix;
+
+/*
+ * Log-probabilities of given tokens: what the actor log-prob stage (App. B Table 2) makes of its head's logits.  With
+ * x = row r of logits (vocabulary = n_cols), T = temperature:
+ *   M = max_v x_v,  S = sum_v exp((x_v - M) / T),  log p_v = (x_v - M) / T - log S,
+ *   d_logprob[r] = log p_{d_token[r]},  d_entropy[r] = -sum_v p_v log p_v  (a token of probability 0 adds 0),
+ *   d_row_stat[2r], [2r+1] = M, log S,
+ *   d_top_token / d_top_logprob[r * n_top + i]: the token with the i-th largest x and its log p; ties to the lowest token.
+ * Everything is computed in 32 bits whatever the logits' type.  The logits are read once.
+ * d_mask (uint8 [n_rows], may be NULL: all rows): a row whose byte is 0 is not read; its token may be anything; it gets
+ * +0 in every float output and -1 as every top token.  For the logits of the packed layout, row t of which predicts token
+ * t + 1, pass the arenas of token ids and masks from their second element on, and the output likewise: the first token of
+ * every sequence is a prompt's and masked, so no row reads across a border of sequences.
+ * A row that holds a NaN or +infinity, or nothing above -infinity, has no distribution: NaN in every float output, -1 as
+ * every top token.  -infinity is a logit of probability 0 like any other (such a token's own log p is -infinity).
+ * d_token and d_logprob go together: both NULL if no token is given.  d_row_stat, d_entropy may be NULL.  n_top 0 ..
+ * DC_MAX_TOP and <= vocabulary; d_top_token / d_top_logprob: one of them may be NULL, with n_top = 0 both are not used.
+ * d_ws: 256-byte aligned, dc_token_logprob_workspace_bytes(logits, n_top) bytes (may be 0: then NULL is fine); holds
+ * nothing the caller needs afterwards.
+ * Host errors: INVALID_ARG, UNSUPPORTED_SIZE (vocabulary above DC_MAX_VOCAB, n_top above DC_MAX_TOP), WORKSPACE, HIP.
+ * Device errors: TOKEN_RANGE (a row with a mask byte != 0 and a token outside 0 .. vocabulary - 1: its d_logprob is NaN).
+ */
+size_t dc_token_logprob_workspace_bytes(const dc_matrix* logits, int32_t n_top);
+dc_status dc_token_logprob(const dc_matrix* logits, double temperature, const int32_t* d_token, const uint8_t* d_mask,
+                           int32_t n_top, float* d_logprob, float* d_row_stat, float* d_entropy,
+                           int32_t* d_top_token, float* d_top_logprob, void* d_ws, size_t ws_bytes,
+                           int32_t* d_status, void* hip_stream);
+
+/*
+ * Gradient of the logits from the gradients of the log-probability and of the entropy:
+ *   grad_logits[r, v] = (1/T) * ( a_r * ((v == d_token[r]) - p_v) - b_r * p_v * (log p_v + H_r) ),
+ * a = d_grad_logprob, b = d_grad_entropy (NULL: 0, and d_entropy may then be NULL), H = d_entropy, p from d_row_stat: as
+ * dc_token_logprob left them for the same logits, temperature, tokens and mask.  Computed in 32 bits and rounded once to
+ * grad_logits' type, which is the logits' (same shape, own row_stride).  grad_logits may be the logits' own memory (same
+ * d_data and row_stride): the gradient then takes their place; it must not overlap them otherwise.
+ * A row with mask byte 0, and one whose a and b are both zero, gets +0 everywhere and its logits are not read.
+ * d_token may be NULL: the first term is then -a_r * p_v.
+ * Host errors: INVALID_ARG, UNSUPPORTED_SIZE, HIP.  Device errors: TOKEN_RANGE (the row's gradient is that without the
+ * token's own 1).
+ */
+dc_status dc_token_logprob_backward(const dc_matrix* logits, double temperature, const int32_t* d_token,
+                                    const uint8_t* d_mask, const float* d_row_stat, const float* d_entropy,
+                                    const float* d_grad_logprob, const float* d_grad_entropy,
+                                    const dc_matrix* grad_logits, int32_t* d_status, void* hip_stream);
+
+/*
+ * Embedding of the packed token ids: out[t, :] = scale * weight[d_token[t], :] for the n_rows tokens of out, the product
+ * in 32 bits, rounded once to out's type (any of f32, bf16, f16, whatever the table's).  vocabulary = weight->n_rows.
+ * d_token[t] == DC_NO_TOKEN: a row of +0.
+ * Host errors: INVALID_ARG, UNSUPPORTED_SIZE, HIP.  Device errors: TOKEN_RANGE (that row becomes +0).
+ */
+dc_status dc_embedding(const dc_matrix* weight, const int32_t* d_token, double scale, const dc_matrix* out,
+                       int32_t* d_status, void* hip_stream);
+
+/*
+ * Gradient of the table: grad_weight[v, :] = scale * sum of grad_out[t, :] over the t with d_token[t] == v, sums in 32 bits
+ * in an order that depends on the tokens alone (identical inputs give identical bits), rounded once.  accumulate == 0:
+ * every row of grad_weight is written, those without a token with +0.  accumulate != 0: the sum is added to the row in 32
+ * bits before it is rounded, and rows without a token are not touched.  Tokens equal to DC_NO_TOKEN add nothing.
+ * d_ws: 256-byte aligned, dc_embedding_backward_workspace_bytes(grad_out, grad_weight) bytes; holds nothing the caller
+ * needs afterwards.  Up to 2^24 tokens.
+ * Host errors: INVALID_ARG, UNSUPPORTED_SIZE, WORKSPACE, HIP.  Device errors: TOKEN_RANGE (that token adds nothing).
+ */
+size_t dc_embedding_backward_workspace_bytes(const dc_matrix* grad_out, const dc_matrix* grad_weight);
+dc_status dc_embedding_backward(const dc_matrix* grad_out, const int32_t* d_token, double scale, int32_t accumulate,
+                                const dc_matrix* grad_weight, void* d_ws, size_t ws_bytes,
+                                int32_t* d_status, void* hip_stream);
+
+/* One tensor of the optimizer.  All arrays have n elements, are contiguous and aligned to their element size (16 bytes: the
+ * faster way). */
+typedef struct dc_adamw_tensor {
+    void*       d_param;             /* param_type: f32, bf16, f16; updated                   */
+    float*      d_master;            /* NULL, or the weights in 32 bits: updated, and d_param becomes their rounded copy */
+    const void* d_grad;              /* grad_type: f32, bf16, f16                             */
+    void*       d_exp_avg;           /* state_type: f32 or e4m3                               */
+    void*       d_exp_avg_sq;        /* state_type                                            */
+    float*      d_exp_avg_scale;     /* e4m3: one per DC_STATE_BLOCK elements; f32: NULL      */
+    float*      d_exp_avg_sq_scale;
+    int64_t     n;
+    double      weight_decay;        /* >= 0                                                  */
+    int32_t     param_type, grad_type, state_type;
+    int32_t     reserved;            /* must be 0                                             */
+} dc_adamw_tensor;
+
+typedef struct dc_adamw_params {
+    double  lr, beta1, beta2, eps;   /* lr >= 0, betas in [0, 1), eps > 0                     */
+    int64_t step;                    /* of this call, from 1 (bias correction)                */
+} dc_adamw_params;
+
+/*
+ * AdamW (Loshchilov and Hutter 2019, arXiv 1711.05101, algorithm 2) over all tensors in one launch, per element in 32 bits:
+ *   g = grad * *d_grad_scale (NULL: 1),  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g g,
+ *   w = w (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps).
+ * w is d_master, or d_param where there is none; d_param is w rounded once.
+ * States in 8 bits: per DC_STATE_BLOCK elements (the last block of a tensor may be shorter) a scale s = the block's largest
+ * magnitude / 448 and e4m3 values, nearest, ties to even: m is stored as such, v as its square root (half the range, and
+ * what is divided by).  A root that is not zero is stored as no less than 2^-9 s, so it never becomes zero.  A block whose
+ * s would be below 2^-120 is stored as zeros.  The step itself uses m and v before they are rounded.  All-zero codes and
+ * scales are the states before the first step.
+ * An element whose gradient is not finite gets a parameter that is not; the 8-bit states of its block are then unspecified.
+ *
+ * dc_adamw_table writes what the kernel reads about the tensors into d_table (256-byte aligned, dc_adamw_table_bytes bytes);
+ * call it once, and again when a pointer, a size, a type or a weight decay changes.  dc_adamw takes the same tensors and
+ * the table, in stream order behind it.  A table that was not made for as many tensors and elements is refused on the
+ * device.  The scalars are read at the call: a captured graph keeps them.
+ * Host errors: INVALID_ARG, UNSUPPORTED_SIZE, WORKSPACE (table_bytes too small), HIP.  Device errors: BAD_LAYOUT (not this
+ * table; nothing is updated).
+ */
+size_t dc_adamw_table_bytes(const dc_adamw_tensor* tensors, int32_t n_tensors);
+dc_status dc_adamw_table(const dc_adamw_tensor* tensors, int32_t n_tensors, void* d_table, size_t table_bytes,
+                         void* hip_stream);
+dc_status dc_adamw(const dc_adamw_tensor* tensors, int32_t n_tensors, const dc_adamw_params* prm, const float* d_grad_scale,
+                   const void* d_table, size_t table_bytes, int32_t* d_status, void* hip_stream);
 
 const char* dc_strerror(dc_status code);
 

@@ -20,6 +20,11 @@ DC_MAX_SHARDS = 1024
 DC_MAX_FIELDS = 8
 DC_MAX_SRC_SHARDS = 16
 DC_REPACK_NOALLOC_WS_BYTES = 8 << 20
+DC_MAX_VOCAB = 1 << 24
+DC_MAX_TOP = 64
+DC_MAX_TENSORS = 65536
+DC_STATE_BLOCK = 256
+DC_NO_TOKEN = -1
 
 DC_OK = 0
 DC_ERR_INVALID_ARG = 1
@@ -31,10 +36,16 @@ DC_ERR_SEQ_EXCEEDS_BUDGET = 6
 DC_ERR_ZERO_LENGTH_SEQ = 7
 DC_ERR_OVERFLOW = 8
 DC_ERR_BAD_LAYOUT = 9
+DC_ERR_TOKEN_RANGE = 10
+
+DC_F32, DC_BF16, DC_F16, DC_E4M3 = range(4)
 
 EXPORTS = ("dc_workspace_bytes", "dc_balance", "dc_group_advantage", "dc_plan", "dc_gather",
            "dc_repack", "dc_scatter_workspace_bytes", "dc_scatter", "dc_gae", "dc_balance_group_advantage",
-           "dc_gather_advantage", "dc_balance_workspace_bytes", "dc_balance_ws", "dc_repack_noalloc", "dc_balance_plan_group_advantage", "dc_gather_timed", "dc_strerror")
+           "dc_gather_advantage", "dc_balance_workspace_bytes", "dc_balance_ws", "dc_repack_noalloc", "dc_balance_plan_group_advantage", "dc_gather_timed",
+           "dc_token_logprob_workspace_bytes", "dc_token_logprob", "dc_token_logprob_backward",
+           "dc_embedding", "dc_embedding_backward_workspace_bytes", "dc_embedding_backward",
+           "dc_adamw_table_bytes", "dc_adamw_table", "dc_adamw", "dc_strerror")
 
 
 class dc_params(C.Structure):
@@ -52,6 +63,23 @@ class dc_source(C.Structure):
 class dc_field(C.Structure):
     _fields_ = [("src_base", C.POINTER(C.c_void_p)), ("d_dst", C.c_void_p),
                 ("elem_bytes", C.c_int32), ("reserved", C.c_int32)]
+
+
+class dc_matrix(C.Structure):
+    _fields_ = [("d_data", C.c_void_p), ("n_rows", C.c_int64), ("n_cols", C.c_int64), ("row_stride", C.c_int64),
+                ("type", C.c_int32), ("reserved", C.c_int32)]
+
+
+class dc_adamw_tensor(C.Structure):
+    _fields_ = [("d_param", C.c_void_p), ("d_master", C.c_void_p), ("d_grad", C.c_void_p), ("d_exp_avg", C.c_void_p),
+                ("d_exp_avg_sq", C.c_void_p), ("d_exp_avg_scale", C.c_void_p), ("d_exp_avg_sq_scale", C.c_void_p),
+                ("n", C.c_int64), ("weight_decay", C.c_double), ("param_type", C.c_int32), ("grad_type", C.c_int32),
+                ("state_type", C.c_int32), ("reserved", C.c_int32)]
+
+
+class dc_adamw_params(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("step", C.c_int64)]
 
 
 class DcError(RuntimeError):
@@ -121,6 +149,26 @@ def load() -> C.CDLL:
         lib.dc_balance_plan_group_advantage.argtypes = [C.POINTER(dc_params), C.POINTER(dc_source), vp, vp, vp, vp, vp, vp, vp,
                                                         C.c_int32, C.POINTER(vp), vp, C.POINTER(vp), C.c_int64,
                                                         vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp, vp]
+        mp = C.POINTER(dc_matrix)
+        lib.dc_token_logprob_workspace_bytes.restype = C.c_size_t
+        lib.dc_token_logprob_workspace_bytes.argtypes = [mp, C.c_int32]
+        lib.dc_token_logprob.restype = C.c_int
+        lib.dc_token_logprob.argtypes = [mp, C.c_double, vp, vp, C.c_int32, vp, vp, vp, vp, vp, vp, C.c_size_t, vp, vp]
+        lib.dc_token_logprob_backward.restype = C.c_int
+        lib.dc_token_logprob_backward.argtypes = [mp, C.c_double, vp, vp, vp, vp, vp, vp, mp, vp, vp]
+        lib.dc_embedding.restype = C.c_int
+        lib.dc_embedding.argtypes = [mp, vp, C.c_double, mp, vp, vp]
+        lib.dc_embedding_backward_workspace_bytes.restype = C.c_size_t
+        lib.dc_embedding_backward_workspace_bytes.argtypes = [mp, mp]
+        lib.dc_embedding_backward.restype = C.c_int
+        lib.dc_embedding_backward.argtypes = [mp, vp, C.c_double, C.c_int32, mp, vp, C.c_size_t, vp, vp]
+        tp = C.POINTER(dc_adamw_tensor)
+        lib.dc_adamw_table_bytes.restype = C.c_size_t
+        lib.dc_adamw_table_bytes.argtypes = [tp, C.c_int32]
+        lib.dc_adamw_table.restype = C.c_int
+        lib.dc_adamw_table.argtypes = [tp, C.c_int32, vp, C.c_size_t, vp]
+        lib.dc_adamw.restype = C.c_int
+        lib.dc_adamw.argtypes = [tp, C.c_int32, C.POINTER(dc_adamw_params), vp, vp, C.c_size_t, vp, vp]
         _lib = lib
     return _lib
 
@@ -353,3 +401,140 @@ def dc_balance_plan_group_advantage(prm: dc_params, src: Source, d_seq_len, d_pe
         _ptr(d_shard_tok_off), _ptr(d_shard_mb_off), _ptr(d_mb_seq_off), _ptr(d_cu_seqlens), _ptr(d_n_mb),
         _ptr(d_ws), int(ws_bytes), _ptr(d_status), _stream(stream)),
         "dc_balance_plan_group_advantage")
+
+
+# ---- the actor's update on the packed training layout ----
+
+_types = None
+
+
+def _dc_type(dtype) -> int:
+    global _types
+    if _types is None:
+        import torch
+        _types = {torch.float32: DC_F32, torch.bfloat16: DC_BF16, torch.float16: DC_F16, torch.float8_e4m3fn: DC_E4M3}
+    if dtype not in _types:
+        raise TypeError(f"no dc_type for {dtype}")
+    return _types[dtype]
+
+
+def make_matrix(t) -> dc_matrix:
+    """dc_matrix of a device tensor [rows, columns] whose columns are neighbours; rows may be any distance apart from the
+    number of columns up.  The struct holds the address only: the tensor has to outlive the calls."""
+    if not t.is_cuda:
+        raise TypeError("expected a device tensor")
+    if t.dim() != 2:
+        raise TypeError("expected a tensor of two dimensions")
+    rows, cols = t.shape
+    stride = t.stride(0) if rows > 1 else cols
+    if (cols > 1 and t.stride(1) != 1) or stride < cols:
+        raise TypeError("expected rows of neighbouring elements that do not overlap")
+    return dc_matrix(t.data_ptr() or None, rows, cols, stride, _dc_type(t.dtype), 0)
+
+
+def _vec(x, n: int, dtype: str, what: str) -> Optional[int]:
+    """Device address of a tensor of at least n elements of one type, both checked (an int or None passes through)."""
+    if x is None or isinstance(x, int):
+        return x
+    if str(x.dtype) != dtype:
+        raise TypeError(f"{what}: expected {dtype}, got {x.dtype}")
+    if x.numel() < n:
+        raise ValueError(f"{what}: {x.numel()} elements, {n} are needed")
+    return _ptr(x)
+
+
+_F32, _I32, _U8 = "torch.float32", "torch.int32", "torch.uint8"
+
+
+def dc_token_logprob_workspace_bytes(logits: dc_matrix, n_top: int) -> int:
+    return int(load().dc_token_logprob_workspace_bytes(C.byref(logits), int(n_top)))
+
+
+def dc_token_logprob(logits: dc_matrix, temperature: float, d_token, d_mask, n_top: int, d_logprob, d_row_stat, d_entropy,
+                     d_top_token, d_top_logprob, d_ws, ws_bytes: int, d_status, stream=None) -> None:
+    n, k = logits.n_rows, int(n_top)
+    _check(load().dc_token_logprob(C.byref(logits), float(temperature), _vec(d_token, n, _I32, "d_token"),
+                                   _vec(d_mask, n, _U8, "d_mask"), k, _vec(d_logprob, n, _F32, "d_logprob"),
+                                   _vec(d_row_stat, 2 * n, _F32, "d_row_stat"), _vec(d_entropy, n, _F32, "d_entropy"),
+                                   _vec(d_top_token, n * k, _I32, "d_top_token"),
+                                   _vec(d_top_logprob, n * k, _F32, "d_top_logprob"), _ptr(d_ws), int(ws_bytes),
+                                   _ptr(d_status), _stream(stream)),
+           "dc_token_logprob")
+
+
+def dc_token_logprob_backward(logits: dc_matrix, temperature: float, d_token, d_mask, d_row_stat, d_entropy, d_grad_logprob,
+                              d_grad_entropy, grad_logits: dc_matrix, d_status, stream=None) -> None:
+    n = logits.n_rows
+    _check(load().dc_token_logprob_backward(C.byref(logits), float(temperature), _vec(d_token, n, _I32, "d_token"),
+                                            _vec(d_mask, n, _U8, "d_mask"), _vec(d_row_stat, 2 * n, _F32, "d_row_stat"),
+                                            _vec(d_entropy, n, _F32, "d_entropy"),
+                                            _vec(d_grad_logprob, n, _F32, "d_grad_logprob"),
+                                            _vec(d_grad_entropy, n, _F32, "d_grad_entropy"), C.byref(grad_logits),
+                                            _ptr(d_status), _stream(stream)),
+           "dc_token_logprob_backward")
+
+
+def dc_embedding(weight: dc_matrix, d_token, scale: float, out: dc_matrix, d_status, stream=None) -> None:
+    _check(load().dc_embedding(C.byref(weight), _vec(d_token, out.n_rows, _I32, "d_token"), float(scale),
+                               C.byref(out), _ptr(d_status), _stream(stream)),
+           "dc_embedding")
+
+
+def dc_embedding_backward_workspace_bytes(grad_out: dc_matrix, grad_weight: dc_matrix) -> int:
+    return int(load().dc_embedding_backward_workspace_bytes(C.byref(grad_out), C.byref(grad_weight)))
+
+
+def dc_embedding_backward(grad_out: dc_matrix, d_token, scale: float, accumulate: bool, grad_weight: dc_matrix, d_ws,
+                          ws_bytes: int, d_status, stream=None) -> None:
+    _check(load().dc_embedding_backward(C.byref(grad_out), _vec(d_token, grad_out.n_rows, _I32, "d_token"), float(scale),
+                                        int(bool(accumulate)), C.byref(grad_weight), _ptr(d_ws), int(ws_bytes),
+                                        _ptr(d_status), _stream(stream)),
+           "dc_embedding_backward")
+
+
+class AdamwTensors:
+    """Host array of dc_adamw_tensor, and the tensors it points into.  items: dicts with param, grad, exp_avg, exp_avg_sq
+    and, where there are any, master, exp_avg_scale, exp_avg_sq_scale, weight_decay."""
+
+    _SCALES = ("exp_avg_scale", "exp_avg_sq_scale")
+
+    def __init__(self, items: Sequence[dict]):
+        self._keep = items
+        self.n = len(items)
+        self.array = (dc_adamw_tensor * max(1, self.n))()
+        for i, it in enumerate(items):
+            param, n = it["param"], it["param"].numel()
+            blocks = -(-n // DC_STATE_BLOCK)
+            for name in ("master", "grad", "exp_avg", "exp_avg_sq", *self._SCALES):
+                t = it.get(name)
+                if t is not None and t.numel() != (blocks if name in self._SCALES else n):
+                    raise ValueError(f"tensor {i}: {name} has {t.numel()} elements, param {n}")
+                if t is not None and (name == "master" or name in self._SCALES) and _dc_type(t.dtype) != DC_F32:
+                    raise TypeError(f"tensor {i}: {name} is not float32")
+            if _dc_type(it["exp_avg"].dtype) != _dc_type(it["exp_avg_sq"].dtype):
+                raise TypeError(f"tensor {i}: the two states differ in type")
+            at = lambda name: (_ptr(it[name]) or None) if it.get(name) is not None else None  # noqa: E731
+            self.array[i] = dc_adamw_tensor(
+                at("param"), at("master"), at("grad"), at("exp_avg"), at("exp_avg_sq"), at("exp_avg_scale"),
+                at("exp_avg_sq_scale"), n, float(it.get("weight_decay", 0.0)), _dc_type(param.dtype),
+                _dc_type(it["grad"].dtype), _dc_type(it["exp_avg"].dtype), 0)
+
+
+def make_adamw(lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, step: int = 1) -> dc_adamw_params:
+    return dc_adamw_params(lr, beta1, beta2, eps, step)
+
+
+def dc_adamw_table_bytes(tensors: AdamwTensors) -> int:
+    return int(load().dc_adamw_table_bytes(tensors.array, tensors.n))
+
+
+def dc_adamw_table(tensors: AdamwTensors, d_table, table_bytes: int, stream=None) -> None:
+    _check(load().dc_adamw_table(tensors.array, tensors.n, _ptr(d_table), int(table_bytes), _stream(stream)),
+           "dc_adamw_table")
+
+
+def dc_adamw(tensors: AdamwTensors, prm: dc_adamw_params, d_grad_scale, d_table, table_bytes: int, d_status,
+             stream=None) -> None:
+    _check(load().dc_adamw(tensors.array, tensors.n, C.byref(prm), _vec(d_grad_scale, 1, _F32, "d_grad_scale"),
+                           _ptr(d_table), int(table_bytes), _ptr(d_status), _stream(stream)),
+           "dc_adamw")

@@ -481,6 +481,7 @@ const char* dc_strerror(dc_status code) {
         case DC_ERR_ZERO_LENGTH_SEQ: return "a sequence length is <= 0 or above DC_MAX_SEQ_LEN";
         case DC_ERR_OVERFLOW: return "packed layout exceeds the destination capacity";
         case DC_ERR_BAD_LAYOUT: return "inconsistent index data (offsets, groups or permutation)";
+        case DC_ERR_TOKEN_RANGE: return "a token id outside the vocabulary";
     }
     return "unknown status";
 }
