@@ -132,7 +132,7 @@ size_t dc_embedding_backward_workspace_bytes(const dc_matrix* grad_out, const dc
     if (!grad_out || !grad_weight || grad_out->n_rows < 0 || grad_out->n_rows > EMB_GRAD_MAX_TOKENS || grad_weight->n_rows < 0 ||
         grad_weight->n_rows > DC_MAX_VOCAB || grad_out->n_cols < 0)
         return 0;
-    return embedding_grad_workspace_bytes(grad_out->n_rows, grad_weight->n_rows, grad_out->n_cols);
+    return embedding_grad_workspace_bytes(grad_out->n_rows, grad_out->n_cols);
 }
 
 dc_status dc_embedding_backward(const dc_matrix* grad_out, const int32_t* d_token, double scale, int32_t accumulate,
@@ -145,7 +145,7 @@ dc_status dc_embedding_backward(const dc_matrix* grad_out, const int32_t* d_toke
     if (grad_weight->n_cols != grad_out->n_cols || !std::isfinite((float)scale)) return DC_ERR_INVALID_ARG;
     if (grad_weight->n_rows > DC_MAX_VOCAB || grad_out->n_rows > EMB_GRAD_MAX_TOKENS) return DC_ERR_UNSUPPORTED_SIZE;
     if (grad_out->n_rows > 0 && (!d_token || !aligned_to(d_token, 4))) return DC_ERR_INVALID_ARG;
-    const size_t need = embedding_grad_workspace_bytes(grad_out->n_rows, grad_weight->n_rows, grad_out->n_cols);
+    const size_t need = embedding_grad_workspace_bytes(grad_out->n_rows, grad_out->n_cols);
     if (need > 0 && (!d_ws || !aligned_to(d_ws, 256))) return DC_ERR_INVALID_ARG;
     if (ws_bytes < need) return DC_ERR_WORKSPACE;
     const EmbeddingGradArgs a = {grad_out->d_data, grad_weight->d_data, grad_out->row_stride, grad_weight->row_stride,

@@ -62,7 +62,7 @@ struct EmbeddingGradArgs {
     const int32_t* token;
     int32_t*       status;
 };
-size_t embedding_grad_workspace_bytes(int64_t n_tokens, int64_t vocab, int64_t dim);
+size_t embedding_grad_workspace_bytes(int64_t n_tokens, int64_t dim);
 hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, int32_t g_type, int32_t dw_type, void* d_ws, hipStream_t st);
 
 // The optimizer's table: a header, the tensors, and for every piece of ADAMW_PIECE elements its tensor and its place there.
