@@ -2,7 +2,7 @@
 //
 // The tokens are sorted by id (stable, so the tokens of one id stay in ascending order), and the sorted sequence is cut
 // into chunks of CHUNK entries: a hot id costs as much per token as a rare one, and no float goes through an atomic.
-//   sort_portions   PORTION tokens per workgroup, radix sort in the LDS
+//   sort_portions   1024 to 8192 tokens per workgroup, radix sort in the LDS
 //   merge_runs      up to MERGE_WAYS sorted runs into one: an entry's place is its own plus, for every other run, how many
 //                   entries there come before it (a binary search each); once for every factor of MERGE_WAYS
 //   add_rows        one wave per chunk and 512 columns: sums the rows of the segments (entries of one id) that start in the
@@ -15,13 +15,12 @@
 namespace dc {
 
 constexpr int SORT_THREADS = 1024, SORT_WAVES = SORT_THREADS / WAVE;
-constexpr int PORTION = 4096, PER_THREAD = PORTION / SORT_THREADS;
-constexpr int MERGE_WAYS = 32, MERGE_THREADS = 256;
-constexpr int CHUNK = 64;
+constexpr int MAX_PORTION = 8192, PER_THREAD = MAX_PORTION / SORT_THREADS;
+constexpr int MERGE_WAYS = 32, MERGE_THREADS = 512, MERGE_SAMPLES = 64;
 constexpr int COLS = 512;                        // columns of a wave: eight to a lane
 constexpr int ADD_THREADS = 256;
 constexpr int FILL_ROWS = 8, FILL_LANES = WAVE / FILL_ROWS;      // rows of the table per wave that looks for those without a token
-constexpr int JOIN_THREADS = 256;
+constexpr int JOIN_THREADS = 512;
 
 static inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
@@ -33,7 +32,10 @@ struct EmbGradWs {
     float*    piece;                             // [2 * n_chunks][dim]: of the segment that reaches into the chunk, of the one that leaves it
     size_t    bytes;
 };
+// Entries of a chunk: fewer where there would be too few waves to hide the loads' latency.
+static int chunk_of(int64_t n_tokens, int64_t dim) { return n_tokens * ((dim + COLS - 1) / COLS) < 32768 * 4 ? 16 : 32; }
 static EmbGradWs carve_emb_grad(void* base, int64_t n_tokens, int64_t dim) {
+    const int64_t CHUNK = chunk_of(n_tokens, dim);
     EmbGradWs w;
     char* p = static_cast<char*>(base);
     size_t off = 0;
@@ -54,22 +56,23 @@ size_t embedding_grad_workspace_bytes(int64_t n_tokens, int64_t dim) {
     return carve_emb_grad(nullptr, n_tokens, dim).bytes;
 }
 
-// A portion's tokens by id: least significant digit first, `digit_bits` (at most 8) at a time.  A wave ranks 64 entries by
+// `per` times SORT_THREADS tokens by id: least significant digit first, `digit_bits` (at most 8) at a time.  A wave ranks 64 entries by
 // ballots over the digit's bits; counts are kept per digit and wave, so the order within a digit is that of the tokens.
-__global__ __launch_bounds__(SORT_THREADS) void sort_portions_kernel(const EmbeddingGradArgs a, EmbGradWs w, int digit_bits, int passes) {
-    __shared__ uint32_t keys[PORTION];
-    __shared__ uint16_t places[PORTION];
-    __shared__ uint32_t counts[256 * SORT_WAVES];
+__global__ __launch_bounds__(SORT_THREADS) void sort_portions_kernel(const EmbeddingGradArgs a, EmbGradWs w, int per_thread, int digit_bits, int passes) {
+    __shared__ uint32_t keys[MAX_PORTION];
+    __shared__ uint16_t places[MAX_PORTION];
+    __shared__ uint16_t counts[256 * SORT_WAVES];
     __shared__ uint32_t tmp[SORT_WAVES];
     const int lane = lane_id(), wave = threadIdx.x / WAVE;
-    const int32_t first = blockIdx.x * PORTION;
+    const int32_t portion = per_thread * SORT_THREADS, first = blockIdx.x * portion;
     if (blockIdx.x == 0 && threadIdx.x == 0) *w.n_long = 0;
 
     uint32_t key[PER_THREAD];
     uint16_t place[PER_THREAD];
 #pragma unroll
     for (int j = 0; j < PER_THREAD; ++j) {
-        const int at = wave * (WAVE * PER_THREAD) + j * WAVE + lane;
+        if (j >= per_thread) break;
+        const int at = wave * (WAVE * per_thread) + j * WAVE + lane;
         const int32_t t = first + at;
         key[j] = 0xFFFFFFFFu;                    // behind the last token: last in every pass
         place[j] = (uint16_t)at;
@@ -89,17 +92,21 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_portions_kernel(const Embed
         uint32_t rank[PER_THREAD];
 #pragma unroll
         for (int j = 0; j < PER_THREAD; ++j) {
+            if (j >= per_thread) break;
             const uint32_t d = (key[j] >> shift) & (digits - 1);
-            uint64_t same = ~0ull;
+            uint32_t same_lo = ~0u, same_hi = ~0u;
             for (int b = 0; b < digit_bits; ++b) {
-                const uint64_t set = __ballot((d >> b) & 1);
-                same &= (d >> b) & 1 ? set : ~set;
+                const uint32_t mine = (uint32_t)((int32_t)(d << (31 - b)) >> 31);        // the bit in every place
+                const uint64_t set = __ballot(mine != 0);
+                same_lo &= ~((uint32_t)set ^ mine);
+                same_hi &= ~((uint32_t)(set >> 32) ^ mine);
             }
-            volatile uint32_t* c = &counts[d * SORT_WAVES + wave];        // this wave's own count
+            const uint64_t same = (uint64_t)same_hi << 32 | same_lo;
+            volatile uint16_t* c = &counts[d * SORT_WAVES + wave];        // this wave's own count
             const uint32_t before = *c;
             __builtin_amdgcn_wave_barrier();
             rank[j] = before + (uint32_t)__popcll(same & below);
-            if ((same & below) == 0) *c = before + (uint32_t)__popcll(same);
+            if ((same & below) == 0) *c = (uint16_t)(before + (uint32_t)__popcll(same));
             __builtin_amdgcn_wave_barrier();
         }
         __syncthreads();
@@ -112,12 +119,13 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_portions_kernel(const Embed
         for (uint32_t i = 0; i < per; ++i)
             if (from + i < digits * SORT_WAVES) {
                 const uint32_t c = counts[from + i];
-                counts[from + i] = run;
+                counts[from + i] = (uint16_t)run;
                 run += c;
             }
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < PER_THREAD; ++j) {
+            if (j >= per_thread) break;
             const uint32_t d = (key[j] >> shift) & (digits - 1);
             const uint32_t to = counts[d * SORT_WAVES + wave] + rank[j];
             keys[to] = key[j];
@@ -126,16 +134,18 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_portions_kernel(const Embed
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < PER_THREAD; ++j) {
-            const int at = wave * (WAVE * PER_THREAD) + j * WAVE + lane;
+            if (j >= per_thread) break;
+            const int at = wave * (WAVE * per_thread) + j * WAVE + lane;
             key[j] = keys[at];
             place[j] = places[at];
         }
         __syncthreads();
     }
-    const int32_t n = min(PORTION, a.n_tokens - first);
+    const int32_t n = min(portion, a.n_tokens - first);
 #pragma unroll
     for (int j = 0; j < PER_THREAD; ++j) {
-        const int at = wave * (WAVE * PER_THREAD) + j * WAVE + lane;
+        if (j >= per_thread) break;
+        const int at = wave * (WAVE * per_thread) + j * WAVE + lane;
         if (at < n) {
             w.key[0][first + at] = key[j];
             w.pos[0][first + at] = first + place[j];
@@ -143,45 +153,64 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_portions_kernel(const Embed
     }
 }
 
-// Runs of `run` sorted entries, MERGE_WAYS neighbouring ones into one.  Four lanes share an entry, each with a quarter of the
-// runs: its searches go side by side, one look in each run per step.
-constexpr int MERGE_LANES = 4, MERGE_EACH = MERGE_WAYS / MERGE_LANES, MERGE_ENTRIES = MERGE_THREADS / MERGE_LANES;
+// Runs of `run` sorted entries, MERGE_WAYS neighbouring ones into one.  Four lanes share an entry, each takes every fourth
+// run, MERGE_SIDE searches side by side.  The first steps look at MERGE_SAMPLES entries of every run, which the workgroup has
+// fetched into the LDS at once.  What bounds it is the instructions of the searches: their number is that of the runs times
+// that of the entries, which is why portions are as long as one workgroup sorts well.
+constexpr int MERGE_LANES = 4, MERGE_SIDE = 4, MERGE_ENTRIES = MERGE_THREADS / MERGE_LANES;
 __global__ __launch_bounds__(MERGE_THREADS) void merge_runs_kernel(const EmbeddingGradArgs a, const uint32_t* __restrict__ key_in,
                                                                    const int32_t* __restrict__ pos_in, uint32_t* __restrict__ key_out,
                                                                    int32_t* __restrict__ pos_out, int32_t run) {
+    static_assert(SORT_THREADS % MERGE_SAMPLES == 0 && SORT_THREADS % MERGE_ENTRIES == 0, "a workgroup's entries are of one run");
+    static_assert(MERGE_WAYS % (MERGE_LANES * MERGE_SIDE) == 0, "searches side by side");
+    __shared__ uint32_t samples[MERGE_WAYS * (MERGE_SAMPLES + 1)];         // (a run's apart from the next one's by a bank)
     const int lane = lane_id(), part = lane / (WAVE / MERGE_LANES);
     const int32_t at = blockIdx.x * MERGE_ENTRIES + (threadIdx.x / WAVE) * (WAVE / MERGE_LANES) + lane % (WAVE / MERGE_LANES);
     const int32_t i = min(at, a.n_tokens - 1);
-    const uint32_t key = key_in[i];
-    const int32_t mine = i / run, first = mine / MERGE_WAYS * MERGE_WAYS;
-    int32_t lo[MERGE_EACH], len[MERGE_EACH];
-#pragma unroll
-    for (int j = 0; j < MERGE_EACH; ++j) {
-        const int64_t from = (int64_t)(first + part * MERGE_EACH + j) * run;      // (may lie behind the last run)
-        lo[j] = (int32_t)min(from, (int64_t)a.n_tokens);
-        len[j] = first + part * MERGE_EACH + j == mine ? 0 : min(run, a.n_tokens - lo[j]);
+    const int32_t mine = (int32_t)(blockIdx.x * MERGE_ENTRIES) / run, first = mine / MERGE_WAYS * MERGE_WAYS;
+    const int32_t begin = first * run, rest = a.n_tokens - begin;          // the group's entries: [begin, begin + rest) or fewer
+    const int ways = (int)min((int64_t)MERGE_WAYS, ((int64_t)rest + run - 1) / run);
+    const int32_t window = run / MERGE_SAMPLES;  // a sample is the last entry of its window
+    for (int q = threadIdx.x; q < ways * MERGE_SAMPLES; q += MERGE_THREADS) {
+        const int64_t from = (int64_t)(q + 1) * window - 1;
+        samples[q / MERGE_SAMPLES * (MERGE_SAMPLES + 1) + q % MERGE_SAMPLES] = from < rest ? key_in[begin + from] : 0xFFFFFFFFu;
     }
-    // entries of an earlier run come first among equals: there the first greater one is looked for
+    const uint32_t key = key_in[i];
+    __syncthreads();
     int32_t to = 0;
+    for (int j0 = 0; j0 * MERGE_LANES < ways; j0 += MERGE_SIDE) {
+        int32_t lo[MERGE_SIDE], len[MERGE_SIDE];
+        uint32_t least[MERGE_SIDE];              // entries of an earlier run come first among equals: those below key + 1
 #pragma unroll
-    for (int j = 0; j < MERGE_EACH; ++j) to -= lo[j];
-    for (int32_t step = run; step > 0; step = step > 1 ? (step + 1) >> 1 : 0) {
+        for (int j = 0; j < MERGE_SIDE; ++j) {
+            const int q = (j0 + j) * MERGE_LANES + part;
+            const bool there = q < ways && first + q != mine;
+            least[j] = key + (first + q < mine ? 1 : 0);
+            const uint32_t* run_samples = samples + (q < ways ? q : 0) * (MERGE_SAMPLES + 1);
+            int w = 0;                           // windows that lie before the entry as a whole
 #pragma unroll
-        for (int j = 0; j < MERGE_EACH; ++j) {
-            const int32_t half = (len[j] + 1) >> 1;
-            const uint32_t k = key_in[min(lo[j] + (half > 0 ? half - 1 : 0), a.n_tokens - 1)];
-            const bool less = k < key || (k == key && first + part * MERGE_EACH + j < mine);
-            if (half > 0) {
+            for (int step = MERGE_SAMPLES / 2; step > 0; step >>= 1) w += run_samples[w + step - 1] < least[j] ? step : 0;
+            w += run_samples[w] < least[j] ? 1 : 0;
+            const int64_t from = (int64_t)q * run + (int64_t)w * window, end = min((int64_t)(q + 1) * run, (int64_t)rest);
+            lo[j] = there ? (int32_t)min(from, end) : 0;
+            len[j] = there ? (int32_t)min((int64_t)window, end - lo[j]) : 0;
+            to -= there ? q * run : 0;
+        }
+        for (int32_t step = window; step > 0; step >>= 1) {
+#pragma unroll
+            for (int j = 0; j < MERGE_SIDE; ++j) {
+                const int32_t half = (len[j] + 1) >> 1;
+                const bool less = half > 0 && key_in[begin + lo[j] + (half > 0 ? half - 1 : 0)] < least[j];
                 lo[j] += less ? half : 0;
-                len[j] = less ? len[j] - half : half - 1;
+                len[j] = less ? len[j] - half : max(half - 1, 0);
             }
         }
+#pragma unroll
+        for (int j = 0; j < MERGE_SIDE; ++j) to += lo[j];
     }
 #pragma unroll
-    for (int j = 0; j < MERGE_EACH; ++j) to += lo[j];
-    to += __shfl_xor(to, WAVE / MERGE_LANES);
-    to += __shfl_xor(to, WAVE / MERGE_LANES * 2);
-    to += first * run + (i - mine * run);
+    for (int d = WAVE / MERGE_LANES; d < WAVE; d <<= 1) to += __shfl_xor(to, d);
+    to += begin + (i - mine * run);
     if (at >= a.n_tokens || part != 0) return;
     key_out[to] = key;
     pos_out[to] = pos_in[i];
@@ -238,7 +267,7 @@ __device__ __forceinline__ void write_row(const EmbeddingGradArgs& a, uint32_t i
     store8<VEC>(static_cast<W*>(a.dw) + (int64_t)id * a.dw_stride, slab, a.dim, out);
 }
 
-template <bool VEC, bool ACC, typename G, typename W>
+template <int CHUNK, bool VEC, bool ACC, typename G, typename W>
 __global__ __launch_bounds__(ADD_THREADS) void add_rows_kernel(const EmbeddingGradArgs a, const uint32_t* __restrict__ skey,
                                                                const int32_t* __restrict__ spos,
                                                                int32_t* n_long, int32_t* long_at, float* __restrict__ piece,
@@ -276,41 +305,39 @@ __global__ __launch_bounds__(ADD_THREADS) void add_rows_kernel(const EmbeddingGr
     }
     const int32_t chunk = (int32_t)((uint64_t)unit / (uint32_t)slabs), slab = (int32_t)(unit - (int64_t)chunk * slabs);
     const int32_t c0 = chunk * CHUNK;
-    // the chunk's entries, those behind it that a segment of it may reach, those before it
+    // the chunk's entries and those behind it that a segment of it may reach, and the entries before it
+    static_assert(2 * CHUNK <= WAVE, "a lane for every entry");
     constexpr uint32_t NONE = 0xFFFFFFFFu;       // (an id that no entry has)
+    constexpr uint64_t IN_CHUNK = (1ull << CHUNK) - 1;
     const uint32_t k1 = c0 + lane < a.n_tokens ? skey[c0 + lane] : NONE;
-    const uint32_t k2 = c0 + CHUNK + lane < a.n_tokens ? skey[c0 + CHUNK + lane] : NONE;
-    const uint32_t k0 = c0 > 0 ? skey[c0 - CHUNK + lane] : NONE;
+    const uint32_t k0 = c0 > 0 ? skey[c0 - CHUNK + lane % CHUNK] : NONE;
     const int32_t p1 = c0 + lane < a.n_tokens ? spos[c0 + lane] : 0;
-    const int32_t p2 = c0 + CHUNK + lane < a.n_tokens ? spos[c0 + CHUNK + lane] : 0;
-    const uint32_t vocab = (uint32_t)a.vocab;
-    const uint32_t before = __shfl(k0, CHUNK - 1), up1 = __shfl_up(k1, 1), up2 = __shfl_up(k2, 1), last1 = __shfl(k1, CHUNK - 1);
-    const uint64_t start1 = __ballot(k1 != (lane ? up1 : before)), start2 = __ballot(k2 != (lane ? up2 : last1));
-    const uint64_t valid1 = __ballot(k1 < vocab);
-    if (!valid1) return;
-    const int n_valid = 64 - __builtin_clzll(valid1);                      // valid entries come first
+    const uint32_t before = __shfl(k0, CHUNK - 1), up1 = __shfl_up(k1, 1);
+    const uint64_t start = __ballot(k1 != (lane ? up1 : before));
+    const uint64_t valid = __ballot(k1 < (uint32_t)a.vocab) & IN_CHUNK;
+    if (!valid) return;
+    const int n_valid = 64 - __builtin_clzll(valid);                       // valid entries come first
 
-    // entries [from, to) are this wave's; a bit of `end1` / `end2` where one is the last of its segment
+    // entries [from, to) are this wave's; a bit of `ends` where one is the last of its segment
     int from, to = n_valid;
     bool lead_long = false, tail_long = false;
-    const int first_start = start1 ? __builtin_ctzll(start1) : CHUNK;
+    const int first_start = start & IN_CHUNK ? __builtin_ctzll(start) : CHUNK;
     if (first_start > 0) {                       // a segment reaches into the chunk: another chunk's, unless it is long,
         const int r = min(first_start, n_valid); // that is, has CHUNK entries before its last one here
-        lead_long = r == CHUNK || __builtin_amdgcn_readlane(k0, (r - 1) & 63) == __builtin_amdgcn_readfirstlane(k1);
+        lead_long = __builtin_amdgcn_readlane(k0, r - 1) == __builtin_amdgcn_readfirstlane(k1);
     }
     from = lead_long ? 0 : first_start;
     if (first_start < n_valid && n_valid == CHUNK) {                       // the last segment may go on behind the chunk
-        const int s = 63 - __builtin_clzll(start1);
-        tail_long = __builtin_amdgcn_readlane(k2, s) == __builtin_amdgcn_readlane(k1, s);      // entry s + CHUNK
-        if (!tail_long) to = CHUNK + (start2 ? __builtin_ctzll(start2) : 0);
+        const int s = 63 - __builtin_clzll(start & IN_CHUNK);
+        tail_long = __builtin_amdgcn_readlane(k1, s + CHUNK) == __builtin_amdgcn_readlane(k1, s);
+        if (!tail_long) to = __builtin_ctzll(start & ~IN_CHUNK);           // (there is one up to entry s + CHUNK)
     }
     if (from >= to) return;
-    uint64_t end1 = start1 >> 1, end2 = 0;
-    if (to <= CHUNK) end1 |= 1ull << (to - 1); else end2 = 1ull << (to - 1 - CHUNK);
+    const uint64_t ends = start >> 1 | 1ull << (to - 1);
 
     const G* grad = static_cast<const G*>(a.g);
-    const auto entry_pos = [&](int e) { return e < WAVE ? __builtin_amdgcn_readlane(p1, e) : __builtin_amdgcn_readlane(p2, e - WAVE); };
-    const auto entry_id = [&](int e) { return (uint32_t)(e < WAVE ? __builtin_amdgcn_readlane(k1, e) : __builtin_amdgcn_readlane(k2, e - WAVE)); };
+    const auto entry_pos = [&](int e) { return __builtin_amdgcn_readlane(p1, e); };
+    const auto entry_id = [&](int e) { return (uint32_t)__builtin_amdgcn_readlane(k1, e); };
     Raw8<G> next[AT_ONCE];
     Raw8<W> next_old[ACC ? AT_ONCE : 1];
     const auto ask = [&](int i) {
@@ -339,7 +366,7 @@ __global__ __launch_bounds__(ADD_THREADS) void add_rows_kernel(const EmbeddingGr
             if (e < to) {
 #pragma unroll
                 for (int c = 0; c < 8; ++c) sum[c] += (float)now[j].e[c];
-                if ((e < CHUNK ? end1 >> e : end2 >> (e - CHUNK)) & 1) {
+                if ((ends >> e) & 1) {
                     const bool lead = lead_long && e < first_start, tail = tail_long && e == CHUNK - 1 && !lead;
                     if (lead || tail) {
                         store8<VEC>(piece + ((int64_t)chunk * 2 + tail) * a.dim, slab, a.dim, sum);
@@ -356,11 +383,11 @@ __global__ __launch_bounds__(ADD_THREADS) void add_rows_kernel(const EmbeddingGr
 }
 
 // One workgroup per long segment and 512 columns, round and round; its waves take every fourth piece each.
-template <bool VEC, bool ACC, typename W>
+template <int CHUNK, bool VEC, bool ACC, typename W>
 __global__ __launch_bounds__(JOIN_THREADS) void join_pieces_kernel(const EmbeddingGradArgs a, const uint32_t* __restrict__ skey,
                                                                    const int32_t* __restrict__ n_long, const int32_t* __restrict__ long_at,
                                                                    const float* __restrict__ piece, int32_t chunks, int32_t slabs) {
-    constexpr int WAVES = JOIN_THREADS / WAVE, AT_ONCE = 4;
+    constexpr int WAVES = JOIN_THREADS / WAVE, AT_ONCE = 8;
     __shared__ float part[WAVES][8][WAVE];
     const int lane = lane_id(), wave = threadIdx.x / WAVE;
     const int64_t units = (int64_t)*n_long * slabs;
@@ -408,18 +435,23 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_pieces_kernel(const Embeddi
 hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, int32_t g_type, int32_t dw_type, void* d_ws, hipStream_t st) {
     if (a.vocab == 0 || a.dim == 0 || (a.n_tokens == 0 && a.accumulate)) return hipSuccess;
     EmbGradWs w = carve_emb_grad(d_ws, a.n_tokens, a.dim);
-    const int64_t portions = a.n_tokens > 0 ? ((int64_t)a.n_tokens + PORTION - 1) / PORTION : 1;
+    // short portions keep more workgroups busy, long ones leave the merge fewer runs (one level of it either way up to
+    // 2^18 tokens): 8192 tokens sorted and merged
+    const int per_thread = a.n_tokens <= SORT_THREADS ? 1 : a.n_tokens <= 16384 ? 2 : a.n_tokens <= 65536 ? 4 : 8;
+    const int64_t portion = (int64_t)per_thread * SORT_THREADS;
+    const int64_t portions = a.n_tokens > 0 ? (a.n_tokens + portion - 1) / portion : 1;
     int bits = 1;
     while ((1 << bits) <= a.vocab) ++bits;       // ids up to and with `vocab`
     const int passes = (bits + 7) / 8, digit_bits = (bits + passes - 1) / passes;
-    sort_portions_kernel<<<(unsigned)portions, SORT_THREADS, 0, st>>>(a, w, digit_bits, passes);
+    sort_portions_kernel<<<(unsigned)portions, SORT_THREADS, 0, st>>>(a, w, per_thread, digit_bits, passes);
     int at = 0;
-    for (int64_t run = PORTION; run < a.n_tokens; run *= MERGE_WAYS) {
+    for (int64_t run = portion; run < a.n_tokens; run *= MERGE_WAYS) {
         merge_runs_kernel<<<(unsigned)((a.n_tokens + MERGE_ENTRIES - 1) / MERGE_ENTRIES), MERGE_THREADS, 0, st>>>(
             a, w.key[at], w.pos[at], w.key[at ^ 1], w.pos[at ^ 1], (int32_t)run);
         at ^= 1;
     }
-    const int64_t chunks = ((int64_t)a.n_tokens + CHUNK - 1) / CHUNK, slabs = (a.dim + COLS - 1) / COLS;
+    const int chunk = chunk_of(a.n_tokens, a.dim);
+    const int64_t chunks = ((int64_t)a.n_tokens + chunk - 1) / chunk, slabs = (a.dim + COLS - 1) / COLS;
     const int64_t fill = a.accumulate ? 0 : ((int64_t)a.vocab + FILL_ROWS - 1) / FILL_ROWS;
     const int64_t units = chunks * slabs + fill, blocks = (units + ADD_THREADS / WAVE - 1) / (ADD_THREADS / WAVE);
     if (blocks > 0x7FFFFFFFLL) return hipErrorInvalidValue;
@@ -431,15 +463,20 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, int32_t g_type, int
                 return (reinterpret_cast<uintptr_t>(p) % 16 == 0) && (size_t)stride * size % 16 == 0;
             };
             const bool vec = a.dim % 8 == 0 && aligned(a.g, a.g_stride, sizeof(G)) && aligned(a.dw, a.dw_stride, sizeof(W));
-            const auto go = [&](auto v, auto acc) {
+            const auto launch = [&](auto c, auto v, auto acc) {
+                constexpr int CHUNK = decltype(c)::value;
                 constexpr bool VEC = decltype(v)::value, ACC = decltype(acc)::value;
-                add_rows_kernel<VEC, ACC, G, W><<<(unsigned)blocks, ADD_THREADS, 0, st>>>(
+                add_rows_kernel<CHUNK, VEC, ACC, G, W><<<(unsigned)blocks, ADD_THREADS, 0, st>>>(
                     a, w.key[at], w.pos[at], w.n_long, w.long_at, w.piece, (int32_t)chunks, (int32_t)slabs);
                 if (a.n_tokens > CHUNK) {
                     const int64_t most = (int64_t)a.n_tokens / (CHUNK + 1) * slabs;      // long segments there can be
-                    join_pieces_kernel<VEC, ACC, W><<<(unsigned)(most < 1024 ? most : 1024), JOIN_THREADS, 0, st>>>(
+                    join_pieces_kernel<CHUNK, VEC, ACC, W><<<(unsigned)(most < 1024 ? most : 1024), JOIN_THREADS, 0, st>>>(
                         a, w.key[at], w.n_long, w.long_at, w.piece, (int32_t)chunks, (int32_t)slabs);
                 }
+            };
+            const auto go = [&](auto v, auto acc) {
+                if (chunk == 16) launch(std::integral_constant<int, 16>{}, v, acc);
+                else launch(std::integral_constant<int, 32>{}, v, acc);
             };
             if (vec && a.accumulate) go(std::true_type{}, std::true_type{});
             else if (vec) go(std::true_type{}, std::false_type{});
