@@ -1,79 +1,383 @@
 // Log-probabilities of given tokens with entropy and top alternatives, and the gradient of the logits.
+//
+// One pass over a row, every thread on its own: with k = log2(e) / T a thread keeps M2 = k * (its largest logit), rounded,
+// s = sum 2^(k x - M2) and u = sum 2^(k x - M2) (k x - M2); both are scaled when M2 grows.  k x - M2 is one fused
+// multiply-add, so M2's rounding is no error: whatever M2 is, it is taken off exactly at the end.
+// The n_top largest: a thread also keeps where the 16 bytes with its largest logit begin.  By (largest logit, place) the
+// n_top first threads hold the n_top largest elements among them: an element of any other thread has n_top greater ones.
+// Their logits are read once more (out of the caches), those that are not below the last of the n_top threads' maxima are
+// ranked by counting.
+// Few rows: a row is cut into parts, one workgroup each, and a second launch joins them.
 #include "actor_device.h"
 
 namespace dc {
 
-constexpr int LP_THREADS = 256;
+constexpr int LP_THREADS = 256, LP_WAVES = LP_THREADS / WAVE;
+constexpr int LP_AT_ONCE = 4;                    // 16-byte loads asked for at once
+constexpr int LP_CANDIDATES = 1024;              // of the largest that are ranked in the LDS; more: one by one
+constexpr float LP_FAR = 0x1p120f;               // |k x| from here on: the sums are made again with differences taken first
 
-// One workgroup per row; the row is read once for its maximum, once for the sums, once per alternative.
+template <typename T> constexpr int CHUNK_ELEMS = 16 / sizeof(T);
+
+// 16 bytes of logits as floats.
 template <typename T>
-__global__ __launch_bounds__(LP_THREADS) void logprob_kernel(const LogprobArgs a) {
-    __shared__ float tmp[LP_THREADS / WAVE];
-    __shared__ uint64_t tmp64[LP_THREADS / WAVE];
-    for (int64_t r = blockIdx.x; r < a.n_rows; r += gridDim.x) {
-        if (a.mask && a.mask[r] == 0) {
-            if (threadIdx.x == 0) {
-                if (a.logprob) a.logprob[r] = 0.0f;
-                if (a.entropy) a.entropy[r] = 0.0f;
-                if (a.stat) { a.stat[2 * r] = 0.0f; a.stat[2 * r + 1] = 0.0f; }
-            }
-            for (int i = threadIdx.x; i < a.n_top; i += LP_THREADS) {
-                if (a.top_token) a.top_token[r * a.n_top + i] = -1;
-                if (a.top_logprob) a.top_logprob[r * a.n_top + i] = 0.0f;
-            }
-            continue;
+__device__ __forceinline__ void unpack(u32x4 q, float (&f)[CHUNK_ELEMS<T>]) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(q[i]);
+    } else if constexpr (std::is_same_v<T, __bf16>) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = __uint_as_float(q[i] << 16);
+            f[2 * i + 1] = __uint_as_float(q[i] & 0xFFFF0000u);
         }
-        const T* x = static_cast<const T*>(a.x) + r * a.stride;
-        float m = -INFINITY;
-        for (int v = threadIdx.x; v < a.vocab; v += LP_THREADS) m = fmaxf(m, (float)x[v]);
-        m = block_reduce(m, tmp, wave_max, [](float p, float q) { return fmaxf(p, q); });
-        float s = 0.0f, u = 0.0f;
-        for (int v = threadIdx.x; v < a.vocab; v += LP_THREADS) {
-            const float d = ((float)x[v] - m) * a.inv_t;
-            const float e = __builtin_amdgcn_exp2f(d * LOG2E);
-            s += e;
-            u += e * fmaxf(d, -1e4f);               // e is 0 long before: -infinity adds 0, not a NaN
-        }
-        const auto add = [](float p, float q) { return p + q; };
-        s = block_reduce(s, tmp, wave_sum, add);
-        u = block_reduce(u, tmp, wave_sum, add);
-        const bool good = s >= 1.0f;                // (the maximum alone adds 1; NaN, +infinity, nothing finite: a NaN)
-        const float log_sum = good ? logf(s) : NAN;
-        if (threadIdx.x == 0) {
-            if (a.token) {
-                const int32_t t = a.token[r];
-                const bool in = t >= 0 && t < a.vocab;
-                if (!in) set_status(a.status, DC_ERR_TOKEN_RANGE);
-                a.logprob[r] = in ? ((float)x[t] - m) * a.inv_t - log_sum : NAN;
-            }
-            if (a.entropy) a.entropy[r] = log_sum - u / s;
-            if (a.stat) { a.stat[2 * r] = good ? m : NAN; a.stat[2 * r + 1] = log_sum; }
-        }
-        uint64_t below = ~0ull;
-        for (int i = 0; i < a.n_top; ++i) {
-            uint64_t best = 0;
-            for (int v = threadIdx.x; v < a.vocab; v += LP_THREADS) {
-                const uint64_t key = ((uint64_t)sortable((float)x[v]) << 32) | (uint32_t)~v;
-                if (key < below && key > best) best = key;
-            }
-            best = block_reduce(best, tmp64, wave_max_u64, [](uint64_t p, uint64_t q) { return p > q ? p : q; });
-            if (threadIdx.x == 0) {
-                if (a.top_token) a.top_token[r * a.n_top + i] = good ? (int32_t)~(uint32_t)best : -1;
-                if (a.top_logprob) a.top_logprob[r * a.n_top + i] = (unsortable((uint32_t)(best >> 32)) - m) * a.inv_t - log_sum;
-            }
-            below = best;
-        }
+    } else {
+        typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+        const h8 h = __builtin_bit_cast(h8, q);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = (float)h[i];
     }
 }
 
-size_t logprob_workspace_bytes(int64_t, int32_t, int32_t, int32_t) { return 0; }
+// What a row comes down to: its largest logit, S = sum exp((x - M)/T), U = sum exp((x - M)/T) * (x - M)/T * log2(e).
+struct RowSums { float m, s, u; };
 
-hipError_t launch_logprob(const LogprobArgs& a, int32_t type, void*, hipStream_t st) {
+struct RowResult { float m, inv_t, log_sum, entropy; bool good; };
+__device__ __forceinline__ RowResult finish(const RowSums& r, float inv_t) {
+    // the largest logit alone adds 1; a NaN, +infinity or nothing above -infinity makes the sum a NaN or 0
+    const bool good = r.s >= 0.5f && r.s < INFINITY;
+    RowResult w = {good ? r.m : NAN, inv_t, good ? logf(r.s) : NAN, 0.0f, good};
+    w.entropy = w.log_sum - r.u / r.s * LN2;
+    return w;
+}
+__device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t r, const RowResult& w, bool in, float x_token) {
+    if (a.logprob) a.logprob[r] = in ? (x_token - w.m) * w.inv_t - w.log_sum : NAN;
+    if (a.entropy) a.entropy[r] = w.good ? w.entropy : NAN;
+    if (a.stat) { a.stat[2 * r] = w.m; a.stat[2 * r + 1] = w.log_sum; }
+}
+__device__ __forceinline__ void write_top(const LogprobArgs& a, int64_t r, int i, const RowResult& w, uint64_t key) {
+    if (a.top_token) a.top_token[r * a.n_top + i] = w.good ? (int32_t)~(uint32_t)key : -1;
+    if (a.top_logprob) a.top_logprob[r * a.n_top + i] = w.good ? (unsortable((uint32_t)(key >> 32)) - w.m) * w.inv_t - w.log_sum : NAN;
+}
+// A masked row.  Every thread of the workgroup comes here.
+__device__ __forceinline__ void write_nothing(const LogprobArgs& a, int64_t r) {
+    if (threadIdx.x == 0) {
+        if (a.logprob) a.logprob[r] = 0.0f;
+        if (a.entropy) a.entropy[r] = 0.0f;
+        if (a.stat) { a.stat[2 * r] = 0.0f; a.stat[2 * r + 1] = 0.0f; }
+    }
+    for (int i = threadIdx.x; i < a.n_top; i += LP_THREADS) {
+        if (a.top_token) a.top_token[r * a.n_top + i] = -1;
+        if (a.top_logprob) a.top_logprob[r * a.n_top + i] = 0.0f;
+    }
+}
+
+// A logit and its place as one number: greater for a larger logit, and among equal ones for the lower place.
+__device__ __forceinline__ uint64_t top_key(float x, int32_t place) { return (uint64_t)sortable(x) << 32 | (uint32_t)~place; }
+
+struct TopLds {
+    uint64_t head[LP_THREADS];                   // keys of the threads (or parts)
+    uint64_t candidate[LP_CANDIDATES];
+    uint64_t tmp[LP_WAVES];
+    uint64_t least;
+    int32_t  chosen[DC_MAX_TOP];
+    uint32_t n_candidates, n_heads;
+};
+
+// Every thread's head key (0: none) against the others': the n_top first go into chosen, least is the last one's (1 where
+// there are fewer than n_top).  Returns how many were chosen.
+__device__ __forceinline__ int choose_heads(TopLds& t, uint64_t key, int n_top) {
+    t.head[threadIdx.x] = key;
+    if (threadIdx.x == 0) { t.least = 1; t.n_candidates = 0; t.n_heads = 0; }
+    __syncthreads();
+    int rank = 0;
+#pragma unroll 16
+    for (int i = 0; i < LP_THREADS; ++i) rank += t.head[i] > key ? 1 : 0;
+    if (key != 0) {
+        if (rank < n_top) {
+            t.chosen[rank] = (int32_t)threadIdx.x;
+            atomicAdd(&t.n_heads, 1u);
+        }
+        if (rank == n_top - 1) t.least = key;
+    }
+    __syncthreads();
+    return (int)t.n_heads;
+}
+__device__ __forceinline__ void add_candidate(TopLds& t, uint64_t key) {
+    const uint32_t at = atomicAdd(&t.n_candidates, 1u);
+    if (at < LP_CANDIDATES) t.candidate[at] = key;
+}
+// The n_top greatest keys, in order, to put(i, key); all keys differ.  all(visit) hands every key there is to visit: used
+// where there are more candidates than the LDS takes, once for every place in the list.
+template <typename All, typename Put>
+__device__ __forceinline__ void rank_candidates(TopLds& t, int n_top, All all, Put put) {
+    __syncthreads();
+    const int n = (int)t.n_candidates;
+    if (n <= LP_CANDIDATES) {
+        for (int i = threadIdx.x; i < n; i += LP_THREADS) {
+            const uint64_t key = t.candidate[i];
+            int rank = 0;
+            for (int j = 0; j < n; ++j) rank += t.candidate[j] > key ? 1 : 0;
+            if (rank < n_top) put(rank, key);
+        }
+        for (int i = n + threadIdx.x; i < n_top; i += LP_THREADS) put(i, 0ull);
+    } else {
+        uint64_t below = ~0ull;
+        for (int i = 0; i < n_top; ++i) {
+            uint64_t best = 0;
+            all([&](uint64_t key) { if (key < below && key > best) best = key; });
+            best = block_reduce(best, t.tmp, wave_max_u64, [](uint64_t p, uint64_t q) { return p > q ? p : q; });
+            if (threadIdx.x == 0) put(i, best);
+            below = best;
+        }
+    }
+    __syncthreads();                             // the LDS is free again
+}
+
+// What a part leaves for the join: its sums, then n_top keys, greatest first (0: the part has no more elements).
+struct PartHead { RowSums sums; float pad; };
+static __host__ __device__ size_t part_bytes(int n_top) { return sizeof(PartHead) + (size_t)n_top * sizeof(uint64_t); }
+
+template <typename T, bool ENTROPY, bool TOP>
+__global__ __launch_bounds__(LP_THREADS) void logprob_kernel(const LogprobArgs a, int32_t parts, int32_t per_part, char* ws) {
+    constexpr int N = CHUNK_ELEMS<T>;
+    __shared__ float red[3][LP_WAVES];
+    __shared__ __attribute__((aligned(16))) char top_lds[TOP ? sizeof(TopLds) : 16];
+    TopLds& top = *reinterpret_cast<TopLds*>(top_lds);
+    const float k = a.inv_t * LOG2E;
+    const int tid = threadIdx.x;
+    for (int64_t unit = blockIdx.x; unit < a.n_rows * parts; unit += gridDim.x) {
+        const int64_t r = unit / parts;
+        const int32_t part = (int32_t)(unit - r * parts);
+        if (a.mask && a.mask[r] == 0) {
+            if (parts == 1) write_nothing(a, r);
+            continue;
+        }
+        const T* row = static_cast<const T*>(a.x) + r * a.stride;
+        // the given token's logit is asked for before everything else
+        const int32_t token = parts == 1 && a.token ? a.token[r] : 0;
+        const bool in = token >= 0 && token < a.vocab;
+        const float x_token = parts == 1 && a.token ? (float)row[in ? token : 0] : 0.0f;
+
+        const int32_t v0 = part * per_part, n = min(per_part, a.vocab - v0);
+        const T* x = row + v0;
+        // up to the first multiple of 16 bytes and behind the last one: an element to a thread
+        const int32_t head = min(n, (int32_t)((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / (int32_t)sizeof(T));
+        const int32_t chunks = (n - head) / N, tail = n - head - chunks * N, tail_at = head + chunks * N;
+        const u32x4* body = reinterpret_cast<const u32x4*>(x + head);
+
+        float m = -INFINITY, m2 = -LP_FAR, s = 0.0f, u = 0.0f;
+        int32_t at = -1;                         // TOP: where the 16 bytes with the first largest logit begin
+        const auto scale_to = [&](float new_m) {
+            m = new_m;
+            const float new_m2 = fmaxf(m * k, -LP_FAR), d = m2 - new_m2, f = __builtin_amdgcn_exp2f(d);
+            if constexpr (ENTROPY) u = f * (u + d * s);
+            s *= f;
+            m2 = new_m2;
+        };
+        const auto one = [&](float v, int32_t place) {
+            if (TOP && (v > m || at < 0)) at = place;
+            if (v > m) scale_to(v);
+            const float d = fmaf(v, k, -m2), e = __builtin_amdgcn_exp2f(d);
+            s += e;
+            if constexpr (ENTROPY) u += e * fmaxf(d, -1e4f);               // (a logit of -infinity adds 0, not a NaN)
+        };
+        u32x4 next[LP_AT_ONCE];
+        const auto ask = [&](int32_t c) {
+#pragma unroll
+            for (int j = 0; j < LP_AT_ONCE; ++j) next[j] = __builtin_nontemporal_load(body + min(c + j * LP_THREADS, chunks - 1));
+        };
+        if (tid < chunks) ask(tid);
+        if (tid < head) one((float)x[tid], v0 + tid);
+        for (int32_t c = tid; c < chunks; c += LP_AT_ONCE * LP_THREADS) {
+            float f[LP_AT_ONCE][N], most[LP_AT_ONCE];
+#pragma unroll
+            for (int j = 0; j < LP_AT_ONCE; ++j) {
+                unpack<T>(next[j], f[j]);
+                if (c + j * LP_THREADS >= chunks)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) f[j][i] = -INFINITY;
+                most[j] = f[j][0];
+#pragma unroll
+                for (int i = 1; i < N; ++i) most[j] = fmaxf(most[j], f[j][i]);
+            }
+            if (c + LP_AT_ONCE * LP_THREADS < chunks) ask(c + LP_AT_ONCE * LP_THREADS);
+            float all = most[0];
+#pragma unroll
+            for (int j = 1; j < LP_AT_ONCE; ++j) all = fmaxf(all, most[j]);
+            if constexpr (TOP) {
+                int32_t first = c;
+#pragma unroll
+                for (int j = LP_AT_ONCE - 1; j > 0; --j) first = most[j] == all ? c + j * LP_THREADS : first;
+                first = most[0] == all ? c : first;
+                if (all > m || at < 0) at = v0 + head + first * N;
+            }
+            if (all > m) scale_to(all);
+#pragma unroll
+            for (int j = 0; j < LP_AT_ONCE; ++j) {
+                float sj = 0.0f, uj = 0.0f;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const float d = fmaf(f[j][i], k, -m2), e = __builtin_amdgcn_exp2f(d);
+                    sj += e;
+                    if constexpr (ENTROPY) uj = fmaf(e, fmaxf(d, -1e4f), uj);
+                }
+                s += sj;
+                if constexpr (ENTROPY) u += uj;
+            }
+        }
+        if (tid < tail) one((float)x[tail_at + tid], v0 + tail_at + tid);
+
+        // the workgroup's: sums relative to the largest logit itself
+        RowSums sums;
+        {
+            const float wm = wave_max(m);
+            if (lane_id() == 0) red[0][tid / WAVE] = wm;
+            __syncthreads();
+            sums.m = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
+            static_assert(LP_WAVES == 4, "four waves");
+            // (nothing above -infinity: sums of 0)
+            const float d = sums.m > -INFINITY ? fmaxf(fmaf(-sums.m, k, m2), -1e4f) : 0.0f, f = __builtin_amdgcn_exp2f(d);
+            float ws_ = wave_sum(f * s), wu = ENTROPY ? wave_sum(f * (u + d * s)) : 0.0f;
+            if (fabsf(sums.m * k) >= LP_FAR && fabsf(sums.m) < INFINITY) {           // (the same in every thread)
+                s = u = 0.0f;
+                for (int32_t v = tid; v < n; v += LP_THREADS) {
+                    const float dv = ((float)x[v] - sums.m) * k, e = __builtin_amdgcn_exp2f(dv);
+                    s += e;
+                    if constexpr (ENTROPY) u += e * fmaxf(dv, -1e4f);
+                }
+                ws_ = wave_sum(s);
+                wu = ENTROPY ? wave_sum(u) : 0.0f;
+            }
+            if (lane_id() == 0) { red[1][tid / WAVE] = ws_; red[2][tid / WAVE] = wu; }
+            __syncthreads();
+            sums.s = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
+            sums.u = (red[2][0] + red[2][1]) + (red[2][2] + red[2][3]);
+        }
+        const RowResult w = finish(sums, a.inv_t);
+        char* mine = ws + unit * part_bytes(a.n_top);
+        if (tid == 0) {
+            if (parts == 1) {
+                if (!in) set_status(a.status, DC_ERR_TOKEN_RANGE);
+                write_row(a, r, w, in, x_token);
+            } else {
+                reinterpret_cast<PartHead*>(mine)->sums = sums;
+            }
+        }
+        if constexpr (TOP) {
+            const auto put = [&](int i, uint64_t key) {
+                if (parts == 1) write_top(a, r, i, w, key);
+                else reinterpret_cast<uint64_t*>(mine + sizeof(PartHead))[i] = key;
+            };
+            const int chosen = choose_heads(top, at < 0 ? 0ull : top_key(m, at), a.n_top);
+            const uint64_t least = top.least, me = top.head[tid];
+            // (a NaN's row has no list; what is ranked for it stays inside the row all the same)
+            if (me >= least) {
+                if (tid < head && top_key((float)x[tid], v0 + tid) >= least) add_candidate(top, top_key((float)x[tid], v0 + tid));
+                if (tid < tail && top_key((float)x[tail_at + tid], v0 + tail_at + tid) >= least)
+                    add_candidate(top, top_key((float)x[tail_at + tid], v0 + tail_at + tid));
+            }
+            const int32_t turns = (chunks + LP_THREADS - 1) / LP_THREADS;
+            for (int32_t q = tid; q < chosen * turns; q += LP_THREADS) {
+                const int32_t c = q / chosen * LP_THREADS + top.chosen[q % chosen];
+                if (c >= chunks) continue;
+                float f[N];
+                unpack<T>(body[c], f);
+                const int32_t place = v0 + head + c * N;
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    if (top_key(f[i], place) >= least) add_candidate(top, top_key(f[i], place + i));
+            }
+            rank_candidates(top, a.n_top, [&](auto visit) {
+                for (int32_t v = tid; v < n; v += LP_THREADS) visit(top_key((float)x[v], v0 + v));
+            }, put);
+        }
+        __syncthreads();                         // red is free again
+    }
+}
+
+// One workgroup per row: its parts' sums and lists as one.
+template <typename T>
+__global__ __launch_bounds__(LP_THREADS) void logprob_join_kernel(const LogprobArgs a, int32_t parts, const char* ws) {
+    __shared__ float red[LP_WAVES];
+    __shared__ TopLds top;
+    const float k = a.inv_t * LOG2E;
+    for (int64_t r = blockIdx.x; r < a.n_rows; r += gridDim.x) {
+        if (a.mask && a.mask[r] == 0) {
+            write_nothing(a, r);
+            continue;
+        }
+        const int32_t token = a.token ? a.token[r] : 0;
+        const bool in = token >= 0 && token < a.vocab;
+        const float x_token = a.token ? (float)(static_cast<const T*>(a.x) + r * a.stride)[in ? token : 0] : 0.0f;
+        const size_t bytes = part_bytes(a.n_top);
+        const char* first = ws + r * parts * bytes;
+        const auto sums_of = [&](int p) { return reinterpret_cast<const PartHead*>(first + p * bytes)->sums; };
+        const auto keys_of = [&](int p) { return reinterpret_cast<const uint64_t*>(first + p * bytes + sizeof(PartHead)); };
+        RowSums all = {-INFINITY, 0.0f, 0.0f};
+        for (int p = threadIdx.x; p < parts; p += LP_THREADS) all.m = fmaxf(all.m, sums_of(p).m);
+        all.m = block_reduce(all.m, red, wave_max, [](float p, float q) { return fmaxf(p, q); });
+        for (int p = threadIdx.x; p < parts; p += LP_THREADS) {
+            const RowSums x = sums_of(p);
+            const float d = (x.m - all.m) * k, f = __builtin_amdgcn_exp2f(d);
+            all.s += f * x.s;
+            all.u += f * (x.u + fmaxf(d, -1e4f) * x.s);
+        }
+        const auto add = [](float p, float q) { return p + q; };
+        all.s = block_reduce(all.s, red, wave_sum, add);
+        all.u = block_reduce(all.u, red, wave_sum, add);
+        const RowResult w = finish(all, a.inv_t);
+        if (threadIdx.x == 0) {
+            if (!in) set_status(a.status, DC_ERR_TOKEN_RANGE);
+            write_row(a, r, w, in, x_token);
+        }
+        if (a.n_top == 0) continue;
+        // as many parts as places at least: an element below the n_top greatest of the parts' first ones has no place
+        const bool heads = parts >= a.n_top && parts <= LP_THREADS;
+        choose_heads(top, heads && (int)threadIdx.x < parts ? keys_of(threadIdx.x)[0] : 0ull, a.n_top);
+        const uint64_t least = top.least;
+        for (int q = threadIdx.x; q < parts * a.n_top; q += LP_THREADS) {
+            const uint64_t key = keys_of(q / a.n_top)[q % a.n_top];
+            if (key >= least) add_candidate(top, key);
+        }
+        rank_candidates(top, a.n_top, [&](auto visit) {
+            for (int q = threadIdx.x; q < parts * a.n_top; q += LP_THREADS) visit(keys_of(q / a.n_top)[q % a.n_top]);
+        }, [&](int i, uint64_t key) { write_top(a, r, i, w, key); });
+    }
+}
+
+// How a row is cut: into parts of at least LP_LEAST logits, so that there are about LP_GROUPS workgroups.
+constexpr int64_t LP_GROUPS = 1024, LP_LEAST = 4096;
+struct Cut { int32_t parts, per_part; };
+static Cut cut_of(int64_t n_rows, int32_t vocab) {
+    int64_t parts = n_rows > 0 ? (LP_GROUPS + n_rows - 1) / n_rows : 1;
+    const int64_t most = (vocab + LP_LEAST - 1) / LP_LEAST;
+    parts = parts < most ? parts : most;
+    const int32_t per = (int32_t)(((vocab + parts - 1) / parts + 63) / 64 * 64);
+    return Cut{(vocab + per - 1) / per, per};
+}
+
+size_t logprob_workspace_bytes(int64_t n_rows, int32_t vocab, int32_t, int32_t n_top) {
+    const Cut c = cut_of(n_rows, vocab);
+    return c.parts > 1 ? (size_t)n_rows * c.parts * part_bytes(n_top) : 0;
+}
+
+hipError_t launch_logprob(const LogprobArgs& a, int32_t type, void* d_ws, hipStream_t st) {
     if (a.n_rows == 0) return hipSuccess;
-    const unsigned grid = (unsigned)(a.n_rows < (1 << 20) ? a.n_rows : 1 << 20);
+    const Cut c = cut_of(a.n_rows, a.vocab);
+    const int64_t units = a.n_rows * c.parts;
+    const unsigned grid = (unsigned)(units < (1 << 20) ? units : 1 << 20), rows = (unsigned)(a.n_rows < (1 << 20) ? a.n_rows : 1 << 20);
     return with_type(type, [&](auto e) {
         using T = typename decltype(e)::type;
-        logprob_kernel<T><<<grid, LP_THREADS, 0, st>>>(a);
+        char* ws = static_cast<char*>(d_ws);
+        const auto go = [&](auto entropy, auto top) {
+            logprob_kernel<T, decltype(entropy)::value, decltype(top)::value><<<grid, LP_THREADS, 0, st>>>(a, c.parts, c.per_part, ws);
+        };
+        if (a.entropy && a.n_top) go(std::true_type{}, std::true_type{});
+        else if (a.entropy) go(std::true_type{}, std::false_type{});
+        else if (a.n_top) go(std::false_type{}, std::true_type{});
+        else go(std::false_type{}, std::false_type{});
+        if (c.parts > 1) logprob_join_kernel<T><<<rows, LP_THREADS, 0, st>>>(a, c.parts, ws);
         return hipGetLastError();
     });
 }
