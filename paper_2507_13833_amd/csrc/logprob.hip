@@ -76,32 +76,42 @@ __device__ __forceinline__ void write_nothing(const LogprobArgs& a, int64_t r) {
 __device__ __forceinline__ uint64_t top_key(float x, int32_t place) { return (uint64_t)sortable(x) << 32 | (uint32_t)~place; }
 
 struct TopLds {
-    uint64_t head[LP_THREADS];                   // keys of the threads (or parts)
     uint64_t candidate[LP_CANDIDATES];
     uint64_t tmp[LP_WAVES];
-    uint64_t least;
-    int32_t  chosen[DC_MAX_TOP];
-    uint32_t n_candidates, n_heads;
+    int32_t  chosen[LP_THREADS];
+    uint32_t n_candidates, n_chosen;
 };
 
-// Every thread's head key (0: none) against the others': the n_top first go into chosen, least is the last one's (1 where
-// there are fewer than n_top).  Returns how many were chosen.
-__device__ __forceinline__ int choose_heads(TopLds& t, uint64_t key, int n_top) {
-    t.head[threadIdx.x] = key;
-    if (threadIdx.x == 0) { t.least = 1; t.n_candidates = 0; t.n_heads = 0; }
-    __syncthreads();
-    int rank = 0;
-#pragma unroll 16
-    for (int i = 0; i < LP_THREADS; ++i) rank += t.head[i] > key ? 1 : 0;
-    if (key != 0) {
-        if (rank < n_top) {
-            t.chosen[rank] = (int32_t)threadIdx.x;
-            atomicAdd(&t.n_heads, 1u);
-        }
-        if (rank == n_top - 1) t.least = key;
+// The n-th greatest of a wave's keys, 0 where there are fewer (0 is no key; all others differ): bit by bit from the top, as
+// long as n of them are no smaller.  The lower half, the place, counts among equal logits alone.
+__device__ __forceinline__ uint64_t wave_nth_key(uint64_t key, int n) {
+    const uint32_t value = (uint32_t)(key >> 32), place = (uint32_t)key;
+    uint32_t v = 0;
+    for (int b = 31; b >= 0; --b) {
+        const uint32_t t = v | 1u << b;
+        if (__popcll(__ballot(value >= t)) >= n) v = t;
     }
+    if (v == 0) return 0;
+    const int left = n - __popcll(__ballot(value > v));      // so many of those with this logit
+    if (__popcll(__ballot(value == v)) == left) return (uint64_t)v << 32;
+    uint32_t p = 0;
+    for (int b = 31; b >= 0; --b) {
+        const uint32_t t = p | 1u << b;
+        if (__popcll(__ballot(value == v && place >= t)) >= left) p = t;
+    }
+    return (uint64_t)v << 32 | p;
+}
+// A key that n of the workgroup's keys are not below, n of one wave alone: no smaller than the n-th greatest of any wave.
+// 0 where no wave has as many.  Every thread gets it; the candidates and the chosen are none.
+__device__ __forceinline__ uint64_t least_key(TopLds& t, uint64_t key, int n) {
+    const uint64_t mine = wave_nth_key(key, n);
+    if (lane_id() == 0) t.tmp[threadIdx.x / WAVE] = mine;
+    if (threadIdx.x == 0) { t.n_candidates = 0; t.n_chosen = 0; }
     __syncthreads();
-    return (int)t.n_heads;
+    uint64_t least = t.tmp[0];
+#pragma unroll
+    for (int w = 1; w < LP_WAVES; ++w) least = t.tmp[w] > least ? t.tmp[w] : least;
+    return least;
 }
 __device__ __forceinline__ void add_candidate(TopLds& t, uint64_t key) {
     const uint32_t at = atomicAdd(&t.n_candidates, 1u);
@@ -117,6 +127,7 @@ __device__ __forceinline__ void rank_candidates(TopLds& t, int n_top, All all, P
         for (int i = threadIdx.x; i < n; i += LP_THREADS) {
             const uint64_t key = t.candidate[i];
             int rank = 0;
+#pragma unroll 8
             for (int j = 0; j < n; ++j) rank += t.candidate[j] > key ? 1 : 0;
             if (rank < n_top) put(rank, key);
         }
@@ -269,14 +280,16 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_kernel(const LogprobArgs a
                 if (parts == 1) write_top(a, r, i, w, key);
                 else reinterpret_cast<uint64_t*>(mine + sizeof(PartHead))[i] = key;
             };
-            const int chosen = choose_heads(top, at < 0 ? 0ull : top_key(m, at), a.n_top);
-            const uint64_t least = top.least, me = top.head[tid];
+            const uint64_t me = at < 0 ? 0ull : top_key(m, at), least = least_key(top, me, a.n_top);
             // (a NaN's row has no list; what is ranked for it stays inside the row all the same)
-            if (me >= least) {
+            if (me != 0 && me >= least) {
+                top.chosen[atomicAdd(&top.n_chosen, 1u)] = tid;
                 if (tid < head && top_key((float)x[tid], v0 + tid) >= least) add_candidate(top, top_key((float)x[tid], v0 + tid));
                 if (tid < tail && top_key((float)x[tail_at + tid], v0 + tail_at + tid) >= least)
                     add_candidate(top, top_key((float)x[tail_at + tid], v0 + tail_at + tid));
             }
+            __syncthreads();
+            const int32_t chosen = (int32_t)top.n_chosen;
             const int32_t turns = (chunks + LP_THREADS - 1) / LP_THREADS;
             for (int32_t q = tid; q < chosen * turns; q += LP_THREADS) {
                 const int32_t c = q / chosen * LP_THREADS + top.chosen[q % chosen];
@@ -332,13 +345,12 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_join_kernel(const LogprobA
             write_row(a, r, w, in, x_token);
         }
         if (a.n_top == 0) continue;
-        // as many parts as places at least: an element below the n_top greatest of the parts' first ones has no place
-        const bool heads = parts >= a.n_top && parts <= LP_THREADS;
-        choose_heads(top, heads && (int)threadIdx.x < parts ? keys_of(threadIdx.x)[0] : 0ull, a.n_top);
-        const uint64_t least = top.least;
+        // every part's nth key has nth keys of that part that are not below it: so many parts together have n_top
+        const int nth = min(a.n_top, (2 * a.n_top + parts - 1) / parts), of_parts = (a.n_top + nth - 1) / nth;
+        const uint64_t least = least_key(top, (int)threadIdx.x < parts ? keys_of(threadIdx.x)[nth - 1] : 0ull, of_parts);
         for (int q = threadIdx.x; q < parts * a.n_top; q += LP_THREADS) {
             const uint64_t key = keys_of(q / a.n_top)[q % a.n_top];
-            if (key >= least) add_candidate(top, key);
+            if (key != 0 && key >= least) add_candidate(top, key);
         }
         rank_candidates(top, a.n_top, [&](auto visit) {
             for (int q = threadIdx.x; q < parts * a.n_top; q += LP_THREADS) visit(keys_of(q / a.n_top)[q % a.n_top]);
