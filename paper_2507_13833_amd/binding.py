@@ -8,6 +8,7 @@ no CPU fallback: if ``libdc.so`` has not been built, loading raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -405,17 +406,23 @@ def dc_balance_plan_group_advantage(prm: dc_params, src: Source, d_seq_len, d_pe
 
 # ---- the actor's update on the packed training layout ----
 
-_types = None
+@functools.lru_cache(maxsize=None)
+def _dtypes() -> dict:
+    import torch
+    return {name: getattr(torch, name) for name in ("float32", "bfloat16", "float16", "float8_e4m3fn", "int32", "uint8")}
+
+
+@functools.lru_cache(maxsize=None)
+def _types() -> dict:
+    d = _dtypes()
+    return {d["float32"]: DC_F32, d["bfloat16"]: DC_BF16, d["float16"]: DC_F16, d["float8_e4m3fn"]: DC_E4M3}
 
 
 def _dc_type(dtype) -> int:
-    global _types
-    if _types is None:
-        import torch
-        _types = {torch.float32: DC_F32, torch.bfloat16: DC_BF16, torch.float16: DC_F16, torch.float8_e4m3fn: DC_E4M3}
-    if dtype not in _types:
-        raise TypeError(f"no dc_type for {dtype}")
-    return _types[dtype]
+    try:
+        return _types()[dtype]
+    except KeyError:
+        raise TypeError(f"no dc_type for {dtype}") from None
 
 
 def make_matrix(t) -> dc_matrix:
@@ -426,8 +433,10 @@ def make_matrix(t) -> dc_matrix:
     if t.dim() != 2:
         raise TypeError("expected a tensor of two dimensions")
     rows, cols = t.shape
-    stride = t.stride(0) if rows > 1 else cols
-    if (cols > 1 and t.stride(1) != 1) or stride < cols:
+    stride, step = t.stride()
+    if rows <= 1:
+        stride = cols
+    if (step != 1 and cols > 1) or stride < cols:
         raise TypeError("expected rows of neighbouring elements that do not overlap")
     return dc_matrix(t.data_ptr() or None, rows, cols, stride, _dc_type(t.dtype), 0)
 
@@ -436,14 +445,17 @@ def _vec(x, n: int, dtype: str, what: str) -> Optional[int]:
     """Device address of a tensor of at least n elements of one type, both checked (an int or None passes through)."""
     if x is None or isinstance(x, int):
         return x
-    if str(x.dtype) != dtype:
+    # (one test where all is well: a call of the smallest sizes takes as long on the host as on the device)
+    if x.is_cuda and x.dtype is _dtypes()[dtype] and x.is_contiguous() and x.numel() >= n:
+        return x.data_ptr()
+    if x.dtype is not _dtypes()[dtype]:
         raise TypeError(f"{what}: expected {dtype}, got {x.dtype}")
     if x.numel() < n:
         raise ValueError(f"{what}: {x.numel()} elements, {n} are needed")
     return _ptr(x)
 
 
-_F32, _I32, _U8 = "torch.float32", "torch.int32", "torch.uint8"
+_F32, _I32, _U8 = "float32", "int32", "uint8"
 
 
 def dc_token_logprob_workspace_bytes(logits: dc_matrix, n_top: int) -> int:

@@ -3,16 +3,15 @@
 // One pass over a row, every thread on its own: with k = log2(e) / T a thread keeps M2 = k * (its largest logit), rounded,
 // s = sum 2^(k x - M2) and u = sum 2^(k x - M2) (k x - M2); both are scaled when M2 grows.  k x - M2 is one fused
 // multiply-add, so M2's rounding is no error: whatever M2 is, it is taken off exactly at the end.
-// The n_top largest: a thread also keeps where the 16 bytes with its largest logit begin.  By (largest logit, place) the
-// n_top first threads hold the n_top largest elements among them: an element of any other thread has n_top greater ones.
-// Their logits are read once more (out of the caches), those that are not below the last of the n_top threads' maxima are
-// ranked by counting.
-// Few rows: a row is cut into parts, one workgroup each, and a second launch joins them.
+// The n_top largest: a thread also keeps where the 16 bytes with its largest logit begin.  An
+// element below the n_top-th greatest of these (logit, place) has no place among the n_top largest.  The threads whose own
+// is not below a bound on it read their logits once more (out of the caches); what is not below it is ranked by counting.
+// A workgroup takes a row; few rows get larger workgroups, and long ones are cut into parts that a second launch joins.
 #include "actor_device.h"
 
 namespace dc {
 
-constexpr int LP_THREADS = 256, LP_WAVES = LP_THREADS / WAVE;
+constexpr int LP_THREADS = 256, LP_WIDE = 1024;  // of a workgroup: where there are many rows, where there are few
 constexpr int LP_AT_ONCE = 4;                    // 16-byte loads asked for at once
 constexpr int LP_CANDIDATES = 1024;              // of the largest that are ranked in the LDS; more: one by one
 constexpr float LP_FAR = 0x1p120f;               // |k x| from here on: the sums are made again with differences taken first
@@ -66,7 +65,7 @@ __device__ __forceinline__ void write_nothing(const LogprobArgs& a, int64_t r) {
         if (a.entropy) a.entropy[r] = 0.0f;
         if (a.stat) { a.stat[2 * r] = 0.0f; a.stat[2 * r + 1] = 0.0f; }
     }
-    for (int i = threadIdx.x; i < a.n_top; i += LP_THREADS) {
+    for (int i = threadIdx.x; i < a.n_top; i += blockDim.x) {
         if (a.top_token) a.top_token[r * a.n_top + i] = -1;
         if (a.top_logprob) a.top_logprob[r * a.n_top + i] = 0.0f;
     }
@@ -75,63 +74,71 @@ __device__ __forceinline__ void write_nothing(const LogprobArgs& a, int64_t r) {
 // A logit and its place as one number: greater for a larger logit, and among equal ones for the lower place.
 __device__ __forceinline__ uint64_t top_key(float x, int32_t place) { return (uint64_t)sortable(x) << 32 | (uint32_t)~place; }
 
+template <int THREADS>
 struct TopLds {
+    static constexpr int WAVES = THREADS / WAVE;
     uint64_t candidate[LP_CANDIDATES];
-    uint64_t tmp[LP_WAVES];
-    int32_t  chosen[LP_THREADS];
+    uint64_t tmp[WAVES];
+    int32_t  chosen[THREADS];
     uint32_t n_candidates, n_chosen;
 };
 
-// The n-th greatest of a wave's keys, 0 where there are fewer (0 is no key; all others differ): bit by bit from the top, as
-// long as n of them are no smaller.  The lower half, the place, counts among equal logits alone.
-__device__ __forceinline__ uint64_t wave_nth_key(uint64_t key, int n) {
-    const uint32_t value = (uint32_t)(key >> 32), place = (uint32_t)key;
+// The largest v of `bits` bits that n lanes' numbers are no smaller than; `in`: the lanes that count.  0 where there are fewer.
+__device__ __forceinline__ uint32_t wave_nth(uint32_t number, uint64_t in, int bits, int n) {
     uint32_t v = 0;
-    for (int b = 31; b >= 0; --b) {
+    for (int b = bits - 1; b >= 0; --b) {
         const uint32_t t = v | 1u << b;
-        if (__popcll(__ballot(value >= t)) >= n) v = t;
+        if (__popcll(__ballot(number >= t) & in) >= n) v = t;
     }
-    if (v == 0) return 0;
-    const int left = n - __popcll(__ballot(value > v));      // so many of those with this logit
-    if (__popcll(__ballot(value == v)) == left) return (uint64_t)v << 32;
-    uint32_t p = 0;
-    for (int b = 31; b >= 0; --b) {
-        const uint32_t t = p | 1u << b;
-        if (__popcll(__ballot(value == v && place >= t)) >= left) p = t;
-    }
-    return (uint64_t)v << 32 | p;
+    return v;
 }
-// A key that n of the workgroup's keys are not below, n of one wave alone: no smaller than the n-th greatest of any wave.
-// 0 where no wave has as many.  Every thread gets it; the candidates and the chosen are none.
-__device__ __forceinline__ uint64_t least_key(TopLds& t, uint64_t key, int n) {
-    const uint64_t mine = wave_nth_key(key, n);
+// The n-th greatest of a wave's keys, 0 where there are fewer (0 is no key; all others differ).  The place counts among
+// equal logits alone.  BITS: of a logit as a sortable number that tell logits of its type apart.
+template <typename T> constexpr int SORT_BITS = std::is_same_v<T, __bf16> ? 16 : std::is_same_v<T, _Float16> ? 20 : 32;
+template <int BITS>
+__device__ __forceinline__ uint64_t wave_nth_key(uint64_t key, int n) {
+    const uint32_t value = (uint32_t)(key >> 32) >> (32 - BITS), place = (uint32_t)key;
+    const uint32_t v = wave_nth(value, ~0ull, BITS, n);
+    if (v == 0) return 0;
+    const uint64_t same = __ballot(value == v);
+    const int left = n - __popcll(__ballot(value > v));      // so many of those with this logit
+    const uint64_t least = (uint64_t)v << (64 - BITS);
+    if (__popcll(same) == left) return least;
+    static_assert(DC_MAX_VOCAB <= 1 << 24, "the upper 8 bits of ~place are set");
+    return least | 0xFF000000u | wave_nth(place & 0xFFFFFFu, same, 24, left);
+}
+// A key that n of the workgroup's keys are not below, near the n-th greatest: every wave's nth key has nth keys that are not
+// below it, so many waves together have n.  0 where there are fewer.  Every thread gets it; the candidates and the chosen are none.
+template <int BITS, int THREADS>
+__device__ __forceinline__ uint64_t least_key(TopLds<THREADS>& t, uint64_t key, int n) {
+    constexpr int WAVES = THREADS / WAVE;
+    const int nth = min(n, (2 * n + WAVES - 1) / WAVES), of_waves = (n + nth - 1) / nth;
+    const uint64_t mine = wave_nth_key<BITS>(key, nth);
     if (lane_id() == 0) t.tmp[threadIdx.x / WAVE] = mine;
     if (threadIdx.x == 0) { t.n_candidates = 0; t.n_chosen = 0; }
     __syncthreads();
-    uint64_t least = t.tmp[0];
-#pragma unroll
-    for (int w = 1; w < LP_WAVES; ++w) least = t.tmp[w] > least ? t.tmp[w] : least;
-    return least;
+    return wave_nth_key<BITS>(lane_id() < WAVES ? t.tmp[lane_id()] : 0ull, of_waves);
 }
-__device__ __forceinline__ void add_candidate(TopLds& t, uint64_t key) {
+template <int THREADS>
+__device__ __forceinline__ void add_candidate(TopLds<THREADS>& t, uint64_t key) {
     const uint32_t at = atomicAdd(&t.n_candidates, 1u);
     if (at < LP_CANDIDATES) t.candidate[at] = key;
 }
 // The n_top greatest keys, in order, to put(i, key); all keys differ.  all(visit) hands every key there is to visit: used
 // where there are more candidates than the LDS takes, once for every place in the list.
-template <typename All, typename Put>
-__device__ __forceinline__ void rank_candidates(TopLds& t, int n_top, All all, Put put) {
+template <int THREADS, typename All, typename Put>
+__device__ __forceinline__ void rank_candidates(TopLds<THREADS>& t, int n_top, All all, Put put) {
     __syncthreads();
     const int n = (int)t.n_candidates;
     if (n <= LP_CANDIDATES) {
-        for (int i = threadIdx.x; i < n; i += LP_THREADS) {
+        for (int i = threadIdx.x; i < n; i += THREADS) {
             const uint64_t key = t.candidate[i];
             int rank = 0;
 #pragma unroll 8
             for (int j = 0; j < n; ++j) rank += t.candidate[j] > key ? 1 : 0;
             if (rank < n_top) put(rank, key);
         }
-        for (int i = n + threadIdx.x; i < n_top; i += LP_THREADS) put(i, 0ull);
+        for (int i = n + threadIdx.x; i < n_top; i += THREADS) put(i, 0ull);
     } else {
         uint64_t below = ~0ull;
         for (int i = 0; i < n_top; ++i) {
@@ -149,12 +156,12 @@ __device__ __forceinline__ void rank_candidates(TopLds& t, int n_top, All all, P
 struct PartHead { RowSums sums; float pad; };
 static __host__ __device__ size_t part_bytes(int n_top) { return sizeof(PartHead) + (size_t)n_top * sizeof(uint64_t); }
 
-template <typename T, bool ENTROPY, bool TOP>
-__global__ __launch_bounds__(LP_THREADS) void logprob_kernel(const LogprobArgs a, int32_t parts, int32_t per_part, char* ws) {
-    constexpr int N = CHUNK_ELEMS<T>;
-    __shared__ float red[3][LP_WAVES];
-    __shared__ __attribute__((aligned(16))) char top_lds[TOP ? sizeof(TopLds) : 16];
-    TopLds& top = *reinterpret_cast<TopLds*>(top_lds);
+template <int THREADS, typename T, bool ENTROPY, bool TOP>
+__global__ __launch_bounds__(THREADS) void logprob_kernel(const LogprobArgs a, int32_t parts, int32_t per_part, char* ws) {
+    constexpr int N = CHUNK_ELEMS<T>, WAVES = THREADS / WAVE;
+    __shared__ float red[3][WAVES];
+    __shared__ __attribute__((aligned(16))) char top_lds[TOP ? sizeof(TopLds<THREADS>) : 16];
+    TopLds<THREADS>& top = *reinterpret_cast<TopLds<THREADS>*>(top_lds);
     const float k = a.inv_t * LOG2E;
     const int tid = threadIdx.x;
     for (int64_t unit = blockIdx.x; unit < a.n_rows * parts; unit += gridDim.x) {
@@ -196,30 +203,30 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_kernel(const LogprobArgs a
         u32x4 next[LP_AT_ONCE];
         const auto ask = [&](int32_t c) {
 #pragma unroll
-            for (int j = 0; j < LP_AT_ONCE; ++j) next[j] = __builtin_nontemporal_load(body + min(c + j * LP_THREADS, chunks - 1));
+            for (int j = 0; j < LP_AT_ONCE; ++j) next[j] = __builtin_nontemporal_load(body + min(c + j * THREADS, chunks - 1));
         };
         if (tid < chunks) ask(tid);
         if (tid < head) one((float)x[tid], v0 + tid);
-        for (int32_t c = tid; c < chunks; c += LP_AT_ONCE * LP_THREADS) {
+        for (int32_t c = tid; c < chunks; c += LP_AT_ONCE * THREADS) {
             float f[LP_AT_ONCE][N], most[LP_AT_ONCE];
 #pragma unroll
             for (int j = 0; j < LP_AT_ONCE; ++j) {
                 unpack<T>(next[j], f[j]);
-                if (c + j * LP_THREADS >= chunks)
+                if (c + j * THREADS >= chunks)
 #pragma unroll
                     for (int i = 0; i < N; ++i) f[j][i] = -INFINITY;
                 most[j] = f[j][0];
 #pragma unroll
                 for (int i = 1; i < N; ++i) most[j] = fmaxf(most[j], f[j][i]);
             }
-            if (c + LP_AT_ONCE * LP_THREADS < chunks) ask(c + LP_AT_ONCE * LP_THREADS);
+            if (c + LP_AT_ONCE * THREADS < chunks) ask(c + LP_AT_ONCE * THREADS);
             float all = most[0];
 #pragma unroll
             for (int j = 1; j < LP_AT_ONCE; ++j) all = fmaxf(all, most[j]);
             if constexpr (TOP) {
                 int32_t first = c;
 #pragma unroll
-                for (int j = LP_AT_ONCE - 1; j > 0; --j) first = most[j] == all ? c + j * LP_THREADS : first;
+                for (int j = LP_AT_ONCE - 1; j > 0; --j) first = most[j] == all ? c + j * THREADS : first;
                 first = most[0] == all ? c : first;
                 if (all > m || at < 0) at = v0 + head + first * N;
             }
@@ -245,14 +252,15 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_kernel(const LogprobArgs a
             const float wm = wave_max(m);
             if (lane_id() == 0) red[0][tid / WAVE] = wm;
             __syncthreads();
-            sums.m = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
-            static_assert(LP_WAVES == 4, "four waves");
+            sums.m = red[0][0];
+#pragma unroll
+            for (int i = 1; i < WAVES; ++i) sums.m = fmaxf(sums.m, red[0][i]);
             // (nothing above -infinity: sums of 0)
             const float d = sums.m > -INFINITY ? fmaxf(fmaf(-sums.m, k, m2), -1e4f) : 0.0f, f = __builtin_amdgcn_exp2f(d);
             float ws_ = wave_sum(f * s), wu = ENTROPY ? wave_sum(f * (u + d * s)) : 0.0f;
             if (fabsf(sums.m * k) >= LP_FAR && fabsf(sums.m) < INFINITY) {           // (the same in every thread)
                 s = u = 0.0f;
-                for (int32_t v = tid; v < n; v += LP_THREADS) {
+                for (int32_t v = tid; v < n; v += THREADS) {
                     const float dv = ((float)x[v] - sums.m) * k, e = __builtin_amdgcn_exp2f(dv);
                     s += e;
                     if constexpr (ENTROPY) u += e * fmaxf(dv, -1e4f);
@@ -262,8 +270,10 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_kernel(const LogprobArgs a
             }
             if (lane_id() == 0) { red[1][tid / WAVE] = ws_; red[2][tid / WAVE] = wu; }
             __syncthreads();
-            sums.s = (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]);
-            sums.u = (red[2][0] + red[2][1]) + (red[2][2] + red[2][3]);
+            sums.s = red[1][0];
+            sums.u = red[2][0];
+#pragma unroll
+            for (int i = 1; i < WAVES; ++i) { sums.s += red[1][i]; sums.u += red[2][i]; }
         }
         const RowResult w = finish(sums, a.inv_t);
         char* mine = ws + unit * part_bytes(a.n_top);
@@ -280,7 +290,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_kernel(const LogprobArgs a
                 if (parts == 1) write_top(a, r, i, w, key);
                 else reinterpret_cast<uint64_t*>(mine + sizeof(PartHead))[i] = key;
             };
-            const uint64_t me = at < 0 ? 0ull : top_key(m, at), least = least_key(top, me, a.n_top);
+            const uint64_t me = at < 0 ? 0ull : top_key(m, at), least = least_key<SORT_BITS<T>>(top, me, a.n_top);
             // (a NaN's row has no list; what is ranked for it stays inside the row all the same)
             if (me != 0 && me >= least) {
                 top.chosen[atomicAdd(&top.n_chosen, 1u)] = tid;
@@ -290,9 +300,9 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_kernel(const LogprobArgs a
             }
             __syncthreads();
             const int32_t chosen = (int32_t)top.n_chosen;
-            const int32_t turns = (chunks + LP_THREADS - 1) / LP_THREADS;
-            for (int32_t q = tid; q < chosen * turns; q += LP_THREADS) {
-                const int32_t c = q / chosen * LP_THREADS + top.chosen[q % chosen];
+            const int32_t turns = (chunks + THREADS - 1) / THREADS;
+            for (int32_t q = tid; q < chosen * turns; q += THREADS) {
+                const int32_t c = q / chosen * THREADS + top.chosen[q % chosen];
                 if (c >= chunks) continue;
                 float f[N];
                 unpack<T>(body[c], f);
@@ -302,7 +312,7 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_kernel(const LogprobArgs a
                     if (top_key(f[i], place) >= least) add_candidate(top, top_key(f[i], place + i));
             }
             rank_candidates(top, a.n_top, [&](auto visit) {
-                for (int32_t v = tid; v < n; v += LP_THREADS) visit(top_key((float)x[v], v0 + v));
+                for (int32_t v = tid; v < n; v += THREADS) visit(top_key((float)x[v], v0 + v));
             }, put);
         }
         __syncthreads();                         // red is free again
@@ -312,8 +322,8 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_kernel(const LogprobArgs a
 // One workgroup per row: its parts' sums and lists as one.
 template <typename T>
 __global__ __launch_bounds__(LP_THREADS) void logprob_join_kernel(const LogprobArgs a, int32_t parts, const char* ws) {
-    __shared__ float red[LP_WAVES];
-    __shared__ TopLds top;
+    __shared__ float red[LP_THREADS / WAVE];
+    __shared__ TopLds<LP_THREADS> top;
     const float k = a.inv_t * LOG2E;
     for (int64_t r = blockIdx.x; r < a.n_rows; r += gridDim.x) {
         if (a.mask && a.mask[r] == 0) {
@@ -346,8 +356,11 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_join_kernel(const LogprobA
         }
         if (a.n_top == 0) continue;
         // every part's nth key has nth keys of that part that are not below it: so many parts together have n_top
-        const int nth = min(a.n_top, (2 * a.n_top + parts - 1) / parts), of_parts = (a.n_top + nth - 1) / nth;
-        const uint64_t least = least_key(top, (int)threadIdx.x < parts ? keys_of(threadIdx.x)[nth - 1] : 0ull, of_parts);
+        const int nth = min(a.n_top, (2 * a.n_top + parts - 1) / min(parts, WAVE)), of_parts = (a.n_top + nth - 1) / nth;
+        // (of the first parts: a wave's worth of them, so that one wave's answer will do)
+        const uint64_t least = wave_nth_key<SORT_BITS<T>>(lane_id() < parts ? keys_of(lane_id())[nth - 1] : 0ull, of_parts);
+        if (threadIdx.x == 0) { top.n_candidates = 0; }
+        __syncthreads();
         for (int q = threadIdx.x; q < parts * a.n_top; q += LP_THREADS) {
             const uint64_t key = keys_of(q / a.n_top)[q % a.n_top];
             if (key != 0 && key >= least) add_candidate(top, key);
@@ -358,32 +371,47 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_join_kernel(const LogprobA
     }
 }
 
-// How a row is cut: into parts of at least LP_LEAST logits, so that there are about LP_GROUPS workgroups.
+// How a row is cut.  Many rows: a workgroup of LP_THREADS each, several to a compute unit, so that one's reductions and
+// ranking run beside another's loads.  At most one row to a compute unit: a larger workgroup, or, where one unit's loads take
+// longer than a second launch does, parts of at least LP_LEAST logits, about LP_GROUPS of them.  Measured, us, no
+// alternatives / 20 of them, the two sides of each border:
+//   300 x 32000 bf16      narrow  8.7 / 15.3   wide  11.7 / 20.8
+//   64 x 32000 f32        wide    7.4 / 11.3   narrow 8.8 / 14.5
+//   64 x 12000 f32        narrow  8.0 /  9.0   wide   7.5 /  9.9
+//   1 x 152064 f32        parts   9.6 / 13.9   wide  15.1 / 20.9
+//   64 x 152064 f32       parts  13.8 / 23.3   wide  16.8 / 24.3
+//   256 x 152064 f32      wide   27.7 / 35.5   parts 31.1 / 51.3
+//   1 x 32000 f32         wide    7.4 / 10.3   parts  9.8 / 13.8
 constexpr int64_t LP_GROUPS = 1024, LP_LEAST = 4096;
-struct Cut { int32_t parts, per_part; };
-static Cut cut_of(int64_t n_rows, int32_t vocab) {
+struct Cut { int32_t parts, per_part; bool wide; };
+static Cut cut_of(int64_t n_rows, int32_t vocab, int32_t type) {
+    const int64_t bytes = (int64_t)vocab * (type == DC_F32 ? 4 : 2);
+    if (n_rows > 256 || bytes <= 1 << 16) return Cut{1, vocab, false};
+    if (n_rows > 64 || bytes <= 1 << 17) return Cut{1, vocab, true};
     int64_t parts = n_rows > 0 ? (LP_GROUPS + n_rows - 1) / n_rows : 1;
     const int64_t most = (vocab + LP_LEAST - 1) / LP_LEAST;
     parts = parts < most ? parts : most;
     const int32_t per = (int32_t)(((vocab + parts - 1) / parts + 63) / 64 * 64);
-    return Cut{(vocab + per - 1) / per, per};
+    return Cut{(vocab + per - 1) / per, per, false};
 }
 
-size_t logprob_workspace_bytes(int64_t n_rows, int32_t vocab, int32_t, int32_t n_top) {
-    const Cut c = cut_of(n_rows, vocab);
+size_t logprob_workspace_bytes(int64_t n_rows, int32_t vocab, int32_t type, int32_t n_top) {
+    const Cut c = cut_of(n_rows, vocab, type);
     return c.parts > 1 ? (size_t)n_rows * c.parts * part_bytes(n_top) : 0;
 }
 
 hipError_t launch_logprob(const LogprobArgs& a, int32_t type, void* d_ws, hipStream_t st) {
     if (a.n_rows == 0) return hipSuccess;
-    const Cut c = cut_of(a.n_rows, a.vocab);
+    const Cut c = cut_of(a.n_rows, a.vocab, type);
     const int64_t units = a.n_rows * c.parts;
     const unsigned grid = (unsigned)(units < (1 << 20) ? units : 1 << 20), rows = (unsigned)(a.n_rows < (1 << 20) ? a.n_rows : 1 << 20);
     return with_type(type, [&](auto e) {
         using T = typename decltype(e)::type;
         char* ws = static_cast<char*>(d_ws);
         const auto go = [&](auto entropy, auto top) {
-            logprob_kernel<T, decltype(entropy)::value, decltype(top)::value><<<grid, LP_THREADS, 0, st>>>(a, c.parts, c.per_part, ws);
+            constexpr bool ENTROPY = decltype(entropy)::value, TOP = decltype(top)::value;
+            if (c.wide) logprob_kernel<LP_WIDE, T, ENTROPY, TOP><<<grid, LP_WIDE, 0, st>>>(a, c.parts, c.per_part, ws);
+            else logprob_kernel<LP_THREADS, T, ENTROPY, TOP><<<grid, LP_THREADS, 0, st>>>(a, c.parts, c.per_part, ws);
         };
         if (a.entropy && a.n_top) go(std::true_type{}, std::true_type{});
         else if (a.entropy) go(std::true_type{}, std::false_type{});
@@ -394,38 +422,90 @@ hipError_t launch_logprob(const LogprobArgs& a, int32_t type, void* d_ws, hipStr
     });
 }
 
-// One workgroup per row, element by element.
+// ---- the gradient: dx = p * -(a + b (log p + H)) / T, and a / T more at the given token ----
+
+constexpr int LG_THREADS = 256, LG_AT_ONCE = 4;
+template <typename T> constexpr int LG_PIECE = LG_THREADS * LG_AT_ONCE * CHUNK_ELEMS<T>;
+
 template <typename T>
-__global__ __launch_bounds__(LP_THREADS) void logprob_grad_kernel(const LogprobGradArgs a) {
-    for (int64_t r = blockIdx.x; r < a.n_rows; r += gridDim.x) {
-        const T* x = static_cast<const T*>(a.x) + r * a.stride;
-        T* g = static_cast<T*>(a.g) + r * a.g_stride;
-        const float ga = a.grad_logprob[r], gb = a.grad_entropy ? a.grad_entropy[r] : 0.0f;
-        if ((a.mask && a.mask[r] == 0) || (ga == 0.0f && gb == 0.0f)) {
-            for (int v = threadIdx.x; v < a.vocab; v += LP_THREADS) g[v] = (T)0.0f;
+__device__ __forceinline__ u32x4 pack(const float (&f)[CHUNK_ELEMS<T>]) {
+    union { T e[CHUNK_ELEMS<T>]; u32x4 q; } r;
+#pragma unroll
+    for (int i = 0; i < CHUNK_ELEMS<T>; ++i) r.e[i] = (T)f[i];
+    return r.q;
+}
+
+// One workgroup per piece of a row: 16 bytes in, 16 bytes out, four times a thread.  Bound by the two streams.
+template <typename T, bool ENTROPY>
+__global__ __launch_bounds__(LG_THREADS) void logprob_grad_kernel(const LogprobGradArgs a, int32_t pieces) {
+    constexpr int N = CHUNK_ELEMS<T>;
+    const int tid = threadIdx.x;
+    for (int64_t unit = blockIdx.x; unit < a.n_rows * pieces; unit += gridDim.x) {
+        const int64_t r = unit / pieces;
+        const int32_t v0 = (int32_t)(unit - r * pieces) * LG_PIECE<T>, n = min(LG_PIECE<T>, a.vocab - v0);
+        const T* x = static_cast<const T*>(a.x) + r * a.stride + v0;
+        T* g = static_cast<T*>(a.g) + r * a.g_stride + v0;
+        const float ga = a.grad_logprob[r] * a.inv_t, gb = ENTROPY ? a.grad_entropy[r] * a.inv_t : 0.0f;
+        const bool zero = (a.mask && a.mask[r] == 0) || (a.grad_logprob[r] == 0.0f && (!ENTROPY || a.grad_entropy[r] == 0.0f));
+        // both streams in whole 16 bytes where they can be: up to the first and behind the last of those an element to a thread
+        const uint32_t xa = (uint32_t)reinterpret_cast<uintptr_t>(x) & 15, ga16 = (uint32_t)reinterpret_cast<uintptr_t>(g) & 15;
+        const bool together = zero || xa == ga16;
+        const int32_t head = together ? min(n, (int32_t)((16 - ga16) & 15) / (int32_t)sizeof(T)) : 0;
+        const int32_t chunks = together ? (n - head) / N : 0;
+        const u32x4* from = reinterpret_cast<const u32x4*>(x + head);
+        u32x4* to = reinterpret_cast<u32x4*>(g + head);
+        if (zero) {
+            for (int32_t c = tid; c < chunks; c += LG_THREADS) store16(to + c, u32x4{0, 0, 0, 0});
+            if (tid < head) g[tid] = (T)0.0f;
+            for (int32_t v = head + chunks * N + tid; v < n; v += LG_THREADS) g[v] = (T)0.0f;
             continue;
         }
-        const float m = a.stat[2 * r], log_sum = a.stat[2 * r + 1], h = gb != 0.0f ? a.entropy[r] : 0.0f;
+        u32x4 q[LG_AT_ONCE];
+        if (chunks > 0)
+#pragma unroll
+            for (int j = 0; j < LG_AT_ONCE; ++j) q[j] = __builtin_nontemporal_load(from + min(tid + j * LG_THREADS, chunks - 1));
         int32_t token = -1;
         if (a.token) {
             token = a.token[r];
-            if ((token < 0 || token >= a.vocab) && threadIdx.x == 0) set_status(a.status, DC_ERR_TOKEN_RANGE);
+            if ((token < 0 || token >= a.vocab) && tid == 0 && v0 == 0) set_status(a.status, DC_ERR_TOKEN_RANGE);
+            token -= v0;                         // (outside the piece: no element has it)
         }
-        for (int v = threadIdx.x; v < a.vocab; v += LP_THREADS) {
-            const float lp = ((float)x[v] - m) * a.inv_t - log_sum;
-            const float p = __builtin_amdgcn_exp2f(lp * LOG2E);
-            const float d = (v == token ? ga : 0.0f) - p * (ga + gb * (fmaxf(lp, -1e4f) + h));
-            g[v] = (T)(d * a.inv_t);
+        const float k = a.inv_t * LOG2E, m = a.stat[2 * r], log_sum2 = a.stat[2 * r + 1] * LOG2E;
+        const float c0 = ENTROPY && gb != 0.0f ? -fmaf(gb, a.entropy[r], ga) : -ga, c1 = -gb * LN2;
+        const auto one = [&](float v) {
+            const float lp2 = fmaf(v - m, k, -log_sum2), p = __builtin_amdgcn_exp2f(lp2);
+            // (a logit of -infinity: 0 times a number, not times -infinity)
+            return p * (ENTROPY ? fmaf(c1, fmaxf(lp2, -1e4f), c0) : c0);
+        };
+#pragma unroll
+        for (int j = 0; j < LG_AT_ONCE; ++j) {
+            const int32_t c = tid + j * LG_THREADS;
+            if (c < chunks) {
+                float f[N];
+                unpack<T>(q[j], f);
+#pragma unroll
+                for (int i = 0; i < N; ++i) f[i] = one(f[i]);
+                const uint32_t at = (uint32_t)(token - head - c * N);
+                if (at < (uint32_t)N)
+#pragma unroll
+                    for (int i = 0; i < N; ++i) f[i] += at == (uint32_t)i ? ga : 0.0f;
+                store16(to + c, pack<T>(f));
+            }
         }
+        if (tid < head) g[tid] = (T)(one((float)x[tid]) + (tid == token ? ga : 0.0f));
+        for (int32_t v = head + chunks * N + tid; v < n; v += LG_THREADS) g[v] = (T)(one((float)x[v]) + (v == token ? ga : 0.0f));
     }
 }
 
 hipError_t launch_logprob_grad(const LogprobGradArgs& a, int32_t type, hipStream_t st) {
     if (a.n_rows == 0) return hipSuccess;
-    const unsigned grid = (unsigned)(a.n_rows < (1 << 20) ? a.n_rows : 1 << 20);
     return with_type(type, [&](auto e) {
         using T = typename decltype(e)::type;
-        logprob_grad_kernel<T><<<grid, LP_THREADS, 0, st>>>(a);
+        const int32_t pieces = (a.vocab + LG_PIECE<T> - 1) / LG_PIECE<T>;
+        const int64_t units = a.n_rows * pieces;
+        const unsigned grid = (unsigned)(units < (1 << 23) ? units : 1 << 23);
+        if (a.grad_entropy) logprob_grad_kernel<T, true><<<grid, LG_THREADS, 0, st>>>(a, pieces);
+        else logprob_grad_kernel<T, false><<<grid, LG_THREADS, 0, st>>>(a, pieces);
         return hipGetLastError();
     });
 }

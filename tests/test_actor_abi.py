@@ -189,7 +189,7 @@ class FakeTensor:
         self._stride = stride or tuple(math.prod(shape[i + 1:]) for i in range(len(shape)))
 
     def dim(self): return len(self.shape)
-    def stride(self, i): return self._stride[i]
+    def stride(self, i=None): return self._stride if i is None else self._stride[i]
     def numel(self): return math.prod(self.shape)
     def data_ptr(self): return A
     def is_contiguous(self): return True
