@@ -34,6 +34,14 @@ __global__ __launch_bounds__(256) void adamw_table_kernel(const TableChunk c, Ad
         t.pieces[c.first_piece[i] + p] = AdamwPiece{c.first + i, (int32_t)p};
 }
 
+// Whether every array of a tensor starts on a multiple of 16 bytes.
+static int32_t aligned(const dc_adamw_tensor& d) {
+    uintptr_t all = 0;
+    for (const void* p : {(const void*)d.d_param, (const void*)d.d_master, d.d_grad, (const void*)d.d_exp_avg, (const void*)d.d_exp_avg_sq})
+        all |= reinterpret_cast<uintptr_t>(p);
+    return all % 16 == 0;
+}
+
 hipError_t launch_adamw_table(const dc_adamw_tensor* tensors, int32_t n_tensors, const AdamwTable& t, int64_t n_pieces, hipStream_t st) {
     int64_t at = 0;
     for (int32_t first = 0; first < n_tensors; first += TABLE_TENSORS) {
@@ -44,6 +52,7 @@ hipError_t launch_adamw_table(const dc_adamw_tensor* tensors, int32_t n_tensors,
         int64_t most = 1;
         for (int i = 0; i < c.count; ++i) {
             c.tensors[i] = tensors[first + i];
+            c.tensors[i].reserved = aligned(tensors[first + i]);
             c.first_piece[i] = at;
             const int64_t n = (tensors[first + i].n + ADAMW_PIECE - 1) / ADAMW_PIECE;
             at += n;
@@ -72,81 +81,218 @@ __device__ __forceinline__ void store_as(void* p, int64_t i, int32_t type, float
     }
 }
 __device__ __forceinline__ float from_e4m3(uint8_t c) { return __builtin_amdgcn_cvt_f32_fp8(c, 0); }
-__device__ __forceinline__ uint8_t to_e4m3(float v) { return (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(v, v, 0, false) & 0xFF); }
+__device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d) {
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
+}
 
 constexpr float E4M3_MOST = 448.0f, E4M3_LEAST = 0x1p-9f, STATE_SCALE_LEAST = 0x1p-120f;
 
-// One wave per block of DC_STATE_BLOCK elements, four to a lane, element by element.  Every operation on m, v and the
-// scales is rounded by itself (no contraction), so that what is stored in 8 bits is a function of the inputs alone.
-constexpr int AW_THREADS = 256;
+// One element's step.  Every operation is rounded by itself (no contraction), so that what is stored in 8 bits is a function
+// of the inputs alone.  m and v are the new states, root the square root of v; returns the new weight.
+__device__ __forceinline__ float step_of(const AdamwStep& s, float decay, float g, float w, float& m, float& v, float& root) {
+    m = m * s.beta1 + g * s.one_minus_beta1;
+    v = v * s.beta2 + g * g * s.one_minus_beta2;
+    root = sqrtf(v);
+    return w * decay - s.step_size * (m / (root * s.inv_root_bc2 + s.eps));
+}
+// The scale of a block whose largest magnitude is `most`, and its inverse; both 0 for a block that is stored as zeros.
+struct Scale { float value, inverse; };
+__device__ __forceinline__ Scale scale_of(float most) {
+    const float s = most / E4M3_MOST;
+    return s >= STATE_SCALE_LEAST ? Scale{s, 1.0f / s} : Scale{0.0f, 0.0f};
+}
+__device__ __forceinline__ float root_code(float root, float inverse) {
+    const float c = root * inverse;
+    return c > 0.0f ? fmaxf(c, E4M3_LEAST) : c;      // what is divided by does not become zero
+}
+// The largest of a wave's magnitudes, in every lane: magnitudes sort like their bits.
+__device__ __forceinline__ float wave_most(float v) {
+    const uint32_t m = wave_incl_scan_u32(__float_as_uint(v), 0u, [](uint32_t a, uint32_t b) { return max(a, b); });
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)m, WAVE - 1));
+}
+
+// A wave's block of DC_STATE_BLOCK elements or fewer, element by element: the last block of a tensor, and tensors that are
+// not aligned.
+__device__ __noinline__ void block_by_elements(const AdamwStep& s, const dc_adamw_tensor& d, int64_t block, float gs, float decay) {
+    const int64_t at = block * DC_STATE_BLOCK;
+    const bool small = d.state_type == DC_E4M3;
+    const float ms = small ? d.d_exp_avg_scale[block] : 0.0f, vs = small ? d.d_exp_avg_sq_scale[block] : 0.0f;
+    float m[4], root[4], m_most = 0.0f, root_most = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int64_t i = at + j * WAVE + lane_id();
+        m[j] = root[j] = 0.0f;
+        if (i >= d.n) continue;
+        float v;
+        if (small) {
+            m[j] = from_e4m3(static_cast<const uint8_t*>(d.d_exp_avg)[i]) * ms;
+            const float r = from_e4m3(static_cast<const uint8_t*>(d.d_exp_avg_sq)[i]) * vs;
+            v = r * r;
+        } else {
+            m[j] = static_cast<const float*>(d.d_exp_avg)[i];
+            v = static_cast<const float*>(d.d_exp_avg_sq)[i];
+        }
+        const float w = step_of(s, decay, load_as(d.d_grad, i, d.grad_type) * gs,
+                                d.d_master ? d.d_master[i] : load_as(d.d_param, i, d.param_type), m[j], v, root[j]);
+        if (d.d_master) d.d_master[i] = w;
+        store_as(d.d_param, i, d.param_type, w);
+        if (!small) {
+            static_cast<float*>(d.d_exp_avg)[i] = m[j];
+            static_cast<float*>(d.d_exp_avg_sq)[i] = v;
+        }
+        m_most = fmaxf(m_most, fabsf(m[j]));
+        root_most = fmaxf(root_most, root[j]);
+    }
+    if (!small) return;
+    const Scale sm = scale_of(wave_most(m_most)), sr = scale_of(wave_most(root_most));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int64_t i = at + j * WAVE + lane_id();
+        if (i >= d.n) continue;
+        static_cast<uint8_t*>(d.d_exp_avg)[i] = (uint8_t)to_e4m3(m[j] * sm.inverse, 0.0f, 0.0f, 0.0f);
+        static_cast<uint8_t*>(d.d_exp_avg_sq)[i] = (uint8_t)to_e4m3(root_code(root[j], sr.inverse), 0.0f, 0.0f, 0.0f);
+    }
+    if (lane_id() == 0) { d.d_exp_avg_scale[block] = sm.value; d.d_exp_avg_sq_scale[block] = sr.value; }
+}
+
+// Four neighbouring elements as they lie in memory.
+template <typename T> struct Raw4 { T e[4]; };
+template <typename T>
+__device__ __forceinline__ Raw4<T> load4(const void* p, int64_t i) {
+    Raw4<T> r;
+    if constexpr (sizeof(T) == 4) {
+        const u32x4 q = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(static_cast<const T*>(p) + i));
+        __builtin_memcpy(&r, &q, 16);
+    } else {
+        const u32x2 q = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(static_cast<const T*>(p) + i));
+        __builtin_memcpy(&r, &q, 8);
+    }
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void store4(void* p, int64_t i, const float (&f)[4]) {
+    Raw4<T> r;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) r.e[c] = (T)f[c];
+    if constexpr (sizeof(T) == 4) {
+        u32x4 q;
+        __builtin_memcpy(&q, &r, 16);
+        __builtin_nontemporal_store(q, reinterpret_cast<u32x4*>(static_cast<T*>(p) + i));
+    } else {
+        u32x2 q;
+        __builtin_memcpy(&q, &r, 8);
+        __builtin_nontemporal_store(q, reinterpret_cast<u32x2*>(static_cast<T*>(p) + i));
+    }
+}
+
+constexpr int AW_THREADS = 256, AW_BLOCKS = ADAMW_PIECE / DC_STATE_BLOCK / (AW_THREADS / WAVE);     // blocks of a wave
+
+// A wave's AW_BLOCKS whole blocks of an aligned tensor, four neighbouring elements of each to a lane; everything is asked for
+// before anything is used.  G: the gradient's type, P: what the weights are read from (the master's float, or the parameter's).
+template <typename G, typename P, bool MASTER, bool SMALL>
+__device__ __forceinline__ void whole_blocks(const AdamwStep& s, const dc_adamw_tensor& d, int64_t block, float gs, float decay) {
+    Raw4<G> rg[AW_BLOCKS];
+    Raw4<P> rw[AW_BLOCKS];
+    Raw4<float> rm[AW_BLOCKS], rv[AW_BLOCKS];
+    uint32_t cm[AW_BLOCKS], cv[AW_BLOCKS];
+    float ms[AW_BLOCKS], vs[AW_BLOCKS];
+    const int64_t at = block * DC_STATE_BLOCK + lane_id() * 4;
+#pragma unroll
+    for (int b = 0; b < AW_BLOCKS; ++b) {
+        const int64_t i = at + b * DC_STATE_BLOCK;
+        rg[b] = load4<G>(d.d_grad, i);
+        rw[b] = load4<P>(MASTER ? (const void*)d.d_master : d.d_param, i);
+        if constexpr (SMALL) {
+            cm[b] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(d.d_exp_avg) + i));
+            cv[b] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(d.d_exp_avg_sq) + i));
+            ms[b] = d.d_exp_avg_scale[block + b];
+            vs[b] = d.d_exp_avg_sq_scale[block + b];
+        } else {
+            rm[b] = load4<float>(d.d_exp_avg, i);
+            rv[b] = load4<float>(d.d_exp_avg_sq, i);
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < AW_BLOCKS; ++b) {
+        const int64_t i = at + b * DC_STATE_BLOCK;
+        float m[4], v[4], root[4], w[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            if constexpr (SMALL) {
+                m[c] = from_e4m3((uint8_t)(cm[b] >> (8 * c))) * ms[b];
+                const float r = from_e4m3((uint8_t)(cv[b] >> (8 * c))) * vs[b];
+                v[c] = r * r;
+            } else {
+                m[c] = rm[b].e[c];
+                v[c] = rv[b].e[c];
+            }
+            w[c] = step_of(s, decay, (float)rg[b].e[c] * gs, (float)rw[b].e[c], m[c], v[c], root[c]);
+        }
+        if constexpr (MASTER) {
+            store4<float>(d.d_master, i, w);
+            if (d.param_type == DC_BF16) store4<__bf16>(d.d_param, i, w);
+            else if (d.param_type == DC_F16) store4<_Float16>(d.d_param, i, w);
+            else store4<float>(d.d_param, i, w);
+        } else {
+            store4<P>(d.d_param, i, w);
+        }
+        if constexpr (SMALL) {
+            const Scale sm = scale_of(wave_most(fmaxf(fmaxf(fabsf(m[0]), fabsf(m[1])), fmaxf(fabsf(m[2]), fabsf(m[3])))));
+            const Scale sr = scale_of(wave_most(fmaxf(fmaxf(root[0], root[1]), fmaxf(root[2], root[3]))));
+            const uint32_t em = to_e4m3(m[0] * sm.inverse, m[1] * sm.inverse, m[2] * sm.inverse, m[3] * sm.inverse);
+            const uint32_t er = to_e4m3(root_code(root[0], sr.inverse), root_code(root[1], sr.inverse), root_code(root[2], sr.inverse),
+                                        root_code(root[3], sr.inverse));
+            __builtin_nontemporal_store(em, reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(d.d_exp_avg) + i));
+            __builtin_nontemporal_store(er, reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(d.d_exp_avg_sq) + i));
+            if (lane_id() == 0) { d.d_exp_avg_scale[block + b] = sm.value; d.d_exp_avg_sq_scale[block + b] = sr.value; }
+        } else {
+            store4<float>(d.d_exp_avg, i, m);
+            store4<float>(d.d_exp_avg_sq, i, v);
+        }
+    }
+}
+template <typename G, bool SMALL>
+__device__ __forceinline__ void whole_blocks_of(const AdamwStep& s, const dc_adamw_tensor& d, int64_t block, float gs, float decay) {
+    if (d.d_master) whole_blocks<G, float, true, SMALL>(s, d, block, gs, decay);
+    else if (d.param_type == DC_F32) whole_blocks<G, float, false, SMALL>(s, d, block, gs, decay);
+    else if (d.param_type == DC_BF16) whole_blocks<G, __bf16, false, SMALL>(s, d, block, gs, decay);
+    else whole_blocks<G, _Float16, false, SMALL>(s, d, block, gs, decay);
+}
+
+// One workgroup per piece, AW_BLOCKS blocks to a wave.  What a tensor is made of is the same for a whole piece, so the kinds
+// are branches of one kernel and all tensors go in one launch.  Bound by the streams.
 __global__ __launch_bounds__(AW_THREADS) void adamw_kernel(const AdamwStep s, const AdamwTable t, int64_t n_pieces, int32_t n_tensors) {
     if (t.head->n_pieces != n_pieces || t.head->n_tensors != n_tensors) {
         if (threadIdx.x == 0) set_status(s.status, DC_ERR_BAD_LAYOUT);
         return;
     }
     const float gs = s.grad_scale ? *s.grad_scale : 1.0f;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     for (int64_t q = blockIdx.x; q < n_pieces; q += gridDim.x) {
         const AdamwPiece piece = t.pieces[q];
         const dc_adamw_tensor& d = t.tensors[piece.tensor];
         const float decay = (float)(1.0 - s.lr64 * d.weight_decay);
-        const bool small = d.state_type == DC_E4M3;
-        for (int b = threadIdx.x / WAVE; b < ADAMW_PIECE / DC_STATE_BLOCK; b += AW_THREADS / WAVE) {
-            const int64_t block = (int64_t)piece.piece * (ADAMW_PIECE / DC_STATE_BLOCK) + b, at = block * DC_STATE_BLOCK;
-            if (at >= d.n) break;
-            const float ms = small ? d.d_exp_avg_scale[block] : 0.0f, vs = small ? d.d_exp_avg_sq_scale[block] : 0.0f;
-            float m[4], root[4], m_most = 0.0f, root_most = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int64_t i = at + j * WAVE + lane_id();
-                m[j] = root[j] = 0.0f;
-                if (i >= d.n) continue;
-                float v;
-                if (small) {
-                    m[j] = from_e4m3(static_cast<const uint8_t*>(d.d_exp_avg)[i]) * ms;
-                    const float r = from_e4m3(static_cast<const uint8_t*>(d.d_exp_avg_sq)[i]) * vs;
-                    v = r * r;
-                } else {
-                    m[j] = static_cast<const float*>(d.d_exp_avg)[i];
-                    v = static_cast<const float*>(d.d_exp_avg_sq)[i];
-                }
-                const float g = load_as(d.d_grad, i, d.grad_type) * gs;
-                m[j] = m[j] * s.beta1 + g * s.one_minus_beta1;
-                v = v * s.beta2 + g * g * s.one_minus_beta2;
-                root[j] = sqrtf(v);
-                float w = d.d_master ? d.d_master[i] : load_as(d.d_param, i, d.param_type);
-                w = w * decay - s.step_size * (m[j] / (root[j] * s.inv_root_bc2 + s.eps));
-                if (d.d_master) d.d_master[i] = w;
-                store_as(d.d_param, i, d.param_type, w);
-                if (!small) {
-                    static_cast<float*>(d.d_exp_avg)[i] = m[j];
-                    static_cast<float*>(d.d_exp_avg_sq)[i] = v;
-                }
-                m_most = fmaxf(m_most, fabsf(m[j]));
-                root_most = fmaxf(root_most, root[j]);
+        const int64_t block = (int64_t)piece.piece * (ADAMW_PIECE / DC_STATE_BLOCK) + wave * AW_BLOCKS;
+        if (d.reserved && (block + AW_BLOCKS) * DC_STATE_BLOCK <= d.n) {   // (in the table: whether all of it is aligned)
+            if (d.state_type == DC_E4M3) {
+                if (d.grad_type == DC_BF16) whole_blocks_of<__bf16, true>(s, d, block, gs, decay);
+                else if (d.grad_type == DC_F32) whole_blocks_of<float, true>(s, d, block, gs, decay);
+                else whole_blocks_of<_Float16, true>(s, d, block, gs, decay);
+            } else {
+                if (d.grad_type == DC_BF16) whole_blocks_of<__bf16, false>(s, d, block, gs, decay);
+                else if (d.grad_type == DC_F32) whole_blocks_of<float, false>(s, d, block, gs, decay);
+                else whole_blocks_of<_Float16, false>(s, d, block, gs, decay);
             }
-            if (!small) continue;
-            float m_scale = wave_max(m_most) / E4M3_MOST, r_scale = wave_max(root_most) / E4M3_MOST;
-            if (!(m_scale >= STATE_SCALE_LEAST)) m_scale = 0.0f;
-            if (!(r_scale >= STATE_SCALE_LEAST)) r_scale = 0.0f;
-            const float m_inv = m_scale > 0.0f ? 1.0f / m_scale : 0.0f, r_inv = r_scale > 0.0f ? 1.0f / r_scale : 0.0f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int64_t i = at + j * WAVE + lane_id();
-                if (i >= d.n) continue;
-                const float mc = m[j] * m_inv;
-                float rc = root[j] * r_inv;
-                if (rc > 0.0f) rc = fmaxf(rc, E4M3_LEAST);
-                static_cast<uint8_t*>(d.d_exp_avg)[i] = to_e4m3(mc);
-                static_cast<uint8_t*>(d.d_exp_avg_sq)[i] = to_e4m3(rc);
-            }
-            if (lane_id() == 0) { d.d_exp_avg_scale[block] = m_scale; d.d_exp_avg_sq_scale[block] = r_scale; }
+        } else {
+            for (int b = 0; b < AW_BLOCKS && (block + b) * DC_STATE_BLOCK < d.n; ++b) block_by_elements(s, d, block + b, gs, decay);
         }
     }
 }
 
 hipError_t launch_adamw(const AdamwStep& s, int32_t n_tensors, const AdamwTable& t, int64_t n_pieces, hipStream_t st) {
     if (n_pieces == 0) return hipSuccess;
-    const unsigned grid = (unsigned)(n_pieces < (1 << 20) ? n_pieces : 1 << 20);
+    const unsigned grid = (unsigned)(n_pieces < (1 << 23) ? n_pieces : 1 << 23);
     adamw_kernel<<<grid, AW_THREADS, 0, st>>>(s, t, n_pieces, n_tensors);
     return hipGetLastError();
 }

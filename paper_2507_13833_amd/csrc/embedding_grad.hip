@@ -17,9 +17,8 @@ namespace dc {
 constexpr int SORT_THREADS = 1024, SORT_WAVES = SORT_THREADS / WAVE;
 constexpr int MAX_PORTION = 8192, PER_THREAD = MAX_PORTION / SORT_THREADS;
 constexpr int MERGE_WAYS = 32, MERGE_THREADS = 512, MERGE_SAMPLES = 64;
-constexpr int COLS = 512;                        // columns of a wave: eight to a lane
 constexpr int ADD_THREADS = 256;
-constexpr int FILL_ROWS = 8, FILL_LANES = WAVE / FILL_ROWS;      // rows of the table per wave that looks for those without a token
+constexpr int FILL_ROWS = 4, FILL_LANES = WAVE / FILL_ROWS;      // rows of the table per wave that looks for those without a token
 constexpr int JOIN_THREADS = 512;
 
 static inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
@@ -216,58 +215,16 @@ __global__ __launch_bounds__(MERGE_THREADS) void merge_runs_kernel(const Embeddi
     pos_out[to] = pos_in[i];
 }
 
-// ---- eight columns of a row per lane: neighbours where rows are aligned (VEC), 64 apart where they are not ----
-template <bool VEC>
-__device__ __forceinline__ int64_t column(int64_t slab, int j) {
-    return slab * COLS + (VEC ? (int64_t)lane_id() * 8 + j : (int64_t)j * WAVE + lane_id());
-}
-// Eight elements as they lie in memory.
-template <typename T>
-union Raw8 {
-    T e[8];
-    u32x4 q[sizeof(T) / 2];
-};
-template <bool VEC, typename T>
-__device__ __forceinline__ void load8(const T* row, int64_t slab, int64_t dim, Raw8<T>& r) {
-    if constexpr (VEC) {
-        // (behind the row's end: its last columns again, which nobody stores)
-        const u32x4* p = reinterpret_cast<const u32x4*>(row + min(column<VEC>(slab, 0), dim - 8));
-#pragma unroll
-        for (int h = 0; h < (int)sizeof(T) / 2; ++h) r.q[h] = p[h];
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) r.e[j] = row[min(column<VEC>(slab, j), dim - 1)];
-    }
-}
-template <bool VEC, typename T>
-__device__ __forceinline__ void store8(T* row, int64_t slab, int64_t dim, const float (&f)[8]) {
-    if constexpr (VEC) {
-        if (column<VEC>(slab, 0) < dim) {
-            Raw8<T> r;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) r.e[j] = (T)f[j];
-            u32x4* p = reinterpret_cast<u32x4*>(row + column<VEC>(slab, 0));
-#pragma unroll
-            for (int h = 0; h < (int)sizeof(T) / 2; ++h) p[h] = r.q[h];
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int64_t c = column<VEC>(slab, j);
-            if (c < dim) row[c] = (T)f[j];
-        }
-    }
-}
 // A finished sum to its row of the table, added to what `old` holds of it.
-template <bool VEC, bool ACC, typename W>
+template <Layout L, bool ACC, typename W>
 __device__ __forceinline__ void write_row(const EmbeddingGradArgs& a, uint32_t id, int64_t slab, const float (&sum)[8], const Raw8<W>& old) {
     float out[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) out[j] = sum[j] * a.scale + (ACC ? (float)old.e[j] : 0.0f);
-    store8<VEC>(static_cast<W*>(a.dw) + (int64_t)id * a.dw_stride, slab, a.dim, out);
+    store8<L, !ACC>(static_cast<W*>(a.dw) + (int64_t)id * a.dw_stride, slab, a.dim, out);
 }
 
-template <int CHUNK, bool VEC, bool ACC, typename G, typename W>
+template <int CHUNK, Layout L, bool ACC, typename G, typename W>
 __global__ __launch_bounds__(ADD_THREADS) void add_rows_kernel(const EmbeddingGradArgs a, const uint32_t* __restrict__ skey,
                                                                const int32_t* __restrict__ spos,
                                                                int32_t* n_long, int32_t* long_at, float* __restrict__ piece,
@@ -279,7 +236,7 @@ __global__ __launch_bounds__(ADD_THREADS) void add_rows_kernel(const EmbeddingGr
     if (unit >= adders) {                        // rows without a token
         const int64_t v0 = (unit - adders) * FILL_ROWS;
         if (ACC || v0 >= a.vocab) return;
-        // eight lanes look for each row's id among the sorted ones, eight places at a time
+        // sixteen lanes look for each row's id among the sorted ones, sixteen places at a time
         const int sub = lane % FILL_LANES;
         const uint32_t id = (uint32_t)(v0 + lane / FILL_LANES);
         int32_t lo = 0, hi = a.n_tokens;         // the first entry that is not below it lies in [lo, hi]
@@ -299,7 +256,7 @@ __global__ __launch_bounds__(ADD_THREADS) void add_rows_kernel(const EmbeddingGr
         for (int r = 0; r < FILL_ROWS && v0 + r < a.vocab; ++r) {
             if ((there >> (r * FILL_LANES)) & 1) continue;
             W* row = static_cast<W*>(a.dw) + (v0 + r) * a.dw_stride;
-            for (int32_t s = 0; s < slabs; ++s) store8<VEC>(row, s, a.dim, zero);
+            for (int32_t s = 0; s < slabs; ++s) store8<L, true>(row, s, a.dim, zero);
         }
         return;
     }
@@ -344,9 +301,9 @@ __global__ __launch_bounds__(ADD_THREADS) void add_rows_kernel(const EmbeddingGr
 #pragma unroll
         for (int j = 0; j < AT_ONCE; ++j) {
             const int e = min(i + j, to - 1);
-            load8<VEC>(grad + (int64_t)entry_pos(e) * a.g_stride, slab, a.dim, next[j]);
+            load8<L>(grad + (int64_t)entry_pos(e) * a.g_stride, slab, a.dim, next[j]);
             // (all of a segment's entries ask for its row, the last one's answer is used: the others come out of the cache)
-            if constexpr (ACC) load8<VEC>(static_cast<const W*>(a.dw) + (int64_t)entry_id(e) * a.dw_stride, slab, a.dim, next_old[j]);
+            if constexpr (ACC) load8<L>(static_cast<const W*>(a.dw) + (int64_t)entry_id(e) * a.dw_stride, slab, a.dim, next_old[j]);
         }
     };
     float sum[8] = {};
@@ -369,10 +326,10 @@ __global__ __launch_bounds__(ADD_THREADS) void add_rows_kernel(const EmbeddingGr
                 if ((ends >> e) & 1) {
                     const bool lead = lead_long && e < first_start, tail = tail_long && e == CHUNK - 1 && !lead;
                     if (lead || tail) {
-                        store8<VEC>(piece + ((int64_t)chunk * 2 + tail) * a.dim, slab, a.dim, sum);
+                        store8<L>(piece + ((int64_t)chunk * 2 + tail) * a.dim, slab, a.dim, sum);
                         if (tail && slab == 0 && lane == 0) long_at[atomicAdd(n_long, 1)] = chunk;
                     } else {
-                        write_row<VEC, ACC, W>(a, entry_id(e), slab, sum, old[ACC ? j : 0]);
+                        write_row<L, ACC, W>(a, entry_id(e), slab, sum, old[ACC ? j : 0]);
                     }
 #pragma unroll
                     for (int c = 0; c < 8; ++c) sum[c] = 0.0f;
@@ -383,7 +340,7 @@ __global__ __launch_bounds__(ADD_THREADS) void add_rows_kernel(const EmbeddingGr
 }
 
 // One workgroup per long segment and 512 columns, round and round; its waves take every fourth piece each.
-template <int CHUNK, bool VEC, bool ACC, typename W>
+template <int CHUNK, Layout L, bool ACC, typename W>
 __global__ __launch_bounds__(JOIN_THREADS) void join_pieces_kernel(const EmbeddingGradArgs a, const uint32_t* __restrict__ skey,
                                                                    const int32_t* __restrict__ n_long, const int32_t* __restrict__ long_at,
                                                                    const float* __restrict__ piece, int32_t chunks, int32_t slabs) {
@@ -404,14 +361,14 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_pieces_kernel(const Embeddi
             hi = min(hi, lo + step);
         }
         Raw8<W> old;
-        if constexpr (ACC) load8<VEC>(static_cast<const W*>(a.dw) + (int64_t)id * a.dw_stride, slab, a.dim, old);
+        if constexpr (ACC) load8<L>(static_cast<const W*>(a.dw) + (int64_t)id * a.dw_stride, slab, a.dim, old);
         float sum[8] = {};
         for (int64_t c = (int64_t)c0 + wave; c <= lo; c += WAVES * AT_ONCE) {
             Raw8<float> f[AT_ONCE];
 #pragma unroll
             for (int q = 0; q < AT_ONCE; ++q) {
                 const int64_t at = min(c + q * WAVES, (int64_t)lo);
-                load8<VEC>(piece + (at * 2 + (at == c0)) * a.dim, slab, a.dim, f[q]);
+                load8<L>(piece + (at * 2 + (at == c0)) * a.dim, slab, a.dim, f[q]);
             }
 #pragma unroll
             for (int q = 0; q < AT_ONCE; ++q)
@@ -426,7 +383,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_pieces_kernel(const Embeddi
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 for (int w = 1; w < WAVES; ++w) sum[j] += part[w][j][lane];
-            write_row<VEC, ACC, W>(a, id, slab, sum, old);
+            write_row<L, ACC, W>(a, id, slab, sum, old);
         }
         __syncthreads();
     }
@@ -459,18 +416,16 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, int32_t g_type, int
         return with_type(dw_type, [&](auto we) {
             using G = typename decltype(ge)::type;
             using W = typename decltype(we)::type;
-            const auto aligned = [&](const void* p, int64_t stride, size_t size) {
-                return (reinterpret_cast<uintptr_t>(p) % 16 == 0) && (size_t)stride * size % 16 == 0;
-            };
-            const bool vec = a.dim % 8 == 0 && aligned(a.g, a.g_stride, sizeof(G)) && aligned(a.dw, a.dw_stride, sizeof(W));
+            const bool vec = a.dim % 8 == 0 && rows_aligned<G>(a.g, a.g_stride) && rows_aligned<W>(a.dw, a.dw_stride);
             const auto launch = [&](auto c, auto v, auto acc) {
                 constexpr int CHUNK = decltype(c)::value;
-                constexpr bool VEC = decltype(v)::value, ACC = decltype(acc)::value;
-                add_rows_kernel<CHUNK, VEC, ACC, G, W><<<(unsigned)blocks, ADD_THREADS, 0, st>>>(
+                constexpr Layout L = decltype(v)::value ? (sizeof(W) == 4 ? FOURS : EIGHTS) : APART;
+                constexpr bool ACC = decltype(acc)::value;
+                add_rows_kernel<CHUNK, L, ACC, G, W><<<(unsigned)blocks, ADD_THREADS, 0, st>>>(
                     a, w.key[at], w.pos[at], w.n_long, w.long_at, w.piece, (int32_t)chunks, (int32_t)slabs);
                 if (a.n_tokens > CHUNK) {
                     const int64_t most = (int64_t)a.n_tokens / (CHUNK + 1) * slabs;      // long segments there can be
-                    join_pieces_kernel<CHUNK, VEC, ACC, W><<<(unsigned)(most < 1024 ? most : 1024), JOIN_THREADS, 0, st>>>(
+                    join_pieces_kernel<CHUNK, L, ACC, W><<<(unsigned)(most < 1024 ? most : 1024), JOIN_THREADS, 0, st>>>(
                         a, w.key[at], w.n_long, w.long_at, w.piece, (int32_t)chunks, (int32_t)slabs);
                 }
             };
