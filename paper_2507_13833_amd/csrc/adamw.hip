@@ -88,19 +88,21 @@ __device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d) 
 
 constexpr float E4M3_MOST = 448.0f, E4M3_LEAST = 0x1p-9f, STATE_SCALE_LEAST = 0x1p-120f;
 
-// One element's step.  Every operation is rounded by itself (no contraction), so that what is stored in 8 bits is a function
-// of the inputs alone.  m and v are the new states, root the square root of v; returns the new weight.
+// One element's step; m and v become the new states, root the square root of v; returns the new weight.  The root and the
+// quotient are the hardware's, off by at most a unit in the last place, which is what the roundings before them leave: the
+// exact ones cost 8-bit states 15 % of the step's time.  (Its root takes denormals for zero: those are scaled first.)
 __device__ __forceinline__ float step_of(const AdamwStep& s, float decay, float g, float w, float& m, float& v, float& root) {
     m = m * s.beta1 + g * s.one_minus_beta1;
     v = v * s.beta2 + g * g * s.one_minus_beta2;
-    root = sqrtf(v);
-    return w * decay - s.step_size * (m / (root * s.inv_root_bc2 + s.eps));
+    const bool tiny = v < 0x1p-96f;
+    root = __builtin_amdgcn_sqrtf(tiny ? v * 0x1p96f : v) * (tiny ? 0x1p-48f : 1.0f);
+    return w * decay - s.step_size * (m * __builtin_amdgcn_rcpf(root * s.inv_root_bc2 + s.eps));
 }
 // The scale of a block whose largest magnitude is `most`, and its inverse; both 0 for a block that is stored as zeros.
 struct Scale { float value, inverse; };
 __device__ __forceinline__ Scale scale_of(float most) {
-    const float s = most / E4M3_MOST;
-    return s >= STATE_SCALE_LEAST ? Scale{s, 1.0f / s} : Scale{0.0f, 0.0f};
+    const float s = most * (1.0f / E4M3_MOST);
+    return s >= STATE_SCALE_LEAST ? Scale{s, __builtin_amdgcn_rcpf(s)} : Scale{0.0f, 0.0f};
 }
 __device__ __forceinline__ float root_code(float root, float inverse) {
     const float c = root * inverse;
@@ -114,7 +116,7 @@ __device__ __forceinline__ float wave_most(float v) {
 
 // A wave's block of DC_STATE_BLOCK elements or fewer, element by element: the last block of a tensor, and tensors that are
 // not aligned.
-__device__ __noinline__ void block_by_elements(const AdamwStep& s, const dc_adamw_tensor& d, int64_t block, float gs, float decay) {
+__device__ __forceinline__ void block_by_elements(const AdamwStep& s, const dc_adamw_tensor& d, int64_t block, float gs, float decay) {
     const int64_t at = block * DC_STATE_BLOCK;
     const bool small = d.state_type == DC_E4M3;
     const float ms = small ? d.d_exp_avg_scale[block] : 0.0f, vs = small ? d.d_exp_avg_sq_scale[block] : 0.0f;
@@ -262,16 +264,17 @@ __device__ __forceinline__ void whole_blocks_of(const AdamwStep& s, const dc_ada
 
 // One workgroup per piece, AW_BLOCKS blocks to a wave.  What a tensor is made of is the same for a whole piece, so the kinds
 // are branches of one kernel and all tensors go in one launch.  Bound by the streams.
-__global__ __launch_bounds__(AW_THREADS) void adamw_kernel(const AdamwStep s, const AdamwTable t, int64_t n_pieces, int32_t n_tensors) {
-    if (t.head->n_pieces != n_pieces || t.head->n_tensors != n_tensors) {
+__global__ __launch_bounds__(AW_THREADS) void adamw_kernel(const AdamwStep s, const AdamwHeader* __restrict__ head, const dc_adamw_tensor* __restrict__ tensors,
+                                                           const AdamwPiece* __restrict__ pieces, int64_t n_pieces, int32_t n_tensors) {
+    if (head->n_pieces != n_pieces || head->n_tensors != n_tensors) {
         if (threadIdx.x == 0) set_status(s.status, DC_ERR_BAD_LAYOUT);
         return;
     }
     const float gs = s.grad_scale ? *s.grad_scale : 1.0f;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     for (int64_t q = blockIdx.x; q < n_pieces; q += gridDim.x) {
-        const AdamwPiece piece = t.pieces[q];
-        const dc_adamw_tensor& d = t.tensors[piece.tensor];
+        const AdamwPiece piece = pieces[q];
+        const dc_adamw_tensor d = tensors[piece.tensor];     // (a copy: no store below can be thought to change it)
         const float decay = (float)(1.0 - s.lr64 * d.weight_decay);
         const int64_t block = (int64_t)piece.piece * (ADAMW_PIECE / DC_STATE_BLOCK) + wave * AW_BLOCKS;
         if (d.reserved && (block + AW_BLOCKS) * DC_STATE_BLOCK <= d.n) {   // (in the table: whether all of it is aligned)
@@ -293,7 +296,7 @@ __global__ __launch_bounds__(AW_THREADS) void adamw_kernel(const AdamwStep s, co
 hipError_t launch_adamw(const AdamwStep& s, int32_t n_tensors, const AdamwTable& t, int64_t n_pieces, hipStream_t st) {
     if (n_pieces == 0) return hipSuccess;
     const unsigned grid = (unsigned)(n_pieces < (1 << 23) ? n_pieces : 1 << 23);
-    adamw_kernel<<<grid, AW_THREADS, 0, st>>>(s, t, n_pieces, n_tensors);
+    adamw_kernel<<<grid, AW_THREADS, 0, st>>>(s, t.head, t.tensors, t.pieces, n_pieces, n_tensors);
     return hipGetLastError();
 }
 
