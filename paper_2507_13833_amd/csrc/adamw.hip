@@ -88,21 +88,31 @@ __device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d) 
 
 constexpr float E4M3_MOST = 448.0f, E4M3_LEAST = 0x1p-9f, STATE_SCALE_LEAST = 0x1p-120f;
 
-// One element's step; m and v become the new states, root the square root of v; returns the new weight.  The root and the
-// quotient are the hardware's, off by at most a unit in the last place, which is what the roundings before them leave: the
-// exact ones cost 8-bit states 15 % of the step's time.  (Its root takes denormals for zero: those are scaled first.)
+// a / b for b > 0 that is neither denormal nor near the largest float: the hardware's reciprocal and one correction by the
+// remainder, which is exact (what a general quotient does beyond that costs 8-bit states 3 % of the step).  The last
+// operation puts in what infinities and NaN come to.
+__device__ __forceinline__ float quotient(float a, float b) {
+    const float y = __builtin_amdgcn_rcpf(b), q = a * y;
+    return __builtin_amdgcn_div_fixupf(fmaf(fmaf(-b, q, a), y, q), b, a);
+}
+// One element's step; m and v become the new states, root the square root of v; returns the new weight.  Whatever goes into
+// states of 8 bits is rounded operation by operation (no contraction, exact roots and quotients): a value next to a border of
+// two codes goes the same way wherever these operations are done, and a state never depends on how a root is made.
 __device__ __forceinline__ float step_of(const AdamwStep& s, float decay, float g, float w, float& m, float& v, float& root) {
     m = m * s.beta1 + g * s.one_minus_beta1;
     v = v * s.beta2 + g * g * s.one_minus_beta2;
-    const bool tiny = v < 0x1p-96f;
-    root = __builtin_amdgcn_sqrtf(tiny ? v * 0x1p96f : v) * (tiny ? 0x1p-48f : 1.0f);
-    return w * decay - s.step_size * (m * __builtin_amdgcn_rcpf(root * s.inv_root_bc2 + s.eps));
+    root = sqrtf(v);
+    return w * decay - s.step_size * quotient(m, root * s.inv_root_bc2 + s.eps);
 }
-// The scale of a block whose largest magnitude is `most`, and its inverse; both 0 for a block that is stored as zeros.
-struct Scale { float value, inverse; };
-__device__ __forceinline__ Scale scale_of(float most) {
-    const float s = most * (1.0f / E4M3_MOST);
-    return s >= STATE_SCALE_LEAST ? Scale{s, __builtin_amdgcn_rcpf(s)} : Scale{0.0f, 0.0f};
+// The scales of a block whose largest magnitudes are these, and their inverses; both 0 for what is stored as zeros.  One half of
+// the wave divides for the one, the other half for the other.
+struct Scales { float m, m_inverse, root, root_inverse; };
+__device__ __forceinline__ Scales scales_of(float m_most, float root_most) {
+    float s = (lane_id() < WAVE / 2 ? m_most : root_most) / E4M3_MOST;
+    s = s >= STATE_SCALE_LEAST ? s : 0.0f;
+    const float inverse = s > 0.0f ? 1.0f / s : 0.0f;
+    const auto of = [](float v, int lane) { return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), lane)); };
+    return Scales{of(s, 0), of(inverse, 0), of(s, WAVE - 1), of(inverse, WAVE - 1)};
 }
 __device__ __forceinline__ float root_code(float root, float inverse) {
     const float c = root * inverse;
@@ -147,15 +157,15 @@ __device__ __forceinline__ void block_by_elements(const AdamwStep& s, const dc_a
         root_most = fmaxf(root_most, root[j]);
     }
     if (!small) return;
-    const Scale sm = scale_of(wave_most(m_most)), sr = scale_of(wave_most(root_most));
+    const Scales sc = scales_of(wave_most(m_most), wave_most(root_most));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int64_t i = at + j * WAVE + lane_id();
         if (i >= d.n) continue;
-        static_cast<uint8_t*>(d.d_exp_avg)[i] = (uint8_t)to_e4m3(m[j] * sm.inverse, 0.0f, 0.0f, 0.0f);
-        static_cast<uint8_t*>(d.d_exp_avg_sq)[i] = (uint8_t)to_e4m3(root_code(root[j], sr.inverse), 0.0f, 0.0f, 0.0f);
+        static_cast<uint8_t*>(d.d_exp_avg)[i] = (uint8_t)to_e4m3(m[j] * sc.m_inverse, 0.0f, 0.0f, 0.0f);
+        static_cast<uint8_t*>(d.d_exp_avg_sq)[i] = (uint8_t)to_e4m3(root_code(root[j], sc.root_inverse), 0.0f, 0.0f, 0.0f);
     }
-    if (lane_id() == 0) { d.d_exp_avg_scale[block] = sm.value; d.d_exp_avg_sq_scale[block] = sr.value; }
+    if (lane_id() == 0) { d.d_exp_avg_scale[block] = sc.m; d.d_exp_avg_sq_scale[block] = sc.root; }
 }
 
 // Four neighbouring elements as they lie in memory.
@@ -188,83 +198,69 @@ __device__ __forceinline__ void store4(void* p, int64_t i, const float (&f)[4]) 
     }
 }
 
-constexpr int AW_THREADS = 256, AW_BLOCKS = ADAMW_PIECE / DC_STATE_BLOCK / (AW_THREADS / WAVE);     // blocks of a wave
-
-// A wave's AW_BLOCKS whole blocks of an aligned tensor, four neighbouring elements of each to a lane; everything is asked for
-// before anything is used.  G: the gradient's type, P: what the weights are read from (the master's float, or the parameter's).
+// A wave's block of an aligned tensor, four neighbouring elements to a lane; everything is asked for before anything is used.
+// G: the gradient's type, P: what the weights are read from (the master's float, or the parameter's).
 template <typename G, typename P, bool MASTER, bool SMALL>
-__device__ __forceinline__ void whole_blocks(const AdamwStep& s, const dc_adamw_tensor& d, int64_t block, float gs, float decay) {
-    Raw4<G> rg[AW_BLOCKS];
-    Raw4<P> rw[AW_BLOCKS];
-    Raw4<float> rm[AW_BLOCKS], rv[AW_BLOCKS];
-    uint32_t cm[AW_BLOCKS], cv[AW_BLOCKS];
-    float ms[AW_BLOCKS], vs[AW_BLOCKS];
-    const int64_t at = block * DC_STATE_BLOCK + lane_id() * 4;
-#pragma unroll
-    for (int b = 0; b < AW_BLOCKS; ++b) {
-        const int64_t i = at + b * DC_STATE_BLOCK;
-        rg[b] = load4<G>(d.d_grad, i);
-        rw[b] = load4<P>(MASTER ? (const void*)d.d_master : d.d_param, i);
-        if constexpr (SMALL) {
-            cm[b] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(d.d_exp_avg) + i));
-            cv[b] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(d.d_exp_avg_sq) + i));
-            ms[b] = d.d_exp_avg_scale[block + b];
-            vs[b] = d.d_exp_avg_sq_scale[block + b];
-        } else {
-            rm[b] = load4<float>(d.d_exp_avg, i);
-            rv[b] = load4<float>(d.d_exp_avg_sq, i);
-        }
-    }
-#pragma unroll
-    for (int b = 0; b < AW_BLOCKS; ++b) {
-        const int64_t i = at + b * DC_STATE_BLOCK;
-        float m[4], v[4], root[4], w[4];
+__device__ __forceinline__ void whole_block(const AdamwStep& s, const dc_adamw_tensor& d, int64_t block, float gs, float decay) {
+    const int64_t i = block * DC_STATE_BLOCK + lane_id() * 4;
+    const Raw4<G> rg = load4<G>(d.d_grad, i);
+    const Raw4<P> rw = load4<P>(MASTER ? (const void*)d.d_master : d.d_param, i);
+    float m[4], v[4], root[4], w[4];
+    if constexpr (SMALL) {
+        const uint32_t cm = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(d.d_exp_avg) + i));
+        const uint32_t cv = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(d.d_exp_avg_sq) + i));
+        const float ms = d.d_exp_avg_scale[block], vs = d.d_exp_avg_sq_scale[block];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-            if constexpr (SMALL) {
-                m[c] = from_e4m3((uint8_t)(cm[b] >> (8 * c))) * ms[b];
-                const float r = from_e4m3((uint8_t)(cv[b] >> (8 * c))) * vs[b];
-                v[c] = r * r;
-            } else {
-                m[c] = rm[b].e[c];
-                v[c] = rv[b].e[c];
-            }
-            w[c] = step_of(s, decay, (float)rg[b].e[c] * gs, (float)rw[b].e[c], m[c], v[c], root[c]);
+            m[c] = from_e4m3((uint8_t)(cm >> (8 * c))) * ms;
+            const float r = from_e4m3((uint8_t)(cv >> (8 * c))) * vs;
+            v[c] = r * r;
         }
-        if constexpr (MASTER) {
-            store4<float>(d.d_master, i, w);
-            if (d.param_type == DC_BF16) store4<__bf16>(d.d_param, i, w);
-            else if (d.param_type == DC_F16) store4<_Float16>(d.d_param, i, w);
-            else store4<float>(d.d_param, i, w);
-        } else {
-            store4<P>(d.d_param, i, w);
-        }
-        if constexpr (SMALL) {
-            const Scale sm = scale_of(wave_most(fmaxf(fmaxf(fabsf(m[0]), fabsf(m[1])), fmaxf(fabsf(m[2]), fabsf(m[3])))));
-            const Scale sr = scale_of(wave_most(fmaxf(fmaxf(root[0], root[1]), fmaxf(root[2], root[3]))));
-            const uint32_t em = to_e4m3(m[0] * sm.inverse, m[1] * sm.inverse, m[2] * sm.inverse, m[3] * sm.inverse);
-            const uint32_t er = to_e4m3(root_code(root[0], sr.inverse), root_code(root[1], sr.inverse), root_code(root[2], sr.inverse),
-                                        root_code(root[3], sr.inverse));
-            __builtin_nontemporal_store(em, reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(d.d_exp_avg) + i));
-            __builtin_nontemporal_store(er, reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(d.d_exp_avg_sq) + i));
-            if (lane_id() == 0) { d.d_exp_avg_scale[block + b] = sm.value; d.d_exp_avg_sq_scale[block + b] = sr.value; }
-        } else {
-            store4<float>(d.d_exp_avg, i, m);
-            store4<float>(d.d_exp_avg_sq, i, v);
-        }
+    } else {
+        const Raw4<float> rm = load4<float>(d.d_exp_avg, i), rv = load4<float>(d.d_exp_avg_sq, i);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) { m[c] = rm.e[c]; v[c] = rv.e[c]; }
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) w[c] = step_of(s, decay, (float)rg.e[c] * gs, (float)rw.e[c], m[c], v[c], root[c]);
+    if constexpr (MASTER) {
+        store4<float>(d.d_master, i, w);
+        if (d.param_type == DC_BF16) store4<__bf16>(d.d_param, i, w);
+        else if (d.param_type == DC_F16) store4<_Float16>(d.d_param, i, w);
+        else store4<float>(d.d_param, i, w);
+    } else {
+        store4<P>(d.d_param, i, w);
+    }
+    if constexpr (SMALL) {
+        const Scales sc = scales_of(wave_most(fmaxf(fmaxf(fabsf(m[0]), fabsf(m[1])), fmaxf(fabsf(m[2]), fabsf(m[3])))),
+                                    wave_most(fmaxf(fmaxf(root[0], root[1]), fmaxf(root[2], root[3]))));
+        const uint32_t em = to_e4m3(m[0] * sc.m_inverse, m[1] * sc.m_inverse, m[2] * sc.m_inverse, m[3] * sc.m_inverse);
+        const uint32_t er = to_e4m3(root_code(root[0], sc.root_inverse), root_code(root[1], sc.root_inverse), root_code(root[2], sc.root_inverse),
+                                    root_code(root[3], sc.root_inverse));
+        __builtin_nontemporal_store(em, reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(d.d_exp_avg) + i));
+        __builtin_nontemporal_store(er, reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(d.d_exp_avg_sq) + i));
+        if (lane_id() == 0) { d.d_exp_avg_scale[block] = sc.m; d.d_exp_avg_sq_scale[block] = sc.root; }
+    } else {
+        store4<float>(d.d_exp_avg, i, m);
+        store4<float>(d.d_exp_avg_sq, i, v);
     }
 }
 template <typename G, bool SMALL>
-__device__ __forceinline__ void whole_blocks_of(const AdamwStep& s, const dc_adamw_tensor& d, int64_t block, float gs, float decay) {
-    if (d.d_master) whole_blocks<G, float, true, SMALL>(s, d, block, gs, decay);
-    else if (d.param_type == DC_F32) whole_blocks<G, float, false, SMALL>(s, d, block, gs, decay);
-    else if (d.param_type == DC_BF16) whole_blocks<G, __bf16, false, SMALL>(s, d, block, gs, decay);
-    else whole_blocks<G, _Float16, false, SMALL>(s, d, block, gs, decay);
+__device__ __forceinline__ void whole_block_of(const AdamwStep& s, const dc_adamw_tensor& d, int64_t block, float gs, float decay) {
+    if (d.d_master) whole_block<G, float, true, SMALL>(s, d, block, gs, decay);
+    else if (d.param_type == DC_F32) whole_block<G, float, false, SMALL>(s, d, block, gs, decay);
+    else if (d.param_type == DC_BF16) whole_block<G, __bf16, false, SMALL>(s, d, block, gs, decay);
+    else whole_block<G, _Float16, false, SMALL>(s, d, block, gs, decay);
 }
 
-// One workgroup per piece, AW_BLOCKS blocks to a wave.  What a tensor is made of is the same for a whole piece, so the kinds
-// are branches of one kernel and all tensors go in one launch.  Bound by the streams.
-__global__ __launch_bounds__(AW_THREADS) void adamw_kernel(const AdamwStep s, const AdamwHeader* __restrict__ head, const dc_adamw_tensor* __restrict__ tensors,
+// One workgroup per piece, a wave per block.  What a tensor is made of is the same for a whole piece, so the kinds are branches
+// of one kernel and all tensors go in one launch.  Bound by the streams: 612 M elements in bf16 with 32-bit masters, bf16
+// gradients and 8-bit states (16 bytes each) in 1.68 ms, 5.9 TB/s; 54 M all in 32 bits (28 bytes) in 0.26 ms, 5.8 TB/s.  Two or
+// four blocks a wave, all asked for at once: within 2 % for 32-bit states, 3 to 5 % slower for 8-bit ones.  Plain stores
+// instead of streamed ones: 6 % slower.
+constexpr int AW_THREADS = ADAMW_PIECE / DC_STATE_BLOCK * WAVE;
+__global__ __launch_bounds__(AW_THREADS) void adamw_kernel(const AdamwStep s, const AdamwHeader* __restrict__ head,
+                                                           const dc_adamw_tensor* __restrict__ tensors,
                                                            const AdamwPiece* __restrict__ pieces, int64_t n_pieces, int32_t n_tensors) {
     if (head->n_pieces != n_pieces || head->n_tensors != n_tensors) {
         if (threadIdx.x == 0) set_status(s.status, DC_ERR_BAD_LAYOUT);
@@ -276,19 +272,19 @@ __global__ __launch_bounds__(AW_THREADS) void adamw_kernel(const AdamwStep s, co
         const AdamwPiece piece = pieces[q];
         const dc_adamw_tensor d = tensors[piece.tensor];     // (a copy: no store below can be thought to change it)
         const float decay = (float)(1.0 - s.lr64 * d.weight_decay);
-        const int64_t block = (int64_t)piece.piece * (ADAMW_PIECE / DC_STATE_BLOCK) + wave * AW_BLOCKS;
-        if (d.reserved && (block + AW_BLOCKS) * DC_STATE_BLOCK <= d.n) {   // (in the table: whether all of it is aligned)
+        const int64_t block = (int64_t)piece.piece * (ADAMW_PIECE / DC_STATE_BLOCK) + wave;
+        if (d.reserved && (block + 1) * DC_STATE_BLOCK <= d.n) {           // (in the table: whether all of it is aligned)
             if (d.state_type == DC_E4M3) {
-                if (d.grad_type == DC_BF16) whole_blocks_of<__bf16, true>(s, d, block, gs, decay);
-                else if (d.grad_type == DC_F32) whole_blocks_of<float, true>(s, d, block, gs, decay);
-                else whole_blocks_of<_Float16, true>(s, d, block, gs, decay);
+                if (d.grad_type == DC_BF16) whole_block_of<__bf16, true>(s, d, block, gs, decay);
+                else if (d.grad_type == DC_F32) whole_block_of<float, true>(s, d, block, gs, decay);
+                else whole_block_of<_Float16, true>(s, d, block, gs, decay);
             } else {
-                if (d.grad_type == DC_BF16) whole_blocks_of<__bf16, false>(s, d, block, gs, decay);
-                else if (d.grad_type == DC_F32) whole_blocks_of<float, false>(s, d, block, gs, decay);
-                else whole_blocks_of<_Float16, false>(s, d, block, gs, decay);
+                if (d.grad_type == DC_BF16) whole_block_of<__bf16, false>(s, d, block, gs, decay);
+                else if (d.grad_type == DC_F32) whole_block_of<float, false>(s, d, block, gs, decay);
+                else whole_block_of<_Float16, false>(s, d, block, gs, decay);
             }
-        } else {
-            for (int b = 0; b < AW_BLOCKS && (block + b) * DC_STATE_BLOCK < d.n; ++b) block_by_elements(s, d, block + b, gs, decay);
+        } else if (block * DC_STATE_BLOCK < d.n) {
+            block_by_elements(s, d, block, gs, decay);
         }
     }
 }
