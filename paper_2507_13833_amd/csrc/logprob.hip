@@ -108,7 +108,8 @@ __device__ __forceinline__ uint64_t wave_nth_key(uint64_t key, int n) {
     return least | 0xFF000000u | wave_nth(place & 0xFFFFFFu, same, 24, left);
 }
 // A key that n of the workgroup's keys are not below, near the n-th greatest: every wave's nth key has nth keys that are not
-// below it, so many waves together have n.  0 where there are fewer.  Every thread gets it; the candidates and the chosen are none.
+// below it, so many waves together have n.  Where too few waves have as many (a short row), one that has n by itself.  0 where
+// there is none either.  Every thread gets it; the candidates and the chosen are none.
 template <int BITS, int THREADS>
 __device__ __forceinline__ uint64_t least_key(TopLds<THREADS>& t, uint64_t key, int n) {
     constexpr int WAVES = THREADS / WAVE;
@@ -117,7 +118,14 @@ __device__ __forceinline__ uint64_t least_key(TopLds<THREADS>& t, uint64_t key, 
     if (lane_id() == 0) t.tmp[threadIdx.x / WAVE] = mine;
     if (threadIdx.x == 0) { t.n_candidates = 0; t.n_chosen = 0; }
     __syncthreads();
-    return wave_nth_key<BITS>(lane_id() < WAVES ? t.tmp[lane_id()] : 0ull, of_waves);
+    uint64_t least = wave_nth_key<BITS>(lane_id() < WAVES ? t.tmp[lane_id()] : 0ull, of_waves);
+    if (least != 0) return least;
+    __syncthreads();
+    const uint64_t alone = wave_nth_key<BITS>(key, n);
+    if (lane_id() == 0) t.tmp[threadIdx.x / WAVE] = alone;
+    __syncthreads();
+    for (int w = 0; w < WAVES; ++w) least = t.tmp[w] > least ? t.tmp[w] : least;
+    return least;
 }
 template <int THREADS>
 __device__ __forceinline__ void add_candidate(TopLds<THREADS>& t, uint64_t key) {
@@ -203,7 +211,11 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(const LogprobArgs a, i
         u32x4 next[LP_AT_ONCE];
         const auto ask = [&](int32_t c) {
 #pragma unroll
-            for (int j = 0; j < LP_AT_ONCE; ++j) next[j] = __builtin_nontemporal_load(body + min(c + j * THREADS, chunks - 1));
+            for (int j = 0; j < LP_AT_ONCE; ++j) {
+                const u32x4* p = body + min(c + j * THREADS, chunks - 1);
+                if constexpr (TOP) next[j] = *p;               // (the caches keep what may be read again)
+                else next[j] = __builtin_nontemporal_load(p);
+            }
         };
         if (tid < chunks) ask(tid);
         if (tid < head) one((float)x[tid], v0 + tid);
@@ -300,16 +312,25 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(const LogprobArgs a, i
             }
             __syncthreads();
             const int32_t chosen = (int32_t)top.n_chosen;
-            const int32_t turns = (chunks + THREADS - 1) / THREADS;
-            for (int32_t q = tid; q < chosen * turns; q += THREADS) {
-                const int32_t c = q / chosen * THREADS + top.chosen[q % chosen];
-                if (c >= chunks) continue;
-                float f[N];
-                unpack<T>(body[c], f);
-                const int32_t place = v0 + head + c * N;
+            const int32_t turns = (chunks + THREADS - 1) / THREADS, again = chosen * turns;
+            for (int32_t q = tid; q < again; q += LP_AT_ONCE * THREADS) {
+                int32_t c[LP_AT_ONCE];
 #pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (top_key(f[i], place) >= least) add_candidate(top, top_key(f[i], place + i));
+                for (int j = 0; j < LP_AT_ONCE; ++j) {
+                    const int32_t at_q = min(q + j * THREADS, again - 1), turn = at_q / chosen;
+                    c[j] = q + j * THREADS < again ? turn * THREADS + top.chosen[at_q - turn * chosen] : chunks;
+                    next[j] = body[min(c[j], chunks - 1)];
+                }
+#pragma unroll
+                for (int j = 0; j < LP_AT_ONCE; ++j) {
+                    if (c[j] >= chunks) continue;
+                    float f[N];
+                    unpack<T>(next[j], f);
+                    const int32_t place = v0 + head + c[j] * N;
+#pragma unroll
+                    for (int i = 0; i < N; ++i)
+                        if (top_key(f[i], place) >= least) add_candidate(top, top_key(f[i], place + i));
+                }
             }
             rank_candidates(top, a.n_top, [&](auto visit) {
                 for (int32_t v = tid; v < n; v += THREADS) visit(top_key((float)x[v], v0 + v));
@@ -319,12 +340,13 @@ __global__ __launch_bounds__(THREADS) void logprob_kernel(const LogprobArgs a, i
     }
 }
 
-// One workgroup per row: its parts' sums and lists as one.
+// One wave per row: its parts' sums and lists as one.
+constexpr int LJ_AT_ONCE = 8;                    // keys asked for at once
 template <typename T>
-__global__ __launch_bounds__(LP_THREADS) void logprob_join_kernel(const LogprobArgs a, int32_t parts, const char* ws) {
-    __shared__ float red[LP_THREADS / WAVE];
-    __shared__ TopLds<LP_THREADS> top;
+__global__ __launch_bounds__(WAVE) void logprob_join_kernel(const LogprobArgs a, int32_t parts, const char* __restrict__ ws) {
+    __shared__ TopLds<WAVE> top;
     const float k = a.inv_t * LOG2E;
+    const int lane = threadIdx.x;
     for (int64_t r = blockIdx.x; r < a.n_rows; r += gridDim.x) {
         if (a.mask && a.mask[r] == 0) {
             write_nothing(a, r);
@@ -337,56 +359,67 @@ __global__ __launch_bounds__(LP_THREADS) void logprob_join_kernel(const LogprobA
         const char* first = ws + r * parts * bytes;
         const auto sums_of = [&](int p) { return reinterpret_cast<const PartHead*>(first + p * bytes)->sums; };
         const auto keys_of = [&](int p) { return reinterpret_cast<const uint64_t*>(first + p * bytes + sizeof(PartHead)); };
+        // every part's nth key has nth keys of that part that are not below it: so many parts together have n_top (of the
+        // first parts alone where there are more than lanes)
+        const int nth = max(1, min(a.n_top, (2 * a.n_top + parts - 1) / min(parts, WAVE))), of_parts = (a.n_top + nth - 1) / nth;
+        const uint64_t bound = a.n_top > 0 && lane < parts ? keys_of(lane)[nth - 1] : 0ull;
         RowSums all = {-INFINITY, 0.0f, 0.0f};
-        for (int p = threadIdx.x; p < parts; p += LP_THREADS) all.m = fmaxf(all.m, sums_of(p).m);
-        all.m = block_reduce(all.m, red, wave_max, [](float p, float q) { return fmaxf(p, q); });
-        for (int p = threadIdx.x; p < parts; p += LP_THREADS) {
+        for (int p = lane; p < parts; p += WAVE) all.m = fmaxf(all.m, sums_of(p).m);
+        all.m = wave_max(all.m);
+        for (int p = lane; p < parts; p += WAVE) {
             const RowSums x = sums_of(p);
             const float d = (x.m - all.m) * k, f = __builtin_amdgcn_exp2f(d);
             all.s += f * x.s;
             all.u += f * (x.u + fmaxf(d, -1e4f) * x.s);
         }
-        const auto add = [](float p, float q) { return p + q; };
-        all.s = block_reduce(all.s, red, wave_sum, add);
-        all.u = block_reduce(all.u, red, wave_sum, add);
+        all.s = wave_sum(all.s);
+        all.u = wave_sum(all.u);
         const RowResult w = finish(all, a.inv_t);
-        if (threadIdx.x == 0) {
+        if (lane == 0) {
             if (!in) set_status(a.status, DC_ERR_TOKEN_RANGE);
             write_row(a, r, w, in, x_token);
+            top.n_candidates = 0;
         }
         if (a.n_top == 0) continue;
-        // every part's nth key has nth keys of that part that are not below it: so many parts together have n_top
-        const int nth = min(a.n_top, (2 * a.n_top + parts - 1) / min(parts, WAVE)), of_parts = (a.n_top + nth - 1) / nth;
-        // (of the first parts: a wave's worth of them, so that one wave's answer will do)
-        const uint64_t least = wave_nth_key<SORT_BITS<T>>(lane_id() < parts ? keys_of(lane_id())[nth - 1] : 0ull, of_parts);
-        if (threadIdx.x == 0) { top.n_candidates = 0; }
+        const uint64_t least = wave_nth_key<SORT_BITS<T>>(bound, of_parts);
         __syncthreads();
-        for (int q = threadIdx.x; q < parts * a.n_top; q += LP_THREADS) {
-            const uint64_t key = keys_of(q / a.n_top)[q % a.n_top];
-            if (key != 0 && key >= least) add_candidate(top, key);
+        const int32_t n_keys = parts * a.n_top;
+        for (int32_t q = lane; q < n_keys; q += LJ_AT_ONCE * WAVE) {
+            uint64_t key[LJ_AT_ONCE];
+#pragma unroll
+            for (int j = 0; j < LJ_AT_ONCE; ++j) {
+                const int32_t at = min(q + j * WAVE, n_keys - 1), p = at / a.n_top;
+                key[j] = keys_of(p)[at - p * a.n_top];
+            }
+#pragma unroll
+            for (int j = 0; j < LJ_AT_ONCE; ++j)
+                if (q + j * WAVE < n_keys && key[j] != 0 && key[j] >= least) add_candidate(top, key[j]);
         }
         rank_candidates(top, a.n_top, [&](auto visit) {
-            for (int q = threadIdx.x; q < parts * a.n_top; q += LP_THREADS) visit(keys_of(q / a.n_top)[q % a.n_top]);
+            for (int32_t q = lane; q < n_keys; q += WAVE) visit(keys_of(q / a.n_top)[q % a.n_top]);
         }, [&](int i, uint64_t key) { write_top(a, r, i, w, key); });
     }
 }
 
 // How a row is cut.  Many rows: a workgroup of LP_THREADS each, several to a compute unit, so that one's reductions and
-// ranking run beside another's loads.  At most one row to a compute unit: a larger workgroup, or, where one unit's loads take
+// ranking run beside another's loads (a larger one for alternatives of rows above 512 KB, whose second look it shortens).  At most one row to a compute unit: a larger workgroup, or, where one unit's loads take
 // longer than a second launch does, parts of at least LP_LEAST logits, about LP_GROUPS of them.  Measured, us, no
 // alternatives / 20 of them, the two sides of each border:
 //   300 x 32000 bf16      narrow  8.7 / 15.3   wide  11.7 / 20.8
 //   64 x 32000 f32        wide    7.4 / 11.3   narrow 8.8 / 14.5
 //   64 x 12000 f32        narrow  8.0 /  9.0   wide   7.5 /  9.9
+//   1000 x 152064 f32     narrow 91.6 /  171   wide  95.5 /  130
+//   1000 x 152064 bf16    narrow 51.0 / 83.8   wide  62.8 / 87.1
 //   1 x 152064 f32        parts   9.6 / 13.9   wide  15.1 / 20.9
-//   64 x 152064 f32       parts  13.8 / 23.3   wide  16.8 / 24.3
+//   64 x 152064 f32       parts  13.8 / 19.2   wide  16.8 / 24.3
 //   256 x 152064 f32      wide   27.7 / 35.5   parts 31.1 / 51.3
 //   1 x 32000 f32         wide    7.4 / 10.3   parts  9.8 / 13.8
-constexpr int64_t LP_GROUPS = 1024, LP_LEAST = 4096;
+// 1024 parts in all instead of 512: 64 x 152064 f32 with 20 alternatives 21.2 us.
+constexpr int64_t LP_GROUPS = 512, LP_LEAST = 4096;
 struct Cut { int32_t parts, per_part; bool wide; };
-static Cut cut_of(int64_t n_rows, int32_t vocab, int32_t type) {
+static Cut cut_of(int64_t n_rows, int32_t vocab, int32_t type, int32_t n_top) {
     const int64_t bytes = (int64_t)vocab * (type == DC_F32 ? 4 : 2);
-    if (n_rows > 256 || bytes <= 1 << 16) return Cut{1, vocab, false};
+    if (n_rows > 256 || bytes <= 1 << 16) return Cut{1, vocab, n_top > 0 && bytes > 1 << 19};
     if (n_rows > 64 || bytes <= 1 << 17) return Cut{1, vocab, true};
     int64_t parts = n_rows > 0 ? (LP_GROUPS + n_rows - 1) / n_rows : 1;
     const int64_t most = (vocab + LP_LEAST - 1) / LP_LEAST;
@@ -396,13 +429,13 @@ static Cut cut_of(int64_t n_rows, int32_t vocab, int32_t type) {
 }
 
 size_t logprob_workspace_bytes(int64_t n_rows, int32_t vocab, int32_t type, int32_t n_top) {
-    const Cut c = cut_of(n_rows, vocab, type);
+    const Cut c = cut_of(n_rows, vocab, type, n_top);
     return c.parts > 1 ? (size_t)n_rows * c.parts * part_bytes(n_top) : 0;
 }
 
 hipError_t launch_logprob(const LogprobArgs& a, int32_t type, void* d_ws, hipStream_t st) {
     if (a.n_rows == 0) return hipSuccess;
-    const Cut c = cut_of(a.n_rows, a.vocab, type);
+    const Cut c = cut_of(a.n_rows, a.vocab, type, a.n_top);
     const int64_t units = a.n_rows * c.parts;
     const unsigned grid = (unsigned)(units < (1 << 20) ? units : 1 << 20), rows = (unsigned)(a.n_rows < (1 << 20) ? a.n_rows : 1 << 20);
     return with_type(type, [&](auto e) {
@@ -417,7 +450,7 @@ hipError_t launch_logprob(const LogprobArgs& a, int32_t type, void* d_ws, hipStr
         else if (a.entropy) go(std::true_type{}, std::false_type{});
         else if (a.n_top) go(std::false_type{}, std::true_type{});
         else go(std::false_type{}, std::false_type{});
-        if (c.parts > 1) logprob_join_kernel<T><<<rows, LP_THREADS, 0, st>>>(a, c.parts, ws);
+        if (c.parts > 1) logprob_join_kernel<T><<<rows, WAVE, 0, st>>>(a, c.parts, ws);
         return hipGetLastError();
     });
 }
