@@ -96,6 +96,7 @@ extern "C" {
 #define DC_MAX_SRC_SHARDS 16
 #define DC_MAX_SEQ_LEN    (1 << 24)
 #define DC_MAX_VOCAB      (1 << 24) /* columns of logits, rows of an embedding table   */
+#define DC_MAX_DIM        65536     /* columns of an embedding table                   */
 #define DC_MAX_TOP        64        /* alternatives of dc_token_logprob                */
 #define DC_MAX_TENSORS    65536     /* of one dc_adamw                                 */
 #define DC_STATE_BLOCK    256       /* elements that share a scale of an 8-bit state   */
@@ -431,7 +432,8 @@ dc_status dc_token_logprob(const dc_matrix* logits, double temperature, const in
  * dc_token_logprob left them for the same logits, temperature, tokens and mask.  Computed in 32 bits and rounded once to
  * grad_logits' type, which is the logits' (same shape, own row_stride).  grad_logits may be the logits' own memory (same
  * d_data and row_stride): the gradient then takes their place; it must not overlap them otherwise.
- * A row with mask byte 0, and one whose a and b are both zero, gets +0 everywhere and its logits are not read.
+ * A row with mask byte 0, and one whose a and b are both zero, gets +0 everywhere and its logits are not read.  A row
+ * without a distribution (NaN in d_row_stat) gets NaN.
  * d_token may be NULL: the first term is then -a_r * p_v.
  * Host errors: INVALID_ARG, UNSUPPORTED_SIZE, HIP.  Device errors: TOKEN_RANGE (the row's gradient is that without the
  * token's own 1).
@@ -445,7 +447,8 @@ dc_status dc_token_logprob_backward(const dc_matrix* logits, double temperature,
  * Embedding of the packed token ids: out[t, :] = scale * weight[d_token[t], :] for the n_rows tokens of out, the product
  * in 32 bits, rounded once to out's type (any of f32, bf16, f16, whatever the table's).  vocabulary = weight->n_rows.
  * d_token[t] == DC_NO_TOKEN: a row of +0.
- * Host errors: INVALID_ARG, UNSUPPORTED_SIZE, HIP.  Device errors: TOKEN_RANGE (that row becomes +0).
+ * Host errors: INVALID_ARG, UNSUPPORTED_SIZE (more than DC_MAX_VOCAB rows or DC_MAX_DIM columns), HIP.  Device errors:
+ * TOKEN_RANGE (that row becomes +0).
  */
 dc_status dc_embedding(const dc_matrix* weight, const int32_t* d_token, double scale, const dc_matrix* out,
                        int32_t* d_status, void* hip_stream);
@@ -456,8 +459,8 @@ dc_status dc_embedding(const dc_matrix* weight, const int32_t* d_token, double s
  * every row of grad_weight is written, those without a token with +0.  accumulate != 0: the sum is added to the row in 32
  * bits before it is rounded, and rows without a token are not touched.  Tokens equal to DC_NO_TOKEN add nothing.
  * d_ws: 256-byte aligned, dc_embedding_backward_workspace_bytes(grad_out, grad_weight) bytes; holds nothing the caller
- * needs afterwards.  Up to 2^24 tokens.
- * Host errors: INVALID_ARG, UNSUPPORTED_SIZE, WORKSPACE, HIP.  Device errors: TOKEN_RANGE (that token adds nothing).
+ * needs afterwards.
+ * Host errors: INVALID_ARG, UNSUPPORTED_SIZE (as above, or more than 2^24 tokens), WORKSPACE, HIP.  Device errors: TOKEN_RANGE (that token adds nothing).
  */
 size_t dc_embedding_backward_workspace_bytes(const dc_matrix* grad_out, const dc_matrix* grad_weight);
 dc_status dc_embedding_backward(const dc_matrix* grad_out, const int32_t* d_token, double scale, int32_t accumulate,

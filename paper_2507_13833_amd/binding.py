@@ -22,6 +22,7 @@ DC_MAX_FIELDS = 8
 DC_MAX_SRC_SHARDS = 16
 DC_REPACK_NOALLOC_WS_BYTES = 8 << 20
 DC_MAX_VOCAB = 1 << 24
+DC_MAX_DIM = 65536
 DC_MAX_TOP = 64
 DC_MAX_TENSORS = 65536
 DC_STATE_BLOCK = 256

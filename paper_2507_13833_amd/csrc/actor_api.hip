@@ -120,7 +120,7 @@ dc_status dc_embedding(const dc_matrix* weight, const int32_t* d_token, double s
     rc = check_matrix(out);
     if (rc != DC_OK) return rc;
     if (weight->n_cols != out->n_cols || !std::isfinite((float)scale)) return DC_ERR_INVALID_ARG;
-    if (weight->n_rows > DC_MAX_VOCAB) return DC_ERR_UNSUPPORTED_SIZE;
+    if (weight->n_rows > DC_MAX_VOCAB || weight->n_cols > DC_MAX_DIM) return DC_ERR_UNSUPPORTED_SIZE;
     if (out->n_rows > 0 && (!d_token || !aligned_to(d_token, 4))) return DC_ERR_INVALID_ARG;
     const EmbeddingArgs a = {weight->d_data, out->d_data, weight->row_stride, out->row_stride, out->n_rows, out->n_cols,
                              (int32_t)weight->n_rows, (float)scale, d_token, d_status};
@@ -130,7 +130,7 @@ dc_status dc_embedding(const dc_matrix* weight, const int32_t* d_token, double s
 
 size_t dc_embedding_backward_workspace_bytes(const dc_matrix* grad_out, const dc_matrix* grad_weight) {
     if (!grad_out || !grad_weight || grad_out->n_rows < 0 || grad_out->n_rows > EMB_GRAD_MAX_TOKENS || grad_weight->n_rows < 0 ||
-        grad_weight->n_rows > DC_MAX_VOCAB || grad_out->n_cols < 0)
+        grad_weight->n_rows > DC_MAX_VOCAB || grad_out->n_cols < 0 || grad_out->n_cols > DC_MAX_DIM)
         return 0;
     return embedding_grad_workspace_bytes(grad_out->n_rows, grad_out->n_cols);
 }
@@ -143,7 +143,9 @@ dc_status dc_embedding_backward(const dc_matrix* grad_out, const int32_t* d_toke
     rc = check_matrix(grad_weight);
     if (rc != DC_OK) return rc;
     if (grad_weight->n_cols != grad_out->n_cols || !std::isfinite((float)scale)) return DC_ERR_INVALID_ARG;
-    if (grad_weight->n_rows > DC_MAX_VOCAB || grad_out->n_rows > EMB_GRAD_MAX_TOKENS) return DC_ERR_UNSUPPORTED_SIZE;
+    if (grad_weight->n_rows > DC_MAX_VOCAB || grad_weight->n_cols > DC_MAX_DIM || grad_out->n_rows > EMB_GRAD_MAX_TOKENS ||
+        grad_out->n_rows * grad_out->n_cols > 1LL << 38)                 // (a launch's threads)
+        return DC_ERR_UNSUPPORTED_SIZE;
     if (grad_out->n_rows > 0 && (!d_token || !aligned_to(d_token, 4))) return DC_ERR_INVALID_ARG;
     const size_t need = embedding_grad_workspace_bytes(grad_out->n_rows, grad_out->n_cols);
     if (need > 0 && (!d_ws || !aligned_to(d_ws, 256))) return DC_ERR_INVALID_ARG;

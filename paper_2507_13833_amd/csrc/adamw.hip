@@ -291,7 +291,7 @@ __global__ __launch_bounds__(AW_THREADS) void adamw_kernel(const AdamwStep s, co
 
 hipError_t launch_adamw(const AdamwStep& s, int32_t n_tensors, const AdamwTable& t, int64_t n_pieces, hipStream_t st) {
     if (n_pieces == 0) return hipSuccess;
-    const unsigned grid = (unsigned)(n_pieces < (1 << 23) ? n_pieces : 1 << 23);
+    const unsigned grid = (unsigned)(n_pieces < (1 << 22) ? n_pieces : 1 << 22);     // (2^31 threads)
     adamw_kernel<<<grid, AW_THREADS, 0, st>>>(s, t.head, t.tensors, t.pieces, n_pieces, n_tensors);
     return hipGetLastError();
 }

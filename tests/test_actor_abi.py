@@ -216,3 +216,34 @@ def test_binding_checks_tensors():
     with pytest.raises(TypeError):
         B.AdamwTensors([dict(param=FakeTensor((8,)), grad=FakeTensor((8,)), exp_avg=FakeTensor((8,)),
                              exp_avg_sq=FakeTensor((8,), "torch.float8_e4m3fn"))])
+
+
+def test_workspaces_and_limits():
+    """Sizes whose rows are cut into parts need a workspace; limits of the embedding."""
+    big = mat(rows=2, cols=152064, type_=B.DC_F32)
+    for n_top in (0, 5):
+        need = B.dc_token_logprob_workspace_bytes(big, n_top)
+        assert need > 0
+        args = (big, 1.0, A, None, n_top, A, None, None, A if n_top else None, None)
+        refuses(B.DC_ERR_WORKSPACE, B.dc_token_logprob, *args, A, need - 1, A)
+        refuses(B.DC_ERR_INVALID_ARG, B.dc_token_logprob, *args, A + 16, need, A)
+        refuses(B.DC_ERR_INVALID_ARG, B.dc_token_logprob, *args, None, need, A)
+    wide = mat(rows=9, cols=B.DC_MAX_DIM + 8)
+    refuses(B.DC_ERR_UNSUPPORTED_SIZE, B.dc_embedding, wide, A, 1.0, wide, A)
+    refuses(B.DC_ERR_UNSUPPORTED_SIZE, B.dc_embedding_backward, wide, A, 1.0, 0, wide, A, 1 << 40, A)
+    many = mat(rows=1 << 24, cols=32768)
+    refuses(B.DC_ERR_UNSUPPORTED_SIZE, B.dc_embedding_backward, many, A, 1.0, 0, mat(rows=9, cols=32768), A, 1 << 62, A)
+    assert B.dc_embedding_backward_workspace_bytes(wide, wide) == 0
+    assert B.dc_embedding_backward_workspace_bytes(mat(rows=0, cols=8), mat(rows=9, cols=8)) > 0
+
+
+def test_nothing_to_do_is_no_error():
+    """Calls without rows return before anything is enqueued, whatever their other pointers."""
+    none = mat(rows=0, data=None)
+    B.dc_token_logprob(none, 1.0, None, None, 3, None, None, None, None, None, None, 0, None, stream=0)
+    B.dc_token_logprob_backward(none, 1.0, None, None, None, None, None, None, none, None, stream=0)
+    B.dc_embedding(mat(rows=50), None, 1.0, none, None, stream=0)
+    t = Tensors()
+    need = B.dc_adamw_table_bytes(t)
+    B.dc_adamw_table(t, A, need, stream=0)
+    B.dc_adamw(t, B.make_adamw(1e-3), None, A, need, None, stream=0)

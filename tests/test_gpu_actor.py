@@ -854,3 +854,52 @@ def test_another_stream_and_a_graph(env):
             assert torch.equal(a, b)
         step()                                                # eager work between the replays
         torch.cuda.synchronize()
+
+
+# ---- places that 32 bits do not reach, more rows than a launch has workgroups ----
+
+def test_rows_far_apart(env):
+    """Rows 2^31 elements apart: every place is computed in 64 bits."""
+    torch, B = env
+    far, vocab = 1 << 31, 3001
+    store = torch.empty(3 * far, dtype=torch.bfloat16, device="cuda")
+    x = store.as_strided((3, vocab), (far, 1), 0)
+    v, token, _ = draw_logits(torch, 3, vocab, torch.bfloat16)
+    x.copy_(v)
+    check_logprob(env, x, 1.0, token, None, 5)
+    stat, entropy, gl, ge = grad_inputs(torch, x, 1.0)
+    ref = x.double()
+    check_grad(env, x, x, 1.0, token, None, stat, entropy, gl, ge, reference=ref)
+    x.copy_(v)
+    dense = v.contiguous()
+    ids = torch.tensor([2, 0, 1, 2], dtype=torch.int32, device="cuda")
+    out, st = torch.empty(4, vocab, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.dc_embedding(B.make_matrix(x), ids, 1.0, B.make_matrix(out), st)
+    assert torch.equal(out, dense[ids.long()])
+    B.dc_embedding(B.make_matrix(dense), ids[:3], 1.0, B.make_matrix(x), st)
+    assert torch.equal(x, dense[ids[:3].long()])
+    g = torch.randn(4, vocab, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).bfloat16()
+    check_embedding_grad(env, g, ids, 1.0, False, x)
+    x.copy_(v)
+    check_embedding_grad(env, x, ids[:3], 1.0, True, torch.ones(3, vocab, device="cuda"))
+    assert int(st) == 0
+
+
+def test_more_rows_than_workgroups(env):
+    torch, B = env
+    rows, vocab = (1 << 20) + 77, 3
+    x, token, mask = draw_logits(torch, rows, vocab, torch.bfloat16)
+    check_logprob(env, x, 1.0, token, mask, 2)
+    stat, entropy, gl, ge = grad_inputs(torch, x, 1.0)
+    check_grad(env, x, torch.full_like(x, math.nan), 1.0, token, mask, stat, entropy, gl, ge)
+
+
+@pytest.mark.parametrize("vocab", [1, 4, 9000, 1 << 24])
+def test_embedding_backward_many_tokens(env, vocab):
+    """More tokens than one level of merges takes, ids of one to three digits."""
+    torch, B = env
+    tokens, dim = 300007, 2
+    gen = torch.Generator(device="cuda").manual_seed(vocab)
+    g = torch.randn(tokens, dim, generator=gen, device="cuda")
+    ids = (torch.rand(tokens, generator=gen, device="cuda").double() ** 2 * vocab).int().clamp_(max=vocab - 1)
+    check_embedding_grad(env, g, ids, 1.0, False, torch.ones(vocab, dim, device="cuda"))
