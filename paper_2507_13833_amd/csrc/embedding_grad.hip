@@ -243,7 +243,7 @@ __global__ __launch_bounds__(ADD_THREADS) void add_rows_kernel(const EmbeddingGr
         while (__ballot(lo < hi)) {
             const int32_t step = (hi - lo + FILL_LANES) / (FILL_LANES + 1);
             const int32_t at = lo + (sub + 1) * step - 1;
-            const bool below = at < hi && skey[at] < id;
+            const bool below = at >= lo && at < hi && skey[at] < id;       // (a row that is found asks for nothing)
             const int n = __popc((uint32_t)(__ballot(below) >> (lane - sub)) & ((1u << FILL_LANES) - 1));
             if (lo < hi) {
                 const int32_t next = lo + n * step;

@@ -903,3 +903,14 @@ def test_embedding_backward_many_tokens(env, vocab):
     g = torch.randn(tokens, dim, generator=gen, device="cuda")
     ids = (torch.rand(tokens, generator=gen, device="cuda").double() ** 2 * vocab).int().clamp_(max=vocab - 1)
     check_embedding_grad(env, g, ids, 1.0, False, torch.ones(vocab, dim, device="cuda"))
+
+
+@pytest.mark.parametrize("tokens", [15, 16, 17, 18, 33, 289, 290])
+def test_embedding_backward_rows_below_the_lowest_token(env, tokens):
+    """Rows of the table that lie before all tokens, and rows between two, sought among so few that the searches of one wave
+    end at different steps."""
+    torch, B = env
+    g = torch.randn(tokens, 8, device="cuda", generator=torch.Generator(device="cuda").manual_seed(tokens))
+    for base in (0, 1, 2, 3, 50):
+        ids = (base + 2 * torch.arange(tokens, device="cuda")).int()
+        check_embedding_grad(env, g, ids, 1.0, False, torch.ones(60 + 2 * tokens, 8, device="cuda"))
