@@ -14,7 +14,9 @@ namespace dc {
 constexpr int LP_THREADS = 256, LP_WIDE = 1024;  // of a workgroup: where there are many rows, where there are few
 constexpr int LP_AT_ONCE = 4;                    // 16-byte loads asked for at once
 constexpr int LP_CANDIDATES = 1024;              // of the largest that are ranked in the LDS; more: one by one
-constexpr float LP_FAR = 0x1p120f;               // |k x| from here on: the sums are made again with differences taken first
+// |k M| from here on: the sums are made again with differences taken first.  Below it M2's rounding is at most 1/2, so the
+// exponents k x - M2 stay as small as the true ones; at 2^31 it would be 128, which no float has the power of.
+constexpr float LP_FAR = 0x1p24f;
 
 template <typename T> constexpr int CHUNK_ELEMS = 16 / sizeof(T);
 

@@ -914,3 +914,31 @@ def test_embedding_backward_rows_below_the_lowest_token(env, tokens):
     for base in (0, 1, 2, 3, 50):
         ids = (base + 2 * torch.arange(tokens, device="cuda")).int()
         check_embedding_grad(env, g, ids, 1.0, False, torch.ones(60 + 2 * tokens, 8, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,vocab", [(2, 700), (2, 152064), (300, 33000)])
+@pytest.mark.parametrize("at", [1.1e7, 3e8, 2.5e9, -2.5e9, -1e10, 7e15, -3e22, 1e30, -1e35])
+def test_logprob_of_far_logits(env, at, rows, vocab, dtype):
+    """A row around a large value, and one of such values and a single ordinary logit."""
+    torch, B = env
+    dt = types(torch)[dtype]
+    x, token, _ = draw_logits(torch, rows, vocab, dt)
+    near = torch.tensor(at, device="cuda").to(dt)
+    x[0] = near
+    x[0, ::3] = torch.nextafter(near, torch.zeros_like(near))
+    x[0, vocab // 2:] = -abs(at) * 1.5
+    x[1] = -abs(at)
+    x[1, vocab - 3] = 2.0
+    check_logprob(env, x, 1.0, token, None, 9)
+    check_logprob(env, x, 1e-3, token, None, 0)
+
+
+def test_logprob_of_far_logits_in_one_long_row(env):
+    """Many masked logits before an ordinary one in the same thread: their sum is taken over before it is left behind."""
+    torch, B = env
+    rows, vocab = 257, 1 << 20
+    x = torch.full((rows, vocab), -1e35, dtype=torch.bfloat16, device="cuda")
+    x[:, -5:] = torch.tensor([1.0, 2.0, 0.5, -1.0, 0.25], device="cuda").bfloat16()
+    token = torch.full((rows,), vocab - 4, dtype=torch.int32, device="cuda")
+    check_logprob(env, x, 1.0, token, None, 3)
