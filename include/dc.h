@@ -484,7 +484,7 @@ typedef struct dc_adamw_tensor {
 } dc_adamw_tensor;
 
 typedef struct dc_adamw_params {
-    double  lr, beta1, beta2, eps;   /* lr >= 0, betas in [0, 1), eps > 0                     */
+    double  lr, beta1, beta2, eps;   /* lr >= 0, betas in [0, 1), eps in 2^-100 .. 2^100      */
     int64_t step;                    /* of this call, from 1 (bias correction)                */
 } dc_adamw_params;
 

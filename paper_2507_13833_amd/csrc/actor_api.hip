@@ -181,7 +181,7 @@ dc_status dc_adamw(const dc_adamw_tensor* tensors, int32_t n_tensors, const dc_a
     const dc_status rc = check_tensors(tensors, n_tensors, &n_pieces);
     if (rc != DC_OK) return rc;
     if (!prm || !(prm->lr >= 0.0 && std::isfinite(prm->lr)) || !(prm->beta1 >= 0.0 && prm->beta1 < 1.0) ||
-        !(prm->beta2 >= 0.0 && prm->beta2 < 1.0) || !((float)prm->eps > 0.0f && std::isfinite((float)prm->eps)) || prm->step < 1)
+        !(prm->beta2 >= 0.0 && prm->beta2 < 1.0) || !(prm->eps >= 0x1p-100 && prm->eps <= 0x1p100) || prm->step < 1)
         return DC_ERR_INVALID_ARG;
     if (!d_table || !aligned_to(d_table, 256) || !aligned_to(d_grad_scale, 4)) return DC_ERR_INVALID_ARG;
     const AdamwTable t = carve_adamw_table(const_cast<void*>(d_table), n_tensors, n_pieces);

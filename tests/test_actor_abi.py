@@ -247,3 +247,10 @@ def test_nothing_to_do_is_no_error():
     need = B.dc_adamw_table_bytes(t)
     B.dc_adamw_table(t, A, need, stream=0)
     B.dc_adamw(t, B.make_adamw(1e-3), None, A, need, None, stream=0)
+
+
+def test_adamw_eps_that_32_bits_cannot_divide_by():
+    t = Tensors(tensor())
+    need = B.dc_adamw_table_bytes(t)
+    for eps in (1e-39, 1e-31, 1e31, 1e38):                    # a denormal; what has no normal reciprocal
+        refuses(B.DC_ERR_INVALID_ARG, B.dc_adamw, t, B.make_adamw(1e-3, eps=eps), None, A, need, A)
