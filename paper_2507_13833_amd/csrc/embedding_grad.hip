@@ -7,9 +7,12 @@
 //                   entries there come before it (a binary search each); once for every factor of MERGE_WAYS
 //   add_rows        one wave per chunk and 512 columns: sums the rows of the segments (entries of one id) that start in the
 //                   chunk, each in ascending token order, and writes them.  A segment of more than CHUNK entries is
-//                   summed in pieces, one per chunk that it touches, into workspace memory.  Further waves write the rows
-//                   without a token.
+//                   summed in pieces, one per chunk that it touches, into workspace memory
 //   join_pieces     the pieces of the long segments, in ascending order
+// The rows without a token, most of a large table, are written beside other work that leaves the memory idle: sort_portions
+// has workgroups for as many as fit into its time (they look through all tokens), add_rows and join_pieces have them for the
+// others (they search the sorted ids).
+#include <algorithm>
 #include "actor_device.h"
 
 namespace dc {
@@ -19,6 +22,7 @@ constexpr int MAX_PORTION = 8192, PER_THREAD = MAX_PORTION / SORT_THREADS;
 constexpr int MERGE_WAYS = 32, MERGE_THREADS = 512, MERGE_SAMPLES = 64;
 constexpr int ADD_THREADS = 256;
 constexpr int FILL_ROWS = 4, FILL_LANES = WAVE / FILL_ROWS;      // rows of the table per wave that looks for those without a token
+constexpr int FILL_GROUPS = 240, FILL_MOST = 4096;               // workgroups that write rows before the sort is done, rows of each
 constexpr int JOIN_THREADS = 512;
 
 static inline size_t round_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
@@ -55,13 +59,62 @@ size_t embedding_grad_workspace_bytes(int64_t n_tokens, int64_t dim) {
     return carve_emb_grad(nullptr, n_tokens, dim).bytes;
 }
 
+// +0 to a row of the table.  Every lane of the wave comes here.
+__device__ __forceinline__ void zero_row(const EmbeddingGradArgs& a, int64_t v) {
+    char* row = static_cast<char*>(a.dw) + v * a.dw_stride * a.dw_bytes;
+    const int64_t bytes = a.dim * a.dw_bytes, whole = a.dw_aligned ? bytes & ~15LL : 0;
+    for (int64_t o = lane_id() * 16; o < whole; o += WAVE * 16) store16(reinterpret_cast<u32x4*>(row + o), u32x4{0, 0, 0, 0});
+    if (a.dw_bytes == 4)
+        for (int64_t o = whole + lane_id() * 4; o < bytes; o += WAVE * 4) *reinterpret_cast<uint32_t*>(row + o) = 0;
+    else
+        for (int64_t o = whole + lane_id() * 2; o < bytes; o += WAVE * 2) *reinterpret_cast<uint16_t*>(row + o) = 0;
+}
+// A workgroup's rows [v0, v0 + rows) that no token names, rows at most FILL_MOST: a bit in the LDS for each, set by a look at
+// all tokens (out of the L2, 16 bytes to a thread eight times over).
+typedef int32_t i32x4_by4 __attribute__((ext_vector_type(4), aligned(4)));
+template <int THREADS>
+__device__ __forceinline__ void fill_unnamed(const EmbeddingGradArgs& a, int64_t v0, int32_t rows, uint32_t* bits) {
+    constexpr int AT_ONCE = 8;
+    for (int i = threadIdx.x; i < FILL_MOST / 32; i += THREADS) bits[i] = 0;
+    __syncthreads();
+    const auto name = [&](int32_t id) {
+        const uint32_t r = (uint32_t)id - (uint32_t)v0;
+        if (r < (uint32_t)rows && ((bits[r / 32] >> (r % 32)) & 1) == 0) atomicOr(&bits[r / 32], 1u << (r % 32));
+    };
+    const i32x4_by4* four = reinterpret_cast<const i32x4_by4*>(a.token);
+    const int32_t fours = a.n_tokens / 4;
+    for (int32_t i = threadIdx.x; i < fours; i += AT_ONCE * THREADS) {
+        i32x4_by4 q[AT_ONCE];
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) q[j] = four[min(i + j * THREADS, fours - 1)];        // (the last ones again: set twice)
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) name(q[j][c]);
+    }
+    if ((int32_t)threadIdx.x < a.n_tokens - fours * 4) name(a.token[fours * 4 + threadIdx.x]);
+    __syncthreads();
+    for (int32_t r = threadIdx.x / WAVE; r < rows; r += THREADS / WAVE)
+        if (((bits[r / 32] >> (r % 32)) & 1) == 0) zero_row(a, v0 + r);
+}
+// Rows [first, first + rows) of the table by `groups` workgroups; `group`: this one.
+struct Fill { int64_t first, rows; int32_t groups; };
+template <int THREADS>
+__device__ __forceinline__ void fill_part(const EmbeddingGradArgs& a, const Fill& f, int32_t group, uint32_t* bits) {
+    const int64_t per = (f.rows + f.groups - 1) / f.groups, from = group * per;
+    if (from < f.rows) fill_unnamed<THREADS>(a, f.first + from, (int32_t)min(per, f.rows - from), bits);
+}
+
 // `per` times SORT_THREADS tokens by id: least significant digit first, `digit_bits` (at most 8) at a time.  A wave ranks 64 entries by
 // ballots over the digit's bits; counts are kept per digit and wave, so the order within a digit is that of the tokens.
-__global__ __launch_bounds__(SORT_THREADS) void sort_portions_kernel(const EmbeddingGradArgs a, EmbGradWs w, int per_thread, int digit_bits, int passes) {
+__global__ __launch_bounds__(SORT_THREADS) void sort_portions_kernel(const EmbeddingGradArgs a, EmbGradWs w, int per_thread, int digit_bits, int passes,
+                                                                     Fill fill) {
     __shared__ uint32_t keys[MAX_PORTION];
     __shared__ uint16_t places[MAX_PORTION];
     __shared__ uint16_t counts[256 * SORT_WAVES];
     __shared__ uint32_t tmp[SORT_WAVES];
+    const int32_t portions = (int32_t)gridDim.x - fill.groups;
+    if ((int32_t)blockIdx.x >= portions) return fill_part<SORT_THREADS>(a, fill, (int32_t)blockIdx.x - portions, keys);
     const int lane = lane_id(), wave = threadIdx.x / WAVE;
     const int32_t portion = per_thread * SORT_THREADS, first = blockIdx.x * portion;
     if (blockIdx.x == 0 && threadIdx.x == 0) *w.n_long = 0;
@@ -215,6 +268,28 @@ __global__ __launch_bounds__(MERGE_THREADS) void merge_runs_kernel(const Embeddi
     pos_out[to] = pos_in[i];
 }
 
+// FILL_ROWS rows of the table by a wave, those without a token: sixteen lanes look for each row's id among the sorted ones,
+// sixteen places at a time.
+__device__ __forceinline__ void fill_sought(const EmbeddingGradArgs& a, const uint32_t* __restrict__ skey, int64_t v0, int64_t end) {
+    const int lane = lane_id(), sub = lane % FILL_LANES;
+    const uint32_t id = (uint32_t)(v0 + lane / FILL_LANES);
+    int32_t lo = 0, hi = a.n_tokens;             // the first entry that is not below it lies in [lo, hi]
+    while (__ballot(lo < hi)) {
+        const int32_t step = (hi - lo + FILL_LANES) / (FILL_LANES + 1);
+        const int32_t at = lo + (sub + 1) * step - 1;
+        const bool below = at >= lo && at < hi && skey[at] < id;           // (a row that is found asks for nothing)
+        const int n = __popc((uint32_t)(__ballot(below) >> (lane - sub)) & ((1u << FILL_LANES) - 1));
+        if (lo < hi) {
+            const int32_t next = lo + n * step;
+            hi = n < FILL_LANES ? min(hi, next + step - 1) : hi;
+            lo = next;
+        }
+    }
+    const uint64_t there = __ballot(lo < a.n_tokens && skey[min(lo, a.n_tokens - 1)] == id);
+    for (int r = 0; r < FILL_ROWS && v0 + r < end; ++r)
+        if (((there >> (r * FILL_LANES)) & 1) == 0) zero_row(a, v0 + r);
+}
+
 // A finished sum to its row of the table, added to what `old` holds of it.
 template <Layout L, bool ACC, typename W>
 __device__ __forceinline__ void write_row(const EmbeddingGradArgs& a, uint32_t id, int64_t slab, const float (&sum)[8], const Raw8<W>& old) {
@@ -224,40 +299,20 @@ __device__ __forceinline__ void write_row(const EmbeddingGradArgs& a, uint32_t i
     store8<L, !ACC>(static_cast<W*>(a.dw) + (int64_t)id * a.dw_stride, slab, a.dim, out);
 }
 
+// Bound by the memory: 131 072 rows of 2048 in bf16 in, 58 000 rows in f32 out and 67 000 written as +0 in 0.30 ms of the
+// call's 0.37 (5.2 TB/s; a large copy reaches 4.7).
 template <int CHUNK, Layout L, bool ACC, typename G, typename W>
 __global__ __launch_bounds__(ADD_THREADS) void add_rows_kernel(const EmbeddingGradArgs a, const uint32_t* __restrict__ skey,
                                                                const int32_t* __restrict__ spos,
                                                                int32_t* n_long, int32_t* long_at, float* __restrict__ piece,
-                                                               int32_t chunks, int32_t slabs) {
+                                                               int32_t chunks, int32_t slabs, Fill fill) {
     constexpr int AT_ONCE = ACC ? 4 : 8;         // rows asked for before the ones before them are added
     const int64_t unit = (int64_t)blockIdx.x * (ADD_THREADS / WAVE) + __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int lane = lane_id();
     const int64_t adders = (int64_t)chunks * slabs;
-    if (unit >= adders) {                        // rows without a token
-        const int64_t v0 = (unit - adders) * FILL_ROWS;
-        if (ACC || v0 >= a.vocab) return;
-        // sixteen lanes look for each row's id among the sorted ones, sixteen places at a time
-        const int sub = lane % FILL_LANES;
-        const uint32_t id = (uint32_t)(v0 + lane / FILL_LANES);
-        int32_t lo = 0, hi = a.n_tokens;         // the first entry that is not below it lies in [lo, hi]
-        while (__ballot(lo < hi)) {
-            const int32_t step = (hi - lo + FILL_LANES) / (FILL_LANES + 1);
-            const int32_t at = lo + (sub + 1) * step - 1;
-            const bool below = at >= lo && at < hi && skey[at] < id;       // (a row that is found asks for nothing)
-            const int n = __popc((uint32_t)(__ballot(below) >> (lane - sub)) & ((1u << FILL_LANES) - 1));
-            if (lo < hi) {
-                const int32_t next = lo + n * step;
-                hi = n < FILL_LANES ? min(hi, next + step - 1) : hi;
-                lo = next;
-            }
-        }
-        const uint64_t there = __ballot(lo < a.n_tokens && skey[min(lo, a.n_tokens - 1)] == id);
-        const float zero[8] = {};
-        for (int r = 0; r < FILL_ROWS && v0 + r < a.vocab; ++r) {
-            if ((there >> (r * FILL_LANES)) & 1) continue;
-            W* row = static_cast<W*>(a.dw) + (v0 + r) * a.dw_stride;
-            for (int32_t s = 0; s < slabs; ++s) store8<L, true>(row, s, a.dim, zero);
-        }
+    if (unit >= adders) {
+        const int64_t v0 = fill.first + (unit - adders) * FILL_ROWS, end = fill.first + fill.rows;
+        if (v0 < end) fill_sought(a, skey, v0, end);
         return;
     }
     const int32_t chunk = (int32_t)((uint64_t)unit / (uint32_t)slabs), slab = (int32_t)(unit - (int64_t)chunk * slabs);
@@ -343,12 +398,18 @@ __global__ __launch_bounds__(ADD_THREADS) void add_rows_kernel(const EmbeddingGr
 template <int CHUNK, Layout L, bool ACC, typename W>
 __global__ __launch_bounds__(JOIN_THREADS) void join_pieces_kernel(const EmbeddingGradArgs a, const uint32_t* __restrict__ skey,
                                                                    const int32_t* __restrict__ n_long, const int32_t* __restrict__ long_at,
-                                                                   const float* __restrict__ piece, int32_t chunks, int32_t slabs) {
+                                                                   const float* __restrict__ piece, int32_t chunks, int32_t slabs,
+                                                                   int32_t joiners, int64_t fill_from, int64_t fill_end) {
     constexpr int WAVES = JOIN_THREADS / WAVE, AT_ONCE = 8;
     __shared__ float part[WAVES][8][WAVE];
+    if ((int32_t)blockIdx.x >= joiners) {
+        const int64_t v0 = fill_from + ((int64_t)((int32_t)blockIdx.x - joiners) * WAVES + threadIdx.x / WAVE) * FILL_ROWS;
+        if (v0 < fill_end) fill_sought(a, skey, v0, fill_end);
+        return;
+    }
     const int lane = lane_id(), wave = threadIdx.x / WAVE;
     const int64_t units = (int64_t)*n_long * slabs;
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+    for (int64_t u = blockIdx.x; u < units; u += joiners) {
         const int32_t c0 = long_at[u / slabs], slab = (int32_t)(u % slabs);
         const uint32_t id = skey[(int64_t)c0 * CHUNK + CHUNK - 1];
         // the last chunk whose first entry is of this segment: 64 looks at a time
@@ -389,7 +450,20 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_pieces_kernel(const Embeddi
     }
 }
 
-hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, int32_t g_type, int32_t dw_type, void* d_ws, hipStream_t st) {
+// Bytes of rows without a token that are written beside the sort (which takes longer the more tokens a thread has) and beside
+// the join; the rest beside add_rows.  Measured, us, gradients in bf16, a table in f32; all of it beside add_rows / beside the
+// sort, 70 MB / 160 MB, no more at the join / 120 MB at the sort (80 MB at the second), 100 MB at the join / everything at
+// the sort:
+//   131072 tokens, 152064 x 2048   391.9 / 380.2 / 377.6 / 374.5 / 397.2
+//   33000 tokens, 152064 x 512      90.6 /  80.4 /  82.3 /  76.8 /  86.3
+//   500 tokens, 152064 x 1024      128.9 / 125.2 / 125.9 / 121.0 / 130.1
+// From the table's start instead of its end, where most rows have tokens: nothing gained.  Beside the merge as well: 1 % slower
+// (its own work takes all compute units).  Stores that stay in the caches: 8 % slower on the first, 4 % faster on the second.
+constexpr double FILL_SORT = 60e6, FILL_SORT_EACH = 8e6, FILL_JOIN = 100e6;
+hipError_t launch_embedding_grad(const EmbeddingGradArgs& args, int32_t g_type, int32_t dw_type, void* d_ws, hipStream_t st) {
+    EmbeddingGradArgs a = args;
+    a.dw_bytes = dw_type == DC_F32 ? 4 : 2;
+    a.dw_aligned = reinterpret_cast<uintptr_t>(a.dw) % 16 == 0 && (size_t)a.dw_stride * a.dw_bytes % 16 == 0;
     if (a.vocab == 0 || a.dim == 0 || (a.n_tokens == 0 && a.accumulate)) return hipSuccess;
     EmbGradWs w = carve_emb_grad(d_ws, a.n_tokens, a.dim);
     // short portions keep more workgroups busy, long ones leave the merge fewer runs (one level of it either way up to
@@ -400,7 +474,14 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, int32_t g_type, int
     int bits = 1;
     while ((1 << bits) <= a.vocab) ++bits;       // ids up to and with `vocab`
     const int passes = (bits + 7) / 8, digit_bits = (bits + passes - 1) / passes;
-    sort_portions_kernel<<<(unsigned)portions, SORT_THREADS, 0, st>>>(a, w, per_thread, digit_bits, passes);
+    // rows without a token, from the table's end, where ids are rare
+    const double row = (double)a.dim * a.dw_bytes;
+    int64_t left = a.accumulate ? 0 : a.vocab;   // rows [0, left) are still to be looked at
+    Fill by_sort = {0, 0, 0};
+    if (portions + FILL_GROUPS <= 256) by_sort.rows = std::min({left, (int64_t)((FILL_SORT + FILL_SORT_EACH * per_thread) / row), (int64_t)FILL_GROUPS * FILL_MOST});
+    by_sort.first = left -= by_sort.rows;
+    by_sort.groups = (int32_t)std::min<int64_t>(by_sort.rows, FILL_GROUPS);
+    sort_portions_kernel<<<(unsigned)(portions + by_sort.groups), SORT_THREADS, 0, st>>>(a, w, per_thread, digit_bits, passes, by_sort);
     int at = 0;
     for (int64_t run = portion; run < a.n_tokens; run *= MERGE_WAYS) {
         merge_runs_kernel<<<(unsigned)((a.n_tokens + MERGE_ENTRIES - 1) / MERGE_ENTRIES), MERGE_THREADS, 0, st>>>(
@@ -409,9 +490,11 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, int32_t g_type, int
     }
     const int chunk = chunk_of(a.n_tokens, a.dim);
     const int64_t chunks = ((int64_t)a.n_tokens + chunk - 1) / chunk, slabs = (a.dim + COLS - 1) / COLS;
-    const int64_t fill = a.accumulate ? 0 : ((int64_t)a.vocab + FILL_ROWS - 1) / FILL_ROWS;
-    const int64_t units = chunks * slabs + fill, blocks = (units + ADD_THREADS / WAVE - 1) / (ADD_THREADS / WAVE);
+    const int64_t by_join = std::min<int64_t>(left, (int64_t)(FILL_JOIN / row));
+    const Fill by_add = {0, left - by_join, 0};
+    const int64_t units = chunks * slabs + (by_add.rows + FILL_ROWS - 1) / FILL_ROWS, blocks = (units + ADD_THREADS / WAVE - 1) / (ADD_THREADS / WAVE);
     if (blocks > 0x7FFFFFFFLL) return hipErrorInvalidValue;
+    const int64_t per_join = JOIN_THREADS / WAVE * FILL_ROWS, fillers = (by_join + per_join - 1) / per_join;
     return with_type(g_type, [&](auto ge) {
         return with_type(dw_type, [&](auto we) {
             using G = typename decltype(ge)::type;
@@ -421,13 +504,14 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, int32_t g_type, int
                 constexpr int CHUNK = decltype(c)::value;
                 constexpr Layout L = decltype(v)::value ? (sizeof(W) == 4 ? FOURS : EIGHTS) : APART;
                 constexpr bool ACC = decltype(acc)::value;
-                add_rows_kernel<CHUNK, L, ACC, G, W><<<(unsigned)blocks, ADD_THREADS, 0, st>>>(
-                    a, w.key[at], w.pos[at], w.n_long, w.long_at, w.piece, (int32_t)chunks, (int32_t)slabs);
-                if (a.n_tokens > CHUNK) {
-                    const int64_t most = (int64_t)a.n_tokens / (CHUNK + 1) * slabs;      // long segments there can be
-                    join_pieces_kernel<CHUNK, L, ACC, W><<<(unsigned)(most < 1024 ? most : 1024), JOIN_THREADS, 0, st>>>(
-                        a, w.key[at], w.n_long, w.long_at, w.piece, (int32_t)chunks, (int32_t)slabs);
-                }
+                if (blocks > 0)
+                    add_rows_kernel<CHUNK, L, ACC, G, W><<<(unsigned)blocks, ADD_THREADS, 0, st>>>(
+                        a, w.key[at], w.pos[at], w.n_long, w.long_at, w.piece, (int32_t)chunks, (int32_t)slabs, by_add);
+                const int64_t most = (int64_t)a.n_tokens / (CHUNK + 1) * slabs;          // long segments there can be
+                const int32_t joiners = (int32_t)(most < 1024 ? most : 1024);
+                if (joiners + fillers > 0)
+                    join_pieces_kernel<CHUNK, L, ACC, W><<<(unsigned)(joiners + fillers), JOIN_THREADS, 0, st>>>(
+                        a, w.key[at], w.n_long, w.long_at, w.piece, (int32_t)chunks, (int32_t)slabs, joiners, left - by_join, left);
             };
             const auto go = [&](auto v, auto acc) {
                 if (chunk == 16) launch(std::integral_constant<int, 16>{}, v, acc);

@@ -942,3 +942,30 @@ def test_logprob_of_far_logits_in_one_long_row(env):
     x[:, -5:] = torch.tensor([1.0, 2.0, 0.5, -1.0, 0.25], device="cuda").bfloat16()
     token = torch.full((rows,), vocab - 4, dtype=torch.int32, device="cuda")
     check_logprob(env, x, 1.0, token, None, 3)
+
+
+@pytest.mark.parametrize("w_type", ["f32", "bf16"])
+@pytest.mark.parametrize("pad,shift", [(0, 0), (3, 1), (8, 8)])
+@pytest.mark.parametrize("tokens,vocab,dim", [(0, 100001, 520), (1, 100001, 1000), (700, 152064, 1024), (30000, 152064, 1023), (100003, 152064, 515),
+                                              (140000, 60000, 520)])
+def test_embedding_backward_rows_without_a_token(env, tokens, vocab, dim, pad, shift, w_type):
+    """Tables of which most rows have no token: +0 in every one, nothing between them touched, exact sums (whole numbers) in
+    the others."""
+    torch, B = env
+    gen = torch.Generator(device="cuda").manual_seed(tokens + dim)
+    g = torch.randint(-1, 2, (tokens, dim), generator=gen, device="cuda").bfloat16()
+    ids = (torch.rand(tokens, generator=gen, device="cuda").double() ** 2 * vocab).int().clamp_(max=vocab - 1)
+    if tokens > 100:
+        ids[::97], ids[3] = -1, 0
+        ids[ids % 1000 == 77] = vocab - 1                     # many of one id, the table's last
+    dt = types(torch)[w_type]
+    store = torch.full((vocab * (dim + pad) + shift + 8,), 77.0, dtype=dt, device="cuda")
+    dw = store.as_strided((vocab, dim), (dim + pad, 1), shift)
+    dw.fill_(math.nan)
+    embedding_grad_call(env, g, ids, 1.0, False, dw)
+    ok = ids >= 0
+    want = torch.zeros(vocab, dim, device="cuda").index_add_(0, ids[ok].long(), g[ok].float())
+    assert torch.equal(dw, want.to(dt))
+    assert bool((store[:shift] == 77.0).all()) and bool((store[-8:] == 77.0).all())
+    if pad:
+        assert bool((store[shift:shift + vocab * (dim + pad)].view(vocab, dim + pad)[:, dim:] == 77.0).all())
