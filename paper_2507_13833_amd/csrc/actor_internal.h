@@ -61,7 +61,7 @@ struct EmbeddingGradArgs {
     int32_t        accumulate;
     const int32_t* token;
     int32_t*       status;
-    int32_t        dw_bytes, dw_aligned;         // the launcher's: of an element; rows on multiples of 16 bytes
+    int32_t        dw_bytes, dw_aligned, dw_stream;        // the launcher's: of an element; rows on multiples of 16 bytes; past the caches
 };
 size_t embedding_grad_workspace_bytes(int64_t n_tokens, int64_t dim);
 hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, int32_t g_type, int32_t dw_type, void* d_ws, hipStream_t st);

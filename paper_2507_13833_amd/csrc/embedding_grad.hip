@@ -1,7 +1,8 @@
 // Gradient of an embedding table: dW[v, :] = scale * sum of g[t, :] over the tokens t with id v.
 //
-// The tokens are sorted by id (stable, so the tokens of one id stay in ascending order), and the sorted sequence is cut
-// into chunks of CHUNK entries: a hot id costs as much per token as a rare one, and no float goes through an atomic.
+// Few tokens: one launch (few_tokens).  Otherwise the tokens are sorted by id (stable, so the tokens of one id stay in
+// ascending order), and the sorted sequence is cut into chunks of CHUNK entries: a hot id costs as much per token as a rare
+// one, and no float goes through an atomic.
 //   sort_portions   1024 to 8192 tokens per workgroup, radix sort in the LDS
 //   merge_runs      up to MERGE_WAYS sorted runs into one: an entry's place is its own plus, for every other run, how many
 //                   entries there come before it (a binary search each); once for every factor of MERGE_WAYS
@@ -63,7 +64,11 @@ size_t embedding_grad_workspace_bytes(int64_t n_tokens, int64_t dim) {
 __device__ __forceinline__ void zero_row(const EmbeddingGradArgs& a, int64_t v) {
     char* row = static_cast<char*>(a.dw) + v * a.dw_stride * a.dw_bytes;
     const int64_t bytes = a.dim * a.dw_bytes, whole = a.dw_aligned ? bytes & ~15LL : 0;
-    for (int64_t o = lane_id() * 16; o < whole; o += WAVE * 16) store16(reinterpret_cast<u32x4*>(row + o), u32x4{0, 0, 0, 0});
+    // (two loops: in one the compiler makes the two stores a plain one)
+    if (a.dw_stream)
+        for (int64_t o = lane_id() * 16; o < whole; o += WAVE * 16) store16(reinterpret_cast<u32x4*>(row + o), u32x4{0, 0, 0, 0});
+    else
+        for (int64_t o = lane_id() * 16; o < whole; o += WAVE * 16) *reinterpret_cast<u32x4*>(row + o) = u32x4{0, 0, 0, 0};
     if (a.dw_bytes == 4)
         for (int64_t o = whole + lane_id() * 4; o < bytes; o += WAVE * 4) *reinterpret_cast<uint32_t*>(row + o) = 0;
     else
@@ -94,7 +99,8 @@ __device__ __forceinline__ void fill_unnamed(const EmbeddingGradArgs& a, int64_t
     }
     if ((int32_t)threadIdx.x < a.n_tokens - fours * 4) name(a.token[fours * 4 + threadIdx.x]);
     __syncthreads();
-    for (int32_t r = threadIdx.x / WAVE; r < rows; r += THREADS / WAVE)
+    const int32_t each = (rows + THREADS / WAVE - 1) / (THREADS / WAVE), mine = (int32_t)(threadIdx.x / WAVE) * each;
+    for (int32_t r = mine; r < min(rows, mine + each); ++r)                // (neighbours to a wave)
         if (((bits[r / 32] >> (r % 32)) & 1) == 0) zero_row(a, v0 + r);
 }
 // Rows [first, first + rows) of the table by `groups` workgroups; `group`: this one.
@@ -299,6 +305,70 @@ __device__ __forceinline__ void write_row(const EmbeddingGradArgs& a, uint32_t i
     store8<L, !ACC>(static_cast<W*>(a.dw) + (int64_t)id * a.dw_stride, slab, a.dim, out);
 }
 
+// Few tokens in one launch: a workgroup per token and 512 columns that sums the rows of all tokens of its id, if no earlier
+// token has it, and workgroups for FEW_FILL rows each for those without a token.  Every wave compares all ids with its own, a
+// ballot per 64; above AT_ONCE rows the waves take equal shares, in ascending order, and join in that order.  Bound by trips to
+// memory in a row, four where the sorted way has a dozen in three launches.  Measured, us, gradients in bf16 added to a table in
+// f32, this way / sorted: 30 tokens of 512 columns 7.5 / 13.6, 300 of 2048 8.2 / 17, 512 of 2048 10.8 / 15.5, 512 of one id 12.4 /
+// 12.6, 1000 of 2048 26 / 19; 300 tokens and a table of 32 000 x 2048 written anew 37 / 50.
+constexpr int FEW_TOKENS = 512, FEW_GROUPS = 2048, FEW_THREADS = 512, FEW_FILL = 32;
+template <Layout L, bool ACC, typename G, typename W>
+__global__ __launch_bounds__(FEW_THREADS) void few_tokens_kernel(const EmbeddingGradArgs a, int32_t slabs, int32_t adders, Fill fill) {
+    constexpr int WAVES = FEW_THREADS / WAVE, WORDS = FEW_TOKENS / WAVE, AT_ONCE = 8;
+    __shared__ float part[WAVES][8][WAVE];
+    __shared__ int32_t place[FEW_TOKENS];
+    static_assert(FILL_MOST / 32 <= FEW_TOKENS, "the bits fit as well");
+    if ((int32_t)blockIdx.x >= adders)
+        return fill_part<FEW_THREADS>(a, fill, (int32_t)blockIdx.x - adders, reinterpret_cast<uint32_t*>(place));
+    const int32_t t = (int32_t)blockIdx.x / slabs, slab = (int32_t)blockIdx.x - t * slabs;
+    const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+    int32_t ids[WORDS];
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) ids[w] = w * WAVE < a.n_tokens ? a.token[min(w * WAVE + lane, a.n_tokens - 1)] : DC_NO_TOKEN;
+    const int32_t id = a.token[t];
+    if (id < 0 || id >= a.vocab) {
+        if (id != DC_NO_TOKEN && slab == 0 && threadIdx.x == 0) set_status(a.status, DC_ERR_TOKEN_RANGE);
+        return;
+    }
+    Raw8<W> old;
+    if constexpr (ACC) load8<L>(static_cast<const W*>(a.dw) + (int64_t)id * a.dw_stride, slab, a.dim, old);
+    const uint64_t below = (1ull << lane) - 1;
+    int32_t count = 0, before = 0;               // tokens of this id; those before token t
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) {
+        const uint64_t same = __ballot(w * WAVE + lane < a.n_tokens && ids[w] == id);
+        if (wave == w % WAVES && (same >> lane) & 1) place[count + __popcll(same & below)] = w * WAVE + lane;
+        const int32_t left = t - w * WAVE;
+        before += __popcll(left >= WAVE ? same : left > 0 ? same & ((1ull << left) - 1) : 0ull);
+        count += __popcll(same);
+    }
+    if (before > 0) return;
+    __syncthreads();
+    const int32_t per = max(AT_ONCE, (count + WAVES - 1) / WAVES), from = wave * per, to = min(count, from + per);
+    float sum[8] = {};
+    for (int32_t k = from; k < to; k += AT_ONCE) {
+        Raw8<G> g[AT_ONCE];
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j)
+            load8<L>(static_cast<const G*>(a.g) + (int64_t)__builtin_amdgcn_readfirstlane(place[min(k + j, to - 1)]) * a.g_stride, slab, a.dim, g[j]);
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j)
+            if (k + j < to)
+#pragma unroll
+                for (int c = 0; c < 8; ++c) sum[c] += (float)g[j].e[c];
+    }
+    if (count > per) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) part[wave][c][lane] = sum[c];
+        __syncthreads();
+        if (wave == 0)
+            for (int w = 1; w * per < count; ++w)
+#pragma unroll
+                for (int c = 0; c < 8; ++c) sum[c] += part[w][c][lane];
+    }
+    if (wave == 0) write_row<L, ACC, W>(a, (uint32_t)id, slab, sum, old);
+}
+
 // Bound by the memory: 131 072 rows of 2048 in bf16 in, 58 000 rows in f32 out and 67 000 written as +0 in 0.30 ms of the
 // call's 0.37 (5.2 TB/s; a large copy reaches 6.2).
 template <int CHUNK, Layout L, bool ACC, typename G, typename W>
@@ -456,15 +526,45 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_pieces_kernel(const Embeddi
 // the sort:
 //   131072 tokens, 152064 x 2048   391.9 / 380.2 / 377.6 / 374.5 / 397.2
 //   33000 tokens, 152064 x 512      90.6 /  80.4 /  82.3 /  76.8 /  86.3
-//   500 tokens, 152064 x 1024      128.9 / 125.2 / 125.9 / 121.0 / 130.1
 // From the table's start instead of its end, where most rows have tokens: nothing gained.  Beside the merge as well: 1 % slower
-// (its own work takes all compute units).  Stores that stay in the caches: 8 % slower on the first, 4 % faster on the second.
+// (its own work takes all compute units).
 constexpr double FILL_SORT = 60e6, FILL_SORT_EACH = 8e6, FILL_JOIN = 100e6;
+// f(layout, whether to accumulate, element types of the gradient and of the table).
+template <typename F>
+static hipError_t with_layout(const EmbeddingGradArgs& a, int32_t g_type, int32_t dw_type, F&& f) {
+    return with_type(g_type, [&](auto ge) {
+        return with_type(dw_type, [&](auto we) {
+            using G = typename decltype(ge)::type;
+            using W = typename decltype(we)::type;
+            const auto go = [&](auto layout) {
+                return a.accumulate ? f(layout, std::true_type{}, ge, we) : f(layout, std::false_type{}, ge, we);
+            };
+            if (a.dim % 8 == 0 && rows_aligned<G>(a.g, a.g_stride) && rows_aligned<W>(a.dw, a.dw_stride))
+                return go(std::integral_constant<Layout, sizeof(W) == 4 ? FOURS : EIGHTS>{});
+            return go(std::integral_constant<Layout, APART>{});
+        });
+    });
+}
+
 hipError_t launch_embedding_grad(const EmbeddingGradArgs& args, int32_t g_type, int32_t dw_type, void* d_ws, hipStream_t st) {
     EmbeddingGradArgs a = args;
     a.dw_bytes = dw_type == DC_F32 ? 4 : 2;
+    // rows of +0 past the caches where the table is several times the Infinity Cache's 256 MB: 1245 MB 375 us (through the caches
+    // 405); through them otherwise: 623 MB 111 us (past them 114), 311 MB 74 (77), 262 MB 37 (48)
+    a.dw_stream = (size_t)a.vocab * a.dw_stride * a.dw_bytes > 768u << 20;
     a.dw_aligned = reinterpret_cast<uintptr_t>(a.dw) % 16 == 0 && (size_t)a.dw_stride * a.dw_bytes % 16 == 0;
     if (a.vocab == 0 || a.dim == 0 || (a.n_tokens == 0 && a.accumulate)) return hipSuccess;
+    const int64_t slabs = (a.dim + COLS - 1) / COLS;
+    if (a.n_tokens <= FEW_TOKENS && a.n_tokens * slabs <= FEW_GROUPS) {
+        const int64_t rows = a.accumulate ? 0 : a.vocab, groups = (rows + FEW_FILL - 1) / FEW_FILL;
+        const Fill fill = {0, rows, (int32_t)groups};
+        const int32_t adders = a.n_tokens * (int32_t)slabs;
+        return with_layout(a, g_type, dw_type, [&](auto layout, auto acc, auto ge, auto we) {
+            few_tokens_kernel<decltype(layout)::value, decltype(acc)::value, typename decltype(ge)::type, typename decltype(we)::type>
+                <<<(unsigned)(adders + groups), FEW_THREADS, 0, st>>>(a, (int32_t)slabs, adders, fill);
+            return hipGetLastError();
+        });
+    }
     EmbGradWs w = carve_emb_grad(d_ws, a.n_tokens, a.dim);
     // short portions keep more workgroups busy, long ones leave the merge fewer runs (one level of it either way up to
     // 2^18 tokens): 8192 tokens sorted and merged
@@ -489,40 +589,29 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& args, int32_t g_type, 
         at ^= 1;
     }
     const int chunk = chunk_of(a.n_tokens, a.dim);
-    const int64_t chunks = ((int64_t)a.n_tokens + chunk - 1) / chunk, slabs = (a.dim + COLS - 1) / COLS;
+    const int64_t chunks = ((int64_t)a.n_tokens + chunk - 1) / chunk;
     const int64_t by_join = std::min<int64_t>(left, (int64_t)(FILL_JOIN / row));
     const Fill by_add = {0, left - by_join, 0};
     const int64_t units = chunks * slabs + (by_add.rows + FILL_ROWS - 1) / FILL_ROWS, blocks = (units + ADD_THREADS / WAVE - 1) / (ADD_THREADS / WAVE);
     if (blocks > 0x7FFFFFFFLL) return hipErrorInvalidValue;
     const int64_t per_join = JOIN_THREADS / WAVE * FILL_ROWS, fillers = (by_join + per_join - 1) / per_join;
-    return with_type(g_type, [&](auto ge) {
-        return with_type(dw_type, [&](auto we) {
-            using G = typename decltype(ge)::type;
-            using W = typename decltype(we)::type;
-            const bool vec = a.dim % 8 == 0 && rows_aligned<G>(a.g, a.g_stride) && rows_aligned<W>(a.dw, a.dw_stride);
-            const auto launch = [&](auto c, auto v, auto acc) {
-                constexpr int CHUNK = decltype(c)::value;
-                constexpr Layout L = decltype(v)::value ? (sizeof(W) == 4 ? FOURS : EIGHTS) : APART;
-                constexpr bool ACC = decltype(acc)::value;
-                if (blocks > 0)
-                    add_rows_kernel<CHUNK, L, ACC, G, W><<<(unsigned)blocks, ADD_THREADS, 0, st>>>(
-                        a, w.key[at], w.pos[at], w.n_long, w.long_at, w.piece, (int32_t)chunks, (int32_t)slabs, by_add);
-                const int64_t most = (int64_t)a.n_tokens / (CHUNK + 1) * slabs;          // long segments there can be
-                const int32_t joiners = (int32_t)(most < 1024 ? most : 1024);
-                if (joiners + fillers > 0)
-                    join_pieces_kernel<CHUNK, L, ACC, W><<<(unsigned)(joiners + fillers), JOIN_THREADS, 0, st>>>(
-                        a, w.key[at], w.n_long, w.long_at, w.piece, (int32_t)chunks, (int32_t)slabs, joiners, left - by_join, left);
-            };
-            const auto go = [&](auto v, auto acc) {
-                if (chunk == 16) launch(std::integral_constant<int, 16>{}, v, acc);
-                else launch(std::integral_constant<int, 32>{}, v, acc);
-            };
-            if (vec && a.accumulate) go(std::true_type{}, std::true_type{});
-            else if (vec) go(std::true_type{}, std::false_type{});
-            else if (a.accumulate) go(std::false_type{}, std::true_type{});
-            else go(std::false_type{}, std::false_type{});
-            return hipGetLastError();
-        });
+    return with_layout(a, g_type, dw_type, [&](auto layout, auto acc, auto ge, auto we) {
+        using G = typename decltype(ge)::type;
+        using W = typename decltype(we)::type;
+        constexpr Layout L = decltype(layout)::value;
+        constexpr bool ACC = decltype(acc)::value;
+        const auto launch = [&](auto c) {
+            constexpr int CHUNK = decltype(c)::value;
+            add_rows_kernel<CHUNK, L, ACC, G, W><<<(unsigned)blocks, ADD_THREADS, 0, st>>>(
+                a, w.key[at], w.pos[at], w.n_long, w.long_at, w.piece, (int32_t)chunks, (int32_t)slabs, by_add);
+            const int64_t most = (int64_t)a.n_tokens / (CHUNK + 1) * slabs;              // long segments there can be
+            const int32_t joiners = (int32_t)(most < 1024 ? most : 1024);
+            join_pieces_kernel<CHUNK, L, ACC, W><<<(unsigned)(joiners + fillers), JOIN_THREADS, 0, st>>>(
+                a, w.key[at], w.n_long, w.long_at, w.piece, (int32_t)chunks, (int32_t)slabs, joiners, left - by_join, left);
+        };
+        if (chunk == 16) launch(std::integral_constant<int, 16>{});
+        else launch(std::integral_constant<int, 32>{});
+        return hipGetLastError();
     });
 }
 

@@ -969,3 +969,17 @@ def test_embedding_backward_rows_without_a_token(env, tokens, vocab, dim, pad, s
     assert bool((store[:shift] == 77.0).all()) and bool((store[-8:] == 77.0).all())
     if pad:
         assert bool((store[shift:shift + vocab * (dim + pad)].view(vocab, dim + pad)[:, dim:] == 77.0).all())
+
+
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("tokens", [1, 2, 8, 9, 63, 64, 65, 129, 511, 1000, 1023, 1024, 1025])
+def test_embedding_backward_few_tokens(env, tokens, accumulate):
+    """On both sides of the sizes that one launch takes: all of one id, an id many times among others, ids once each."""
+    torch, B = env
+    vocab, dim = 1500, 600
+    gen = torch.Generator(device="cuda").manual_seed(tokens)
+    at = torch.arange(tokens, device="cuda")
+    for ids in (at * 0 + 7, torch.where(at % 3 == 0, 1499, at), at, torch.where(at % 5 == 0, -1, at // 9)):
+        g = torch.randn(tokens, dim, generator=gen, device="cuda").bfloat16()
+        check_embedding_grad(env, g, ids.int(), 1.5, accumulate, torch.ones(vocab, dim, device="cuda"))
+        check_embedding_grad(env, rows_of(torch, g, 1, 1), ids.int(), 1.5, accumulate, torch.ones(vocab, dim, device="cuda").bfloat16())
