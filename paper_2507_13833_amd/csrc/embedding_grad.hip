@@ -113,8 +113,8 @@ __device__ __forceinline__ void fill_part(const EmbeddingGradArgs& a, const Fill
 
 // `per` times SORT_THREADS tokens by id: least significant digit first, `digit_bits` (at most 8) at a time.  A wave ranks 64 entries by
 // ballots over the digit's bits; counts are kept per digit and wave, so the order within a digit is that of the tokens.
-__global__ __launch_bounds__(SORT_THREADS) void sort_portions_kernel(const EmbeddingGradArgs a, EmbGradWs w, int per_thread, int digit_bits, int passes,
-                                                                     Fill fill) {
+__global__ __launch_bounds__(SORT_THREADS) void sort_portions_kernel(const EmbeddingGradArgs a, EmbGradWs w, int per_thread, int digit_bits,
+                                                                     int passes, Fill fill) {
     __shared__ uint32_t keys[MAX_PORTION];
     __shared__ uint16_t places[MAX_PORTION];
     __shared__ uint16_t counts[256 * SORT_WAVES];
@@ -350,7 +350,8 @@ __global__ __launch_bounds__(FEW_THREADS) void few_tokens_kernel(const Embedding
         Raw8<G> g[AT_ONCE];
 #pragma unroll
         for (int j = 0; j < AT_ONCE; ++j)
-            load8<L>(static_cast<const G*>(a.g) + (int64_t)__builtin_amdgcn_readfirstlane(place[min(k + j, to - 1)]) * a.g_stride, slab, a.dim, g[j]);
+            load8<L>(static_cast<const G*>(a.g) + (int64_t)__builtin_amdgcn_readfirstlane(place[min(k + j, to - 1)]) * a.g_stride,
+                     slab, a.dim, g[j]);
 #pragma unroll
         for (int j = 0; j < AT_ONCE; ++j)
             if (k + j < to)
@@ -570,7 +571,7 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& args, int32_t g_type, 
     // 2^18 tokens): 8192 tokens sorted and merged
     const int per_thread = a.n_tokens <= SORT_THREADS ? 1 : a.n_tokens <= 16384 ? 2 : a.n_tokens <= 65536 ? 4 : 8;
     const int64_t portion = (int64_t)per_thread * SORT_THREADS;
-    const int64_t portions = a.n_tokens > 0 ? (a.n_tokens + portion - 1) / portion : 1;
+    const int64_t portions = (a.n_tokens + portion - 1) / portion;
     int bits = 1;
     while ((1 << bits) <= a.vocab) ++bits;       // ids up to and with `vocab`
     const int passes = (bits + 7) / 8, digit_bits = (bits + passes - 1) / passes;
@@ -578,7 +579,8 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& args, int32_t g_type, 
     const double row = (double)a.dim * a.dw_bytes;
     int64_t left = a.accumulate ? 0 : a.vocab;   // rows [0, left) are still to be looked at
     Fill by_sort = {0, 0, 0};
-    if (portions + FILL_GROUPS <= 256) by_sort.rows = std::min({left, (int64_t)((FILL_SORT + FILL_SORT_EACH * per_thread) / row), (int64_t)FILL_GROUPS * FILL_MOST});
+    if (portions + FILL_GROUPS <= 256)           // (a compute unit for each)
+        by_sort.rows = std::min({left, (int64_t)((FILL_SORT + FILL_SORT_EACH * per_thread) / row), (int64_t)FILL_GROUPS * FILL_MOST});
     by_sort.first = left -= by_sort.rows;
     by_sort.groups = (int32_t)std::min<int64_t>(by_sort.rows, FILL_GROUPS);
     sort_portions_kernel<<<(unsigned)(portions + by_sort.groups), SORT_THREADS, 0, st>>>(a, w, per_thread, digit_bits, passes, by_sort);
@@ -592,7 +594,8 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& args, int32_t g_type, 
     const int64_t chunks = ((int64_t)a.n_tokens + chunk - 1) / chunk;
     const int64_t by_join = std::min<int64_t>(left, (int64_t)(FILL_JOIN / row));
     const Fill by_add = {0, left - by_join, 0};
-    const int64_t units = chunks * slabs + (by_add.rows + FILL_ROWS - 1) / FILL_ROWS, blocks = (units + ADD_THREADS / WAVE - 1) / (ADD_THREADS / WAVE);
+    const int64_t units = chunks * slabs + (by_add.rows + FILL_ROWS - 1) / FILL_ROWS;
+    const int64_t blocks = (units + ADD_THREADS / WAVE - 1) / (ADD_THREADS / WAVE);
     if (blocks > 0x7FFFFFFFLL) return hipErrorInvalidValue;
     const int64_t per_join = JOIN_THREADS / WAVE * FILL_ROWS, fillers = (by_join + per_join - 1) / per_join;
     return with_layout(a, g_type, dw_type, [&](auto layout, auto acc, auto ge, auto we) {

@@ -406,9 +406,10 @@ __global__ __launch_bounds__(WAVE) void logprob_join_kernel(const LogprobArgs a,
 }
 
 // How a row is cut.  Many rows: a workgroup of LP_THREADS each, several to a compute unit, so that one's reductions and
-// ranking run beside another's loads (a larger one for alternatives of rows above 512 KB, whose second look it
-// shortens).  At most one row to a compute unit: a larger workgroup, or, where one unit's loads take longer than a second launch does, parts of at least LP_LEAST logits, about LP_GROUPS of them.  Measured, us, no
-// alternatives / 20 of them, the two sides of each border:
+// ranking run beside another's loads (a larger one for alternatives of rows above 512 KB, whose second look it shortens).  At
+// most one row to a compute unit: a larger workgroup, or, where one unit's loads take longer than a second launch does, parts
+// of at least LP_LEAST logits, about LP_GROUPS of them.  Measured, us, no alternatives / 20 of them, the two sides of each
+// border:
 //   300 x 32000 bf16      narrow  8.7 / 15.3   wide  11.7 / 20.8
 //   64 x 32000 f32        wide    7.4 / 11.3   narrow 8.8 / 14.5
 //   64 x 12000 f32        narrow  8.0 /  9.0   wide   7.5 /  9.9

@@ -983,3 +983,15 @@ def test_embedding_backward_few_tokens(env, tokens, accumulate):
         g = torch.randn(tokens, dim, generator=gen, device="cuda").bfloat16()
         check_embedding_grad(env, g, ids.int(), 1.5, accumulate, torch.ones(vocab, dim, device="cuda"))
         check_embedding_grad(env, rows_of(torch, g, 1, 1), ids.int(), 1.5, accumulate, torch.ones(vocab, dim, device="cuda").bfloat16())
+
+
+@pytest.mark.parametrize("tokens", [15, 16, 17, 33])
+def test_embedding_backward_widest_rows(env, tokens):
+    """Rows of DC_MAX_DIM columns: few tokens, and those that are too many workgroups for one launch."""
+    torch, B = env
+    gen = torch.Generator(device="cuda").manual_seed(tokens)
+    for dim in (B.DC_MAX_DIM, B.DC_MAX_DIM - 3):
+        g = torch.randn(tokens, dim, generator=gen, device="cuda").bfloat16()
+        for ids in (torch.arange(tokens, device="cuda") * 0 + 3, torch.arange(tokens, device="cuda") % 7 - 1):
+            for accumulate in (False, True):
+                check_embedding_grad(env, g, ids.int(), 1.0, accumulate, torch.ones(40, dim, device="cuda"))
