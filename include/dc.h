@@ -497,8 +497,10 @@ typedef struct dc_adamw_params {
  * magnitude / 448 and e4m3 values, nearest, ties to even: m is stored as such, v as its square root (half the range, and
  * what is divided by).  A root that is not zero is stored as no less than 2^-9 s, so it never becomes zero.  A block whose
  * s would be below 2^-120 is stored as zeros.  The step itself uses m and v before they are rounded.  All-zero codes and
- * scales are the states before the first step.
- * An element whose gradient is not finite gets a parameter that is not; the 8-bit states of its block are then unspecified.
+ * scales are the states before the first step.  The root is in the range of 32 bits for every finite gradient, also where v is
+ * not (gradients above 1.8e19).
+ * An element whose gradient (times *d_grad_scale) is not finite gets a parameter that is not; the 8-bit states of its block
+ * are then unspecified.
  *
  * dc_adamw_table writes what the kernel reads about the tensors into d_table (256-byte aligned, dc_adamw_table_bytes bytes);
  * call it once, and again when a pointer, a size, a type or a weight decay changes.  dc_adamw takes the same tensors and

@@ -104,6 +104,16 @@ __device__ __forceinline__ float step_of(const AdamwStep& s, float decay, float 
     root = sqrtf(v);
     return w * decay - s.step_size * quotient(m, root * s.inv_root_bc2 + s.eps);
 }
+// Behind it, for an element whose v is beyond 32 bits (a gradient above 1.8e19) but not its root, which is what 8 bits keep: the
+// root and the weight again from what they were, with everything 2^-80 times as large, where a square fits and eps is nothing.
+__device__ __forceinline__ float far_step_of(const AdamwStep& s, float decay, float g, float w, float& m, float& root) {
+    constexpr float LESS = 0x1p-80f, MOST = 0x1.fffffep127f;
+    const float gl = g * LESS, rl = root * LESS, root_l = sqrtf(rl * rl * s.beta2 + gl * gl * s.one_minus_beta2);
+    // (averages of finite numbers: only their rounding can pass the largest)
+    root = fminf(root_l / LESS, MOST);
+    if (fabsf(g) <= MOST) m = fminf(fmaxf(m, -MOST), MOST);
+    return w * decay - s.step_size * quotient(m * LESS, root_l * s.inv_root_bc2);
+}
 // The scales of a block whose largest magnitudes are these, and their inverses; both 0 for what is stored as zeros.  One half of
 // the wave divides for the one, the other half for the other.
 struct Scales { float m, m_inverse, root, root_inverse; };
@@ -124,8 +134,8 @@ __device__ __forceinline__ float wave_most(float v) {
     return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)m, WAVE - 1));
 }
 
-// A wave's block of DC_STATE_BLOCK elements or fewer, element by element: the last block of a tensor, and tensors that are
-// not aligned.
+// A wave's block of DC_STATE_BLOCK elements or fewer, element by element: the last block of a tensor, tensors that are not
+// aligned, and blocks of 8-bit states with a v beyond 32 bits.
 __device__ __forceinline__ void block_by_elements(const AdamwStep& s, const dc_adamw_tensor& d, int64_t block, float gs, float decay) {
     const int64_t at = block * DC_STATE_BLOCK;
     const bool small = d.state_type == DC_E4M3;
@@ -136,17 +146,22 @@ __device__ __forceinline__ void block_by_elements(const AdamwStep& s, const dc_a
         const int64_t i = at + j * WAVE + lane_id();
         m[j] = root[j] = 0.0f;
         if (i >= d.n) continue;
-        float v;
+        float v, old_root = 0.0f;
         if (small) {
             m[j] = from_e4m3(static_cast<const uint8_t*>(d.d_exp_avg)[i]) * ms;
-            const float r = from_e4m3(static_cast<const uint8_t*>(d.d_exp_avg_sq)[i]) * vs;
-            v = r * r;
+            old_root = from_e4m3(static_cast<const uint8_t*>(d.d_exp_avg_sq)[i]) * vs;
+            v = old_root * old_root;
         } else {
             m[j] = static_cast<const float*>(d.d_exp_avg)[i];
             v = static_cast<const float*>(d.d_exp_avg_sq)[i];
         }
-        const float w = step_of(s, decay, load_as(d.d_grad, i, d.grad_type) * gs,
-                                d.d_master ? d.d_master[i] : load_as(d.d_param, i, d.param_type), m[j], v, root[j]);
+        const float g = load_as(d.d_grad, i, d.grad_type) * gs;
+        const float old_w = d.d_master ? d.d_master[i] : load_as(d.d_param, i, d.param_type);
+        float w = step_of(s, decay, g, old_w, m[j], v, root[j]);
+        if (small && v == INFINITY) {
+            root[j] = old_root;
+            w = far_step_of(s, decay, g, old_w, m[j], root[j]);
+        }
         if (d.d_master) d.d_master[i] = w;
         store_as(d.d_param, i, d.param_type, w);
         if (!small) {
@@ -199,9 +214,10 @@ __device__ __forceinline__ void store4(void* p, int64_t i, const float (&f)[4]) 
 }
 
 // A wave's block of an aligned tensor, four neighbouring elements to a lane; everything is asked for before anything is used.
-// G: the gradient's type, P: what the weights are read from (the master's float, or the parameter's).
+// G: the gradient's type, P: what the weights are read from (the master's float, or the parameter's).  False, and nothing
+// written, where the block has to go by elements: a v beyond 32 bits in 8-bit states.
 template <typename G, typename P, bool MASTER, bool SMALL>
-__device__ __forceinline__ void whole_block(const AdamwStep& s, const dc_adamw_tensor& d, int64_t block, float gs, float decay) {
+__device__ __forceinline__ bool whole_block(const AdamwStep& s, const dc_adamw_tensor& d, int64_t block, float gs, float decay) {
     const int64_t i = block * DC_STATE_BLOCK + lane_id() * 4;
     const Raw4<G> rg = load4<G>(d.d_grad, i);
     const Raw4<P> rw = load4<P>(MASTER ? (const void*)d.d_master : d.d_param, i);
@@ -223,6 +239,15 @@ __device__ __forceinline__ void whole_block(const AdamwStep& s, const dc_adamw_t
     }
 #pragma unroll
     for (int c = 0; c < 4; ++c) w[c] = step_of(s, decay, (float)rg.e[c] * gs, (float)rw.e[c], m[c], v[c], root[c]);
+    float root_most = 0.0f;                      // this lane's
+    if constexpr (SMALL) {
+        // (the weights and m are there before the branch: left to itself the compiler asks for what they are made of behind it,
+        // which takes 8 % more time)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) asm volatile("" : "+v"(w[c]), "+v"(m[c]));
+        root_most = fmaxf(fmaxf(root[0], root[1]), fmaxf(root[2], root[3]));
+        if (__ballot(root_most == INFINITY)) return false;
+    }
     if constexpr (MASTER) {
         store4<float>(d.d_master, i, w);
         if (d.param_type == DC_BF16) store4<__bf16>(d.d_param, i, w);
@@ -233,7 +258,7 @@ __device__ __forceinline__ void whole_block(const AdamwStep& s, const dc_adamw_t
     }
     if constexpr (SMALL) {
         const Scales sc = scales_of(wave_most(fmaxf(fmaxf(fabsf(m[0]), fabsf(m[1])), fmaxf(fabsf(m[2]), fabsf(m[3])))),
-                                    wave_most(fmaxf(fmaxf(root[0], root[1]), fmaxf(root[2], root[3]))));
+                                    wave_most(root_most));
         const uint32_t em = to_e4m3(m[0] * sc.m_inverse, m[1] * sc.m_inverse, m[2] * sc.m_inverse, m[3] * sc.m_inverse);
         const uint32_t er = to_e4m3(root_code(root[0], sc.root_inverse), root_code(root[1], sc.root_inverse), root_code(root[2], sc.root_inverse),
                                     root_code(root[3], sc.root_inverse));
@@ -244,13 +269,14 @@ __device__ __forceinline__ void whole_block(const AdamwStep& s, const dc_adamw_t
         store4<float>(d.d_exp_avg, i, m);
         store4<float>(d.d_exp_avg_sq, i, v);
     }
+    return true;
 }
 template <typename G, bool SMALL>
-__device__ __forceinline__ void whole_block_of(const AdamwStep& s, const dc_adamw_tensor& d, int64_t block, float gs, float decay) {
-    if (d.d_master) whole_block<G, float, true, SMALL>(s, d, block, gs, decay);
-    else if (d.param_type == DC_F32) whole_block<G, float, false, SMALL>(s, d, block, gs, decay);
-    else if (d.param_type == DC_BF16) whole_block<G, __bf16, false, SMALL>(s, d, block, gs, decay);
-    else whole_block<G, _Float16, false, SMALL>(s, d, block, gs, decay);
+__device__ __forceinline__ bool whole_block_of(const AdamwStep& s, const dc_adamw_tensor& d, int64_t block, float gs, float decay) {
+    if (d.d_master) return whole_block<G, float, true, SMALL>(s, d, block, gs, decay);
+    if (d.param_type == DC_F32) return whole_block<G, float, false, SMALL>(s, d, block, gs, decay);
+    if (d.param_type == DC_BF16) return whole_block<G, __bf16, false, SMALL>(s, d, block, gs, decay);
+    return whole_block<G, _Float16, false, SMALL>(s, d, block, gs, decay);
 }
 
 // One workgroup per piece, a wave per block.  What a tensor is made of is the same for a whole piece, so the kinds are branches
@@ -273,19 +299,19 @@ __global__ __launch_bounds__(AW_THREADS) void adamw_kernel(const AdamwStep s, co
         const dc_adamw_tensor d = tensors[piece.tensor];     // (a copy: no store below can be thought to change it)
         const float decay = (float)(1.0 - s.lr64 * d.weight_decay);
         const int64_t block = (int64_t)piece.piece * (ADAMW_PIECE / DC_STATE_BLOCK) + wave;
+        bool done = block * DC_STATE_BLOCK >= d.n;
         if (d.reserved && (block + 1) * DC_STATE_BLOCK <= d.n) {           // (in the table: whether all of it is aligned)
             if (d.state_type == DC_E4M3) {
-                if (d.grad_type == DC_BF16) whole_block_of<__bf16, true>(s, d, block, gs, decay);
-                else if (d.grad_type == DC_F32) whole_block_of<float, true>(s, d, block, gs, decay);
-                else whole_block_of<_Float16, true>(s, d, block, gs, decay);
+                if (d.grad_type == DC_BF16) done = whole_block_of<__bf16, true>(s, d, block, gs, decay);
+                else if (d.grad_type == DC_F32) done = whole_block_of<float, true>(s, d, block, gs, decay);
+                else done = whole_block_of<_Float16, true>(s, d, block, gs, decay);
             } else {
-                if (d.grad_type == DC_BF16) whole_block_of<__bf16, false>(s, d, block, gs, decay);
-                else if (d.grad_type == DC_F32) whole_block_of<float, false>(s, d, block, gs, decay);
-                else whole_block_of<_Float16, false>(s, d, block, gs, decay);
+                if (d.grad_type == DC_BF16) done = whole_block_of<__bf16, false>(s, d, block, gs, decay);
+                else if (d.grad_type == DC_F32) done = whole_block_of<float, false>(s, d, block, gs, decay);
+                else done = whole_block_of<_Float16, false>(s, d, block, gs, decay);
             }
-        } else if (block * DC_STATE_BLOCK < d.n) {
-            block_by_elements(s, d, block, gs, decay);
         }
+        if (!done) block_by_elements(s, d, block, gs, decay);
     }
 }
 

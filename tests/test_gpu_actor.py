@@ -995,3 +995,24 @@ def test_embedding_backward_widest_rows(env, tokens):
         for ids in (torch.arange(tokens, device="cuda") * 0 + 3, torch.arange(tokens, device="cuda") % 7 - 1):
             for accumulate in (False, True):
                 check_embedding_grad(env, g, ids.int(), 1.0, accumulate, torch.ones(40, dim, device="cuda"))
+
+
+@pytest.mark.parametrize("n,shift", [(2048, 0), (1000, 0), (1000, 3)])
+@pytest.mark.parametrize("grad,master", [("f32", False), ("bf16", True)])
+@pytest.mark.parametrize("most", [1e20, 1e30, 3e38])
+def test_adamw_finite_gradients_whose_squares_are_not(env, most, grad, master, n, shift):
+    """In 8 bits the second moment is kept as its root: a finite gradient whose square is beyond 32 bits leaves finite states
+    and weights, and what 64 bits make of it, in that step and in those behind it."""
+    torch, B = env
+    it = adamw_tensors(torch, [n], "bf16" if master else "f32", grad, master, 8, seed=4, shift=shift)[0]
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    for step in range(1, 5):
+        it["grad"].copy_(torch.randn(n, generator=gen, device="cuda"))
+        if step < 3:
+            it["grad"][[5, 300, n - 1]] = torch.tensor([most, -most, most / 3], device="cuda").to(it["grad"].dtype)
+        before = snapshot(it)
+        prm = B.make_adamw(1e-2, 0.9, 0.95, 1e-8, step)
+        adamw_call(env, [it], prm)
+        for k in ("param", "master", "exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale"):
+            assert it[k] is None or bool(it[k].float().isfinite().all()), (step, k)
+        check_adamw(torch, before, it, prm, 1.0)
