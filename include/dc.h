@@ -495,8 +495,12 @@ typedef struct dc_adamw_params {
  * w is d_master, or d_param where there is none; d_param is w rounded once.
  * States in 8 bits: per DC_STATE_BLOCK elements (the last block of a tensor may be shorter) a scale s = the block's largest
  * magnitude / 448 and e4m3 values, nearest, ties to even: m is stored as such, v as its square root (half the range, and
- * what is divided by).  A root that is not zero is stored as no less than 2^-9 s, so it never becomes zero.  A block whose
- * s would be below 2^-120 is stored as zeros.  The step itself uses m and v before they are rounded.  All-zero codes and
+ * what is divided by).  Where a step's gradient has less than 1/24 of v, (1 - beta2) / (1 - beta2^step) < 1/24 (beta2 above
+ * 23/24, behind the first steps), a root moves by less in a step than e4m3 values are apart and nearest would hold it where it
+ * is: there it becomes the value below or above it, by chance and the likelier the nearer, so that it follows v on average.
+ * The chance is a function of the step, the element's place in its tensor and its gradient: identical inputs give identical
+ * bits.  A root that is not zero is stored as no less than 2^-9 s, so it never becomes zero.  A block whose s would be below
+ * 2^-120 is stored as zeros.  The step itself uses m and v before they are rounded.  All-zero codes and
  * scales are the states before the first step.  The root is in the range of 32 bits for every finite gradient, also where v is
  * not (gradients above 1.8e19).
  * An element whose gradient (times *d_grad_scale) is not finite gets a parameter that is not; the 8-bit states of its block

@@ -187,9 +187,13 @@ dc_status dc_adamw(const dc_adamw_tensor* tensors, int32_t n_tensors, const dc_a
     const AdamwTable t = carve_adamw_table(const_cast<void*>(d_table), n_tensors, n_pieces);
     if (table_bytes < t.bytes) return DC_ERR_WORKSPACE;
     const double bc1 = 1.0 - std::pow(prm->beta1, (double)prm->step), bc2 = 1.0 - std::pow(prm->beta2, (double)prm->step);
+    // the share that this step's gradient has in v, once the average is corrected for its start at 0
+    const bool dither = (1.0 - prm->beta2) / bc2 < 1.0 / 24;
+    uint64_t seed = (uint64_t)prm->step * 0x9E3779B97F4A7C15u;             // (an odd multiple of each step: all differ)
+    seed = (seed ^ seed >> 32) * 0xD6E8FEB86659FD93u;
     const AdamwStep s = {(float)prm->lr, (float)(prm->lr / bc1), (float)prm->beta1, (float)(1.0 - prm->beta1),
                          (float)prm->beta2, (float)(1.0 - prm->beta2), (float)(1.0 / std::sqrt(bc2)), (float)prm->eps,
-                         prm->lr, d_grad_scale, d_status};
+                         prm->lr, dither, (uint32_t)(seed >> 32), d_grad_scale, d_status};
     const hipError_t e = launch_adamw(s, n_tensors, t, n_pieces, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? DC_OK : DC_ERR_HIP;
 }

@@ -1016,3 +1016,62 @@ def test_adamw_finite_gradients_whose_squares_are_not(env, most, grad, master, n
         for k in ("param", "master", "exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale"):
             assert it[k] is None or bool(it[k].float().isfinite().all()), (step, k)
         check_adamw(torch, before, it, prm, 1.0)
+
+
+@pytest.mark.parametrize("beta2,steps", [(0.95, 400), (0.97, 600), (0.98, 600), (0.99, 1000), (0.999, 6000)])
+def test_adamw_8_bit_second_moment_follows(env, beta2, steps):
+    """Many steps with 8-bit states beside the second moment in 64 bits: at a sixth of the steps the gradients of every other
+    element fall to a tenth, and the kept roots have to fall with them.  A root moves by about (1 - beta2) / 2 of itself in a
+    step, the block's scale by as much; rounded by chance to codes at most 1/8 apart each move adds at most its own size times
+    1/8 to the variance, and a step takes 1 - beta2 of what there is off: a relative variance of at most 1/16.  A median is
+    off by no more than the mean's bias of that size twice, 5 of 100 by no more than two deviations."""
+    torch, B = env
+    n, gen = 64 * 256, torch.Generator(device="cuda").manual_seed(9)
+    it = dict(param=torch.zeros(n, device="cuda"), master=None, grad=torch.empty(n, device="cuda"),
+              exp_avg=torch.zeros(n, dtype=torch.float8_e4m3fn, device="cuda"), exp_avg_scale=torch.zeros(n // 256, device="cuda"),
+              exp_avg_sq=torch.zeros(n, dtype=torch.float8_e4m3fn, device="cuda"), exp_avg_sq_scale=torch.zeros(n // 256, device="cuda"))
+    ts = B.AdamwTensors([it])
+    need = B.dc_adamw_table_bytes(ts)
+    table, st = torch.empty(need, dtype=torch.uint8, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.dc_adamw_table(ts, table, need)
+    v = torch.zeros(n, dtype=torch.float64, device="cuda")
+    for step in range(1, steps + 1):
+        it["grad"].normal_(generator=gen)
+        if step > steps // 6:
+            it["grad"][1::2] *= 0.1
+        v.mul_(beta2).add_(it["grad"].double() ** 2, alpha=1 - beta2)
+        B.dc_adamw(ts, B.make_adamw(1e-3, 0.9, beta2, 1e-8, step), None, table, need, st)
+    ratio = it["exp_avg_sq"].double() * spread(torch, it["exp_avg_sq_scale"], n) / v.sqrt()
+    assert int(st) == 0
+    for part in (ratio[1::2], ratio[0::2]):
+        low, mid, high = part.quantile(torch.tensor([0.05, 0.5, 0.95], dtype=torch.float64, device="cuda")).tolist()
+        assert abs(mid - 1) <= 2 / 16 and low >= 0.5 and high <= 1.5 + 2 / 16, (beta2, low, mid, high)
+
+
+@pytest.mark.parametrize("shift", [0, 3])
+def test_adamw_8_bit_roots_by_chance(env, shift):
+    """Behind the first steps of a large beta2 every root becomes the code below or above it, without a bias, the same again
+    for the same inputs and another way in another step."""
+    torch, B = env
+    n = 200 * 256 + 77
+    before = adamw_tensors(torch, [n], "f32", "f32", False, 8, seed=6, shift=shift)[0]
+    held = torch.arange(127, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn).double()         # all that e4m3 has from 0 up
+    got = []
+    for step in (24000, 24000, 24001):
+        it = adamw_tensors(torch, [n], "f32", "f32", False, 8, seed=6, shift=shift)[0]
+        adamw_call(env, [it], B.make_adamw(1e-3, 0.9, 0.999, 1e-8, step))
+        got.append(it["exp_avg_sq"].clone())
+        old = before["exp_avg_sq"].double() * spread(torch, before["exp_avg_sq_scale"], n)
+        root = (0.999 * old ** 2 + 0.001 * before["grad"].double() ** 2).sqrt()
+        c = root / spread(torch, it["exp_avg_sq_scale"], n)   # off by the scale's, the root's and the products' roundings
+        code, near = it["exp_avg_sq"].double(), 16 * U * c
+        above = torch.searchsorted(held, c + near).clamp(max=126)
+        below = (torch.searchsorted(held, c - near, right=True) - 1).clamp(min=1)
+        assert bool(((code >= held[below]) & (code <= held[above])).all())
+        inside = (c > 2.0 ** -9) & (c < 447)
+        gap = torch.where(c < 2.0 ** -6, 2.0 ** -9, torch.exp2(torch.floor(torch.log2(c)) - 3))
+        off = ((code - c) / gap)[inside]
+        # each is off by a number of mean 0 and a variance of at most 1/4: six deviations of the mean
+        assert abs(float(off.mean())) <= 6 * 0.5 / math.sqrt(off.numel()) and float(off.abs().max()) < 1 + 1e-4
+    assert torch.equal(got[0].view(torch.uint8), got[1].view(torch.uint8))
+    assert float((got[0].view(torch.uint8) != got[2].view(torch.uint8)).double().mean()) > 0.1
