@@ -1,5 +1,6 @@
 // C-ABI entry points of the actor's update: host-side validation and launches, nothing else.
 #include <cmath>
+#include <cstring>
 #include "actor_internal.h"
 
 namespace dc {
@@ -52,6 +53,31 @@ static dc_status check_tensors(const dc_adamw_tensor* t, int32_t n, int64_t* n_p
     }
     *n_pieces = pieces;
     return DC_OK;
+}
+
+// What dc_adamw_table writes and dc_adamw looks for at the table's start: 64 bits of everything that the kernel would take out of
+// the table, so that one made for other tensors, or for these before they changed, is not used.
+static AdamwHeader header_of(const dc_adamw_tensor* t, int32_t n, int64_t n_pieces) {
+    uint64_t print = 0x9E3779B97F4A7C15u;
+    const auto add = [&](uint64_t word) {        // (one to one in the word and in what came before)
+        print = (print ^ word) * 0xD6E8FEB86659FD93u;
+        print ^= print >> 32;
+    };
+    for (int32_t i = 0; i < n; ++i) {
+        const dc_adamw_tensor& d = t[i];
+        add((uint64_t)d.n);
+        if (d.n == 0) continue;
+        for (const void* p : {(const void*)d.d_param, (const void*)d.d_master, d.d_grad, (const void*)d.d_exp_avg, (const void*)d.d_exp_avg_sq})
+            add(reinterpret_cast<uintptr_t>(p));
+        if (d.state_type == DC_E4M3)
+            for (const void* p : {(const void*)d.d_exp_avg_scale, (const void*)d.d_exp_avg_sq_scale}) add(reinterpret_cast<uintptr_t>(p));
+        const double decay = d.weight_decay + 0.0;               // (a zero's sign does not count)
+        uint64_t bits;
+        std::memcpy(&bits, &decay, sizeof bits);
+        add(bits);
+        add((uint64_t)d.param_type << 16 | (uint64_t)d.grad_type << 8 | (uint64_t)d.state_type);
+    }
+    return AdamwHeader{n_pieces, print, n, 0};
 }
 
 }  // namespace dc
@@ -171,7 +197,7 @@ dc_status dc_adamw_table(const dc_adamw_tensor* tensors, int32_t n_tensors, void
     if (!d_table || !aligned_to(d_table, 256)) return DC_ERR_INVALID_ARG;
     const AdamwTable t = carve_adamw_table(d_table, n_tensors, n_pieces);
     if (table_bytes < t.bytes) return DC_ERR_WORKSPACE;
-    const hipError_t e = launch_adamw_table(tensors, n_tensors, t, n_pieces, static_cast<hipStream_t>(hip_stream));
+    const hipError_t e = launch_adamw_table(tensors, header_of(tensors, n_tensors, n_pieces), t, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? DC_OK : DC_ERR_HIP;
 }
 
@@ -194,7 +220,7 @@ dc_status dc_adamw(const dc_adamw_tensor* tensors, int32_t n_tensors, const dc_a
     const AdamwStep s = {(float)prm->lr, (float)(prm->lr / bc1), (float)prm->beta1, (float)(1.0 - prm->beta1),
                          (float)prm->beta2, (float)(1.0 - prm->beta2), (float)(1.0 / std::sqrt(bc2)), (float)prm->eps,
                          prm->lr, dither, (uint32_t)(seed >> 32), d_grad_scale, d_status};
-    const hipError_t e = launch_adamw(s, n_tensors, t, n_pieces, static_cast<hipStream_t>(hip_stream));
+    const hipError_t e = launch_adamw(s, header_of(tensors, n_tensors, n_pieces), t, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? DC_OK : DC_ERR_HIP;
 }
 

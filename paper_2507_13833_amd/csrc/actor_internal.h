@@ -69,7 +69,7 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, int32_t g_type, int
 // The optimizer's table: a header, the tensors, and for every piece of ADAMW_PIECE elements its tensor and its place there.
 constexpr int ADAMW_PIECE = 2048;
 static_assert(ADAMW_PIECE % DC_STATE_BLOCK == 0, "a block of an 8-bit state lies in one piece");
-struct AdamwHeader { int64_t n_pieces; int32_t n_tensors, pad; };
+struct AdamwHeader { int64_t n_pieces; uint64_t print; int32_t n_tensors, pad; };       // print: of the tensors that it was made for
 struct AdamwPiece  { int32_t tensor, piece; };
 struct AdamwTable  { AdamwHeader* head; dc_adamw_tensor* tensors; AdamwPiece* pieces; size_t bytes; };
 AdamwTable carve_adamw_table(void* base, int32_t n_tensors, int64_t n_pieces);
@@ -81,7 +81,7 @@ struct AdamwStep {
     const float* grad_scale;
     int32_t* status;
 };
-hipError_t launch_adamw_table(const dc_adamw_tensor* tensors, int32_t n_tensors, const AdamwTable& t, int64_t n_pieces, hipStream_t st);
-hipError_t launch_adamw(const AdamwStep& s, int32_t n_tensors, const AdamwTable& t, int64_t n_pieces, hipStream_t st);
+hipError_t launch_adamw_table(const dc_adamw_tensor* tensors, const AdamwHeader& head, const AdamwTable& t, hipStream_t st);
+hipError_t launch_adamw(const AdamwStep& s, const AdamwHeader& head, const AdamwTable& t, hipStream_t st);
 
 }  // namespace dc

@@ -42,11 +42,12 @@ static int32_t aligned(const dc_adamw_tensor& d) {
     return all % 16 == 0;
 }
 
-hipError_t launch_adamw_table(const dc_adamw_tensor* tensors, int32_t n_tensors, const AdamwTable& t, int64_t n_pieces, hipStream_t st) {
+hipError_t launch_adamw_table(const dc_adamw_tensor* tensors, const AdamwHeader& head, const AdamwTable& t, hipStream_t st) {
+    const int32_t n_tensors = head.n_tensors;
     int64_t at = 0;
     for (int32_t first = 0; first < n_tensors; first += TABLE_TENSORS) {
         TableChunk c = {};
-        c.head = AdamwHeader{n_pieces, n_tensors, 0};
+        c.head = head;
         c.first = first;
         c.count = n_tensors - first < TABLE_TENSORS ? n_tensors - first : TABLE_TENSORS;
         int64_t most = 1;
@@ -316,10 +317,11 @@ __device__ __forceinline__ bool whole_block_of(const AdamwStep& s, const dc_adam
 // four blocks a wave, all asked for at once: within 2 % for 32-bit states, 3 to 5 % slower for 8-bit ones.  Plain stores
 // instead of streamed ones: 6 % slower.
 constexpr int AW_THREADS = ADAMW_PIECE / DC_STATE_BLOCK * WAVE;
-__global__ __launch_bounds__(AW_THREADS) void adamw_kernel(const AdamwStep s, const AdamwHeader* __restrict__ head,
+__global__ __launch_bounds__(AW_THREADS) void adamw_kernel(const AdamwStep s, const AdamwHeader want, const AdamwHeader* __restrict__ head,
                                                            const dc_adamw_tensor* __restrict__ tensors,
-                                                           const AdamwPiece* __restrict__ pieces, int64_t n_pieces, int32_t n_tensors) {
-    if (head->n_pieces != n_pieces || head->n_tensors != n_tensors) {
+                                                           const AdamwPiece* __restrict__ pieces) {
+    const int64_t n_pieces = want.n_pieces;
+    if (head->n_pieces != n_pieces || head->n_tensors != want.n_tensors || head->print != want.print) {
         if (threadIdx.x == 0) set_status(s.status, DC_ERR_BAD_LAYOUT);
         return;
     }
@@ -346,10 +348,10 @@ __global__ __launch_bounds__(AW_THREADS) void adamw_kernel(const AdamwStep s, co
     }
 }
 
-hipError_t launch_adamw(const AdamwStep& s, int32_t n_tensors, const AdamwTable& t, int64_t n_pieces, hipStream_t st) {
-    if (n_pieces == 0) return hipSuccess;
-    const unsigned grid = (unsigned)(n_pieces < (1 << 22) ? n_pieces : 1 << 22);     // (2^31 threads)
-    adamw_kernel<<<grid, AW_THREADS, 0, st>>>(s, t.head, t.tensors, t.pieces, n_pieces, n_tensors);
+hipError_t launch_adamw(const AdamwStep& s, const AdamwHeader& head, const AdamwTable& t, hipStream_t st) {
+    if (head.n_pieces == 0) return hipSuccess;
+    const unsigned grid = (unsigned)(head.n_pieces < (1 << 22) ? head.n_pieces : 1 << 22);     // (2^31 threads)
+    adamw_kernel<<<grid, AW_THREADS, 0, st>>>(s, head, t.head, t.tensors, t.pieces);
     return hipGetLastError();
 }
 

@@ -1075,3 +1075,33 @@ def test_adamw_8_bit_roots_by_chance(env, shift):
         assert abs(float(off.mean())) <= 6 * 0.5 / math.sqrt(off.numel()) and float(off.abs().max()) < 1 + 1e-4
     assert torch.equal(got[0].view(torch.uint8), got[1].view(torch.uint8))
     assert float((got[0].view(torch.uint8) != got[2].view(torch.uint8)).double().mean()) > 0.1
+
+
+@pytest.mark.parametrize("change", ["shorter", "swapped", "gradient", "decay", "state"])
+def test_adamw_refuses_a_table_of_as_many_pieces(env, change):
+    """Tables with the right numbers of tensors and of pieces, but of other tensors.  Every buffer has room for all of them."""
+    torch, B = env
+    room = adamw_tensors(torch, [4096, 4096], "f32", "f32", False, 32)
+    other = torch.zeros(4096, device="cuda")
+
+    def tensors(sizes, **more):
+        return [{k: v[:n] if hasattr(v, "numel") else v for k, v in it.items()} | (more if i == 0 else {})
+                for i, (it, n) in enumerate(zip(room, sizes))]
+    made = tensors([2000, 4000])
+    now = {"shorter": tensors([1, 4000]), "swapped": tensors([2000, 4000])[::-1], "gradient": tensors([2000, 4000], grad=other[:2000]),
+           "decay": tensors([2000, 4000], weight_decay=0.5), "state": tensors([2000, 4000], exp_avg=other[:2000])}[change]
+    ts, table, need, st = adamw_call(env, made, B.make_adamw(1e-3))
+    again = B.AdamwTensors(now)
+    assert B.dc_adamw_table_bytes(again) == need
+    before = [snapshot(it) for it in room]
+    B.dc_adamw(again, B.make_adamw(1e-3, step=2), None, table, need, st)
+    torch.cuda.synchronize()
+    assert int(st) == B.DC_ERR_BAD_LAYOUT
+    for b, it in zip(before, room):
+        for k in ("param", "grad", "exp_avg", "exp_avg_sq"):
+            assert torch.equal(b[k], it[k])
+    st.zero_()
+    B.dc_adamw_table(again, table, need)                      # made again it serves
+    B.dc_adamw(again, B.make_adamw(1e-3, step=2), None, table, need, st)
+    torch.cuda.synchronize()
+    assert int(st) == 0 and not torch.equal(before[1]["param"], room[1]["param"])
