@@ -506,13 +506,14 @@ def dc_embedding_backward(grad_out: dc_matrix, d_token, scale: float, accumulate
 
 
 class AdamwTensors:
-    """Host array of dc_adamw_tensor, and the tensors it points into.  items: dicts with param, grad, exp_avg, exp_avg_sq
-    and, where there are any, master, exp_avg_scale, exp_avg_sq_scale, weight_decay."""
+    """Host array of dc_adamw_tensor, and the tensors it points into, which it keeps whatever becomes of the dicts.  items:
+    dicts with param, grad, exp_avg, exp_avg_sq and, where there are any, master, exp_avg_scale, exp_avg_sq_scale,
+    weight_decay."""
 
     _SCALES = ("exp_avg_scale", "exp_avg_sq_scale")
 
     def __init__(self, items: Sequence[dict]):
-        self._keep = items
+        items = self._keep = [dict(it) for it in items]
         self.n = len(items)
         self.array = (dc_adamw_tensor * max(1, self.n))()
         for i, it in enumerate(items):

@@ -254,3 +254,22 @@ def test_adamw_eps_that_32_bits_cannot_divide_by():
     need = B.dc_adamw_table_bytes(t)
     for eps in (1e-39, 1e-31, 1e31, 1e38):                    # a denormal; what has no normal reciprocal
         refuses(B.DC_ERR_INVALID_ARG, B.dc_adamw, t, B.make_adamw(1e-3, eps=eps), None, A, need, A)
+
+
+def test_adamw_tensors_outlive_the_dicts_they_came_in():
+    """The array holds addresses, so what they belong to stays, also when a program puts another gradient, or none, in its dict."""
+    import gc
+    import weakref
+    item = {k: FakeTensor((8,)) for k in ("param", "grad", "exp_avg", "exp_avg_sq")}
+    seen = {k: weakref.ref(t) for k, t in item.items()}
+    items = [item]
+    t = B.AdamwTensors(items)
+    item["grad"] = None
+    item["param"] = FakeTensor((8,))
+    items.clear()
+    del item
+    gc.collect()
+    assert t.n == 1 and all(ref() is not None for ref in seen.values())
+    del t
+    gc.collect()
+    assert all(ref() is None for ref in seen.values())
