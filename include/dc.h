@@ -458,8 +458,8 @@ dc_status dc_embedding(const dc_matrix* weight, const int32_t* d_token, double s
  * in an order that depends on the tokens alone (identical inputs give identical bits), rounded once.  accumulate == 0:
  * every row of grad_weight is written, those without a token with +0.  accumulate != 0: the sum is added to the row in 32
  * bits before it is rounded, and rows without a token are not touched.  Tokens equal to DC_NO_TOKEN add nothing.
- * d_ws: 256-byte aligned, dc_embedding_backward_workspace_bytes(grad_out, grad_weight) bytes; holds nothing the caller
- * needs afterwards.
+ * d_ws: 256-byte aligned, dc_embedding_backward_workspace_bytes(grad_out, grad_weight) bytes, which also serve every call of
+ * fewer tokens, fewer columns or both; holds nothing the caller needs afterwards.
  * Host errors: INVALID_ARG, UNSUPPORTED_SIZE (as above, or more than 2^24 tokens), WORKSPACE, HIP.  Device errors: TOKEN_RANGE (that token adds nothing).
  */
 size_t dc_embedding_backward_workspace_bytes(const dc_matrix* grad_out, const dc_matrix* grad_weight);

@@ -173,7 +173,7 @@ dc_status dc_embedding_backward(const dc_matrix* grad_out, const int32_t* d_toke
         grad_out->n_rows * grad_out->n_cols > 1LL << 38)                 // (a launch's threads)
         return DC_ERR_UNSUPPORTED_SIZE;
     if (grad_out->n_rows > 0 && (!d_token || !aligned_to(d_token, 4))) return DC_ERR_INVALID_ARG;
-    const size_t need = embedding_grad_workspace_bytes(grad_out->n_rows, grad_out->n_cols);
+    const size_t need = embedding_grad_workspace_need(grad_out->n_rows, grad_out->n_cols);
     if (need > 0 && (!d_ws || !aligned_to(d_ws, 256))) return DC_ERR_INVALID_ARG;
     if (ws_bytes < need) return DC_ERR_WORKSPACE;
     const EmbeddingGradArgs a = {grad_out->d_data, grad_weight->d_data, grad_out->row_stride, grad_weight->row_stride,

@@ -63,7 +63,8 @@ struct EmbeddingGradArgs {
     int32_t*       status;
     int32_t        dw_bytes, dw_aligned, dw_stream;        // the launcher's: of an element; rows on multiples of 16 bytes; past the caches
 };
-size_t embedding_grad_workspace_bytes(int64_t n_tokens, int64_t dim);
+size_t embedding_grad_workspace_need(int64_t n_tokens, int64_t dim);      // of this call
+size_t embedding_grad_workspace_bytes(int64_t n_tokens, int64_t dim);     // of it and of every smaller one
 hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, int32_t g_type, int32_t dw_type, void* d_ws, hipStream_t st);
 
 // The optimizer's table: a header, the tensors, and for every piece of ADAMW_PIECE elements its tensor and its place there.

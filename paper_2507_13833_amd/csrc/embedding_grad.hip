@@ -37,7 +37,8 @@ struct EmbGradWs {
     size_t    bytes;
 };
 // Entries of a chunk: fewer where there would be too few waves to hide the loads' latency.
-static int chunk_of(int64_t n_tokens, int64_t dim) { return n_tokens * ((dim + COLS - 1) / COLS) < 32768 * 4 ? 16 : 32; }
+constexpr int64_t FEW_WAVES = 32768 * 4;
+static int chunk_of(int64_t n_tokens, int64_t dim) { return n_tokens * ((dim + COLS - 1) / COLS) < FEW_WAVES ? 16 : 32; }
 static EmbGradWs carve_emb_grad(void* base, int64_t n_tokens, int64_t dim) {
     const int64_t CHUNK = chunk_of(n_tokens, dim);
     EmbGradWs w;
@@ -56,8 +57,15 @@ static EmbGradWs carve_emb_grad(void* base, int64_t n_tokens, int64_t dim) {
     w.bytes = off;
     return w;
 }
+size_t embedding_grad_workspace_need(int64_t n_tokens, int64_t dim) { return carve_emb_grad(nullptr, n_tokens, dim).bytes; }
+// As much as any call of at most these tokens and columns needs.  Chunks of either size need no more for fewer of both; but the
+// short ones, of calls below the border, may need more than the long ones of this call: for each number of slabs as wide a row
+// and as many tokens as still have them.
 size_t embedding_grad_workspace_bytes(int64_t n_tokens, int64_t dim) {
-    return carve_emb_grad(nullptr, n_tokens, dim).bytes;
+    size_t most = embedding_grad_workspace_need(n_tokens, dim);
+    for (int64_t slabs = 1; (slabs - 1) * COLS < dim; ++slabs)
+        most = std::max(most, embedding_grad_workspace_need(std::min(n_tokens, (FEW_WAVES - 1) / slabs), std::min<int64_t>(dim, slabs * COLS)));
+    return most;
 }
 
 // +0 to a row of the table.  Every lane of the wave comes here.

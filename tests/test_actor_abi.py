@@ -273,3 +273,22 @@ def test_adamw_tensors_outlive_the_dicts_they_came_in():
     del t
     gc.collect()
     assert all(ref() is None for ref in seen.values())
+
+
+def test_embedding_backward_workspace_of_the_largest_call_serves_smaller_ones():
+    """A program that sizes it once, for its largest micro-batch: the sizes do not fall where the kernels are cut otherwise."""
+    def size(tokens, dim):
+        return B.dc_embedding_backward_workspace_bytes(mat(rows=tokens, cols=dim), mat(rows=50000, cols=dim))
+    counts = sorted({n + d for k in (0, 16, 32, 512, 1024, 8192, 16384, 1 << 24) for n in (k, 131072 // max(1, k // 512)) for d in (-1, 0, 1)
+                     if 0 <= n + d <= 1 << 24} | {21845, 26214, 32767, 32768, 40000, 43690, 43691, 65535, 65536, 87381, 131071, 131072, 262144})
+    dims = [1, 100, 511, 512, 513, 1024, 1025, 1536, 2047, 2048, 2049, 4096, 8192, 16384, 16385, 65536]
+    of = {(n, d): size(n, d) for n in counts for d in dims if n * d <= 1 << 38}
+    assert all(v > 0 and v % 256 == 0 for k, v in of.items() if k[0] > 0)
+    for n, d in of:
+        for n2, d2 in ((counts[min(counts.index(n) + 1, len(counts) - 1)], d), (n, dims[min(dims.index(d) + 1, len(dims) - 1)])):
+            if (n2, d2) in of:
+                assert of[n, d] <= of[n2, d2], (n, d, n2, d2)
+    for tokens, dim in ((32767, 2048), (16700, 2048), (40000, 2048), (65535, 1024), (131071, 512), (9000, 2048)):
+        # refused for less than the call needs, whatever the largest call would need: half its pieces are too few
+        refuses(B.DC_ERR_WORKSPACE, B.dc_embedding_backward, mat(rows=tokens, cols=dim), A, 1.0, 0, mat(rows=50000, cols=dim), A,
+                size(tokens, dim) // 2, A)
