@@ -414,7 +414,8 @@ typedef struct dc_matrix {
  * every top token.  -infinity is a logit of probability 0 like any other (such a token's own log p is -infinity).
  * d_token and d_logprob go together: both NULL if no token is given.  d_row_stat, d_entropy may be NULL.  n_top 0 ..
  * DC_MAX_TOP and <= vocabulary; d_top_token / d_top_logprob: one of them may be NULL, with n_top = 0 both are not used.
- * d_ws: 256-byte aligned, dc_token_logprob_workspace_bytes(logits, n_top) bytes (may be 0: then NULL is fine); holds
+ * d_ws: 256-byte aligned, dc_token_logprob_workspace_bytes(logits, n_top) bytes (may be 0: then NULL is fine), which also serve
+ * every call of fewer rows of this type and width, fewer alternatives or both; more than 64 rows need none themselves.  Holds
  * nothing the caller needs afterwards.
  * Host errors: INVALID_ARG, UNSUPPORTED_SIZE (vocabulary above DC_MAX_VOCAB, n_top above DC_MAX_TOP), WORKSPACE, HIP.
  * Device errors: TOKEN_RANGE (a row with a mask byte != 0 and a token outside 0 .. vocabulary - 1: its d_logprob is NaN).

@@ -106,7 +106,7 @@ dc_status dc_token_logprob(const dc_matrix* logits, double temperature, const in
     for (const void* p : {(const void*)d_token, (const void*)d_logprob, (const void*)d_row_stat, (const void*)d_entropy,
                           (const void*)d_top_token, (const void*)d_top_logprob})
         if (!aligned_to(p, 4)) return DC_ERR_INVALID_ARG;
-    const size_t need = logprob_workspace_bytes(logits->n_rows, (int32_t)logits->n_cols, logits->type, n_top);
+    const size_t need = logprob_workspace_need(logits->n_rows, (int32_t)logits->n_cols, logits->type, n_top);
     if (need > 0 && (!d_ws || !aligned_to(d_ws, 256))) return DC_ERR_INVALID_ARG;
     if (ws_bytes < need) return DC_ERR_WORKSPACE;
     const LogprobArgs a = {logits->d_data, logits->row_stride, logits->n_rows, (int32_t)logits->n_cols, n_top,

@@ -21,7 +21,8 @@ struct LogprobArgs {
     float*         top_logprob;
     int32_t*       status;
 };
-size_t logprob_workspace_bytes(int64_t n_rows, int32_t vocab, int32_t type, int32_t n_top);
+size_t logprob_workspace_need(int64_t n_rows, int32_t vocab, int32_t type, int32_t n_top);       // of this call
+size_t logprob_workspace_bytes(int64_t n_rows, int32_t vocab, int32_t type, int32_t n_top);      // of it and of those of fewer rows or alternatives
 hipError_t launch_logprob(const LogprobArgs& a, int32_t type, void* d_ws, hipStream_t st);
 
 struct LogprobGradArgs {

@@ -9,6 +9,7 @@
 // A workgroup takes a row; few rows get larger workgroups, and long ones are cut into parts that a second launch joins.
 // Bound by reading the logits where there are many rows (8192 x 152064 bf16, 2.5 GB: 0.37 ms, 6.7 TB/s), by two launches' trips to
 // memory where there are few (1 x 152064: 7.5 + 4.6 us).
+#include <algorithm>
 #include "actor_device.h"
 
 namespace dc {
@@ -420,12 +421,12 @@ __global__ __launch_bounds__(WAVE) void logprob_join_kernel(const LogprobArgs a,
 //   256 x 152064 f32      wide   27.7 / 35.5   parts 31.1 / 51.3
 //   1 x 32000 f32         wide    7.4 / 10.3   parts  9.8 / 13.8
 // 1024 parts in all instead of 512: 64 x 152064 f32 with 20 alternatives 21.2 us.
-constexpr int64_t LP_GROUPS = 512, LP_LEAST = 4096;
+constexpr int64_t LP_GROUPS = 512, LP_LEAST = 4096, LP_CUT_ROWS = 64;
 struct Cut { int32_t parts, per_part; bool wide; };
 static Cut cut_of(int64_t n_rows, int32_t vocab, int32_t type, int32_t n_top) {
     const int64_t bytes = (int64_t)vocab * (type == DC_F32 ? 4 : 2);
     if (n_rows > 256 || bytes <= 1 << 16) return Cut{1, vocab, n_top > 0 && bytes > 1 << 19};
-    if (n_rows > 64 || bytes <= 1 << 17) return Cut{1, vocab, true};
+    if (n_rows > LP_CUT_ROWS || bytes <= 1 << 17) return Cut{1, vocab, true};
     int64_t parts = n_rows > 0 ? (LP_GROUPS + n_rows - 1) / n_rows : 1;
     const int64_t most = (vocab + LP_LEAST - 1) / LP_LEAST;
     parts = parts < most ? parts : most;
@@ -433,9 +434,16 @@ static Cut cut_of(int64_t n_rows, int32_t vocab, int32_t type, int32_t n_top) {
     return Cut{(vocab + per - 1) / per, per, false};
 }
 
-size_t logprob_workspace_bytes(int64_t n_rows, int32_t vocab, int32_t type, int32_t n_top) {
+size_t logprob_workspace_need(int64_t n_rows, int32_t vocab, int32_t type, int32_t n_top) {
     const Cut c = cut_of(n_rows, vocab, type, n_top);
     return c.parts > 1 ? (size_t)n_rows * c.parts * part_bytes(n_top) : 0;
+}
+// As much as any call of at most these rows and alternatives needs: the number of parts in all goes up and down with the rows, and
+// many rows have none.
+size_t logprob_workspace_bytes(int64_t n_rows, int32_t vocab, int32_t type, int32_t n_top) {
+    size_t most = 0;
+    for (int64_t n = 1; n <= std::min(n_rows, LP_CUT_ROWS); ++n) most = std::max(most, logprob_workspace_need(n, vocab, type, n_top));
+    return most;
 }
 
 hipError_t launch_logprob(const LogprobArgs& a, int32_t type, void* d_ws, hipStream_t st) {

@@ -292,3 +292,16 @@ def test_embedding_backward_workspace_of_the_largest_call_serves_smaller_ones():
         # refused for less than the call needs, whatever the largest call would need: half its pieces are too few
         refuses(B.DC_ERR_WORKSPACE, B.dc_embedding_backward, mat(rows=tokens, cols=dim), A, 1.0, 0, mat(rows=50000, cols=dim), A,
                 size(tokens, dim) // 2, A)
+
+
+def test_logprob_workspace_of_the_largest_call_serves_smaller_ones():
+    """A program that sizes it once, for its largest batch, decodes with fewer rows: the size does not fall with them."""
+    for cols in (1, 32000, 32769, 65537, 70000, 131073, 152064, 1 << 20, B.DC_MAX_VOCAB):
+        for type_ in (B.DC_F32, B.DC_BF16, B.DC_F16):
+            for n_top in (0, 1, 5, 20, 64):
+                if n_top > cols:
+                    continue
+                size = [B.dc_token_logprob_workspace_bytes(mat(rows=r, cols=cols, type_=type_), n_top) for r in (*range(131), 256, 257, 1 << 20)]
+                assert all(a <= b for a, b in zip(size, size[1:])), (cols, type_, n_top)
+                assert n_top == 0 or size[64] >= B.dc_token_logprob_workspace_bytes(mat(rows=64, cols=cols, type_=type_), n_top - 1)
+    assert B.dc_token_logprob_workspace_bytes(mat(rows=100, cols=152064), 5) > 0
