@@ -485,7 +485,8 @@ typedef struct dc_adamw_tensor {
 } dc_adamw_tensor;
 
 typedef struct dc_adamw_params {
-    double  lr, beta1, beta2, eps;   /* lr >= 0, betas in [0, 1), eps in 2^-100 .. 2^100      */
+    double  lr, beta1, beta2, eps;   /* lr >= 0, betas in [0, 1), eps in 2^-100 .. 2^100; lr / (1 - beta1^step) and
+                                        1 - lr * weight_decay within the range of 32 bits     */
     int64_t step;                    /* of this call, from 1 (bias correction)                */
 } dc_adamw_params;
 

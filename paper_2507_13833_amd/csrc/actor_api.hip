@@ -213,6 +213,10 @@ dc_status dc_adamw(const dc_adamw_tensor* tensors, int32_t n_tensors, const dc_a
     const AdamwTable t = carve_adamw_table(const_cast<void*>(d_table), n_tensors, n_pieces);
     if (table_bytes < t.bytes) return DC_ERR_WORKSPACE;
     const double bc1 = 1.0 - std::pow(prm->beta1, (double)prm->step), bc2 = 1.0 - std::pow(prm->beta2, (double)prm->step);
+    // what the kernel multiplies by, in 32 bits
+    if (!std::isfinite((float)(prm->lr / bc1))) return DC_ERR_INVALID_ARG;
+    for (int32_t i = 0; i < n_tensors; ++i)
+        if (!std::isfinite((float)(1.0 - prm->lr * tensors[i].weight_decay))) return DC_ERR_INVALID_ARG;
     // the share that this step's gradient has in v, once the average is corrected for its start at 0
     const bool dither = (1.0 - prm->beta2) / bc2 < 1.0 / 24;
     uint64_t seed = (uint64_t)prm->step * 0x9E3779B97F4A7C15u;             // (an odd multiple of each step: all differ)

@@ -305,3 +305,12 @@ def test_logprob_workspace_of_the_largest_call_serves_smaller_ones():
                 assert all(a <= b for a, b in zip(size, size[1:])), (cols, type_, n_top)
                 assert n_top == 0 or size[64] >= B.dc_token_logprob_workspace_bytes(mat(rows=64, cols=cols, type_=type_), n_top - 1)
     assert B.dc_token_logprob_workspace_bytes(mat(rows=100, cols=152064), 5) > 0
+
+
+def test_adamw_factors_that_32_bits_do_not_hold():
+    t, strong = Tensors(tensor()), Tensors(tensor(decay=0.1), tensor(n=0, decay=0.0), tensor(decay=1e10))
+    need = max(B.dc_adamw_table_bytes(t), B.dc_adamw_table_bytes(strong))
+    for kw in (dict(lr=1e39), dict(lr=3e38, beta1=0.9), dict(lr=1e308), dict(lr=1e30, beta1=1 - 1e-12)):
+        refuses(B.DC_ERR_INVALID_ARG, B.dc_adamw, t, B.make_adamw(**kw), None, A, need, A)
+    refuses(B.DC_ERR_INVALID_ARG, B.dc_adamw, strong, B.make_adamw(1e30), None, A, need, A)
+    refuses(B.DC_ERR_INVALID_ARG, B.dc_adamw, strong, B.make_adamw(1e300, step=1 << 40), None, A, need, A)
