@@ -1105,3 +1105,24 @@ def test_adamw_refuses_a_table_of_as_many_pieces(env, change):
     B.dc_adamw(again, B.make_adamw(1e-3, step=2), None, table, need, st)
     torch.cuda.synchronize()
     assert int(st) == 0 and not torch.equal(before[1]["param"], room[1]["param"])
+
+
+@pytest.mark.parametrize("g_type,w_type", [("bf16", "f32"), ("bf16", "bf16"), ("f32", "f32"), ("f32", "bf16")])
+@pytest.mark.parametrize("tokens,vocab,dim", [(140000, 60000, 520), (66000, 3000, 1024)])
+def test_embedding_backward_adds_in_long_chunks(env, tokens, vocab, dim, g_type, w_type):
+    """Chunks of 32 entries, whole lines, two slabs of columns, segments of every length, added to whole numbers: exact sums,
+    rows without a token as they were."""
+    torch, B = env
+    gen = torch.Generator(device="cuda").manual_seed(tokens + dim)
+    g = torch.randint(-1, 2, (tokens, dim), generator=gen, device="cuda").to(types(torch)[g_type])
+    ids = (torch.rand(tokens, generator=gen, device="cuda").double() ** 3 * vocab).int().clamp_(max=vocab - 1)
+    ids[::97] = -1
+    ids[ids % 500 == 77] = vocab - 1
+    ids[ids % 7 == 3] -= 1
+    dw = torch.randint(-8, 9, (vocab, dim), generator=gen, device="cuda").to(types(torch)[w_type])
+    ok = ids >= 0
+    named = torch.zeros(vocab, dtype=torch.bool, device="cuda").index_fill_(0, ids[ok].long(), True)
+    dw[~named] = 0.3
+    want = dw.float().index_add_(0, ids[ok].long(), g[ok].float()).to(dw.dtype)
+    embedding_grad_call(env, g, ids, 1.0, True, dw)
+    assert not bool(named.all()) and torch.equal(dw, want)
