@@ -133,12 +133,13 @@ __device__ __forceinline__ uint32_t chance(uint32_t seed, int64_t place, float g
     return fold(fold((((uint32_t)place * 0x9E3779B1u ^ seed) + __float_as_uint(g)) ^ 0x6A09E667u, 0xBB67AE85u) ^ 0x3C6EF372u, 0xA54FF53Bu);
 }
 // What a root becomes in 8 bits, before the conversion rounds it to nearest.  Where an average moves by less in a step than codes
-// are apart, nearest would put a root back where it was, time and again: there (AdamwStep::dither) it goes to the code above or below it,
+// are apart, nearest would put a root back where it was, time and again: there (CHANCE) it goes to the code above or below it,
 // by chance and the likelier the nearer, so that it moves as far as it should on average.  Median of the kept root over that of
 // 32 bits, elements whose gradients fall to a tenth halfway through 1000 steps (0.999: 10 000), nearest / by chance: beta2 0.95
 // 1.04 / -, 0.96 1.09 / 0.99, 0.97 2.4 / 0.99, 0.98 12.7 / 0.98, 0.99 9.2 / 0.99, 0.999 6.7 / 0.99.  The first moment needs none
 // of it: 0.0133 off at beta1 from 0.9 to 0.99 by nearest, 0.019 by chance (rms, gradients of 1), for its gradients and the
-// block's scale move it from code to code.  612 M elements: 1.82 ms, by nearest 1.73.
+// block's scale move it from code to code.  612 M elements: 1.78 ms, by nearest 1.69; a
+// kernel of its own, for the branch alone costs the others 0.6 %.
 __device__ __forceinline__ float by_chance(float c, uint32_t chance) {
     // 20 bits behind those that a code holds; what is below a code's smallest power of two gets that power in front
     const float front = c < 0x1p-6f ? 0x1p-6f : 0.0f;
@@ -146,9 +147,9 @@ __device__ __forceinline__ float by_chance(float c, uint32_t chance) {
 }
 __device__ __forceinline__ float not_zero(float c, float exact) { return exact > 0.0f ? fmaxf(c, E4M3_LEAST) : c; }      // (it is divided by)
 // Codes of neighbouring elements, the first of them at `place`.
-template <int N>
+template <bool CHANCE, int N>
 __device__ __forceinline__ void root_codes(const AdamwStep& s, const float (&root)[N], float inverse, int64_t place, const float (&g)[N], float (&code)[N]) {
-    if (s.dither) {
+    if constexpr (CHANCE) {
 #pragma unroll
         for (int c = 0; c < N; ++c) code[c] = not_zero(by_chance(root[c] * inverse, chance(s.seed, place + c, g[c])), root[c] * inverse);
     } else {
@@ -164,6 +165,7 @@ __device__ __forceinline__ float wave_most(float v) {
 
 // A wave's block of DC_STATE_BLOCK elements or fewer, element by element: the last block of a tensor, tensors that are not
 // aligned, and blocks of 8-bit states with a v beyond 32 bits.
+template <bool CHANCE>
 __device__ __forceinline__ void block_by_elements(const AdamwStep& s, const dc_adamw_tensor& d, int64_t block, float gs, float decay) {
     const int64_t at = block * DC_STATE_BLOCK;
     const bool small = d.state_type == DC_E4M3;
@@ -207,7 +209,7 @@ __device__ __forceinline__ void block_by_elements(const AdamwStep& s, const dc_a
         if (i >= d.n) continue;
         static_cast<uint8_t*>(d.d_exp_avg)[i] = (uint8_t)to_e4m3(m[j] * sc.m_inverse, 0.0f, 0.0f, 0.0f);
         float code[1];
-        root_codes<1>(s, {root[j]}, sc.root_inverse, i, {g[j]}, code);
+        root_codes<CHANCE, 1>(s, {root[j]}, sc.root_inverse, i, {g[j]}, code);
         static_cast<uint8_t*>(d.d_exp_avg_sq)[i] = (uint8_t)to_e4m3(code[0], 0.0f, 0.0f, 0.0f);
     }
     if (lane_id() == 0) { d.d_exp_avg_scale[block] = sc.m; d.d_exp_avg_sq_scale[block] = sc.root; }
@@ -246,7 +248,7 @@ __device__ __forceinline__ void store4(void* p, int64_t i, const float (&f)[4]) 
 // A wave's block of an aligned tensor, four neighbouring elements to a lane; everything is asked for before anything is used.
 // G: the gradient's type, P: what the weights are read from (the master's float, or the parameter's).  False, and nothing
 // written, where the block has to go by elements: a v beyond 32 bits in 8-bit states.
-template <typename G, typename P, bool MASTER, bool SMALL>
+template <typename G, typename P, bool MASTER, bool SMALL, bool CHANCE>
 __device__ __forceinline__ bool whole_block(const AdamwStep& s, const dc_adamw_tensor& d, int64_t block, float gs, float decay) {
     const int64_t i = block * DC_STATE_BLOCK + lane_id() * 4;
     const Raw4<G> rg = load4<G>(d.d_grad, i);
@@ -292,7 +294,7 @@ __device__ __forceinline__ bool whole_block(const AdamwStep& s, const dc_adamw_t
         const uint32_t em = to_e4m3(m[0] * sc.m_inverse, m[1] * sc.m_inverse, m[2] * sc.m_inverse, m[3] * sc.m_inverse);
         const float g[4] = {(float)rg.e[0] * gs, (float)rg.e[1] * gs, (float)rg.e[2] * gs, (float)rg.e[3] * gs};
         float code[4];
-        root_codes(s, root, sc.root_inverse, i, g, code);
+        root_codes<CHANCE>(s, root, sc.root_inverse, i, g, code);
         const uint32_t er = to_e4m3(code[0], code[1], code[2], code[3]);
         __builtin_nontemporal_store(em, reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(d.d_exp_avg) + i));
         __builtin_nontemporal_store(er, reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(d.d_exp_avg_sq) + i));
@@ -303,12 +305,12 @@ __device__ __forceinline__ bool whole_block(const AdamwStep& s, const dc_adamw_t
     }
     return true;
 }
-template <typename G, bool SMALL>
+template <typename G, bool SMALL, bool CHANCE>
 __device__ __forceinline__ bool whole_block_of(const AdamwStep& s, const dc_adamw_tensor& d, int64_t block, float gs, float decay) {
-    if (d.d_master) return whole_block<G, float, true, SMALL>(s, d, block, gs, decay);
-    if (d.param_type == DC_F32) return whole_block<G, float, false, SMALL>(s, d, block, gs, decay);
-    if (d.param_type == DC_BF16) return whole_block<G, __bf16, false, SMALL>(s, d, block, gs, decay);
-    return whole_block<G, _Float16, false, SMALL>(s, d, block, gs, decay);
+    if (d.d_master) return whole_block<G, float, true, SMALL, CHANCE>(s, d, block, gs, decay);
+    if (d.param_type == DC_F32) return whole_block<G, float, false, SMALL, CHANCE>(s, d, block, gs, decay);
+    if (d.param_type == DC_BF16) return whole_block<G, __bf16, false, SMALL, CHANCE>(s, d, block, gs, decay);
+    return whole_block<G, _Float16, false, SMALL, CHANCE>(s, d, block, gs, decay);
 }
 
 // One workgroup per piece, a wave per block.  What a tensor is made of is the same for a whole piece, so the kinds are branches
@@ -317,6 +319,7 @@ __device__ __forceinline__ bool whole_block_of(const AdamwStep& s, const dc_adam
 // four blocks a wave, all asked for at once: within 2 % for 32-bit states, 3 to 5 % slower for 8-bit ones.  Plain stores
 // instead of streamed ones: 6 % slower.
 constexpr int AW_THREADS = ADAMW_PIECE / DC_STATE_BLOCK * WAVE;
+template <bool CHANCE>
 __global__ __launch_bounds__(AW_THREADS) void adamw_kernel(const AdamwStep s, const AdamwHeader want, const AdamwHeader* __restrict__ head,
                                                            const dc_adamw_tensor* __restrict__ tensors,
                                                            const AdamwPiece* __restrict__ pieces) {
@@ -335,23 +338,24 @@ __global__ __launch_bounds__(AW_THREADS) void adamw_kernel(const AdamwStep s, co
         bool done = block * DC_STATE_BLOCK >= d.n;
         if (d.reserved && (block + 1) * DC_STATE_BLOCK <= d.n) {           // (in the table: whether all of it is aligned)
             if (d.state_type == DC_E4M3) {
-                if (d.grad_type == DC_BF16) done = whole_block_of<__bf16, true>(s, d, block, gs, decay);
-                else if (d.grad_type == DC_F32) done = whole_block_of<float, true>(s, d, block, gs, decay);
-                else done = whole_block_of<_Float16, true>(s, d, block, gs, decay);
+                if (d.grad_type == DC_BF16) done = whole_block_of<__bf16, true, CHANCE>(s, d, block, gs, decay);
+                else if (d.grad_type == DC_F32) done = whole_block_of<float, true, CHANCE>(s, d, block, gs, decay);
+                else done = whole_block_of<_Float16, true, CHANCE>(s, d, block, gs, decay);
             } else {
-                if (d.grad_type == DC_BF16) done = whole_block_of<__bf16, false>(s, d, block, gs, decay);
-                else if (d.grad_type == DC_F32) done = whole_block_of<float, false>(s, d, block, gs, decay);
-                else done = whole_block_of<_Float16, false>(s, d, block, gs, decay);
+                if (d.grad_type == DC_BF16) done = whole_block_of<__bf16, false, false>(s, d, block, gs, decay);
+                else if (d.grad_type == DC_F32) done = whole_block_of<float, false, false>(s, d, block, gs, decay);
+                else done = whole_block_of<_Float16, false, false>(s, d, block, gs, decay);
             }
         }
-        if (!done) block_by_elements(s, d, block, gs, decay);
+        if (!done) block_by_elements<CHANCE>(s, d, block, gs, decay);
     }
 }
 
 hipError_t launch_adamw(const AdamwStep& s, const AdamwHeader& head, const AdamwTable& t, hipStream_t st) {
     if (head.n_pieces == 0) return hipSuccess;
     const unsigned grid = (unsigned)(head.n_pieces < (1 << 22) ? head.n_pieces : 1 << 22);     // (2^31 threads)
-    adamw_kernel<<<grid, AW_THREADS, 0, st>>>(s, head, t.head, t.tensors, t.pieces);
+    if (s.dither) adamw_kernel<true><<<grid, AW_THREADS, 0, st>>>(s, head, t.head, t.tensors, t.pieces);
+    else adamw_kernel<false><<<grid, AW_THREADS, 0, st>>>(s, head, t.head, t.tensors, t.pieces);
     return hipGetLastError();
 }
 
