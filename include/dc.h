@@ -511,7 +511,8 @@ typedef struct dc_adamw_params {
  * dc_adamw_table writes what the kernel reads about the tensors into d_table (256-byte aligned, dc_adamw_table_bytes bytes);
  * call it once, and again when a pointer, a size, a type or a weight decay changes.  dc_adamw takes the same tensors and
  * the table, in stream order behind it.  A table that was not made for exactly these tensors (pointers, sizes, types, weight
- * decays and their order, by 64 bits made of them) is refused on the device.  The scalars are read at the call: a captured graph keeps them.
+ * decays and their order, by 64 bits made of them) is refused on the device.  The scalars are read at the call: a captured
+ * graph keeps them, the step of the bias correction and of the chance above among them.
  * Host errors: INVALID_ARG, UNSUPPORTED_SIZE, WORKSPACE (table_bytes too small), HIP.  Device errors: BAD_LAYOUT (not this
  * table; nothing is updated).
  */

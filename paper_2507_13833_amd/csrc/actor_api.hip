@@ -221,7 +221,7 @@ dc_status dc_adamw(const dc_adamw_tensor* tensors, int32_t n_tensors, const dc_a
     const bool dither = (1.0 - prm->beta2) / bc2 < 1.0 / 24;
     uint64_t seed = (uint64_t)prm->step * 0x9E3779B97F4A7C15u;             // (an odd multiple of each step: all differ)
     seed = (seed ^ seed >> 32) * 0xD6E8FEB86659FD93u;
-    const AdamwStep s = {(float)prm->lr, (float)(prm->lr / bc1), (float)prm->beta1, (float)(1.0 - prm->beta1),
+    const AdamwStep s = {(float)(prm->lr / bc1), (float)prm->beta1, (float)(1.0 - prm->beta1),
                          (float)prm->beta2, (float)(1.0 - prm->beta2), (float)(1.0 / std::sqrt(bc2)), (float)prm->eps,
                          prm->lr, dither, (uint32_t)(seed >> 32), d_grad_scale, d_status};
     const hipError_t e = launch_adamw(s, header_of(tensors, n_tensors, n_pieces), t, static_cast<hipStream_t>(hip_stream));

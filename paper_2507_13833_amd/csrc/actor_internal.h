@@ -76,7 +76,7 @@ struct AdamwPiece  { int32_t tensor, piece; };
 struct AdamwTable  { AdamwHeader* head; dc_adamw_tensor* tensors; AdamwPiece* pieces; size_t bytes; };
 AdamwTable carve_adamw_table(void* base, int32_t n_tensors, int64_t n_pieces);
 struct AdamwStep {
-    float lr, step_size, beta1, one_minus_beta1, beta2, one_minus_beta2, inv_root_bc2, eps;
+    float step_size, beta1, one_minus_beta1, beta2, one_minus_beta2, inv_root_bc2, eps;
     double lr64;                    // the factor of the weight decay is 1 - lr * weight_decay, rounded once
     int32_t dither;                 // roots in 8 bits go up or down by chance; `seed`: the step's
     uint32_t seed;

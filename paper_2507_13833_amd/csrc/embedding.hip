@@ -7,7 +7,8 @@ constexpr int EMB_THREADS = 256;
 
 // One wave per ROWS tokens and 512 columns; the rows are asked for together.  Bound by the streams: a row of the table in,
 // a row out.  Many rows leave past the caches, which then keep rows of the table that come again (131 072 tokens of 2048
-// bf16 out of 152 064: 146 us, 5.3 TB/s; 162 us with plain stores; two or eight rows a wave: within 4 %).
+// bf16 out of 152 064: 146 us, 5.3 TB/s; 162 us with plain stores; two or eight rows a wave: within 4 %).  Rows that do not start
+// on 16 bytes or whose width is no multiple of 8 go element by element: 207 us for 2047 columns.
 template <int ROWS, Layout L, typename W, typename O>
 __global__ __launch_bounds__(EMB_THREADS) void embedding_kernel(const EmbeddingArgs a, int64_t units, int32_t slabs) {
     const int lane = lane_id();

@@ -1,8 +1,10 @@
 // Gradient of an embedding table: dW[v, :] = scale * sum of g[t, :] over the tokens t with id v.
 //
 // Few tokens: one launch (few_tokens).  Otherwise the tokens are sorted by id (stable, so the tokens of one id stay in
-// ascending order), and the sorted sequence is cut into chunks of CHUNK entries: a hot id costs as much per token as a rare
-// one, and no float goes through an atomic.
+// ascending order), and the sorted sequence is cut into chunks of CHUNK entries, so that a hot id's rows are summed by many
+// waves; no float goes through an atomic.  131 072 tokens of 2048 columns, bf16 added to f32, ids as text has them / all the
+// same: 364 / 271 us; a table of 152 064 rows written anew 373 / 462 (one id's 4096 pieces are joined by four workgroups, one per
+// 512 columns, and then all rows but one are without a token).
 //   sort_portions   1024 to 8192 tokens per workgroup, radix sort in the LDS
 //   merge_runs      up to MERGE_WAYS sorted runs into one: an entry's place is its own plus, for every other run, how many
 //                   entries there come before it (a binary search each); once for every factor of MERGE_WAYS
@@ -473,7 +475,7 @@ __global__ __launch_bounds__(ADD_THREADS) void add_rows_kernel(const EmbeddingGr
     }
 }
 
-// One workgroup per long segment and 512 columns, round and round; its waves take every fourth piece each.
+// One workgroup per long segment and 512 columns, round and round; its waves take every eighth piece each.
 template <int CHUNK, Layout L, bool ACC, typename W>
 __global__ __launch_bounds__(JOIN_THREADS) void join_pieces_kernel(const EmbeddingGradArgs a, const uint32_t* __restrict__ skey,
                                                                    const int32_t* __restrict__ n_long, const int32_t* __restrict__ long_at,
@@ -538,7 +540,9 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_pieces_kernel(const Embeddi
 // From the table's start instead of its end, where most rows have tokens: nothing gained.  Beside the merge as well: 1 % slower
 // (its own work takes all compute units).
 constexpr double FILL_SORT = 60e6, FILL_SORT_EACH = 8e6, FILL_JOIN = 100e6;
-// f(layout, whether to accumulate, element types of the gradient and of the table).
+// f(layout, whether to accumulate, element types of the gradient and of the table).  Rows that do not start on 16 bytes or whose
+// width is no multiple of 8 go element by element: 131 072 tokens of 2047 columns, a table of 152 064 in f32 written anew, 428 us
+// (373 for 2048), 8192 of 1023 added to 32 000 33 us (29).
 template <typename F>
 static hipError_t with_layout(const EmbeddingGradArgs& a, int32_t g_type, int32_t dw_type, F&& f) {
     return with_type(g_type, [&](auto ge) {

@@ -420,7 +420,8 @@ __global__ __launch_bounds__(WAVE) void logprob_join_kernel(const LogprobArgs a,
 //   64 x 152064 f32       parts  13.8 / 19.2   wide  16.8 / 24.3
 //   256 x 152064 f32      wide   27.7 / 35.5   parts 31.1 / 51.3
 //   1 x 32000 f32         wide    7.4 / 10.3   parts  9.8 / 13.8
-// 1024 parts in all instead of 512: 64 x 152064 f32 with 20 alternatives 21.2 us.
+// The row of 12000 is narrow for the sake of its alternatives; 65 to 255 long rows, between the two sides of their border, were not
+// measured.  1024 parts in all instead of 512: 64 x 152064 f32 with 20 alternatives 21.2 us.
 constexpr int64_t LP_GROUPS = 512, LP_LEAST = 4096, LP_CUT_ROWS = 64;
 struct Cut { int32_t parts, per_part; bool wide; };
 static Cut cut_of(int64_t n_rows, int32_t vocab, int32_t type, int32_t n_top) {
@@ -483,7 +484,9 @@ __device__ __forceinline__ u32x4 pack(const float (&f)[CHUNK_ELEMS<T>]) {
 
 // One workgroup per piece of a row: 16 bytes in, 16 bytes out, four times a thread.  Bound by the two streams: 8192 x 152064 in
 // bf16, 5.0 GB, in 0.82 ms, 6.1 TB/s, what a large copy reaches; with a quarter of the rows masked 5.8 TB/s.  64 registers, so that
-// a SIMD holds 8 waves: 1 to 4 % quicker than 7 of them.  Half as much a workgroup: 5 % slower.
+// a SIMD holds 8 waves: 1 to 4 % quicker than 7 of them, although two registers are spilled for 16-bit logits with an entropy.
+// Half as much a workgroup: 5 % slower.  Rows of x and of the gradient that lie differently to 16 bytes go element by element:
+// 8192 x 152063 in 1.96 ms (0.90 where they lie alike).
 template <typename T, bool ENTROPY>
 __global__ __launch_bounds__(LG_THREADS, 8) void logprob_grad_kernel(const LogprobGradArgs a, int32_t pieces) {
     constexpr int N = CHUNK_ELEMS<T>;
