@@ -500,6 +500,8 @@ typedef struct dc_adamw_params {
  * what is divided by).  Where a step's gradient has less than 1/24 of v, (1 - beta2) / (1 - beta2^step) < 1/24 (beta2 above
  * 23/24, behind the first steps), a root moves by less in a step than e4m3 values are apart and nearest would hold it where it
  * is: there it becomes the value below or above it, by chance and the likelier the nearer, so that it follows v on average.
+ * Below that it is the spread of a block's gradients from step to step that lets nearest follow: gradients that keep their
+ * size exactly, all of a block, may leave a root where it was (beta2 0.95: for good).
  * The chance is a function of the step, the element's place in its tensor and its gradient: identical inputs give identical
  * bits.  A root that is not zero is stored as no less than 2^-9 s, so it never becomes zero.  A block whose s would be below
  * 2^-120 is stored as zeros.  The step itself uses m and v before they are rounded.  All-zero codes and
