@@ -235,6 +235,11 @@ def _matrix(s, name):
     return None if s[name] is None else s["B"].make_matrix(s[name])
 
 
+def _norm_params(s):
+    case = s["case"]
+    return s["B"].make_norm(EPS, case["residual_scale"], case["block_scale"], gate_rows=case["gate"] == "token")
+
+
 def _own_head(s):
     case = s["case"]
     s["B"].dc_head_logprob(_matrix(s, "hidden"), _matrix(s, "weight"), case["temperature"], s["token"], s["mask"], case["top"],
@@ -252,9 +257,8 @@ def _own_head_grad(s):
 
 
 def _own_norm(s):
-    case = s["case"]
     s["B"].dc_residual_norm(_matrix(s, "block"), _matrix(s, "post"), _matrix(s, "gate"), _matrix(s, "stream"),
-                            _matrix(s, "pre"), s["B"].make_norm(EPS, case["residual_scale"], case["block_scale"]),
+                            _matrix(s, "pre"), _norm_params(s),
                             _matrix(s, "stream_out"), _matrix(s, "out"), s["stat"])
     return _outputs(s, *_NORM)
 
@@ -263,7 +267,7 @@ def _own_norm_grad(s):
     case = s["case"]
     s["B"].dc_residual_norm_backward(
         _matrix(s, "block"), _matrix(s, "post"), _matrix(s, "gate"), _matrix(s, "stream_out"), _matrix(s, "pre"),
-        s["B"].make_norm(EPS, case["residual_scale"], case["block_scale"]), s["stat"], _matrix(s, "grad_stream_out"),
+        _norm_params(s), s["stat"], _matrix(s, "grad_stream_out"),
         _matrix(s, "grad_out"), _matrix(s, "grad_block"), _matrix(s, "grad_stream"), case["accumulate"],
         _matrix(s, "grad_post"), _matrix(s, "grad_gate"), _matrix(s, "grad_pre"), s["ws"], s["ws_bytes"])
     return _outputs(s, *_NORM_GRAD)
