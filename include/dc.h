@@ -32,6 +32,12 @@
  *                       the stage behind the transition (actor log-prob, App. B Table 2): log-probabilities of
  *                       the packed token ids under the head's logits, with entropy and top alternatives, and
  *                       the gradient of the logits.
+ *   dc_head_logprob, dc_head_logprob_backward
+ *                       the same from hidden states and the head's weights, without a matrix of logits, and the
+ *                       gradients of both.
+ *   dc_residual_norm, dc_residual_norm_backward
+ *                       the residual stream from one block of the actor to the next: the block's result normed,
+ *                       gated and added, the sum normed for what follows; and the gradients.
  *   dc_embedding, dc_embedding_backward
  *                       the rows of the packed token ids, scaled, and the table's gradient.
  *   dc_adamw_table, dc_adamw
@@ -98,6 +104,7 @@ extern "C" {
 #define DC_MAX_VOCAB      (1 << 24) /* columns of logits, rows of an embedding table   */
 #define DC_MAX_DIM        65536     /* columns of an embedding table                   */
 #define DC_MAX_TOP        64        /* alternatives of dc_token_logprob                */
+#define DC_MAX_HEAD_ROWS  (1 << 22) /* rows of hidden states of one dc_head_logprob   */
 #define DC_MAX_TENSORS    65536     /* of one dc_adamw                                 */
 #define DC_STATE_BLOCK    256       /* elements that share a scale of an 8-bit state   */
 #define DC_NO_TOKEN       (-1)      /* a place that holds no token (padding)           */
@@ -443,6 +450,100 @@ dc_status dc_token_logprob_backward(const dc_matrix* logits, double temperature,
                                     const uint8_t* d_mask, const float* d_row_stat, const float* d_entropy,
                                     const float* d_grad_logprob, const float* d_grad_entropy,
                                     const dc_matrix* grad_logits, int32_t* d_status, void* hip_stream);
+
+/*
+ * dc_token_logprob without a matrix of logits: x = hidden weight^T is made in pieces on the chip, where a row's sums are taken.
+ *   x_v = sum_c hidden[r, c] * weight[v, c]  for the n_rows of hidden and the vocabulary = weight->n_rows; then as above.
+ * hidden and weight have the same type and n_cols.  Products of 16-bit numbers are exact, of 32-bit ones right to 2^-24 or so
+ * of the two factors' magnitude, and sums are held in 32 bits.  Arguments, masks, rows without a distribution, top
+ * alternatives (ties to the lowest token) and device errors are those of dc_token_logprob; hidden rows of masked tokens are not
+ * looked at.  An infinity or a NaN in a row of hidden, or in weight, may make a row one without a distribution.
+ * With n_top > 0 the logits of 128 rows at a time pass through the workspace.
+ * d_ws: 256-byte aligned, dc_head_logprob_workspace_bytes(hidden, weight, n_top) bytes, which also serve every call of fewer rows
+ * of these matrices, fewer alternatives or both; holds nothing the caller needs afterwards.
+ * Host errors: INVALID_ARG, UNSUPPORTED_SIZE (vocabulary above DC_MAX_VOCAB, n_cols above DC_MAX_DIM, more than DC_MAX_HEAD_ROWS
+ * rows, n_top above DC_MAX_TOP), WORKSPACE, HIP.  Device errors: TOKEN_RANGE.
+ */
+size_t dc_head_logprob_workspace_bytes(const dc_matrix* hidden, const dc_matrix* weight, int32_t n_top);
+dc_status dc_head_logprob(const dc_matrix* hidden, const dc_matrix* weight, double temperature, const int32_t* d_token,
+                          const uint8_t* d_mask, int32_t n_top, float* d_logprob, float* d_row_stat, float* d_entropy,
+                          int32_t* d_top_token, float* d_top_logprob, void* d_ws, size_t ws_bytes,
+                          int32_t* d_status, void* hip_stream);
+
+/*
+ * Gradients of the hidden states and of the head's weights.  With G the gradient of the logits as dc_token_logprob_backward has it
+ * (same arguments; d_row_stat and d_entropy as dc_head_logprob left them):
+ *   grad_hidden[r, :] = sum_v G[r, v] weight[v, :],   grad_weight[v, :] (+)= sum_r G[r, v] hidden[r, :].
+ * Either may be NULL.  grad_hidden: hidden's type and shape; rows with mask byte 0, and those whose a and b are both zero, get +0 and
+ * their hidden rows are not looked at.  grad_weight: weight's shape, weight's type or f32; accumulate == 0: written, != 0: added to
+ * in 32 bits before it is rounded.  Neither may overlap another array of the call.
+ * Sums are held in 32 bits, in an order that depends on the sizes and on which rows take part (identical inputs give identical bits),
+ * and rounded once.  With 16-bit types G itself is rounded: to 11 bits for results of 16 bits, to 22 for a grad_weight
+ * in f32; below 2^-38 of the row's largest possible value it becomes 0.  hidden rows of a row-wise gradient below 2^-38 of the batch's
+ * largest (row's gradient times row's largest magnitude) add nothing to grad_weight.
+ * A row without a distribution (NaN in d_row_stat) that takes part gets NaN in grad_hidden, and grad_weight is NaN.
+ * d_ws: 256-byte aligned, dc_head_logprob_backward_workspace_bytes(hidden, weight, grad_weight) bytes (grad_weight NULL: for calls
+ * without it), which also serve every call of fewer rows of these matrices; holds nothing the caller needs afterwards.
+ * Host errors: INVALID_ARG, UNSUPPORTED_SIZE (as above), WORKSPACE, HIP.  Device errors: TOKEN_RANGE (the row's gradient is that
+ * without the token's own 1).
+ */
+size_t dc_head_logprob_backward_workspace_bytes(const dc_matrix* hidden, const dc_matrix* weight, const dc_matrix* grad_weight);
+dc_status dc_head_logprob_backward(const dc_matrix* hidden, const dc_matrix* weight, double temperature, const int32_t* d_token,
+                                   const uint8_t* d_mask, const float* d_row_stat, const float* d_entropy,
+                                   const float* d_grad_logprob, const float* d_grad_entropy, const dc_matrix* grad_hidden,
+                                   int32_t accumulate, const dc_matrix* grad_weight, void* d_ws, size_t ws_bytes,
+                                   int32_t* d_status, void* hip_stream);
+
+typedef struct dc_norm_params {
+    double  eps;                    /* > 0, what 32 bits can hold                              */
+    double  residual_scale;
+    double  block_scale;
+    int32_t gate_rows;              /* 0: gate is one row for all, 1: one for each             */
+    int32_t reserved;               /* must be 0                                              */
+} dc_norm_params;
+
+/*
+ * The residual stream from one block to the next, row by row (norms as in Zhang and Sennrich 2019, arXiv 1910.07467):
+ *   u = block * r1 * post_weight,  r1 = 1 / sqrt(mean(block^2) + eps)      (post_weight NULL: u = block, no norm)
+ *   h = residual_scale * residual + block_scale * gate * u                 (gate NULL: 1)
+ *   out = h * r2 * pre_weight,     r2 = 1 / sqrt(mean(h^2) + eps)          (pre_weight and out NULL: no norm)
+ *   residual_out = h;  d_row_stat[2r], [2r+1] = r1, r2 (0 where there is no norm; d_row_stat may be NULL).
+ * All in 32 bits, each output rounded once, out and r2 from h before it is rounded.
+ * block, residual, residual_out, out: n_rows x n_cols; out has block's type and residual_out residual's, the two types may differ.
+ * post_weight, pre_weight: one row, any type.  gate: one row (any type) for all rows, or with
+ * gate_rows n_rows of them in block's type.
+ * residual_out may be residual's own memory (same d_data and row_stride), out may be block's; no output overlaps another array
+ * otherwise.
+ * Host errors: INVALID_ARG, UNSUPPORTED_SIZE (n_cols above DC_MAX_DIM), HIP.
+ */
+dc_status dc_residual_norm(const dc_matrix* block, const dc_matrix* post_weight, const dc_matrix* gate, const dc_matrix* residual,
+                           const dc_matrix* pre_weight, const dc_norm_params* prm, const dc_matrix* residual_out,
+                           const dc_matrix* out, float* d_row_stat, void* hip_stream);
+
+/*
+ * Gradients of dc_residual_norm.  With dy = grad_out and dh = grad_residual_out (either may be NULL: 0, grad_out is where there is no
+ * pre_weight), n1 = block * r1, n2 = residual_out * r2, and r1, r2 = d_row_stat (needed where there is a norm):
+ *   dh += r2 * (dy * pre_weight - n2 * mean(dy * pre_weight * n2)),      grad_pre_weight = sum_r dy * n2
+ *   grad_residual = residual_scale * dh,
+ *   du = block_scale * dh,   grad_gate = du * u (summed over the rows without gate_rows),   du *= gate,
+ *   grad_post_weight = sum_r du * n1,   grad_block = r1 * (du * post_weight - n1 * mean(du * post_weight * n1))
+ * (no post_weight: grad_block = du).
+ * grad_out, grad_block and a gate gradient of n_rows have block's type, grad_residual_out and grad_residual residual_out's; the others,
+ * of one row, any type.  Any of the gradients that are written may be NULL: not wanted.  accumulate != 0: those others are added to
+ * in 32 bits before they are rounded.  Sums over rows are held in 32 bits in an order that depends on the sizes alone.
+ * grad_block may be block's or grad_out's own memory, grad_residual grad_residual_out's (same d_data and row_stride); no output
+ * overlaps another array otherwise.
+ * d_ws: 256-byte aligned, dc_residual_norm_backward_workspace_bytes(block) bytes, which also serve every call of fewer rows, fewer
+ * columns or both; holds nothing the caller needs afterwards.
+ * Host errors: INVALID_ARG, UNSUPPORTED_SIZE (n_cols above DC_MAX_DIM), WORKSPACE, HIP.
+ */
+size_t dc_residual_norm_backward_workspace_bytes(const dc_matrix* block);
+dc_status dc_residual_norm_backward(const dc_matrix* block, const dc_matrix* post_weight, const dc_matrix* gate,
+                                    const dc_matrix* residual_out, const dc_matrix* pre_weight, const dc_norm_params* prm,
+                                    const float* d_row_stat, const dc_matrix* grad_residual_out, const dc_matrix* grad_out,
+                                    const dc_matrix* grad_block, const dc_matrix* grad_residual, int32_t accumulate,
+                                    const dc_matrix* grad_post_weight, const dc_matrix* grad_gate, const dc_matrix* grad_pre_weight,
+                                    void* d_ws, size_t ws_bytes, void* hip_stream);
 
 /*
  * Embedding of the packed token ids: out[t, :] = scale * weight[d_token[t], :] for the n_rows tokens of out, the product

@@ -24,6 +24,7 @@ DC_REPACK_NOALLOC_WS_BYTES = 8 << 20
 DC_MAX_VOCAB = 1 << 24
 DC_MAX_DIM = 65536
 DC_MAX_TOP = 64
+DC_MAX_HEAD_ROWS = 1 << 22
 DC_MAX_TENSORS = 65536
 DC_STATE_BLOCK = 256
 DC_NO_TOKEN = -1
@@ -46,6 +47,8 @@ EXPORTS = ("dc_workspace_bytes", "dc_balance", "dc_group_advantage", "dc_plan", 
            "dc_repack", "dc_scatter_workspace_bytes", "dc_scatter", "dc_gae", "dc_balance_group_advantage",
            "dc_gather_advantage", "dc_balance_workspace_bytes", "dc_balance_ws", "dc_repack_noalloc", "dc_balance_plan_group_advantage", "dc_gather_timed",
            "dc_token_logprob_workspace_bytes", "dc_token_logprob", "dc_token_logprob_backward",
+           "dc_head_logprob_workspace_bytes", "dc_head_logprob", "dc_head_logprob_backward_workspace_bytes", "dc_head_logprob_backward",
+           "dc_residual_norm", "dc_residual_norm_backward_workspace_bytes", "dc_residual_norm_backward",
            "dc_embedding", "dc_embedding_backward_workspace_bytes", "dc_embedding_backward",
            "dc_adamw_table_bytes", "dc_adamw_table", "dc_adamw", "dc_strerror")
 
@@ -70,6 +73,11 @@ class dc_field(C.Structure):
 class dc_matrix(C.Structure):
     _fields_ = [("d_data", C.c_void_p), ("n_rows", C.c_int64), ("n_cols", C.c_int64), ("row_stride", C.c_int64),
                 ("type", C.c_int32), ("reserved", C.c_int32)]
+
+
+class dc_norm_params(C.Structure):
+    _fields_ = [("eps", C.c_double), ("residual_scale", C.c_double), ("block_scale", C.c_double),
+                ("gate_rows", C.c_int32), ("reserved", C.c_int32)]
 
 
 class dc_adamw_tensor(C.Structure):
@@ -158,6 +166,21 @@ def load() -> C.CDLL:
         lib.dc_token_logprob.argtypes = [mp, C.c_double, vp, vp, C.c_int32, vp, vp, vp, vp, vp, vp, C.c_size_t, vp, vp]
         lib.dc_token_logprob_backward.restype = C.c_int
         lib.dc_token_logprob_backward.argtypes = [mp, C.c_double, vp, vp, vp, vp, vp, vp, mp, vp, vp]
+        lib.dc_head_logprob_workspace_bytes.restype = C.c_size_t
+        lib.dc_head_logprob_workspace_bytes.argtypes = [mp, mp, C.c_int32]
+        lib.dc_head_logprob.restype = C.c_int
+        lib.dc_head_logprob.argtypes = [mp, mp, C.c_double, vp, vp, C.c_int32, vp, vp, vp, vp, vp, vp, C.c_size_t, vp, vp]
+        lib.dc_head_logprob_backward_workspace_bytes.restype = C.c_size_t
+        lib.dc_head_logprob_backward_workspace_bytes.argtypes = [mp, mp, mp]
+        lib.dc_head_logprob_backward.restype = C.c_int
+        lib.dc_head_logprob_backward.argtypes = [mp, mp, C.c_double, vp, vp, vp, vp, vp, vp, mp, C.c_int32, mp, vp, C.c_size_t, vp, vp]
+        np_ = C.POINTER(dc_norm_params)
+        lib.dc_residual_norm.restype = C.c_int
+        lib.dc_residual_norm.argtypes = [mp, mp, mp, mp, mp, np_, mp, mp, vp, vp]
+        lib.dc_residual_norm_backward_workspace_bytes.restype = C.c_size_t
+        lib.dc_residual_norm_backward_workspace_bytes.argtypes = [mp]
+        lib.dc_residual_norm_backward.restype = C.c_int
+        lib.dc_residual_norm_backward.argtypes = [mp, mp, mp, mp, mp, np_, vp, mp, mp, mp, mp, C.c_int32, mp, mp, mp, vp, C.c_size_t, vp]
         lib.dc_embedding.restype = C.c_int
         lib.dc_embedding.argtypes = [mp, vp, C.c_double, mp, vp, vp]
         lib.dc_embedding_backward_workspace_bytes.restype = C.c_size_t
@@ -485,6 +508,77 @@ def dc_token_logprob_backward(logits: dc_matrix, temperature: float, d_token, d_
                                             _vec(d_grad_entropy, n, _F32, "d_grad_entropy"), C.byref(grad_logits),
                                             _ptr(d_status), _stream(stream)),
            "dc_token_logprob_backward")
+
+
+def _ref(m: Optional[dc_matrix]):
+    """A matrix by reference; None (a null pointer) stays None."""
+    return None if m is None else C.byref(m)
+
+
+def dc_head_logprob_workspace_bytes(hidden: dc_matrix, weight: dc_matrix, n_top: int) -> int:
+    return int(load().dc_head_logprob_workspace_bytes(C.byref(hidden), C.byref(weight), int(n_top)))
+
+
+def dc_head_logprob(hidden: dc_matrix, weight: dc_matrix, temperature: float, d_token, d_mask, n_top: int, d_logprob, d_row_stat,
+                    d_entropy, d_top_token, d_top_logprob, d_ws, ws_bytes: int, d_status, stream=None) -> None:
+    n, k = hidden.n_rows, int(n_top)
+    _check(load().dc_head_logprob(C.byref(hidden), C.byref(weight), float(temperature), _vec(d_token, n, _I32, "d_token"),
+                                  _vec(d_mask, n, _U8, "d_mask"), k, _vec(d_logprob, n, _F32, "d_logprob"),
+                                  _vec(d_row_stat, 2 * n, _F32, "d_row_stat"), _vec(d_entropy, n, _F32, "d_entropy"),
+                                  _vec(d_top_token, n * k, _I32, "d_top_token"),
+                                  _vec(d_top_logprob, n * k, _F32, "d_top_logprob"), _ptr(d_ws), int(ws_bytes),
+                                  _ptr(d_status), _stream(stream)),
+           "dc_head_logprob")
+
+
+def dc_head_logprob_backward_workspace_bytes(hidden: dc_matrix, weight: dc_matrix, grad_weight: Optional[dc_matrix]) -> int:
+    return int(load().dc_head_logprob_backward_workspace_bytes(C.byref(hidden), C.byref(weight), _ref(grad_weight)))
+
+
+def dc_head_logprob_backward(hidden: dc_matrix, weight: dc_matrix, temperature: float, d_token, d_mask, d_row_stat, d_entropy,
+                             d_grad_logprob, d_grad_entropy, grad_hidden: Optional[dc_matrix], accumulate: bool,
+                             grad_weight: Optional[dc_matrix], d_ws, ws_bytes: int, d_status, stream=None) -> None:
+    n = hidden.n_rows
+    _check(load().dc_head_logprob_backward(C.byref(hidden), C.byref(weight), float(temperature), _vec(d_token, n, _I32, "d_token"),
+                                           _vec(d_mask, n, _U8, "d_mask"), _vec(d_row_stat, 2 * n, _F32, "d_row_stat"),
+                                           _vec(d_entropy, n, _F32, "d_entropy"),
+                                           _vec(d_grad_logprob, n, _F32, "d_grad_logprob"),
+                                           _vec(d_grad_entropy, n, _F32, "d_grad_entropy"), _ref(grad_hidden),
+                                           int(bool(accumulate)), _ref(grad_weight), _ptr(d_ws), int(ws_bytes), _ptr(d_status),
+                                           _stream(stream)),
+           "dc_head_logprob_backward")
+
+
+def make_norm(eps: float = 1e-6, residual_scale: float = 1.0, block_scale: float = 1.0,
+              gate_rows: bool = False) -> dc_norm_params:
+    return dc_norm_params(eps, residual_scale, block_scale, int(bool(gate_rows)), 0)
+
+
+def dc_residual_norm(block: dc_matrix, post_weight: Optional[dc_matrix], gate: Optional[dc_matrix], residual: dc_matrix,
+                     pre_weight: Optional[dc_matrix], prm: dc_norm_params, residual_out: dc_matrix, out: Optional[dc_matrix],
+                     d_row_stat=None, stream=None) -> None:
+    _check(load().dc_residual_norm(C.byref(block), _ref(post_weight), _ref(gate), C.byref(residual), _ref(pre_weight),
+                                   C.byref(prm), C.byref(residual_out), _ref(out),
+                                   _vec(d_row_stat, 2 * block.n_rows, _F32, "d_row_stat"), _stream(stream)),
+           "dc_residual_norm")
+
+
+def dc_residual_norm_backward_workspace_bytes(block: dc_matrix) -> int:
+    return int(load().dc_residual_norm_backward_workspace_bytes(C.byref(block)))
+
+
+def dc_residual_norm_backward(block: dc_matrix, post_weight: Optional[dc_matrix], gate: Optional[dc_matrix],
+                              residual_out: Optional[dc_matrix], pre_weight: Optional[dc_matrix], prm: dc_norm_params, d_row_stat,
+                              grad_residual_out: Optional[dc_matrix], grad_out: Optional[dc_matrix], grad_block: Optional[dc_matrix],
+                              grad_residual: Optional[dc_matrix], accumulate: bool, grad_post_weight: Optional[dc_matrix],
+                              grad_gate: Optional[dc_matrix], grad_pre_weight: Optional[dc_matrix], d_ws, ws_bytes: int,
+                              stream=None) -> None:
+    _check(load().dc_residual_norm_backward(C.byref(block), _ref(post_weight), _ref(gate), _ref(residual_out), _ref(pre_weight),
+                                            C.byref(prm), _vec(d_row_stat, 2 * block.n_rows, _F32, "d_row_stat"),
+                                            _ref(grad_residual_out), _ref(grad_out), _ref(grad_block), _ref(grad_residual),
+                                            int(bool(accumulate)), _ref(grad_post_weight), _ref(grad_gate), _ref(grad_pre_weight),
+                                            _ptr(d_ws), int(ws_bytes), _stream(stream)),
+           "dc_residual_norm_backward")
 
 
 def dc_embedding(weight: dc_matrix, d_token, scale: float, out: dc_matrix, d_status, stream=None) -> None:

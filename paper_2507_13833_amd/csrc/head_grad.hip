@@ -1,0 +1,497 @@
+// Gradients of the hidden states and of the head's weights from those of the log-probabilities and entropies.  With
+// G[r, v] = (1/T) (a_r ((v == token_r) - p_v) - b_r p_v (log p_v + H_r)), the gradient of the logits that are never kept:
+//   grad_hidden = G weight,  grad_weight = G^T hidden.
+//
+// A piece of the vocabulary at a time: its logits are made again tile by tile and become G in the tile's registers, which goes to
+// the workspace once along the rows and once along the vocabulary; two products of matrices read it there.  Rows that add nothing
+// (masked, or a = b = 0) take part in none of it: the live rows are numbered first.
+//
+// 16-bit operands: G, the weights and the hidden states are held in f16 (11 bits, three more than bf16's), each times a power of
+// two that takes its largest magnitude to just below 2^15: per row for G (from |a|, |b| and H, which bound it), undone in the row's
+// hidden gradient and in the row's hidden state, per piece for the weights.  G in one f16 is off by at most 2^-11 of each value,
+// before sums of 32 bits that are rounded to 16 bits themselves; a gradient of the weights in 32 bits takes G in two (2^-22).
+// Numbers of 32 bits are taken apart into three of bf16 everywhere, as in the forward direction.
+#include <algorithm>
+#include "head_rows.h"
+
+namespace dc {
+
+// ---- per row ----
+
+constexpr int NO_EXPONENT = -100000;
+__device__ __forceinline__ int exponent_above(float magnitude) {         // 2^it is above; infinities and NaN: 129
+    return (int)(__float_as_uint(magnitude) >> 23) - 126;
+}
+
+struct TermArgs {
+    const void*    x;
+    int64_t        stride, n_rows;
+    int32_t        dim, vocab, scaled;           // scaled: operands have powers of two of their own
+    float          inv_t;
+    const int32_t* token;
+    const float*   stat;
+    const float*   entropy;
+    const float*   a;
+    const float*   b;
+    const int32_t* pos;
+    RowTerm*       term;
+    int32_t*       top;             // [0]: of the hidden states, [1 ..]: of the pieces of the weights
+    int32_t*       status;
+};
+
+__global__ __launch_bounds__(256) void no_exponents_kernel(int32_t* top, int32_t n) {
+    for (int32_t i = threadIdx.x; i < n; i += 256) top[i] = NO_EXPONENT;
+}
+
+// A wave per row.
+template <typename T>
+__global__ __launch_bounds__(256) void head_terms_kernel(const TermArgs t) {
+    const int lane = lane_id();
+    int most = NO_EXPONENT;
+    for (int64_t r = blockIdx.x * 4LL + threadIdx.x / WAVE; r < t.n_rows; r += gridDim.x * 4LL) {
+        const int32_t at = t.pos[r];
+        if (at < 0) continue;
+        const float a = t.a[r] * t.inv_t, b = t.b ? t.b[r] * t.inv_t : 0.0f, h = b != 0.0f ? t.entropy[r] : 0.0f;
+        int e = 0;
+        if (t.scaled) {
+            // |p (log p + H)| <= max(1 / e, H)
+            const float bound = fabsf(a) + fabsf(b) * (fabsf(h) + 1.0f);
+            e = max(-120, min(100, 14 - exponent_above(bound)));
+            if (!(bound < INFINITY)) e = 0;
+            uint32_t big = 0;
+            const T* x = static_cast<const T*>(t.x) + r * t.stride;
+            for (int32_t c = lane; c < t.dim; c += WAVE) big = max(big, __float_as_uint(fabsf((float)x[c])));
+#pragma unroll
+            for (int d = 1; d < WAVE; d <<= 1) big = max(big, (uint32_t)__shfl_xor((int)big, d));
+            most = max(most, exponent_above(__uint_as_float(big)) - e);
+        }
+        if (lane == 0) {
+            int32_t token = -1;
+            if (t.token) {
+                token = t.token[r];
+                if (token < 0 || token >= t.vocab) {
+                    set_status(t.status, DC_ERR_TOKEN_RANGE);
+                    token = -1;
+                }
+            }
+            t.term[at] = RowTerm{t.stat[2 * r], t.stat[2 * r + 1] * LOG2E, ldexpf(b != 0.0f ? -fmaf(b, h, a) : -a, e), ldexpf(-b * LN2, e),
+                                 ldexpf(a, e), token, e, 0};
+        }
+    }
+    if (t.scaled && lane == 0 && most != NO_EXPONENT) atomicMax(t.top, most);
+}
+
+// The largest magnitude of a piece of the weights.
+template <typename T>
+__global__ __launch_bounds__(256) void head_top_kernel(const T* w, int64_t stride, int64_t rows, int32_t cols, int32_t* top) {
+    uint32_t big = 0;
+    for (int64_t r = blockIdx.x * 4LL + threadIdx.x / WAVE; r < rows; r += gridDim.x * 4LL)
+        for (int32_t c = lane_id(); c < cols; c += WAVE) big = max(big, __float_as_uint(fabsf((float)w[r * stride + c])));
+#pragma unroll
+    for (int d = 1; d < WAVE; d <<= 1) big = max(big, (uint32_t)__shfl_xor((int)big, d));
+    if (lane_id() == 0) atomicMax(top, exponent_above(__uint_as_float(big)));
+}
+
+// ---- G of a piece ----
+
+struct HeadPieceArgs {
+    Operand        w, x;
+    Parts          parts;
+    int32_t        steps, v0, vocab_end, tiles, row_tiles;
+    const int32_t* count;
+    const RowTerm* term;
+    float          k;
+    char*          g;               // [plane][row][width], NULL: not wanted
+    char*          gt;              // [plane][vocabulary entry][rows_pad], NULL: not wanted
+    int64_t        width, rows_pad;
+};
+
+// T: of the operands, D: of G; PLANES of it along the vocabulary (gt) and, for bf16, along the rows too (f16: one there).
+template <typename T, typename D, int PLANES>
+__global__ __launch_bounds__(P_THREADS, 2) void head_piece_kernel(const HeadPieceArgs h) {
+    __shared__ __attribute__((aligned(1024))) char lds[P_LDS];
+    const TilePair at = tile_pair(by_chiplet(blockIdx.x, h.row_tiles * h.tiles), h.row_tiles, h.tiles);
+    const int32_t n_rows = *h.count, first = at.first * PN, t = at.second;
+    if (first >= n_rows) return;
+    const int lane = lane_id(), wave = threadIdx.x / WAVE;
+    f32x4 acc[P_MT][P_NT];
+    {
+        TileOfA a;
+        TileOfB b;
+        place_tile(a, h.w, t * PM, h.vocab_end - h.v0);
+        place_tile(b, h.x, first, n_rows);
+        product<T>(acc, a, b, h.parts, h.steps, lds);
+    }
+    const int32_t u = t * PM + wave / 2 * (PM / 2) + (lane >> 4) * 4, row = first + wave % 2 * (PN / 2) + (lane & 15);
+    constexpr int ROW_PLANES = std::is_same_v<D, _Float16> ? 1 : PLANES;
+    const int64_t g_plane = h.width * h.rows_pad * 2;
+#pragma unroll
+    for (int j = 0; j < P_NT; ++j) {
+        const int32_t r = row + 16 * j;
+        const bool live = r < n_rows;
+        RowTerm q = {};
+        if (live) q = h.term[r];
+        const uint32_t own = (uint32_t)(q.token - h.v0 - u);
+#pragma unroll
+        for (int i = 0; i < P_MT; ++i) {
+            float f[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float l2 = (acc[i][j][e] - q.m) * h.k - q.l2, p = __builtin_amdgcn_exp2f(l2);
+                f[e] = p * fmaf(q.c1, fmaxf(l2, -1e4f), q.c0);
+                if (own == (uint32_t)(16 * i + e)) f[e] += q.ga;
+                if (!live || h.v0 + u + 16 * i + e >= h.vocab_end) f[e] = 0.0f;
+            }
+            D d[PLANES][4];
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) d[p][e] = take_part<D>(f[e]);
+            if (h.g)
+#pragma unroll
+                for (int p = 0; p < ROW_PLANES; ++p)
+                    *reinterpret_cast<uint64_t*>(h.g + p * g_plane + (r * h.width + u + 16 * i) * 2) =
+                        *reinterpret_cast<const uint64_t*>(d[p]);
+            if (h.gt)
+#pragma unroll
+                for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        reinterpret_cast<D*>(h.gt + p * g_plane)[(int64_t)(u + 16 * i + e) * h.rows_pad + r] = d[p][e];
+        }
+    }
+}
+
+// ---- the two products ----
+
+struct HeadHiddenArgs {             // slab[split][row][col] (+)= sum over this split's share of the piece
+    Operand        wt, g;
+    Parts          parts;
+    int32_t        steps, splits, col_tiles, row_tiles, dim;
+    const int32_t* count;
+    const int32_t* top;
+    bool           add;
+    float*         slab;
+    int64_t        rows_pad, pitch;
+};
+template <typename D>
+__global__ __launch_bounds__(P_THREADS, 2) void head_hidden_kernel(const HeadHiddenArgs h) {
+    __shared__ __attribute__((aligned(1024))) char lds[P_LDS];
+    const int32_t others = h.col_tiles * h.splits;
+    const TilePair at = tile_pair(by_chiplet(blockIdx.x, h.row_tiles * others), h.row_tiles, others);
+    const int32_t n_rows = *h.count, first = at.first * PN, tile = at.second % h.col_tiles, split = at.second / h.col_tiles;
+    if (first >= n_rows) return;
+    const int32_t each = (h.steps + h.splits - 1) / h.splits, from = split * each, steps = min(each, h.steps - from);
+    const int lane = lane_id(), wave = threadIdx.x / WAVE;
+    f32x4 acc[P_MT][P_NT];
+    {
+        TileOfA a;
+        TileOfB b;
+        place_tile(a, h.wt, tile * PM, h.dim);
+        place_tile(b, h.g, first, n_rows);
+        a.base += from * (PK * 2LL);
+        b.base += from * (PK * 2LL);
+        product<D>(acc, a, b, h.parts, max(steps, 0), lds);
+    }
+    const int up = std::is_same_v<D, _Float16> ? *h.top - 15 : 0;
+    const int32_t col = tile * PM + wave / 2 * (PM / 2) + (lane >> 4) * 4, row = first + wave % 2 * (PN / 2) + (lane & 15);
+#pragma unroll
+    for (int j = 0; j < P_NT; ++j)
+        if (row + 16 * j < n_rows)
+#pragma unroll
+            for (int i = 0; i < P_MT; ++i)
+                if (col + 16 * i < h.pitch) {        // (a multiple of 4)
+                    f32x4* to = reinterpret_cast<f32x4*>(h.slab + ((int64_t)split * h.rows_pad + row + 16 * j) * h.pitch + col + 16 * i);
+                    f32x4 v = acc[i][j];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = ldexpf(v[e], up);
+                    if (h.add) v += *to;
+                    *to = v;
+                }
+}
+
+// A row's hidden gradient: the slabs' sum, its own power of two undone, rounded once.  Rows that take no part: +0.
+template <typename T>
+__global__ __launch_bounds__(256) void head_hidden_join_kernel(const float* slab, int32_t splits, int64_t rows_pad, int64_t pitch,
+                                                               const int32_t* pos, const RowTerm* term, T* out, int64_t stride, int64_t rows,
+                                                               int32_t dim) {
+    const int64_t each = pitch / 4;
+    for (int64_t q = blockIdx.x * 256LL + threadIdx.x; q < rows * each; q += gridDim.x * 256LL) {
+        const int64_t r = q / each;
+        const int32_t c = (int32_t)(q - r * each) * 4, at = pos[r];
+        f32x4 sum = {0, 0, 0, 0};
+        if (at >= 0) {
+            for (int32_t s = 0; s < splits; ++s) sum += *reinterpret_cast<const f32x4*>(slab + (s * rows_pad + at) * pitch + c);
+            const int e = -term[at].exponent;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] = ldexpf(sum[i], e);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c + i < dim) out[r * stride + c + i] = (T)sum[i];
+    }
+}
+
+struct HeadWeightArgs {             // grad_weight[v0 + row of gt][col] (+)= sum over the live rows
+    Operand        xt, gt;
+    Parts          parts;
+    int32_t        n, row_tiles, col_tiles, dim;
+    const int32_t* count;
+    const int32_t* top;
+    bool           add, fours;      // fours: four neighbours are stored at once
+    void*          out;             // of the piece's first entry
+    int64_t        stride;
+};
+template <typename D, typename T>
+__global__ __launch_bounds__(P_THREADS, 2) void head_weight_kernel(const HeadWeightArgs h) {
+    __shared__ __attribute__((aligned(1024))) char lds[P_LDS];
+    const TilePair at = tile_pair(by_chiplet(blockIdx.x, h.row_tiles * h.col_tiles), h.row_tiles, h.col_tiles);
+    const int32_t first = at.first * PN, tile = at.second;
+    const int lane = lane_id(), wave = threadIdx.x / WAVE;
+    f32x4 acc[P_MT][P_NT];
+    {
+        TileOfA a;
+        TileOfB b;
+        place_tile(a, h.xt, tile * PM, h.dim);
+        place_tile(b, h.gt, first, h.n);
+        product<D>(acc, a, b, h.parts, (*h.count + PK - 1) / PK, lds);
+    }
+    const int up = std::is_same_v<D, _Float16> ? *h.top - 15 : 0;
+    const int32_t col = tile * PM + wave / 2 * (PM / 2) + (lane >> 4) * 4, row = first + wave % 2 * (PN / 2) + (lane & 15);
+#pragma unroll
+    for (int j = 0; j < P_NT; ++j) {
+        if (row + 16 * j >= h.n) continue;
+        T* to = static_cast<T*>(h.out) + (row + 16 * j) * h.stride + col;
+#pragma unroll
+        for (int i = 0; i < P_MT; ++i) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][j][e] = ldexpf(acc[i][j][e], up);
+            if (h.fours && col + 16 * i + 4 <= h.dim) {
+                struct alignas(4 * sizeof(T)) Four { T e[4]; } four;
+                if (h.add) four = *reinterpret_cast<const Four*>(to + 16 * i);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) four.e[e] = (T)(h.add ? acc[i][j][e] + (float)four.e[e] : acc[i][j][e]);
+                *reinterpret_cast<Four*>(to + 16 * i) = four;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (col + 16 * i + e < h.dim)
+                        to[16 * i + e] = (T)(h.add ? acc[i][j][e] + (float)to[16 * i + e] : acc[i][j][e]);
+            }
+        }
+    }
+}
+
+// ---- the workspace ----
+
+constexpr int64_t HG_AREA = 1 << 27;             // elements of G, or of the weights laid out, held at once
+constexpr int32_t HG_SLOTS = 512, HG_MOST_SPLITS = 16;
+
+namespace {
+struct HeadGradWs {
+    LiveRows live;
+    RowTerm* term;
+    int32_t* top;
+    int32_t  pieces, piece;         // entries of the vocabulary to a piece, a multiple of PM
+    char*    hidden; int64_t hidden_plane;
+    char*    weight; int64_t weight_plane;
+    char*    xt;     int64_t xt_plane;
+    char*    wt;     int64_t wt_plane;
+    char*    g;
+    char*    gt;     int64_t g_plane;
+    float*   slab;   int64_t pitch; int32_t splits;
+    size_t   bytes;
+};
+}
+static int64_t g_area(int64_t rows_pad, int64_t vocab_pad) {
+    return std::min(rows_pad * vocab_pad, std::max(HG_AREA, rows_pad * 8 * PM));
+}
+// Every area grows with the rows, so that what serves a call serves those of fewer.
+static HeadGradWs carve_grad(void* base, const dc_matrix& hidden, const dc_matrix& weight, int32_t grad_weight_type) {
+    HeadGradWs w = {};
+    const HeadShape sh = head_shape(hidden, weight, true);
+    int64_t at = 0;
+    const auto take = [&](int64_t bytes) {
+        char* p = static_cast<char*>(base) + at;
+        at += align256(bytes);
+        return p;
+    };
+    const bool f32 = hidden.type == DC_F32;
+    const int64_t rows = hidden.n_rows, dim = hidden.n_cols, planes = f32 ? 3 : 1, g_planes = f32 ? 3 : grad_weight_type == DC_F32 ? 2 : 1;
+    const int64_t vocab_pad = whole(weight.n_rows, PM);
+    w.live.list = reinterpret_cast<int32_t*>(take(rows * 4));
+    w.live.pos = reinterpret_cast<int32_t*>(take(rows * 4));
+    w.live.count = reinterpret_cast<int32_t*>(take(4));
+    w.term = reinterpret_cast<RowTerm*>(take(rows * (int64_t)sizeof(RowTerm)));
+    w.top = reinterpret_cast<int32_t*>(take((vocab_pad / PM + 1) * 4));
+    const int64_t area = g_area(sh.rows_pad, vocab_pad);
+    // (the weights laid out along the columns: at most HG_AREA elements too)
+    const int64_t width = std::min(area / sh.rows_pad, std::max<int64_t>(HG_AREA / whole(dim, PM), 8 * PM));
+    w.piece = (int32_t)std::min<int64_t>(vocab_pad, width / PM * PM);
+    w.pieces = (int32_t)((vocab_pad + w.piece - 1) / w.piece);
+    w.piece = (int32_t)whole((vocab_pad + w.pieces - 1) / w.pieces, PM);
+    w.pieces = (int32_t)((vocab_pad + w.piece - 1) / w.piece);
+    const int64_t widest = std::min(vocab_pad, std::max<int64_t>(HG_AREA / whole(dim, PM), 8 * PM));
+    w.hidden_plane = rows * sh.k_pad * 2;
+    w.hidden = take(sh.copy_hidden ? planes * w.hidden_plane : 0);
+    w.weight_plane = (int64_t)w.piece * sh.k_pad * 2;
+    w.weight = take(sh.copy_weight ? planes * widest * sh.k_pad * 2 : 0);
+    w.xt_plane = dim * sh.rows_pad * 2;
+    w.xt = take(planes * w.xt_plane);
+    w.wt_plane = dim * w.piece * 2;
+    w.wt = take(planes * dim * widest * 2);
+    w.g_plane = sh.rows_pad * w.piece * 2;
+    w.g = take((f32 ? 3 : 1) * area * 2);
+    w.gt = take(g_planes * area * 2);
+    w.pitch = whole(dim, 4);
+    const int64_t row_tiles = sh.rows_pad / PN, col_tiles = (dim + PM - 1) / PM;
+    w.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(HG_MOST_SPLITS, HG_SLOTS / (row_tiles * col_tiles)));
+    w.slab = reinterpret_cast<float*>(take(std::max(row_tiles, std::min<int64_t>(HG_MOST_SPLITS * row_tiles, HG_SLOTS / col_tiles)) * PN * w.pitch * 4));
+    w.bytes = (size_t)at;
+    return w;
+}
+size_t head_grad_workspace_bytes(const dc_matrix& hidden, const dc_matrix& weight, int32_t grad_weight_type) {
+    return hidden.n_rows > 0 ? carve_grad(nullptr, hidden, weight, grad_weight_type).bytes : 0;
+}
+
+// grad_weight of a call without rows.
+template <typename T>
+__global__ __launch_bounds__(256) void head_no_rows_kernel(T* out, int64_t stride, int64_t rows, int32_t dim) {
+    for (int64_t q = blockIdx.x * 256LL + threadIdx.x; q < rows * dim; q += gridDim.x * 256LL) out[q / dim * stride + q % dim] = (T)0.0f;
+}
+
+hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
+    const int64_t rows = a.hidden.n_rows;
+    const dc_matrix &gh = a.grad_hidden, &gw = a.grad_weight;
+    const int32_t vocab = (int32_t)a.weight.n_rows, dim = (int32_t)a.hidden.n_cols, type = a.hidden.type;
+    if (rows == 0) {
+        if (!gw.d_data || a.accumulate) return hipSuccess;
+        return with_type(gw.type, [&](auto e) {
+            using T = typename decltype(e)::type;
+            head_no_rows_kernel<T><<<2048, 256, 0, st>>>(static_cast<T*>(gw.d_data), gw.row_stride, vocab, dim);
+            return hipGetLastError();
+        });
+    }
+    const HeadGradWs w = carve_grad(d_ws, a.hidden, a.weight, gw.d_data ? gw.type : type);
+    const HeadShape sh = head_shape(a.hidden, a.weight, true);
+    const bool f32 = type == DC_F32;
+    hipError_t e = launch_live_rows(a.mask, a.grad_logprob, a.grad_entropy, rows, w.live, st);
+    if (e != hipSuccess) return e;
+    no_exponents_kernel<<<1, 256, 0, st>>>(w.top, w.pieces + 1);
+    const TermArgs t = {a.hidden.d_data, a.hidden.row_stride, rows, dim, vocab, !f32, a.inv_t, a.token, a.stat, a.entropy,
+                        a.grad_logprob, a.grad_entropy, w.live.pos, w.term, w.top, a.status};
+    const unsigned waves4 = (unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 14);
+    e = with_type(type, [&](auto el) {
+        head_terms_kernel<typename decltype(el)::type><<<waves4, 256, 0, st>>>(t);
+        return hipGetLastError();
+    });
+    HeadPieceArgs p = {};
+    p.steps = sh.k_pad / PK;
+    p.parts = parts_of(type, w.weight_plane, w.hidden_plane);
+    p.row_tiles = (int32_t)(sh.rows_pad / PN);
+    p.count = w.live.count;
+    p.term = w.term;
+    p.k = a.inv_t * LOG2E;
+    p.g = gh.d_data ? w.g : nullptr;
+    p.gt = gw.d_data ? w.gt : nullptr;
+    p.width = w.piece;
+    p.rows_pad = sh.rows_pad;
+    if (sh.copy_hidden) {
+        if (e == hipSuccess) e = launch_lay_rows(a.hidden, 0, rows, w.live.list, w.live.count, sh.k_pad, w.hidden, w.hidden_plane, st);
+        p.x = Operand{w.hidden, sh.k_pad * 2, nullptr};
+    } else {
+        p.x = Operand{static_cast<const char*>(a.hidden.d_data), a.hidden.row_stride * 2, w.live.list};
+    }
+    const int32_t* const top_x = f32 ? nullptr : w.top;
+    if (gw.d_data && e == hipSuccess)
+        e = launch_lay_columns(a.hidden, 0, rows, w.live.list, w.live.count, f32 ? 3 : 1, sh.rows_pad, top_x, f32 ? nullptr : w.term, w.xt,
+                               w.xt_plane, st);
+    HeadHiddenArgs hh = {};
+    hh.wt = Operand{w.wt, w.piece * 2LL, nullptr};
+    hh.g = Operand{w.g, w.piece * 2LL, nullptr};
+    hh.parts = parts_of(type, w.wt_plane, w.g_plane);
+    hh.splits = w.splits;
+    hh.col_tiles = (dim + PM - 1) / PM;
+    hh.row_tiles = p.row_tiles;
+    hh.dim = dim;
+    hh.count = w.live.count;
+    hh.slab = w.slab;
+    hh.rows_pad = sh.rows_pad;
+    hh.pitch = w.pitch;
+    HeadWeightArgs hw = {};
+    hw.xt = Operand{w.xt, sh.rows_pad * 2, nullptr};
+    hw.gt = Operand{w.gt, sh.rows_pad * 2, nullptr};
+    hw.parts = parts_of(type, w.xt_plane, w.g_plane);
+    const bool two = gw.d_data && !f32 && gw.type == DC_F32;
+    if (two) hw.parts = Parts{2, {0, 0}, {w.g_plane, 0}};
+    hw.col_tiles = hh.col_tiles;
+    hw.dim = dim;
+    hw.count = w.live.count;
+    hw.top = top_x;
+    hw.add = a.accumulate;
+    hw.stride = gw.row_stride;
+    const int64_t out_bytes = gw.type == DC_F32 ? 4 : 2;
+    hw.fours = reinterpret_cast<uintptr_t>(gw.d_data) % (4 * out_bytes) == 0 && gw.row_stride % 4 == 0;
+    for (int32_t i = 0; i < w.pieces && e == hipSuccess; ++i) {
+        const int32_t v0 = i * w.piece, n = std::min(w.piece, vocab - v0);
+        const int32_t* const top_w = f32 ? nullptr : w.top + 1 + i;
+        if (gh.d_data) {
+            if (!f32)
+                e = with_type(type, [&](auto el) {
+                    using T = typename decltype(el)::type;
+                    head_top_kernel<T><<<(unsigned)std::min(2048, (n + 3) / 4), 256, 0, st>>>(
+                        static_cast<const T*>(a.weight.d_data) + v0 * a.weight.row_stride, a.weight.row_stride, n, dim, w.top + 1 + i);
+                    return hipGetLastError();
+                });
+            if (e == hipSuccess)
+                e = launch_lay_columns(a.weight, v0, n, nullptr, nullptr, f32 ? 3 : 1, w.piece, top_w, nullptr, w.wt, w.wt_plane, st);
+        }
+        if (sh.copy_weight) {
+            if (e == hipSuccess) e = launch_lay_rows(a.weight, v0, n, nullptr, nullptr, sh.k_pad, w.weight, w.weight_plane, st);
+            p.w = Operand{w.weight, sh.k_pad * 2, nullptr};
+        } else {
+            p.w = Operand{static_cast<const char*>(a.weight.d_data) + v0 * a.weight.row_stride * 2, a.weight.row_stride * 2, nullptr};
+        }
+        if (e != hipSuccess) break;
+        p.v0 = v0;
+        p.vocab_end = v0 + n;
+        p.tiles = (n + PM - 1) / PM;
+        const unsigned blocks = (unsigned)(p.row_tiles * p.tiles);
+        if (f32) head_piece_kernel<__bf16, __bf16, 3><<<blocks, P_THREADS, 0, st>>>(p);
+        else if (type == DC_BF16 && two) head_piece_kernel<__bf16, _Float16, 2><<<blocks, P_THREADS, 0, st>>>(p);
+        else if (type == DC_BF16) head_piece_kernel<__bf16, _Float16, 1><<<blocks, P_THREADS, 0, st>>>(p);
+        else if (two) head_piece_kernel<_Float16, _Float16, 2><<<blocks, P_THREADS, 0, st>>>(p);
+        else head_piece_kernel<_Float16, _Float16, 1><<<blocks, P_THREADS, 0, st>>>(p);
+        if (gh.d_data) {
+            hh.steps = (n + PK - 1) / PK;
+            hh.top = top_w;
+            hh.add = i > 0;
+            const unsigned b = (unsigned)(hh.row_tiles * hh.col_tiles * hh.splits);
+            if (f32) head_hidden_kernel<__bf16><<<b, P_THREADS, 0, st>>>(hh);
+            else head_hidden_kernel<_Float16><<<b, P_THREADS, 0, st>>>(hh);
+        }
+        if (gw.d_data) {
+            hw.n = n;
+            hw.row_tiles = (n + PN - 1) / PN;
+            hw.out = static_cast<char*>(gw.d_data) + v0 * gw.row_stride * out_bytes;
+            const unsigned b = (unsigned)(hw.row_tiles * hw.col_tiles);
+            e = with_type(gw.type, [&](auto el) {
+                using T = typename decltype(el)::type;
+                if (f32) head_weight_kernel<__bf16, T><<<b, P_THREADS, 0, st>>>(hw);
+                else head_weight_kernel<_Float16, T><<<b, P_THREADS, 0, st>>>(hw);
+                return hipGetLastError();
+            });
+        }
+        if (e == hipSuccess) e = hipGetLastError();
+    }
+    if (gh.d_data && e == hipSuccess)
+        e = with_type(gh.type, [&](auto el) {
+            using T = typename decltype(el)::type;
+            head_hidden_join_kernel<T><<<(unsigned)std::min<int64_t>((rows * (w.pitch / 4) + 255) / 256, 1 << 14), 256, 0, st>>>(
+                w.slab, w.splits, sh.rows_pad, w.pitch, w.live.pos, w.term, static_cast<T*>(gh.d_data), gh.row_stride, rows, dim);
+            return hipGetLastError();
+        });
+    return e;
+}
+
+}  // namespace dc

@@ -1,0 +1,40 @@
+// Which rows of the head's operands take part, and operands laid out for the product: shared by the two directions.
+#pragma once
+#include "head_device.h"
+
+namespace dc {
+
+struct HeadShape {
+    int64_t rows_pad;               // rows, to whole tiles of B
+    int32_t k_pad;                  // columns, to whole steps
+    bool    copy_hidden, copy_weight;   // not as the product reads it: laid out in the workspace first
+};
+HeadShape head_shape(const dc_matrix& hidden, const dc_matrix& weight, bool listed);
+
+constexpr int64_t align256(int64_t n) { return (n + 255) / 256 * 256; }
+constexpr int64_t whole(int64_t n, int64_t of) { return (n + of - 1) / of * of; }
+
+// Rows `list` (or all) of src as PARTS planes of [rows][k_pad] 16-bit numbers, columns behind the last one 0.
+// *count (or n) rows, the planes `plane` bytes apart.
+hipError_t launch_lay_rows(const dc_matrix& src, int64_t first, int64_t n, const int32_t* list, const int32_t* count, int32_t k_pad,
+                           char* dst, int64_t plane, hipStream_t st);
+
+// The same the other way round: planes of [cols][rows_pad], rows behind the last one 0 to the next multiple of 64, `cols` of src's.
+// Values become 2^(15 - *top - term's exponent) times as much where `top` is not NULL (a row's own exponent where there are terms).
+struct RowTerm;
+hipError_t launch_lay_columns(const dc_matrix& src, int64_t first, int64_t n, const int32_t* list, const int32_t* count, int32_t planes,
+                              int64_t rows_pad, const int32_t* top, const RowTerm* term, char* dst, int64_t plane, hipStream_t st);
+
+// What the gradient of a live row's logits is made of: g_v = 2^exponent / T * (a (v == token) - p_v (a + b (log p_v + H))) with
+// log2 p_v = (x_v - m) k - l2:  g_v = ga (v == token) + p_v (c0 + c1 log2 p_v).
+struct alignas(16) RowTerm { float m, l2, c0, c1, ga; int32_t token, exponent, pad; };
+
+// The live rows of a batch, in order: list, their number, and where each row went (-1: nowhere).
+struct LiveRows { int32_t* list; int32_t* pos; int32_t* count; };
+// A row is live where its mask byte is not 0 (mask NULL: everywhere) and, where a is given, a or b is not 0.
+hipError_t launch_live_rows(const uint8_t* mask, const float* a, const float* b, int64_t n, const LiveRows& l, hipStream_t st);
+
+// Which of the planes of two operands are multiplied.
+Parts parts_of(int32_t type, int64_t a_plane, int64_t b_plane);
+
+}  // namespace dc

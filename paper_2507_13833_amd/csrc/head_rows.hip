@@ -1,0 +1,144 @@
+// Operands of the head laid out for the product on the matrix cores.
+#include <algorithm>
+#include "head_rows.h"
+
+namespace dc {
+
+static bool readable(const dc_matrix& m, bool listed) {
+    if (m.type == DC_F32 || m.n_cols % PK != 0 || reinterpret_cast<uintptr_t>(m.d_data) % 16 != 0) return false;
+    const int64_t pitch = m.row_stride * 2;
+    return pitch % 16 == 0 && pitch <= P_MOST_PITCH && (!listed || pitch * m.n_rows < 1LL << 32);
+}
+
+HeadShape head_shape(const dc_matrix& hidden, const dc_matrix& weight, bool listed) {
+    return HeadShape{whole(hidden.n_rows, PN), (int32_t)whole(hidden.n_cols, PK), !readable(hidden, listed), !readable(weight, false)};
+}
+
+// A thread takes eight neighbouring columns.  Bound by the bytes; sources of any alignment are read an element at a time.
+template <typename S, typename D, int PARTS>
+__global__ __launch_bounds__(256) void lay_rows_kernel(const S* src, int64_t stride, int64_t first, int64_t n, int32_t cols,
+                                                       const int32_t* list, const int32_t* count, int32_t k_pad, char* dst, int64_t plane) {
+    const int64_t rows = count ? *count : n;
+    const int32_t each = k_pad / 8;
+    for (int64_t q = blockIdx.x * 256LL + threadIdx.x; q < rows * each; q += gridDim.x * 256LL) {
+        const int64_t r = q / each;
+        const int32_t c = (int32_t)(q - r * each) * 8;
+        const S* from = src + (list ? list[r] : first + r) * stride + c;
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = c + j < cols ? (float)from[j] : 0.0f;
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            Raw8<D> out;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if constexpr (PARTS == 1) out.e[j] = (D)f[j];
+                else out.e[j] = take_part<D>(f[j]);
+            }
+            *reinterpret_cast<u32x4*>(dst + p * plane + (r * k_pad + c) * 2) = out.q[0];
+        }
+    }
+}
+
+hipError_t launch_lay_rows(const dc_matrix& src, int64_t first, int64_t n, const int32_t* list, const int32_t* count, int32_t k_pad,
+                           char* dst, int64_t plane, hipStream_t st) {
+    const int64_t blocks = std::min<int64_t>((n * (k_pad / 8) + 255) / 256, 8192);
+    if (blocks == 0) return hipSuccess;
+    const auto go = [&](auto s, auto d, auto parts) {
+        using S = decltype(s);
+        lay_rows_kernel<S, decltype(d), decltype(parts)::value><<<(unsigned)blocks, 256, 0, st>>>(
+            static_cast<const S*>(src.d_data), src.row_stride, first, n, (int32_t)src.n_cols, list, count, k_pad, dst, plane);
+    };
+    if (src.type == DC_F32) go(float{}, __bf16{}, std::integral_constant<int, 3>{});
+    else if (src.type == DC_BF16) go(__bf16{}, __bf16{}, std::integral_constant<int, 1>{});
+    else go(_Float16{}, _Float16{}, std::integral_constant<int, 1>{});
+    return hipGetLastError();
+}
+
+// Tiles of 64 x 64 through the LDS: read along the rows, written along the columns.
+template <typename S, typename D, int PARTS>
+__global__ __launch_bounds__(256) void lay_columns_kernel(const S* src, int64_t stride, int64_t first, int64_t n, int32_t cols,
+                                                          const int32_t* list, const int32_t* count, int64_t rows_pad, const int32_t* top,
+                                                          const RowTerm* term, char* dst, int64_t plane) {
+    __shared__ float tile[64][65];
+    const int64_t rows = count ? *count : n, r0 = blockIdx.x * 64LL;
+    if (r0 >= rows) return;
+    const int32_t c0 = blockIdx.y * 64, tid = threadIdx.x;
+    const int up = top ? 15 - *top : 0;
+    for (int i = tid / 64; i < 64; i += 4) {
+        const int64_t r = r0 + i;
+        const int32_t c = c0 + (tid & 63);
+        float v = 0.0f;
+        if (r < rows && c < cols) {
+            v = (float)src[(list ? list[r] : first + r) * stride + c];
+            if (top) v = ldexpf(v, up - (term ? term[r].exponent : 0));
+        }
+        tile[i][tid & 63] = v;
+    }
+    __syncthreads();
+    const int32_t c = tid / 4;
+    if (c0 + c >= cols) return;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int32_t i = tid % 4 * 8 + h * 32;
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = tile[i + j][c];
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            Raw8<D> out;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if constexpr (PARTS == 1) out.e[j] = (D)f[j];
+                else out.e[j] = take_part<D>(f[j]);
+            }
+            *reinterpret_cast<u32x4*>(dst + p * plane + ((c0 + c) * rows_pad + r0 + i) * 2) = out.q[0];
+        }
+    }
+}
+
+hipError_t launch_lay_columns(const dc_matrix& src, int64_t first, int64_t n, const int32_t* list, const int32_t* count, int32_t planes,
+                              int64_t rows_pad, const int32_t* top, const RowTerm* term, char* dst, int64_t plane, hipStream_t st) {
+    if (n == 0) return hipSuccess;
+    const dim3 grid((unsigned)((n + 63) / 64), (unsigned)((src.n_cols + 63) / 64));
+    const auto go = [&](auto s, auto d, auto parts) {
+        using S = decltype(s);
+        lay_columns_kernel<S, decltype(d), decltype(parts)::value><<<grid, 256, 0, st>>>(
+            static_cast<const S*>(src.d_data), src.row_stride, first, n, (int32_t)src.n_cols, list, count, rows_pad, top, term, dst, plane);
+    };
+    if (src.type == DC_F32) go(float{}, __bf16{}, std::integral_constant<int, 3>{});
+    else if (src.type == DC_BF16) go(__bf16{}, _Float16{}, std::integral_constant<int, 1>{});
+    else go(_Float16{}, _Float16{}, std::integral_constant<int, 1>{});
+    return hipGetLastError();
+}
+
+constexpr int LIVE_THREADS = 1024;
+__global__ __launch_bounds__(LIVE_THREADS) void live_rows_kernel(const uint8_t* mask, const float* a, const float* b, int64_t n, LiveRows l) {
+    __shared__ int32_t tmp[LIVE_THREADS / WAVE];
+    int32_t before = 0;
+    for (int64_t r0 = 0; r0 < n; r0 += LIVE_THREADS) {
+        const int64_t r = r0 + threadIdx.x;
+        int32_t live = r < n && (!mask || mask[r] != 0);
+        if (live && a) live = a[r] != 0.0f || (b && b[r] != 0.0f);
+        int32_t total;
+        const int32_t at = before + block_excl_scan_add(live, tmp, &total);
+        if (r < n) l.pos[r] = live ? at : -1;
+        if (live) l.list[at] = (int32_t)r;
+        before += total;
+    }
+    if (threadIdx.x == 0) *l.count = before;
+}
+hipError_t launch_live_rows(const uint8_t* mask, const float* a, const float* b, int64_t n, const LiveRows& l, hipStream_t st) {
+    live_rows_kernel<<<1, LIVE_THREADS, 0, st>>>(mask, a, b, n, l);
+    return hipGetLastError();
+}
+
+Parts parts_of(int32_t type, int64_t a_plane, int64_t b_plane) {
+    if (type != DC_F32) return Parts{1, {0}, {0}};
+    Parts p = {6, {}, {}};
+    const int pair[6][2] = {{0, 2}, {2, 0}, {1, 1}, {0, 1}, {1, 0}, {0, 0}};
+    for (int i = 0; i < 6; ++i) { p.a[i] = pair[i][0] * a_plane; p.b[i] = pair[i][1] * b_plane; }
+    return p;
+}
+
+}  // namespace dc
