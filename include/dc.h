@@ -458,7 +458,7 @@ dc_status dc_token_logprob_backward(const dc_matrix* logits, double temperature,
  * of the two factors' magnitude, and sums are held in 32 bits.  Arguments, masks, rows without a distribution, top
  * alternatives (ties to the lowest token) and device errors are those of dc_token_logprob; hidden rows of masked tokens are not
  * looked at.  An infinity or a NaN in a row of hidden, or in weight, may make a row one without a distribution.
- * With n_top > 0 the logits of 128 rows at a time pass through the workspace.
+ * Up to 64 rows, and 256 at a time where n_top > 0, go through logits in the workspace.
  * d_ws: 256-byte aligned, dc_head_logprob_workspace_bytes(hidden, weight, n_top) bytes, which also serve every call of fewer rows
  * of these matrices, fewer alternatives or both; holds nothing the caller needs afterwards.
  * Host errors: INVALID_ARG, UNSUPPORTED_SIZE (vocabulary above DC_MAX_VOCAB, n_cols above DC_MAX_DIM, more than DC_MAX_HEAD_ROWS

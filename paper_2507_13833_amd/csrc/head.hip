@@ -25,73 +25,115 @@ struct HeadStatArgs {
     float*         x_token;
 };
 
+// What a lane's sums of a row are relative to, in powers of two: k m for its largest logit m until now, rounded (k x less it is one
+// operation then), or from LOGIT_FAR on, where that rounding would be felt, k m itself, by differences taken first.
+constexpr float LOGIT_FAR = 0x1p24f;
+// How far what a lane's sums were relative to (for the largest logit m until now) lies below what they become relative to.
+__device__ __forceinline__ float less_reference(float m, float k, float base, float base2, bool far) {
+    const float m2 = m * k;
+    const bool was_far = fabsf(m2) >= LOGIT_FAR;
+    if (far) return was_far ? (m - base) * k : fmaf(-base, k, m2);
+    return was_far ? fmaf(m, k, -base2) : m2 - base2;
+}
+
 template <typename T, bool ENTROPY>
-__global__ __launch_bounds__(P_THREADS, 2) void head_stat_kernel(const HeadStatArgs h) {
+__global__ __launch_bounds__(P_THREADS, 1) void head_stat_kernel(const HeadStatArgs h) {
     __shared__ __attribute__((aligned(1024))) char lds[P_LDS];
     const int32_t blocks = h.row_tiles * h.segments;
     const TilePair at = tile_pair(by_chiplet(blockIdx.x, blocks), h.row_tiles, h.segments);
     const int32_t n_rows = h.count ? *h.count : h.n_rows, first = at.first * PN;
     if (first >= n_rows) return;
     const int lane = lane_id(), wave = threadIdx.x / WAVE;
-    const int32_t my_row = first + wave % 2 * (PN / 2) + (lane & 15);        // and 16, 32, 48 behind it
+    const int32_t my_row = first + place_b();        // and the seven behind it
     int32_t token[P_NT];
     float m[P_NT], s[P_NT], u[P_NT];
 #pragma unroll
     for (int j = 0; j < P_NT; ++j) {
-        const int32_t r = my_row + 16 * j;
+        const int32_t r = my_row + j;
         token[j] = -1;
         if (h.token && r < n_rows) token[j] = h.token[h.list ? h.list[r] : r];
         m[j] = -INFINITY;
         s[j] = u[j] = 0.0f;
     }
-    TileOfB b;
-    place_tile(b, h.x, first, n_rows);
+    Product<T> product;
+    product.parts = h.parts;
+    product.steps = h.steps;
+    int32_t asked = at.second;                   // the tile whose numbers are on their way
+    const auto next = [&] {
+        if (asked + h.segments < h.tiles) place_tile(product.a, h.w, (asked += h.segments) * PM, h.vocab_end - h.v0);
+    };
+    if (asked < h.tiles) {                       // (the last piece of a vocabulary may have fewer tiles than there are segments)
+        place_tile(product.a, h.w, asked * PM, h.vocab_end - h.v0);
+        place_tile(product.b, h.x, first, n_rows);
+        product.begin(lds, next);
+    }
     for (int32_t t = at.second; t < h.tiles; t += h.segments) {
-        TileOfA a;
-        place_tile(a, h.w, t * PM, h.vocab_end - h.v0);
         f32x4 acc[P_MT][P_NT];
-        product<T>(acc, a, b, h.parts, h.steps, lds);
-        const int32_t v = h.v0 + t * PM + wave / 2 * (PM / 2) + (lane >> 4) * 4;     // of acc[0][.][0]
-        if (h.v0 + (t + 1) * PM > h.vocab_end)
+        product.tile(acc, next);
+        const int32_t v = h.v0 + t * PM + place_a();       // of acc[0][.][0]
+        const bool whole = h.v0 + (t + 1) * PM <= h.vocab_end;
+#pragma unroll
+        for (int j = 0; j < P_NT; ++j) {             // a row at a time
+            float x[P_MT][4];
 #pragma unroll
             for (int i = 0; i < P_MT; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (v + 16 * i + e >= h.vocab_end)
-#pragma unroll
-                        for (int j = 0; j < P_NT; ++j) acc[i][j][e] = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < P_NT; ++j) {
+                for (int e = 0; e < 4; ++e) x[i][e] = sum_of(acc[i][j][e]);
             const uint32_t off = (uint32_t)(token[j] - v);
-            if (off < PM / 2 && (off & 12) == 0) {
-                float x = 0.0f;
+            if (off < PM / 2 && off % 32 < 8) {
+                float own = 0.0f;
 #pragma unroll
                 for (int i = 0; i < P_MT; ++i)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x = off == (uint32_t)(16 * i + e) ? acc[i][j][e] : x;
-                h.x_token[my_row + 16 * j] = x;
+                    for (int e = 0; e < 4; ++e) own = off == (uint32_t)along_a(i, e) ? x[i][e] : own;
+                h.x_token[my_row + j] = own;
             }
+            if (!whole)
+#pragma unroll
+                for (int i = 0; i < P_MT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[i][e] = v + along_a(i, e) < h.vocab_end ? x[i][e] : -INFINITY;
             float most = m[j];
 #pragma unroll
             for (int i = 0; i < P_MT; ++i)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) most = fmaxf(most, acc[i][j][e]);
-            const float base = most > -INFINITY ? most : 0.0f;
-            const float d0 = fmaxf((m[j] - base) * h.k, -1e4f), f = __builtin_amdgcn_exp2f(d0);
+                for (int e = 0; e < 4; e += 2) most = fmaxf(fmaxf(x[i][e], x[i][e + 1]), most);
+            const float base = most > -INFINITY ? most : 0.0f, base2 = base * h.k;
+            const bool far = fabsf(base2) >= LOGIT_FAR;
+            const float d0 = fmaxf(less_reference(m[j], h.k, base, base2, far), -1e4f), f = __builtin_amdgcn_exp2f(d0);
             if constexpr (ENTROPY) u[j] = f * (u[j] + d0 * s[j]);
             s[j] *= f;
             m[j] = most;
+            const auto take_in = [&](auto plain) {
+                constexpr bool PLAIN = decltype(plain)::value;
 #pragma unroll
-            for (int i = 0; i < P_MT; ++i)
+                for (int i = 0; i < P_MT; ++i) {
+                    float d[4], p[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float d = (acc[i][j][e] - base) * h.k, p = __builtin_amdgcn_exp2f(d);
-                    s[j] += p;
-                    if constexpr (ENTROPY) u[j] = fmaf(p, fmaxf(d, -1e4f), u[j]);     // (a logit of -infinity adds 0, not a NaN)
+                    for (int e = 0; e < 4; ++e) d[e] = !PLAIN && far ? (x[i][e] - base) * h.k : fmaf(x[i][e], h.k, -base2);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(d[e]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        s[j] += p[e];
+                        // (outside the vocabulary 0 is added, not a NaN)
+                        if constexpr (ENTROPY) u[j] = fmaf(p[e], PLAIN ? d[e] : fmaxf(d[e], -1e4f), u[j]);
+                    }
                 }
+            };
+            if (whole && !__any(far)) take_in(std::true_type{}); else take_in(std::false_type{});
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     // the four lanes and the two waves that share a row
+    // (from here on relative to the largest logit itself)
+#pragma unroll
+    for (int j = 0; j < P_NT; ++j) {
+        const float base = m[j] > -INFINITY ? m[j] : 0.0f, base2 = base * h.k;
+        const float d = fabsf(base2) >= LOGIT_FAR ? 0.0f : fmaf(-base, h.k, base2), f = __builtin_amdgcn_exp2f(d);
+        u[j] = f * (u[j] + d * s[j]);
+        s[j] *= f;
+    }
     const auto join = [&](RowSums p, RowSums q) {
         RowSums r = {fmaxf(p.m, q.m), 0.0f, 0.0f};
         const float base = r.m > -INFINITY ? r.m : 0.0f;
@@ -102,18 +144,18 @@ __global__ __launch_bounds__(P_THREADS, 2) void head_stat_kernel(const HeadStatA
         return r;
     };
     RowSums* tmp = reinterpret_cast<RowSums*>(lds);
-    bare_barrier();
+    product.end();
 #pragma unroll
     for (int j = 0; j < P_NT; ++j) {
         RowSums r = {m[j], s[j], u[j]};
 #pragma unroll
         for (int d = 16; d < 64; d <<= 1) r = join(r, RowSums{__shfl_xor(r.m, d), __shfl_xor(r.s, d), __shfl_xor(r.u, d)});
-        if (lane < 16) tmp[wave * (PN / 2) + 16 * j + lane] = r;
+        if (lane < 16) tmp[wave * (PN / 2) + 8 * lane + j] = r;
     }
     __syncthreads();
-    const int32_t row = first + threadIdx.x;
-    if (threadIdx.x < PN && row < n_rows) {
-        RowSums r = join(tmp[threadIdx.x], tmp[PN + threadIdx.x]);
+    for (int32_t i = threadIdx.x; i < PN && first + i < n_rows; i += P_THREADS) {
+        const int32_t row = first + i;
+        RowSums r = join(tmp[i], tmp[PN + i]);
         RowSums* to = h.sums + (int64_t)row * h.segments + at.second;
         if (h.add) r = join(*to, r);
         *to = r;
@@ -122,25 +164,276 @@ __global__ __launch_bounds__(P_THREADS, 2) void head_stat_kernel(const HeadStatA
 
 // A row's logits in 32 bits, for rows whose alternatives are wanted.
 template <typename T>
-__global__ __launch_bounds__(P_THREADS, 2) void head_logits_kernel(const HeadStatArgs h, float* logits, int64_t pitch) {
+__global__ __launch_bounds__(P_THREADS, 1) void head_logits_kernel(const HeadStatArgs h, float* logits, int64_t pitch) {
     __shared__ __attribute__((aligned(1024))) char lds[P_LDS];
     const TilePair at = tile_pair(by_chiplet(blockIdx.x, h.row_tiles * h.tiles), h.row_tiles, h.tiles);
     const int32_t first = at.first * PN, t = at.second;
-    const int lane = lane_id(), wave = threadIdx.x / WAVE;
     TileOfA a;
     TileOfB b;
     place_tile(a, h.w, t * PM, h.vocab_end - h.v0);
     place_tile(b, h.x, first, h.n_rows);
     f32x4 acc[P_MT][P_NT];
     product<T>(acc, a, b, h.parts, h.steps, lds);
-    const int32_t v = h.v0 + t * PM + wave / 2 * (PM / 2) + (lane >> 4) * 4, row = first + wave % 2 * (PN / 2) + (lane & 15);
+    const int32_t v = h.v0 + t * PM + place_a(), row = first + place_b();
 #pragma unroll
     for (int j = 0; j < P_NT; ++j)
-        if (row + 16 * j < h.n_rows)
+        if (row + j < h.n_rows)
 #pragma unroll
             for (int i = 0; i < P_MT; ++i)
-                if (v + 16 * i < h.vocab_end)        // (the pitch is a multiple of 4)
-                    *reinterpret_cast<f32x4*>(logits + (row + 16 * j) * pitch + v + 16 * i) = acc[i][j];
+                if (v + along_a(i, 0) < h.vocab_end)         // (the pitch is a multiple of 4)
+                    *reinterpret_cast<f32x4*>(logits + (row + j) * pitch + v + along_a(i, 0)) = acc[i][j];
+}
+
+// ---- few rows: bound by reading the weights ----
+
+struct FewArgs {
+    const void*  w;
+    int64_t      w_stride;
+    int32_t      vocab, dim;
+    const char*  x;
+    int64_t      x_pitch, x_plane;
+    int32_t      n_rows;
+    float*       logits;
+    int64_t      pitch;
+};
+template <typename W> struct FewTypes { using T = W; static constexpr int PLANES = 1; };
+template <> struct FewTypes<float> { using T = __bf16; static constexpr int PLANES = 3; };
+
+// Eight numbers as one of 16 bits each, or as three of bf16.
+template <typename W> union Eight { u32x4 q[sizeof(W) / 2]; W e[8]; };
+template <typename W>
+__device__ __forceinline__ void take_apart(const Eight<W>& from, Raw8<typename FewTypes<W>::T> (&part)[FewTypes<W>::PLANES]) {
+    if constexpr (sizeof(W) == 2) {
+        part[0].q[0] = from.q[0];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float rest = from.e[e];
+#pragma unroll
+            for (int p = 0; p < 3; ++p) part[p].e[e] = take_part<__bf16>(rest);
+        }
+    }
+}
+// sum += a b, all parts
+template <typename W>
+__device__ __forceinline__ void multiply_parts(const Raw8<typename FewTypes<W>::T> (&a)[FewTypes<W>::PLANES],
+                                               const Raw8<typename FewTypes<W>::T> (&b)[FewTypes<W>::PLANES], f32x4& sum) {
+    using M = Mfma<typename FewTypes<W>::T>;
+    using Frag = typename M::Frag;
+    const auto one = [&](int i, int j) { sum = M::sum(__builtin_bit_cast(Frag, a[i].q[0]), __builtin_bit_cast(Frag, b[j].q[0]), sum); };
+    if constexpr (sizeof(W) == 4) { one(0, 2); one(2, 0); one(1, 1); one(0, 1); one(1, 0); }
+    one(0, 0);
+}
+
+// A workgroup goes through its share of the vocabulary, TILE entries at a time: BYTES of each, and of every row, at a time come into the
+// LDS, STAGES - 1 of them ahead and on into the next tile, so that memory never waits.  A wave has a quarter of the entries and all
+// rows.  Numbers of 32 bits lie in the LDS as they are and are taken apart on the way to the matrix cores.
+// 152064 x 2048 bf16 (622 MB), us, one row: 512 bytes of 64 entries and one workgroup to a compute unit 99 (6.3 TB/s), 256 of 64 and two
+// 106, 128 of 128 and two 120; without the loads' hint not to keep the weights 119 instead of 106.  64 rows, which come out of the L2
+// once per stage: 128 bytes of 128 entries and two workgroups 151, 256 bytes of 64 entries 159; a wave of its own that asks 170.
+template <typename W, int NB, int BYTES, int W_STAGE, int GROUPS>
+__global__ __launch_bounds__(256) void head_few_kernel(const FewArgs f) {
+    constexpr int TILE = W_STAGE / BYTES, MT = TILE / 64, LANES = BYTES / 16, AT_ONCE = 256 / LANES;     // rows of BYTES that a load of all threads fills
+    constexpr int ROWS = NB * 16 < AT_ONCE ? AT_ONCE : NB * 16, STAGE = (TILE + ROWS) * BYTES, LOADS = (TILE + ROWS) / AT_ONCE;
+    constexpr int STAGES = 163840 / (GROUPS / 256) / STAGE;      // GROUPS / 256 workgroups fill a compute unit's LDS
+    constexpr int STEP = BYTES / sizeof(W), HALVES = STEP / 32;
+    static_assert(STAGES >= 2 && (STAGES - 2) * LOADS < 64 && TILE % 64 == 0, "what a wave can wait for");
+    __shared__ __attribute__((aligned(1024))) char lds[STAGES * STAGE];
+    const int lane = lane_id(), tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
+    // a share in whole 16 entries
+    const int32_t units = (f.vocab + 15) / 16;
+    const int32_t first = (int32_t)((int64_t)units * blockIdx.x / gridDim.x) * 16;
+    const int32_t end = min((int32_t)((int64_t)units * (blockIdx.x + 1) / gridDim.x) * 16, f.vocab);
+    const int32_t tiles = (end - first + TILE - 1) / TILE, steps = f.dim / STEP;
+    if (tiles <= 0) return;
+    const int place = tid / LANES, piece = tid % LANES ^ (place & 7);
+    static_assert(AT_ONCE % 8 == 0, "a thread's pieces are the same in all its rows");
+    const char* const w0 = static_cast<const char*>(f.w) + first * f.w_stride * (int64_t)sizeof(W);
+    int64_t w_at[TILE / AT_ONCE], x_at[ROWS / AT_ONCE];
+    int32_t asked_tile = 0, asked_step = 0, to = 0;
+    const auto place_entries = [&](int32_t tile) {
+#pragma unroll
+        for (int j = 0; j < TILE / AT_ONCE; ++j)
+            w_at[j] = min(tile * TILE + place + AT_ONCE * j, end - first - 1) * f.w_stride * (int64_t)sizeof(W) + 16 * piece;
+    };
+    place_entries(0);
+#pragma unroll
+    for (int j = 0; j < ROWS / AT_ONCE; ++j) x_at[j] = min(place + AT_ONCE * j, f.n_rows - 1) * f.x_pitch + 16 * piece;
+    const auto ask = [&] {
+        char* s = lds + to * STAGE + wave * 1024;
+#pragma unroll
+        for (int j = 0; j < TILE / AT_ONCE; ++j) load_to_lds<true>(w0 + w_at[j] + asked_step * BYTES, s + j * 4096);
+#pragma unroll
+        for (int j = 0; j < ROWS / AT_ONCE; ++j) load_to_lds(f.x + x_at[j] + asked_step * BYTES, s + TILE * BYTES + j * 4096);
+        to = to + 1 == STAGES ? 0 : to + 1;
+        if (++asked_step == steps) {             // (behind the last tile: that one again, for nobody)
+            asked_step = 0;
+            if (asked_tile + 1 < tiles) place_entries(++asked_tile);
+        }
+    };
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) ask();
+    const int row = lane & 15;
+    const auto read = [&](const char* rows, int first_piece, Eight<W>& e) {          // neighbouring pieces of a row
+#pragma unroll
+        for (int q = 0; q < (int)sizeof(W) / 2; ++q)
+            e.q[q] = *reinterpret_cast<const u32x4*>(rows + row * BYTES + ((first_piece + q) ^ (row & 7)) * 16);
+    };
+    int32_t now = 0;
+    for (int32_t tile = 0; tile < tiles; ++tile) {
+        f32x4 acc[MT][NB] = {};
+        for (int32_t k = 0; k < steps; ++k) {
+            wait_loads<(STAGES - 2) * LOADS>();
+            bare_barrier();
+            ask();
+            const char* stage = lds + now * STAGE;
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h) {
+                const int at = h * (int)(2 * sizeof(W)) + (lane >> 4) * (int)(sizeof(W) / 2);
+                Raw8<typename FewTypes<W>::T> a[MT][FewTypes<W>::PLANES], b[NB][FewTypes<W>::PLANES];
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    Eight<W> e;
+                    read(stage + (wave * 16 * MT + 16 * i) * BYTES, at, e);
+                    take_apart<W>(e, a[i]);
+                }
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    Eight<W> e;
+                    read(stage + (TILE + 16 * j) * BYTES, at, e);
+                    take_apart<W>(e, b[j]);
+                }
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NB; ++j) multiply_parts<W>(a[i], b[j], acc[i][j]);
+            }
+            now = now + 1 == STAGES ? 0 : now + 1;
+        }
+        const int32_t v = first + tile * TILE + wave * 16 * MT + (lane >> 4) * 4;
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+            if (16 * j + row < f.n_rows)
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+                    if (v + 16 * i < end)        // (the pitch is a multiple of 4)
+                        *reinterpret_cast<f32x4*>(f.logits + (16 * j + row) * f.pitch + v + 16 * i) = acc[i][j];
+    }
+    wait_loads<0>();
+}
+
+// The same for weights and rows that lie anyhow: a wave per 16 MT entries and 16 NB rows, the weights straight into the places that the
+// matrix cores want, AHEAD steps of 32 elements before they are multiplied; the rows, laid out with k_pad columns, 0 behind the last
+// one, come out of the L2.
+template <typename W, int MT, int NB, int AHEAD>
+__global__ __launch_bounds__(256) void head_few_any_kernel(const FewArgs f) {
+    using T = typename FewTypes<W>::T;
+    constexpr int PLANES = FewTypes<W>::PLANES;
+    using Piece = std::conditional_t<sizeof(W) == 4, u32x4_a4, u32x4_a2>;
+    const int lane = lane_id();
+    const int32_t v0 = (blockIdx.x * 4 + threadIdx.x / WAVE) * 16 * MT;
+    if (v0 >= f.vocab) return;
+    const W* w[MT];
+    const char* x[NB];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) w[i] = static_cast<const W*>(f.w) + min(v0 + 16 * i + (lane & 15), f.vocab - 1) * f.w_stride + (lane >> 4) * 8;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) x[j] = f.x + min(16 * j + (lane & 15), f.n_rows - 1) * f.x_pitch + (lane >> 4) * 16;
+    f32x4 acc[MT][NB] = {};
+    struct Steps { Eight<W> a[AHEAD][MT]; Raw8<T> b[AHEAD][NB][PLANES]; } first, second;
+    const int32_t steps = f.dim / 32;
+    const auto ask = [&](Steps& s, int32_t k) {              // (behind the last step: that one again)
+#pragma unroll
+        for (int h = 0; h < AHEAD; ++h) {
+            const int32_t at = min(k + h, steps - 1) * 32;
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int q = 0; q < (int)sizeof(W) / 2; ++q)
+                    s.a[h][i].q[q] = *(reinterpret_cast<const Piece*>(w[i] + at) + q);
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) s.b[h][j][p].q[0] = *reinterpret_cast<const u32x4*>(x[j] + p * f.x_plane + at * 2);
+        }
+    };
+    const auto multiply = [&](const Eight<W> (&a)[MT], const Raw8<T> (&b)[NB][PLANES]) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            Raw8<T> part[PLANES];
+            take_apart<W>(a[i], part);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) multiply_parts<W>(part, b[j], acc[i][j]);
+        }
+    };
+    const auto multiply_all = [&](const Steps& s, int32_t k) {
+#pragma unroll
+        for (int h = 0; h < AHEAD; ++h)
+            if (k + h < steps) multiply(s.a[h], s.b[h]);
+    };
+    if (steps > 0) ask(first, 0);
+    for (int32_t k = 0; k < steps; k += 2 * AHEAD) {
+        ask(second, k + AHEAD);
+        multiply_all(first, k);
+        if (k + AHEAD >= steps) break;
+        ask(first, k + 2 * AHEAD);
+        multiply_all(second, k + AHEAD);
+    }
+    if (steps * 32 < f.dim) {                    // what is left, an element at a time
+        Eight<W> a[MT];
+        Raw8<T> b[NB][PLANES];
+        const int32_t left = f.dim - steps * 32 - (lane >> 4) * 8;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) a[i].e[e] = e < left ? w[i][steps * 32 + e] : (W)0.0f;
+#pragma unroll
+        for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) b[j][p].q[0] = *reinterpret_cast<const u32x4*>(x[j] + p * f.x_plane + steps * 64);
+        multiply(a, b);
+    }
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+        if (16 * j + (lane & 15) < f.n_rows)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+                if (v0 + 16 * i + (lane >> 4) * 4 < f.vocab)         // (the pitch is a multiple of 4)
+                    *reinterpret_cast<f32x4*>(f.logits + (16 * j + (lane & 15)) * f.pitch + v0 + 16 * i + (lane >> 4) * 4) = acc[i][j];
+}
+
+constexpr int64_t FEW_ROWS = 64;
+// Rows that are read 128 bytes at a time.
+static bool in_whole_steps(const dc_matrix& m) {
+    const int64_t each = m.type == DC_F32 ? 4 : 2;
+    return reinterpret_cast<uintptr_t>(m.d_data) % 16 == 0 && m.row_stride * each % 16 == 0 && m.n_cols * each % 128 == 0;
+}
+template <int BYTES, int STAGE, int GROUPS, typename F>
+static void launch_with(F&& f) {
+    f(std::integral_constant<int, BYTES>{}, std::integral_constant<int, STAGE>{}, std::integral_constant<int, GROUPS>{});
+}
+static hipError_t launch_few(const FewArgs& f, int32_t type, bool any, hipStream_t st) {
+    return with_type(type, [&](auto el) {
+        using W = typename decltype(el)::type;
+        using std::integral_constant;
+        constexpr bool F32 = std::is_same_v<W, float>;
+        const auto go = [&](auto mt, auto nb, auto ahead) {
+            constexpr int MT = decltype(mt)::value, NB = decltype(nb)::value, AHEAD = decltype(ahead)::value;
+            if (any) head_few_any_kernel<W, MT, NB, AHEAD><<<(unsigned)((f.vocab + 64 * MT - 1) / (64 * MT)), 256, 0, st>>>(f);
+            else {
+                const auto launch = [&](auto bytes, auto stage, auto groups) {
+                    constexpr int GROUPS = decltype(groups)::value;
+                    head_few_kernel<W, NB, decltype(bytes)::value, decltype(stage)::value, GROUPS><<<(unsigned)std::min((f.vocab + 15) / 16, GROUPS), 256, 0, st>>>(f);
+                };
+                if (NB < 4 && f.dim * sizeof(W) % 512 == 0) launch_with<512, 32768, 256>(launch);
+                else launch_with<128, 16384, 512>(launch);
+            }
+        };
+        if (f.n_rows <= 16) go(integral_constant<int, 1>{}, integral_constant<int, 1>{}, integral_constant<int, F32 ? 2 : 8>{});
+        else if (f.n_rows <= 32) go(integral_constant<int, F32 ? 1 : 2>{}, integral_constant<int, 2>{}, integral_constant<int, 2>{});
+        else go(integral_constant<int, 2>{}, integral_constant<int, 4>{}, integral_constant<int, F32 ? 1 : 2>{});
+        return hipGetLastError();
+    });
 }
 
 // A wave per row: its segments' sums as one, and the results.
@@ -170,6 +463,7 @@ __global__ __launch_bounds__(256) void head_join_kernel(const LogprobArgs a, con
         }
         all.s = wave_sum(all.s);
         all.u = wave_sum(all.u);
+        if (!(fabsf(all.u) < INFINITY)) all.s = NAN;         // (an infinite logit)
         if (lane == 0) {
             const int32_t token = a.token ? a.token[r] : 0;
             const bool in = token >= 0 && token < a.vocab;
@@ -181,7 +475,7 @@ __global__ __launch_bounds__(256) void head_join_kernel(const LogprobArgs a, con
 
 // How the vocabulary is shared out over workgroups: `segments` to each tile of rows, so that two to a compute unit finish at
 // about the same time.
-constexpr int32_t HEAD_SLOTS = 512, HEAD_MOST_BLOCKS = 4 * HEAD_SLOTS;
+constexpr int32_t HEAD_SLOTS = 256, HEAD_MOST_BLOCKS = 4 * HEAD_SLOTS;
 static int32_t segments_of(int64_t row_tiles, int32_t tiles) {
     int32_t best = 1;
     int64_t least = -1;
@@ -192,7 +486,7 @@ static int32_t segments_of(int64_t row_tiles, int32_t tiles) {
     return best;
 }
 
-constexpr int64_t HEAD_TOP_ROWS = PN;            // rows whose logits are held at once
+constexpr int64_t HEAD_TOP_ROWS = PN;            // rows whose logits are held at once, where alternatives are wanted
 constexpr int64_t HEAD_PIECE_BYTES = 256LL << 20;    // of weights laid out at once
 static int32_t weight_piece(const HeadShape& sh, const dc_matrix& w) {
     if (!sh.copy_weight) return (int32_t)w.n_rows;
@@ -212,7 +506,7 @@ struct HeadWs {
     size_t   bytes;
 };
 }
-// Areas for rows and sums grow with the rows; which of the two ways needs which does not matter for the layout.
+// Up to FEW_ROWS rows, and HEAD_TOP_ROWS at a time with alternatives, go through their logits, others straight to sums.
 static HeadWs carve(void* base, const dc_matrix& hidden, const dc_matrix& weight, int32_t n_top) {
     HeadWs w = {};
     const HeadShape sh = head_shape(hidden, weight, true);
@@ -223,13 +517,14 @@ static HeadWs carve(void* base, const dc_matrix& hidden, const dc_matrix& weight
         return p;
     };
     const int64_t rows = hidden.n_rows, planes = hidden.type == DC_F32 ? 3 : 1;
+    const bool few = rows <= FEW_ROWS;
     w.hidden_plane = rows * sh.k_pad * 2;
-    w.hidden = take(sh.copy_hidden ? planes * w.hidden_plane : 0);
+    w.hidden = take(sh.copy_hidden || few ? planes * w.hidden_plane : 0);
     w.piece = weight_piece(sh, weight);
     w.weight_plane = (int64_t)w.piece * sh.k_pad * 2;
-    w.weight = take(sh.copy_weight ? planes * w.weight_plane : 0);
+    w.weight = take(sh.copy_weight && !few ? planes * w.weight_plane : 0);
     w.pitch = whole(weight.n_rows, 4);
-    if (n_top > 0) {
+    if (few || n_top > 0) {
         w.logits = reinterpret_cast<float*>(take(std::min(rows, HEAD_TOP_ROWS) * w.pitch * 4));
         w.logprob = take((int64_t)logprob_workspace_bytes(std::min(rows, HEAD_TOP_ROWS), (int32_t)weight.n_rows, DC_F32, n_top));
     } else {
@@ -249,7 +544,10 @@ size_t head_workspace_need(const dc_matrix& hidden, const dc_matrix& weight, int
     return hidden.n_rows > 0 ? carve(nullptr, hidden, weight, n_top).bytes : 0;
 }
 size_t head_workspace_bytes(const dc_matrix& hidden, const dc_matrix& weight, int32_t n_top) {
-    return std::max(head_workspace_need(hidden, weight, 0), head_workspace_need(hidden, weight, n_top));
+    dc_matrix fewer = hidden;
+    fewer.n_rows = std::min(hidden.n_rows, FEW_ROWS);
+    return std::max(std::max(head_workspace_need(hidden, weight, 0), head_workspace_need(hidden, weight, n_top)),
+                    std::max(head_workspace_need(fewer, weight, 0), head_workspace_need(fewer, weight, n_top)));
 }
 
 hipError_t launch_head(const HeadArgs& a, void* d_ws, hipStream_t st) {
@@ -259,6 +557,22 @@ hipError_t launch_head(const HeadArgs& a, void* d_ws, hipStream_t st) {
     const HeadWs w = carve(d_ws, a.hidden, a.weight, a.n_top);
     const HeadShape sh = head_shape(a.hidden, a.weight, true);
     hipError_t e = hipSuccess;
+    LogprobArgs out = {nullptr, w.pitch, rows, vocab, a.n_top, a.inv_t, a.token, a.mask, a.logprob, a.stat, a.entropy,
+                       a.top_token, a.top_logprob, a.status};
+    if (rows <= FEW_ROWS) {
+        const bool any = !in_whole_steps(a.hidden) || !in_whole_steps(a.weight);
+        FewArgs f = {a.weight.d_data, a.weight.row_stride, vocab, (int32_t)a.hidden.n_cols, static_cast<const char*>(a.hidden.d_data),
+                     a.hidden.row_stride * (type == DC_F32 ? 4 : 2), 0, (int32_t)rows, w.logits, w.pitch};
+        if (any) {
+            e = launch_lay_rows(a.hidden, 0, rows, nullptr, nullptr, sh.k_pad, w.hidden, w.hidden_plane, st);
+            f.x = w.hidden;
+            f.x_pitch = sh.k_pad * 2;
+            f.x_plane = w.hidden_plane;
+        }
+        if (e == hipSuccess) e = launch_few(f, type, any, st);
+        out.x = w.logits;
+        return e == hipSuccess ? launch_logprob(out, DC_F32, w.logprob, st) : e;
+    }
     const bool live = a.n_top == 0 && a.mask;
     if (live) e = launch_live_rows(a.mask, nullptr, nullptr, rows, w.live, st);
     HeadStatArgs h = {};
@@ -279,8 +593,6 @@ hipError_t launch_head(const HeadArgs& a, void* d_ws, hipStream_t st) {
     } else {
         h.x = Operand{static_cast<const char*>(a.hidden.d_data), a.hidden.row_stride * 2, h.list};
     }
-    LogprobArgs out = {nullptr, w.pitch, rows, vocab, a.n_top, a.inv_t, a.token, a.mask, a.logprob, a.stat, a.entropy,
-                       a.top_token, a.top_logprob, a.status};
     for (int64_t r0 = 0; r0 < rows && e == hipSuccess; r0 += HEAD_TOP_ROWS) {
         if (a.n_top > 0) {                       // so many rows at a time
             h.n_rows = (int32_t)std::min(HEAD_TOP_ROWS, rows - r0);

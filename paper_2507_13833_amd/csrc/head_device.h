@@ -7,26 +7,47 @@
 namespace dc {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));         // 16 bytes wherever a 16-bit element may lie
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // D[i, j] += sum_k A[i, k] B[j, k] for 16 x 16 places and 32 k.  Lane l brings A[l % 16, 8 (l / 16) ..] and B likewise, and holds
-// D[4 (l / 16) + 0..3, l % 16].
+// D[4 (l / 16) + 0..3, l % 16].  The sums stay in the accumulation registers, which the compiler would share out otherwise and copy
+// from and to in the loop (add; sum is the ordinary way); it does not know these instructions for what they are, so settle_sums() keeps their distance from
+// ordinary ones that write or read the sums.
 template <typename T> struct Mfma;
 template <> struct Mfma<__bf16> {
     using Frag = bf16x8;
-    static __device__ __forceinline__ f32x4 add(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ void add(const Frag& a, const Frag& b, f32x4& c) {
+        asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+    }
+    static __device__ __forceinline__ f32x4 sum(const Frag& a, const Frag& b, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 };
 template <> struct Mfma<_Float16> {
     using Frag = f16x8;
-    static __device__ __forceinline__ f32x4 add(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+    static __device__ __forceinline__ void add(const Frag& a, const Frag& b, f32x4& c) {
+        asm volatile("v_mfma_f32_16x16x32_f16 %0, %1, %2, %0" : "+a"(c) : "v"(a), "v"(b));
+    }
+    static __device__ __forceinline__ f32x4 sum(const Frag& a, const Frag& b, const f32x4& c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 };
+// A sum out of its register, read where this stands and not kept.
+__device__ __forceinline__ float sum_of(float c) {
+    float v;
+    asm volatile("v_accvgpr_read_b32 %0, %1" : "=v"(v) : "a"(c));
+    return v;
+}
+// 32 cycles: more than any of the distances (18 at most, behind the longest of these instructions).
+__device__ __forceinline__ void settle_sums() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
 
-// A workgroup makes PM rows of A times PN rows of B: four waves, two by two, 128 x 64 each.
-constexpr int PM = 256, PN = 128, PK = 32, P_THREADS = 256;
-constexpr int P_STAGES = 3, P_STAGE = (PM + PN) * PK * 2, P_LDS = P_STAGES * P_STAGE;
-constexpr int P_MT = PM / 32, P_NT = PN / 32;            // 16 x 16 places of a wave
-constexpr int P_MOST_PARTS = 6;
+// A workgroup makes PM rows of A times PN rows of B: four waves, two by two, 128 x 128 each, one to a SIMD, with all its 256 sums of a
+// lane in registers.
+constexpr int PM = 256, PN = 256, PK = 64, P_THREADS = 256;
+constexpr int P_STAGE = (PM + PN) * PK * 2, P_LDS = 2 * P_STAGE;
+constexpr int P_MT = PM / 2 / 16, P_NT = PN / 2 / 16;    // 16 x 16 places of a wave
 
 struct Operand {
     const char*    p;               // 16-byte aligned
@@ -34,14 +55,17 @@ struct Operand {
     const int32_t* list;            // which rows, by their numbers (the last one's end below 4 GB then); NULL: as they lie
 };
 constexpr int64_t P_MOST_PITCH = 1 << 23;
-// The sum goes over parts: pairs of places, in bytes from the operands' starts, with `steps` times PK elements each.
-struct Parts { int32_t n; int64_t a[P_MOST_PARTS], b[P_MOST_PARTS]; };
+// The sum goes over n parts of `steps` times PK elements each: part i multiplies plane (a >> 2 i) % 4 of A, planes a_plane bytes apart,
+// by plane (b >> 2 i) % 4 of B.
+struct Parts { int32_t n; uint32_t a, b; int64_t a_plane, b_plane; };
 
 typedef const __attribute__((address_space(1))) void GlobalVoid;
 typedef __attribute__((address_space(3))) void LdsVoid;
 // 16 bytes a lane from memory to the LDS, lane after lane from `to` on (the same in every lane).
+// STREAM: not kept in the caches.
+template <bool STREAM = false>
 __device__ __forceinline__ void load_to_lds(const char* from, char* to) {
-    __builtin_amdgcn_global_load_lds((GlobalVoid*)from, (LdsVoid*)to, 16, 0, 0);
+    __builtin_amdgcn_global_load_lds((GlobalVoid*)from, (LdsVoid*)to, 16, 0, STREAM ? 2 : 0);
 }
 // Waits until at most `N` of the wave's loads and stores are under way, and all its LDS reads are done.
 template <int N>
@@ -56,73 +80,170 @@ __device__ __forceinline__ void bare_barrier() {
     asm volatile("" ::: "memory");
 }
 
-// What of a tile a thread loads: rows tid / 4 + 64 j, 16 bytes each.  The four 16-byte pieces of a row's 64 bytes lie in the LDS at
-// piece ^ (row / 2 % 4), so that eight rows' same piece fills all banks.
-struct TileOfA { const char* base; uint32_t at[PM / 64]; };
-struct TileOfB { const char* base; uint32_t at[PN / 64]; };
-template <typename Tile>
-__device__ __forceinline__ void place_tile(Tile& t, const Operand& o, int32_t first, int32_t n_rows) {
-    const int row = threadIdx.x / 4, piece = (threadIdx.x & 3) ^ (row >> 1 & 3);
+// What of a tile a thread loads: the rows that lie at tid / 8 + 32 j in the LDS, 16 bytes each.  The eight 16-byte pieces of a row's
+// 128 bytes lie there at piece ^ (place % 8), so that eight rows' same piece fills all banks.  Rows of the tile are dealt out to the
+// places so that a lane comes to hold neighbours, which its stores want: of each 128 rows of A, place 16 i + p takes row
+// 32 (i / 2) + 8 (p / 4) + 4 (i % 2) + p % 4; of each 128 of B, place 16 j + q row 8 q + j.
+template <int ROWS> struct Tile { const char* base; uint32_t at[ROWS / 32]; };
+struct TileOfA : Tile<PM> {
+    static __device__ __forceinline__ int row_at(int x) { return (x & ~31) + (x >> 2 & 3) * 8 + (x >> 4 & 1) * 4 + (x & 3); }
+};
+struct TileOfB : Tile<PN> {
+    static __device__ __forceinline__ int row_at(int x) { return (x & ~127) + (x & 15) * 8 + (x >> 4 & 7); }
+};
+template <typename T>
+__device__ __forceinline__ void place_tile(T& t, const Operand& o, int32_t first, int32_t n_rows) {
+    const int place = threadIdx.x / 8, piece = (threadIdx.x ^ place) & 7;
     t.base = o.list ? o.p : o.p + first * o.pitch;
 #pragma unroll
     for (int j = 0; j < (int)(sizeof(t.at) / 4); ++j) {
-        const int32_t r = min(first + row + 64 * j, n_rows - 1);         // (behind the last row: that one again)
+        const int32_t r = min(first + T::row_at(place + 32 * j), n_rows - 1);        // (behind the last row: that one again)
         t.at[j] = (uint32_t)(o.list ? o.list[r] : r - first) * (uint32_t)o.pitch + 16 * piece;
     }
 }
 
-// acc = the tile's sums (0 without steps).  Three stages of PK elements: while one is multiplied the next two are on their way.
+// Where a lane's rows begin in a tile of A and of B: acc[i][j][e] is of A's row place_a() + along_a(i, e) and B's place_b() + j.
+__device__ __forceinline__ int place_a() { return threadIdx.x / (2 * WAVE) * (PM / 2) + (lane_id() >> 4) * 8; }
+__device__ __forceinline__ int place_b() { return threadIdx.x / WAVE % 2 * (PN / 2) + (lane_id() & 15) * 8; }
+constexpr __device__ __host__ int along_a(int i, int e) { return i / 2 * 32 + i % 2 * 4 + e; }
+
+// The workgroup's tiles one after the other.  Two stages of PK elements lie in the LDS, each multiplied in two halves; a half's numbers
+// are read into registers while the half before is multiplied.  Once the second half of a stage is in registers its place is free:
+// the stage after next is asked for there, a whole stage ahead and on into the next tile.  next() makes a and b that next tile (or
+// leaves them: what is asked for then is not used).  Steps and parts are the same for all tiles, and there is at least one of each.
 template <typename T>
-__device__ __forceinline__ void product(f32x4 (&acc)[P_MT][P_NT], const TileOfA& a, const TileOfB& b, const Parts& parts, int32_t steps,
-                                        char* lds) {
+struct Product {
     using Frag = typename Mfma<T>::Frag;
-    const int tid = threadIdx.x, lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
-#pragma unroll
-    for (int i = 0; i < P_MT; ++i)
-#pragma unroll
-        for (int j = 0; j < P_NT; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
-    const int32_t all = steps * parts.n;
-    if (all <= 0) return;
-    int32_t part = 0, left = steps;
-    const char *pa = a.base + parts.a[0], *pb = b.base + parts.b[0];
-    char* to = lds + wave * 1024;
-    const auto ask = [&](char* stage) {
-#pragma unroll
-        for (int j = 0; j < PM / 64; ++j) load_to_lds(pa + a.at[j], stage + j * 4096);
-#pragma unroll
-        for (int j = 0; j < PN / 64; ++j) load_to_lds(pb + b.at[j], stage + PM * 64 + j * 4096);
+    TileOfA     a;
+    TileOfB     b;
+    Parts       parts;
+    int32_t     steps, part, left, stage;
+    const char *pa, *pb;
+    char*       to;
+    const char *from_a, *from_b;
+    int         at_half[2];
+    Frag        fa[2][P_MT], fb[2][P_NT];
+
+    __device__ __forceinline__ void start_of(int32_t i) {
+        part = i;
+        left = steps;
+        pa = a.base + (parts.a >> 2 * i & 3) * parts.a_plane;
+        pb = b.base + (parts.b >> 2 * i & 3) * parts.b_plane;
+    }
+    __device__ __forceinline__ void ask_a(int j) { load_to_lds(pa + a.at[j], to + (stage & 1) * P_STAGE + j * 4096); }
+    __device__ __forceinline__ void ask_b(int j) { load_to_lds(pb + b.at[j], to + (stage & 1) * P_STAGE + PM * 128 + j * 4096); }
+    template <typename Next>
+    __device__ __forceinline__ void asked(Next&& next) {
         pa += PK * 2;
         pb += PK * 2;
-        if (--left == 0 && ++part < parts.n) {
-            pa = a.base + parts.a[part];
-            pb = b.base + parts.b[part];
-            left = steps;
+        ++stage;
+        if (--left == 0) {
+            if (part + 1 < parts.n) {
+                start_of(part + 1);
+            } else {
+                next();
+                start_of(0);
+            }
         }
-    };
-    bare_barrier();                              // (the LDS may still be read)
-    ask(to);
-    if (all > 1) ask(to + P_STAGE);
-    const int row = lane & 15, piece = (lane >> 4) ^ (row >> 1 & 3);
-    const char* from_a = lds + (wave / 2 * (PM / 2) + row) * 64 + piece * 16;
-    const char* from_b = lds + PM * 64 + (wave % 2 * (PN / 2) + row) * 64 + piece * 16;
-    int32_t now = 0, then = 2 * P_STAGE;
-    for (int32_t k = 0; k < all; ++k) {
-        if (k + 1 < all) wait_loads<(PM + PN) / 64>(); else wait_loads<0>();
+    }
+    __device__ __forceinline__ void read_a(int32_t s, int h, int i) {
+        fa[h][i] = *reinterpret_cast<const Frag*>(from_a + (s & 1) * P_STAGE + at_half[h] + i * 2048);
+    }
+    __device__ __forceinline__ void read_b(int32_t s, int h, int j) {
+        fb[h][j] = *reinterpret_cast<const Frag*>(from_b + (s & 1) * P_STAGE + at_half[h] + j * 2048);
+    }
+
+    // a, b, parts and steps are set
+    template <typename Next>
+    __device__ __forceinline__ void begin(char* lds, Next&& next) {
+        const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+        const int row = lane & 15, piece = (lane >> 4) ^ (row & 7);
+        to = lds + wave * 1024;
+        from_a = lds + (wave / 2 * (PM / 2) + row) * 128;
+        from_b = lds + PM * 128 + (wave % 2 * (PN / 2) + row) * 128;
+        at_half[0] = piece * 16;
+        at_half[1] = (piece ^ 4) * 16;
+        stage = 0;
+        start_of(0);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int j = 0; j < PM / 32; ++j) ask_a(j);
+#pragma unroll
+            for (int j = 0; j < PN / 32; ++j) ask_b(j);
+            asked(next);
+        }
+        wait_loads<(PM + PN) / 32>();
         bare_barrier();
-        if (k + 2 < all) ask(to + then);
-        Frag fa[P_MT], fb[P_NT];
 #pragma unroll
-        for (int j = 0; j < P_NT; ++j) fb[j] = *reinterpret_cast<const Frag*>(from_b + now + j * 1024);
+        for (int i = 0; i < P_MT; ++i) read_a(0, 0, i);
 #pragma unroll
-        for (int i = 0; i < P_MT; ++i) fa[i] = *reinterpret_cast<const Frag*>(from_a + now + i * 1024);
+        for (int j = 0; j < P_NT; ++j) read_b(0, 0, j);
+    }
+
+    // acc = the sums of the tile whose turn it is
+    template <typename Next>
+    __device__ __forceinline__ void tile(f32x4 (&acc)[P_MT][P_NT], Next&& next) {
+        static_assert(P_MT == 8 && P_NT == 8, "four products to a read");
 #pragma unroll
         for (int i = 0; i < P_MT; ++i)
 #pragma unroll
-            for (int j = 0; j < P_NT; ++j) acc[i][j] = Mfma<T>::add(fa[i], fb[j], acc[i][j]);
-        now = now == 2 * P_STAGE ? 0 : now + P_STAGE;
-        then = then == 2 * P_STAGE ? 0 : then + P_STAGE;
+            for (int j = 0; j < P_NT; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+        settle_sums();
+        const int32_t all = steps * parts.n, first = stage - 2;
+        for (int32_t s = first; s < first + all; ++s) {
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) Mfma<T>::add(fa[0][q / 2], fb[0][q % 2 * 4 + e], acc[q / 2][q % 2 * 4 + e]);
+                // (the first products of the next half want all of B and the first of A)
+                if (q < 8) read_b(s, 1, q); else read_a(s, 1, q - 8);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            wait_loads<0>();
+            bare_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) Mfma<T>::add(fa[1][q / 2], fb[1][q % 2 * 4 + e], acc[q / 2][q % 2 * 4 + e]);
+                if (q < 8) ask_a(q); else ask_b(q - 8);
+                if (q < 8) read_b(s + 1, 0, q); else read_a(s + 1, 0, q - 8);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            asked(next);
+        }
+        settle_sums();
     }
-    wait_loads<0>();
+
+    // the LDS is free again
+    __device__ __forceinline__ void end() {
+        wait_loads<0>();
+        bare_barrier();
+    }
+};
+// One tile alone, already placed.
+template <typename T>
+__device__ __forceinline__ void product(f32x4 (&acc)[P_MT][P_NT], const TileOfA& a, const TileOfB& b, const Parts& parts, int32_t steps,
+                                        char* lds) {
+    if (steps <= 0) {
+#pragma unroll
+        for (int i = 0; i < P_MT; ++i)
+#pragma unroll
+            for (int j = 0; j < P_NT; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+        return;
+    }
+    Product<T> p;
+    p.a = a;
+    p.b = b;
+    p.parts = parts;
+    p.steps = steps;
+    const auto next = [] {};
+    p.begin(lds, next);
+    p.tile(acc, next);
+    p.end();
 }
 
 // Workgroups are handed to the eight chiplets in turn.  The n-th of those that share a chiplet (and its L2) come to lie side by side.

