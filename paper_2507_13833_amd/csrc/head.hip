@@ -14,7 +14,7 @@ namespace dc {
 struct HeadStatArgs {
     Operand        w, x;
     Parts          parts;
-    int32_t        steps, v0, vocab_end, tiles;      // vocabulary entries v0 .. vocab_end - 1 are rows 0 .. of w; tiles: of PM
+    int32_t        steps, v0, vocab_end, tiles;      // vocabulary entries v0 .. vocab_end - 1 are rows 0 .. of w; tiles: of P_SIDE
     int32_t        row_tiles, segments, n_rows;
     const int32_t* count;           // NULL: n_rows
     const int32_t* list;            // of the rows, for their tokens; NULL: as they lie
@@ -36,66 +36,67 @@ __device__ __forceinline__ float less_reference(float m, float k, float base, fl
     return was_far ? fmaf(m, k, -base2) : m2 - base2;
 }
 
-template <typename T, bool ENTROPY>
-__global__ __launch_bounds__(P_THREADS, 1) void head_stat_kernel(const HeadStatArgs h) {
-    __shared__ __attribute__((aligned(1024))) char lds[P_LDS];
+template <typename T, bool ENTROPY, int Q>
+__global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_stat_kernel(const HeadStatArgs h) {
+    constexpr int SIDE = P_SIDE<Q>;
+    __shared__ __attribute__((aligned(1024))) char lds[P_LDS<Q>];
     const int32_t blocks = h.row_tiles * h.segments;
     const TilePair at = tile_pair(by_chiplet(blockIdx.x, blocks), h.row_tiles, h.segments);
-    const int32_t n_rows = h.count ? *h.count : h.n_rows, first = at.first * PN;
+    const int32_t n_rows = h.count ? *h.count : h.n_rows, first = at.first * SIDE;
     if (first >= n_rows) return;
     const int lane = lane_id(), wave = threadIdx.x / WAVE;
-    const int32_t my_row = first + place_b();        // and the seven behind it
-    int32_t token[P_NT];
-    float m[P_NT], s[P_NT], u[P_NT];
+    const int32_t my_row = first + place_b<Q>();        // and the Q - 1 behind it
+    int32_t token[Q];
+    float m[Q], s[Q], u[Q];
 #pragma unroll
-    for (int j = 0; j < P_NT; ++j) {
+    for (int j = 0; j < Q; ++j) {
         const int32_t r = my_row + j;
         token[j] = -1;
         if (h.token && r < n_rows) token[j] = h.token[h.list ? h.list[r] : r];
         m[j] = -INFINITY;
         s[j] = u[j] = 0.0f;
     }
-    Product<T> product;
+    Product<T, Q> product;
     product.parts = h.parts;
     product.steps = h.steps;
     int32_t asked = at.second;                   // the tile whose numbers are on their way
     const auto next = [&] {
-        if (asked + h.segments < h.tiles) place_tile(product.a, h.w, (asked += h.segments) * PM, h.vocab_end - h.v0);
+        if (asked + h.segments < h.tiles) place_tile(product.a, h.w, (asked += h.segments) * SIDE, h.vocab_end - h.v0);
     };
     if (asked < h.tiles) {                       // (the last piece of a vocabulary may have fewer tiles than there are segments)
-        place_tile(product.a, h.w, asked * PM, h.vocab_end - h.v0);
+        place_tile(product.a, h.w, asked * SIDE, h.vocab_end - h.v0);
         place_tile(product.b, h.x, first, n_rows);
         product.begin(lds, next);
     }
     for (int32_t t = at.second; t < h.tiles; t += h.segments) {
-        f32x4 acc[P_MT][P_NT];
+        f32x4 acc[Q][Q];
         product.tile(acc, next);
-        const int32_t v = h.v0 + t * PM + place_a();       // of acc[0][.][0]
-        const bool whole = h.v0 + (t + 1) * PM <= h.vocab_end;
+        const int32_t v = h.v0 + t * SIDE + place_a<Q>();       // of acc[0][.][0]
+        const bool whole = h.v0 + (t + 1) * SIDE <= h.vocab_end;
 #pragma unroll
-        for (int j = 0; j < P_NT; ++j) {             // a row at a time
-            float x[P_MT][4];
+        for (int j = 0; j < Q; ++j) {             // a row at a time
+            float x[Q][4];
 #pragma unroll
-            for (int i = 0; i < P_MT; ++i)
+            for (int i = 0; i < Q; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) x[i][e] = sum_of(acc[i][j][e]);
             const uint32_t off = (uint32_t)(token[j] - v);
-            if (off < PM / 2 && off % 32 < 8) {
+            if (off < SIDE / 2 && off % 32 < 8) {
                 float own = 0.0f;
 #pragma unroll
-                for (int i = 0; i < P_MT; ++i)
+                for (int i = 0; i < Q; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) own = off == (uint32_t)along_a(i, e) ? x[i][e] : own;
                 h.x_token[my_row + j] = own;
             }
             if (!whole)
 #pragma unroll
-                for (int i = 0; i < P_MT; ++i)
+                for (int i = 0; i < Q; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x[i][e] = v + along_a(i, e) < h.vocab_end ? x[i][e] : -INFINITY;
             float most = m[j];
 #pragma unroll
-            for (int i = 0; i < P_MT; ++i)
+            for (int i = 0; i < Q; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; e += 2) most = fmaxf(fmaxf(x[i][e], x[i][e + 1]), most);
             const float base = most > -INFINITY ? most : 0.0f, base2 = base * h.k;
@@ -107,7 +108,7 @@ __global__ __launch_bounds__(P_THREADS, 1) void head_stat_kernel(const HeadStatA
             const auto take_in = [&](auto plain) {
                 constexpr bool PLAIN = decltype(plain)::value;
 #pragma unroll
-                for (int i = 0; i < P_MT; ++i) {
+                for (int i = 0; i < Q; ++i) {
                     float d[4], p[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) d[e] = !PLAIN && far ? (x[i][e] - base) * h.k : fmaf(x[i][e], h.k, -base2);
@@ -128,7 +129,7 @@ __global__ __launch_bounds__(P_THREADS, 1) void head_stat_kernel(const HeadStatA
     // the four lanes and the two waves that share a row
     // (from here on relative to the largest logit itself)
 #pragma unroll
-    for (int j = 0; j < P_NT; ++j) {
+    for (int j = 0; j < Q; ++j) {
         const float base = m[j] > -INFINITY ? m[j] : 0.0f, base2 = base * h.k;
         const float d = fabsf(base2) >= LOGIT_FAR ? 0.0f : fmaf(-base, h.k, base2), f = __builtin_amdgcn_exp2f(d);
         u[j] = f * (u[j] + d * s[j]);
@@ -146,16 +147,16 @@ __global__ __launch_bounds__(P_THREADS, 1) void head_stat_kernel(const HeadStatA
     RowSums* tmp = reinterpret_cast<RowSums*>(lds);
     product.end();
 #pragma unroll
-    for (int j = 0; j < P_NT; ++j) {
+    for (int j = 0; j < Q; ++j) {
         RowSums r = {m[j], s[j], u[j]};
 #pragma unroll
         for (int d = 16; d < 64; d <<= 1) r = join(r, RowSums{__shfl_xor(r.m, d), __shfl_xor(r.s, d), __shfl_xor(r.u, d)});
-        if (lane < 16) tmp[wave * (PN / 2) + 8 * lane + j] = r;
+        if (lane < 16) tmp[wave * (SIDE / 2) + Q * lane + j] = r;
     }
     __syncthreads();
-    for (int32_t i = threadIdx.x; i < PN && first + i < n_rows; i += P_THREADS) {
+    for (int32_t i = threadIdx.x; i < SIDE && first + i < n_rows; i += P_THREADS) {
         const int32_t row = first + i;
-        RowSums r = join(tmp[i], tmp[PN + i]);
+        RowSums r = join(tmp[i], tmp[SIDE + i]);
         RowSums* to = h.sums + (int64_t)row * h.segments + at.second;
         if (h.add) r = join(*to, r);
         *to = r;
@@ -163,23 +164,24 @@ __global__ __launch_bounds__(P_THREADS, 1) void head_stat_kernel(const HeadStatA
 }
 
 // A row's logits in 32 bits, for rows whose alternatives are wanted.
-template <typename T>
-__global__ __launch_bounds__(P_THREADS, 1) void head_logits_kernel(const HeadStatArgs h, float* logits, int64_t pitch) {
-    __shared__ __attribute__((aligned(1024))) char lds[P_LDS];
+template <typename T, int Q>
+__global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_logits_kernel(const HeadStatArgs h, float* logits, int64_t pitch) {
+    constexpr int SIDE = P_SIDE<Q>;
+    __shared__ __attribute__((aligned(1024))) char lds[P_LDS<Q>];
     const TilePair at = tile_pair(by_chiplet(blockIdx.x, h.row_tiles * h.tiles), h.row_tiles, h.tiles);
-    const int32_t first = at.first * PN, t = at.second;
-    TileOfA a;
-    TileOfB b;
-    place_tile(a, h.w, t * PM, h.vocab_end - h.v0);
+    const int32_t first = at.first * SIDE, t = at.second;
+    TileOfA<Q> a;
+    TileOfB<Q> b;
+    place_tile(a, h.w, t * SIDE, h.vocab_end - h.v0);
     place_tile(b, h.x, first, h.n_rows);
-    f32x4 acc[P_MT][P_NT];
-    product<T>(acc, a, b, h.parts, h.steps, lds);
-    const int32_t v = h.v0 + t * PM + place_a(), row = first + place_b();
+    f32x4 acc[Q][Q];
+    product<T, Q>(acc, a, b, h.parts, h.steps, lds);
+    const int32_t v = h.v0 + t * SIDE + place_a<Q>(), row = first + place_b<Q>();
 #pragma unroll
-    for (int j = 0; j < P_NT; ++j)
+    for (int j = 0; j < Q; ++j)
         if (row + j < h.n_rows)
 #pragma unroll
-            for (int i = 0; i < P_MT; ++i)
+            for (int i = 0; i < Q; ++i)
                 if (v + along_a(i, 0) < h.vocab_end)         // (the pitch is a multiple of 4)
                     *reinterpret_cast<f32x4*>(logits + (row + j) * pitch + v + along_a(i, 0)) = acc[i][j];
 }
@@ -475,23 +477,23 @@ __global__ __launch_bounds__(256) void head_join_kernel(const LogprobArgs a, con
 
 // How the vocabulary is shared out over workgroups: `segments` to each tile of rows, so that two to a compute unit finish at
 // about the same time.
-constexpr int32_t HEAD_SLOTS = 256, HEAD_MOST_BLOCKS = 4 * HEAD_SLOTS;
-static int32_t segments_of(int64_t row_tiles, int32_t tiles) {
+constexpr int32_t HEAD_MOST_BLOCKS = 2048;
+static int32_t segments_of(int64_t row_tiles, int32_t tiles, int32_t slots) {
     int32_t best = 1;
     int64_t least = -1;
     for (int32_t s = 1; s <= tiles && row_tiles * s <= HEAD_MOST_BLOCKS; ++s) {
-        const int64_t rounds = (row_tiles * s + HEAD_SLOTS - 1) / HEAD_SLOTS * ((tiles + s - 1) / s);
+        const int64_t rounds = (row_tiles * s + slots - 1) / slots * ((tiles + s - 1) / s);
         if (least < 0 || rounds < least) { least = rounds; best = s; }
     }
     return best;
 }
 
-constexpr int64_t HEAD_TOP_ROWS = PN;            // rows whose logits are held at once, where alternatives are wanted
+constexpr int64_t HEAD_TOP_ROWS = 256;           // rows whose logits are held at once, where alternatives are wanted
 constexpr int64_t HEAD_PIECE_BYTES = 256LL << 20;    // of weights laid out at once
 static int32_t weight_piece(const HeadShape& sh, const dc_matrix& w) {
     if (!sh.copy_weight) return (int32_t)w.n_rows;
     const int64_t row = sh.k_pad * 2LL * (w.type == DC_F32 ? 3 : 1);
-    return (int32_t)std::min<int64_t>(whole(w.n_rows, PM), std::max<int64_t>(PM, HEAD_PIECE_BYTES / row / PM * PM));
+    return (int32_t)std::min<int64_t>(whole(w.n_rows, P_MOST_SIDE), std::max<int64_t>(P_MOST_SIDE, HEAD_PIECE_BYTES / row / P_MOST_SIDE * P_MOST_SIDE));
 }
 
 namespace {
@@ -533,9 +535,12 @@ static HeadWs carve(void* base, const dc_matrix& hidden, const dc_matrix& weight
         w.live.count = reinterpret_cast<int32_t*>(take(4));
         w.x_token = reinterpret_cast<float*>(take(rows * 4));
         // (as many segments as any number of tiles of rows up to this one's has: blocks never pass their limit, nor tiles of both)
-        const int64_t row_tiles = sh.rows_pad / PN, tiles = whole(weight.n_rows, PM) / PM;
-        const int64_t blocks = std::max<int64_t>(row_tiles, std::min<int64_t>(HEAD_MOST_BLOCKS, row_tiles * tiles));
-        w.sums = reinterpret_cast<RowSums*>(take(blocks * PN * (int64_t)sizeof(RowSums)));
+        int64_t sums = 0;
+        for (const int64_t side : {P_SIDE<4>, P_SIDE<8>}) {
+            const int64_t row_tiles = whole(rows, side) / side, tiles = whole(weight.n_rows, side) / side;
+            sums = std::max(sums, side * std::max<int64_t>(row_tiles, std::min<int64_t>(HEAD_MOST_BLOCKS, row_tiles * tiles)));
+        }
+        w.sums = reinterpret_cast<RowSums*>(take(sums * (int64_t)sizeof(RowSums)));
     }
     w.bytes = (size_t)at;
     return w;
@@ -582,11 +587,13 @@ hipError_t launch_head(const HeadArgs& a, void* d_ws, hipStream_t st) {
     h.token = a.token;
     h.sums = w.sums;
     h.x_token = w.x_token;
-    h.row_tiles = (int32_t)(sh.rows_pad / PN);
+    const bool small = cut_product(a.n_top > 0 ? std::min(rows, HEAD_TOP_ROWS) : rows, std::min(w.piece, vocab), h.steps * h.parts.n, 1).small;
+    const int32_t side = small ? P_SIDE<4> : P_SIDE<8>;
+    h.row_tiles = (int32_t)((rows + side - 1) / side);
     h.n_rows = (int32_t)rows;
     h.count = live ? w.live.count : nullptr;
     h.list = live ? w.live.list : nullptr;
-    h.segments = segments_of(h.row_tiles, (std::min(w.piece, vocab) + PM - 1) / PM);
+    h.segments = segments_of(h.row_tiles, (std::min(w.piece, vocab) + side - 1) / side, small ? P_SLOTS<4> : P_SLOTS<8>);
     if (sh.copy_hidden) {
         if (e == hipSuccess) e = launch_lay_rows(a.hidden, 0, rows, h.list, h.count, sh.k_pad, w.hidden, w.hidden_plane, st);
         h.x = Operand{w.hidden, sh.k_pad * 2, nullptr};
@@ -596,7 +603,7 @@ hipError_t launch_head(const HeadArgs& a, void* d_ws, hipStream_t st) {
     for (int64_t r0 = 0; r0 < rows && e == hipSuccess; r0 += HEAD_TOP_ROWS) {
         if (a.n_top > 0) {                       // so many rows at a time
             h.n_rows = (int32_t)std::min(HEAD_TOP_ROWS, rows - r0);
-            h.row_tiles = 1;
+            h.row_tiles = (h.n_rows + side - 1) / side;
         }
         for (int32_t v0 = 0; v0 < vocab && e == hipSuccess; v0 += w.piece) {
             const int32_t n = std::min(w.piece, vocab - v0);
@@ -609,15 +616,19 @@ hipError_t launch_head(const HeadArgs& a, void* d_ws, hipStream_t st) {
             if (e != hipSuccess) break;
             h.v0 = v0;
             h.vocab_end = v0 + n;
-            h.tiles = (n + PM - 1) / PM;
+            h.tiles = (n + side - 1) / side;
             h.add = v0 > 0;
-            const auto go = [&](auto t) {
+            const auto go = [&](auto t, auto q) {
                 using T = decltype(t);
-                if (a.n_top > 0) head_logits_kernel<T><<<h.tiles, P_THREADS, 0, st>>>(h, w.logits, w.pitch);
-                else if (a.entropy) head_stat_kernel<T, true><<<h.row_tiles * h.segments, P_THREADS, 0, st>>>(h);
-                else head_stat_kernel<T, false><<<h.row_tiles * h.segments, P_THREADS, 0, st>>>(h);
+                constexpr int Q = decltype(q)::value;
+                if (a.n_top > 0) head_logits_kernel<T, Q><<<h.row_tiles * h.tiles, P_THREADS, 0, st>>>(h, w.logits, w.pitch);
+                else if (a.entropy) head_stat_kernel<T, true, Q><<<h.row_tiles * h.segments, P_THREADS, 0, st>>>(h);
+                else head_stat_kernel<T, false, Q><<<h.row_tiles * h.segments, P_THREADS, 0, st>>>(h);
             };
-            if (type == DC_F16) go(_Float16{}); else go(__bf16{});
+            const auto with_q = [&](auto t) {
+                if (small) go(t, std::integral_constant<int, 4>{}); else go(t, std::integral_constant<int, 8>{});
+            };
+            if (type == DC_F16) with_q(_Float16{}); else with_q(__bf16{});
             e = hipGetLastError();
         }
         if (a.n_top == 0) break;

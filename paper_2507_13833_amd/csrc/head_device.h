@@ -43,11 +43,15 @@ __device__ __forceinline__ void settle_sums() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
-// A workgroup makes PM rows of A times PN rows of B: four waves, two by two, 128 x 128 each, one to a SIMD, with all its 256 sums of a
-// lane in registers.
-constexpr int PM = 256, PN = 256, PK = 64, P_THREADS = 256;
-constexpr int P_STAGE = (PM + PN) * PK * 2, P_LDS = 2 * P_STAGE;
-constexpr int P_MT = PM / 2 / 16, P_NT = PN / 2 / 16;    // 16 x 16 places of a wave
+// A workgroup makes 32 Q rows of A times 32 Q rows of B: four waves, two by two, Q by Q places of 16 x 16 each.  Q = 8: a wave to a SIMD,
+// all 256 sums of its lanes in registers, the most products for what is read.  Q = 4: two workgroups to a compute unit, one begins
+// and ends beside the other's products, where there are few tiles or few steps.
+constexpr int PK = 64, P_THREADS = 256;
+template <int Q> constexpr int P_SIDE = 32 * Q;
+template <int Q> constexpr int P_STAGE = 2 * P_SIDE<Q> * PK * 2;
+template <int Q> constexpr int P_LDS = 2 * P_STAGE<Q>;
+template <int Q> constexpr int P_SLOTS = Q == 8 ? 256 : 512;         // workgroups at once
+constexpr int P_MOST_SIDE = P_SIDE<8>;
 
 struct Operand {
     const char*    p;               // 16-byte aligned
@@ -82,14 +86,14 @@ __device__ __forceinline__ void bare_barrier() {
 
 // What of a tile a thread loads: the rows that lie at tid / 8 + 32 j in the LDS, 16 bytes each.  The eight 16-byte pieces of a row's
 // 128 bytes lie there at piece ^ (place % 8), so that eight rows' same piece fills all banks.  Rows of the tile are dealt out to the
-// places so that a lane comes to hold neighbours, which its stores want: of each 128 rows of A, place 16 i + p takes row
-// 32 (i / 2) + 8 (p / 4) + 4 (i % 2) + p % 4; of each 128 of B, place 16 j + q row 8 q + j.
-template <int ROWS> struct Tile { const char* base; uint32_t at[ROWS / 32]; };
-struct TileOfA : Tile<PM> {
+// places so that a lane comes to hold neighbours, which its stores want: of each 16 Q rows of A, place 16 i + p takes row
+// 32 (i / 2) + 8 (p / 4) + 4 (i % 2) + p % 4; of each 16 Q of B, place 16 j + q row Q q + j.
+template <int Q> struct Tile { const char* base; uint32_t at[Q]; };
+template <int Q> struct TileOfA : Tile<Q> {
     static __device__ __forceinline__ int row_at(int x) { return (x & ~31) + (x >> 2 & 3) * 8 + (x >> 4 & 1) * 4 + (x & 3); }
 };
-struct TileOfB : Tile<PN> {
-    static __device__ __forceinline__ int row_at(int x) { return (x & ~127) + (x & 15) * 8 + (x >> 4 & 7); }
+template <int Q> struct TileOfB : Tile<Q> {
+    static __device__ __forceinline__ int row_at(int x) { return (x & -16 * Q) + (x & 15) * Q + (x >> 4 & (Q - 1)); }
 };
 template <typename T>
 __device__ __forceinline__ void place_tile(T& t, const Operand& o, int32_t first, int32_t n_rows) {
@@ -103,26 +107,27 @@ __device__ __forceinline__ void place_tile(T& t, const Operand& o, int32_t first
 }
 
 // Where a lane's rows begin in a tile of A and of B: acc[i][j][e] is of A's row place_a() + along_a(i, e) and B's place_b() + j.
-__device__ __forceinline__ int place_a() { return threadIdx.x / (2 * WAVE) * (PM / 2) + (lane_id() >> 4) * 8; }
-__device__ __forceinline__ int place_b() { return threadIdx.x / WAVE % 2 * (PN / 2) + (lane_id() & 15) * 8; }
+template <int Q> __device__ __forceinline__ int place_a() { return threadIdx.x / (2 * WAVE) * (16 * Q) + (lane_id() >> 4) * 8; }
+template <int Q> __device__ __forceinline__ int place_b() { return threadIdx.x / WAVE % 2 * (16 * Q) + (lane_id() & 15) * Q; }
 constexpr __device__ __host__ int along_a(int i, int e) { return i / 2 * 32 + i % 2 * 4 + e; }
 
 // The workgroup's tiles one after the other.  Two stages of PK elements lie in the LDS, each multiplied in two halves; a half's numbers
 // are read into registers while the half before is multiplied.  Once the second half of a stage is in registers its place is free:
 // the stage after next is asked for there, a whole stage ahead and on into the next tile.  next() makes a and b that next tile (or
 // leaves them: what is asked for then is not used).  Steps and parts are the same for all tiles, and there is at least one of each.
-template <typename T>
+template <typename T, int Q>
 struct Product {
     using Frag = typename Mfma<T>::Frag;
-    TileOfA     a;
-    TileOfB     b;
+    static constexpr int STAGE = P_STAGE<Q>, B_AT = P_SIDE<Q> * 128;     // where B's rows lie in a stage
+    TileOfA<Q>  a;
+    TileOfB<Q>  b;
     Parts       parts;
     int32_t     steps, part, left, stage;
     const char *pa, *pb;
     char*       to;
     const char *from_a, *from_b;
     int         at_half[2];
-    Frag        fa[2][P_MT], fb[2][P_NT];
+    Frag        fa[2][Q], fb[2][Q];
 
     __device__ __forceinline__ void start_of(int32_t i) {
         part = i;
@@ -130,8 +135,8 @@ struct Product {
         pa = a.base + (parts.a >> 2 * i & 3) * parts.a_plane;
         pb = b.base + (parts.b >> 2 * i & 3) * parts.b_plane;
     }
-    __device__ __forceinline__ void ask_a(int j) { load_to_lds(pa + a.at[j], to + (stage & 1) * P_STAGE + j * 4096); }
-    __device__ __forceinline__ void ask_b(int j) { load_to_lds(pb + b.at[j], to + (stage & 1) * P_STAGE + PM * 128 + j * 4096); }
+    __device__ __forceinline__ void ask_a(int j) { load_to_lds(pa + a.at[j], to + (stage & 1) * STAGE + j * 4096); }
+    __device__ __forceinline__ void ask_b(int j) { load_to_lds(pb + b.at[j], to + (stage & 1) * STAGE + B_AT + j * 4096); }
     template <typename Next>
     __device__ __forceinline__ void asked(Next&& next) {
         pa += PK * 2;
@@ -147,10 +152,10 @@ struct Product {
         }
     }
     __device__ __forceinline__ void read_a(int32_t s, int h, int i) {
-        fa[h][i] = *reinterpret_cast<const Frag*>(from_a + (s & 1) * P_STAGE + at_half[h] + i * 2048);
+        fa[h][i] = *reinterpret_cast<const Frag*>(from_a + (s & 1) * STAGE + at_half[h] + i * 2048);
     }
     __device__ __forceinline__ void read_b(int32_t s, int h, int j) {
-        fb[h][j] = *reinterpret_cast<const Frag*>(from_b + (s & 1) * P_STAGE + at_half[h] + j * 2048);
+        fb[h][j] = *reinterpret_cast<const Frag*>(from_b + (s & 1) * STAGE + at_half[h] + j * 2048);
     }
 
     // a, b, parts and steps are set
@@ -159,8 +164,8 @@ struct Product {
         const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
         const int row = lane & 15, piece = (lane >> 4) ^ (row & 7);
         to = lds + wave * 1024;
-        from_a = lds + (wave / 2 * (PM / 2) + row) * 128;
-        from_b = lds + PM * 128 + (wave % 2 * (PN / 2) + row) * 128;
+        from_a = lds + (wave / 2 * (16 * Q) + row) * 128;
+        from_b = lds + B_AT + (wave % 2 * (16 * Q) + row) * 128;
         at_half[0] = piece * 16;
         at_half[1] = (piece ^ 4) * 16;
         stage = 0;
@@ -168,49 +173,48 @@ struct Product {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
 #pragma unroll
-            for (int j = 0; j < PM / 32; ++j) ask_a(j);
+            for (int j = 0; j < Q; ++j) ask_a(j);
 #pragma unroll
-            for (int j = 0; j < PN / 32; ++j) ask_b(j);
+            for (int j = 0; j < Q; ++j) ask_b(j);
             asked(next);
         }
-        wait_loads<(PM + PN) / 32>();
+        wait_loads<2 * Q>();
         bare_barrier();
 #pragma unroll
-        for (int i = 0; i < P_MT; ++i) read_a(0, 0, i);
+        for (int i = 0; i < Q; ++i) read_a(0, 0, i);
 #pragma unroll
-        for (int j = 0; j < P_NT; ++j) read_b(0, 0, j);
+        for (int j = 0; j < Q; ++j) read_b(0, 0, j);
     }
 
     // acc = the sums of the tile whose turn it is
     template <typename Next>
-    __device__ __forceinline__ void tile(f32x4 (&acc)[P_MT][P_NT], Next&& next) {
-        static_assert(P_MT == 8 && P_NT == 8, "four products to a read");
+    __device__ __forceinline__ void tile(f32x4 (&acc)[Q][Q], Next&& next) {
 #pragma unroll
-        for (int i = 0; i < P_MT; ++i)
+        for (int i = 0; i < Q; ++i)
 #pragma unroll
-            for (int j = 0; j < P_NT; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+            for (int j = 0; j < Q; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
         settle_sums();
         const int32_t all = steps * parts.n, first = stage - 2;
         for (int32_t s = first; s < first + all; ++s) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int q = 0; q < 16; ++q) {
+            for (int q = 0; q < 2 * Q; ++q) {    // half a row of places to a read
 #pragma unroll
-                for (int e = 0; e < 4; ++e) Mfma<T>::add(fa[0][q / 2], fb[0][q % 2 * 4 + e], acc[q / 2][q % 2 * 4 + e]);
+                for (int e = 0; e < Q / 2; ++e) Mfma<T>::add(fa[0][q / 2], fb[0][q % 2 * (Q / 2) + e], acc[q / 2][q % 2 * (Q / 2) + e]);
                 // (the first products of the next half want all of B and the first of A)
-                if (q < 8) read_b(s, 1, q); else read_a(s, 1, q - 8);
+                if (q < Q) read_b(s, 1, q); else read_a(s, 1, q - Q);
                 __builtin_amdgcn_sched_barrier(0);
             }
             wait_loads<0>();
             bare_barrier();
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int q = 0; q < 16; ++q) {
+            for (int q = 0; q < 2 * Q; ++q) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) Mfma<T>::add(fa[1][q / 2], fb[1][q % 2 * 4 + e], acc[q / 2][q % 2 * 4 + e]);
-                if (q < 8) ask_a(q); else ask_b(q - 8);
-                if (q < 8) read_b(s + 1, 0, q); else read_a(s + 1, 0, q - 8);
+                for (int e = 0; e < Q / 2; ++e) Mfma<T>::add(fa[1][q / 2], fb[1][q % 2 * (Q / 2) + e], acc[q / 2][q % 2 * (Q / 2) + e]);
+                if (q < Q) ask_a(q); else ask_b(q - Q);
+                if (q < Q) read_b(s + 1, 0, q); else read_a(s + 1, 0, q - Q);
                 __builtin_amdgcn_sched_barrier(0);
             }
             asked(next);
@@ -225,17 +229,17 @@ struct Product {
     }
 };
 // One tile alone, already placed.
-template <typename T>
-__device__ __forceinline__ void product(f32x4 (&acc)[P_MT][P_NT], const TileOfA& a, const TileOfB& b, const Parts& parts, int32_t steps,
+template <typename T, int Q>
+__device__ __forceinline__ void product(f32x4 (&acc)[Q][Q], const TileOfA<Q>& a, const TileOfB<Q>& b, const Parts& parts, int32_t steps,
                                         char* lds) {
     if (steps <= 0) {
 #pragma unroll
-        for (int i = 0; i < P_MT; ++i)
+        for (int i = 0; i < Q; ++i)
 #pragma unroll
-            for (int j = 0; j < P_NT; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+            for (int j = 0; j < Q; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
         return;
     }
-    Product<T> p;
+    Product<T, Q> p;
     p.a = a;
     p.b = b;
     p.parts = parts;

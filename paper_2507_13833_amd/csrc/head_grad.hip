@@ -140,45 +140,46 @@ struct HeadPieceArgs {
 };
 
 // T: of the operands, D: of G; PLANES of it along the vocabulary (gt) and, for bf16, along the rows too (f16: one there).
-template <typename T, typename D, int PLANES>
-__global__ __launch_bounds__(P_THREADS, 1) void head_piece_kernel(const HeadPieceArgs h) {
-    __shared__ __attribute__((aligned(1024))) char lds[P_LDS];
+template <typename T, typename D, int PLANES, int Q>
+__global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_piece_kernel(const HeadPieceArgs h) {
+    constexpr int SIDE = P_SIDE<Q>;
+    __shared__ __attribute__((aligned(1024))) char lds[P_LDS<Q>];
     const TilePair at = tile_pair(by_chiplet(blockIdx.x, h.row_tiles * h.tiles), h.row_tiles, h.tiles);
-    const int32_t n_rows = *h.count, first = at.first * PN, t = at.second;
+    const int32_t n_rows = *h.count, first = at.first * SIDE, t = at.second;
     if (first >= n_rows) return;
-    f32x4 acc[P_MT][P_NT];
+    f32x4 acc[Q][Q];
     {
-        TileOfA a;
-        TileOfB b;
-        place_tile(a, h.w, t * PM, h.vocab_end - h.v0);
+        TileOfA<Q> a;
+        TileOfB<Q> b;
+        place_tile(a, h.w, t * SIDE, h.vocab_end - h.v0);
         place_tile(b, h.x, first, n_rows);
-        product<T>(acc, a, b, h.parts, h.steps, lds);
+        product<T, Q>(acc, a, b, h.parts, h.steps, lds);
     }
-    const int32_t u = t * PM + place_a(), row = first + place_b();
+    const int32_t u = t * SIDE + place_a<Q>(), row = first + place_b<Q>();
     constexpr int ROW_PLANES = std::is_same_v<D, _Float16> ? 1 : PLANES;
     const int64_t g_plane = h.width * h.rows_pad * 2;
     // whole: all of the tile's rows and entries are there
     const auto put = [&](auto whole) {
         constexpr bool WHOLE = decltype(whole)::value;
-        RowTerm q[P_NT];
+        RowTerm of[Q];
 #pragma unroll
-        for (int j = 0; j < P_NT; ++j) q[j] = h.term[WHOLE ? row + j : min(row + j, n_rows - 1)];
+        for (int j = 0; j < Q; ++j) of[j] = h.term[WHOLE ? row + j : min(row + j, n_rows - 1)];
 #pragma unroll
-        for (int i = 0; i < P_MT; i += 2) {
-            // eight entries of eight rows
+        for (int i = 0; i < Q; i += 2) {
+            // eight entries of Q rows
             const int32_t v = u + along_a(i, 0);
-            float f[8][P_NT];
+            float f[8][Q];
 #pragma unroll
-            for (int j = 0; j < P_NT; ++j) {
+            for (int j = 0; j < Q; ++j) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float l2 = fmaf(acc[i + e / 4][j][e % 4] - q[j].m, h.k, -q[j].l2), p = __builtin_amdgcn_exp2f(l2);
-                    f[e][j] = p * fmaf(q[j].c1, WHOLE ? l2 : fmaxf(l2, -1e4f), q[j].c0);
+                    const float l2 = fmaf(acc[i + e / 4][j][e % 4] - of[j].m, h.k, -of[j].l2), p = __builtin_amdgcn_exp2f(l2);
+                    f[e][j] = p * fmaf(of[j].c1, WHOLE ? l2 : fmaxf(l2, -1e4f), of[j].c0);
                 }
-                const uint32_t own = (uint32_t)(q[j].token - h.v0 - v);
+                const uint32_t own = (uint32_t)(of[j].token - h.v0 - v);
                 if (own < 8)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) f[e][j] += own == (uint32_t)e ? q[j].ga : 0.0f;
+                    for (int e = 0; e < 8; ++e) f[e][j] += own == (uint32_t)e ? of[j].ga : 0.0f;
                 if constexpr (!WHOLE)
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
@@ -186,28 +187,28 @@ __global__ __launch_bounds__(P_THREADS, 1) void head_piece_kernel(const HeadPiec
             }
 #pragma unroll
             for (int p = 0; p < PLANES; ++p) {
-                Raw8<D> along[8];                    // of a row
+                Raw8<D> along[Q];                    // of a row
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
 #pragma unroll
-                    for (int j = 0; j < P_NT; ++j) along[j].e[e] = take_part<D>(f[e][j]);
+                    for (int j = 0; j < Q; ++j) along[j].e[e] = take_part<D>(f[e][j]);
                 if (h.g && p < ROW_PLANES)
 #pragma unroll
-                    for (int j = 0; j < P_NT; ++j)
+                    for (int j = 0; j < Q; ++j)
                         *reinterpret_cast<u32x4*>(h.g + p * g_plane + ((row + j) * h.width + v) * 2) = along[j].q[0];
                 if (h.gt)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        Raw8<D> down;                // of an entry
+                        struct alignas(2 * Q) { D e[Q]; } down;      // of an entry
 #pragma unroll
-                        for (int j = 0; j < P_NT; ++j) down.e[j] = along[j].e[e];
-                        *reinterpret_cast<u32x4*>(h.gt + p * g_plane + ((v + e) * h.rows_pad + row) * 2) = down.q[0];
+                        for (int j = 0; j < Q; ++j) down.e[j] = along[j].e[e];
+                        *reinterpret_cast<decltype(down)*>(h.gt + p * g_plane + ((v + e) * h.rows_pad + row) * 2) = down;
                     }
             }
             __builtin_amdgcn_sched_barrier(0);       // (so many at a time in registers)
         }
     };
-    if (first + PN <= n_rows && h.v0 + (t + 1) * PM <= h.vocab_end) put(std::true_type{}); else put(std::false_type{});
+    if (first + SIDE <= n_rows && h.v0 + (t + 1) * SIDE <= h.vocab_end) put(std::true_type{}); else put(std::false_type{});
 }
 
 // ---- the two products ----
@@ -222,31 +223,32 @@ struct HeadHiddenArgs {             // slab[split][row][col] (+)= sum over this 
     float*         slab;
     int64_t        rows_pad, pitch;
 };
-template <typename D>
-__global__ __launch_bounds__(P_THREADS, 1) void head_hidden_kernel(const HeadHiddenArgs h) {
-    __shared__ __attribute__((aligned(1024))) char lds[P_LDS];
+template <typename D, int Q>
+__global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_hidden_kernel(const HeadHiddenArgs h) {
+    constexpr int SIDE = P_SIDE<Q>;
+    __shared__ __attribute__((aligned(1024))) char lds[P_LDS<Q>];
     const int32_t others = h.col_tiles * h.splits;
     const TilePair at = tile_pair(by_chiplet(blockIdx.x, h.row_tiles * others), h.row_tiles, others);
-    const int32_t n_rows = *h.count, first = at.first * PN, tile = at.second % h.col_tiles, split = at.second / h.col_tiles;
+    const int32_t n_rows = *h.count, first = at.first * SIDE, tile = at.second % h.col_tiles, split = at.second / h.col_tiles;
     if (first >= n_rows) return;
     const int32_t each = (h.steps + h.splits - 1) / h.splits, from = split * each, steps = min(each, h.steps - from);
-    f32x4 acc[P_MT][P_NT];
+    f32x4 acc[Q][Q];
     {
-        TileOfA a;
-        TileOfB b;
-        place_tile(a, h.wt, tile * PM, h.dim);
+        TileOfA<Q> a;
+        TileOfB<Q> b;
+        place_tile(a, h.wt, tile * SIDE, h.dim);
         place_tile(b, h.g, first, n_rows);
         a.base += from * (PK * 2LL);
         b.base += from * (PK * 2LL);
-        product<D>(acc, a, b, h.parts, max(steps, 0), lds);
+        product<D, Q>(acc, a, b, h.parts, max(steps, 0), lds);
     }
     const int up = std::is_same_v<D, _Float16> ? *h.top - 15 : 0;
-    const int32_t col = tile * PM + place_a(), row = first + place_b();
+    const int32_t col = tile * SIDE + place_a<Q>(), row = first + place_b<Q>();
 #pragma unroll
-    for (int j = 0; j < P_NT; ++j)
+    for (int j = 0; j < Q; ++j)
         if (row + j < n_rows)
 #pragma unroll
-            for (int i = 0; i < P_MT; ++i)
+            for (int i = 0; i < Q; ++i)
                 if (col + along_a(i, 0) < h.pitch) {         // (a multiple of 4)
                     f32x4* to = reinterpret_cast<f32x4*>(h.slab + ((int64_t)split * h.rows_pad + row + j) * h.pitch + col + along_a(i, 0));
                     f32x4 v = acc[i][j];
@@ -289,27 +291,28 @@ struct HeadWeightArgs {             // grad_weight[v0 + row of gt][col] (+)= sum
     void*          out;             // of the piece's first entry
     int64_t        stride;
 };
-template <typename D, typename T>
-__global__ __launch_bounds__(P_THREADS, 1) void head_weight_kernel(const HeadWeightArgs h) {
-    __shared__ __attribute__((aligned(1024))) char lds[P_LDS];
+template <typename D, typename T, int Q>
+__global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_weight_kernel(const HeadWeightArgs h) {
+    constexpr int SIDE = P_SIDE<Q>;
+    __shared__ __attribute__((aligned(1024))) char lds[P_LDS<Q>];
     const TilePair at = tile_pair(by_chiplet(blockIdx.x, h.row_tiles * h.col_tiles), h.row_tiles, h.col_tiles);
-    const int32_t first = at.first * PN, tile = at.second;
-    f32x4 acc[P_MT][P_NT];
+    const int32_t first = at.first * SIDE, tile = at.second;
+    f32x4 acc[Q][Q];
     {
-        TileOfA a;
-        TileOfB b;
-        place_tile(a, h.xt, tile * PM, h.dim);
+        TileOfA<Q> a;
+        TileOfB<Q> b;
+        place_tile(a, h.xt, tile * SIDE, h.dim);
         place_tile(b, h.gt, first, h.n);
-        product<D>(acc, a, b, h.parts, (*h.count + PK - 1) / PK, lds);
+        product<D, Q>(acc, a, b, h.parts, (*h.count + PK - 1) / PK, lds);
     }
     const int up = std::is_same_v<D, _Float16> ? *h.top - 15 : 0;
-    const int32_t col = tile * PM + place_a(), row = first + place_b();
+    const int32_t col = tile * SIDE + place_a<Q>(), row = first + place_b<Q>();
 #pragma unroll
-    for (int j = 0; j < P_NT; ++j) {
+    for (int j = 0; j < Q; ++j) {
         if (row + j >= h.n) continue;
         T* to = static_cast<T*>(h.out) + (row + j) * h.stride + col;
 #pragma unroll
-        for (int i = 0; i < P_MT; i += 2) {
+        for (int i = 0; i < Q; i += 2) {
             const int at = along_a(i, 0);
             float f[8];
 #pragma unroll
@@ -339,26 +342,26 @@ __global__ __launch_bounds__(P_THREADS, 1) void head_weight_kernel(const HeadWei
 // ---- the workspace ----
 
 constexpr int64_t HG_AREA = 1 << 27;             // elements of G, or of the weights laid out, held at once
-constexpr int32_t HG_SLOTS = 256, HG_MOST_SPLITS = 32;
+constexpr int32_t HG_MOST_SPLITS = 32;
 
 namespace {
 struct HeadGradWs {
     LiveRows live;
     RowTerm* term;
     int32_t* top;
-    int32_t  pieces, piece;         // entries of the vocabulary to a piece, a multiple of PM
+    int32_t  pieces, piece;         // entries of the vocabulary to a piece, a multiple of P_MOST_SIDE
     char*    hidden; int64_t hidden_plane;
     char*    weight; int64_t weight_plane;
     char*    xt;     int64_t xt_plane;
     char*    wt;     int64_t wt_plane;
     char*    g;
     char*    gt;     int64_t g_plane;
-    float*   slab;   int64_t pitch; int32_t splits;
+    float*   slab;   int64_t pitch; ProductCut cut_hidden;
     size_t   bytes;
 };
 }
 static int64_t g_area(int64_t rows_pad, int64_t vocab_pad) {
-    return std::min(rows_pad * vocab_pad, std::max(HG_AREA, rows_pad * 8 * PM));
+    return std::min(rows_pad * vocab_pad, std::max(HG_AREA, rows_pad * 8 * P_MOST_SIDE));
 }
 // Every area grows with the rows, so that what serves a call serves those of fewer.
 static HeadGradWs carve_grad(void* base, const dc_matrix& hidden, const dc_matrix& weight, int32_t grad_weight_type) {
@@ -372,20 +375,20 @@ static HeadGradWs carve_grad(void* base, const dc_matrix& hidden, const dc_matri
     };
     const bool f32 = hidden.type == DC_F32;
     const int64_t rows = hidden.n_rows, dim = hidden.n_cols, planes = f32 ? 3 : 1, g_planes = f32 ? 3 : grad_weight_type == DC_F32 ? 2 : 1;
-    const int64_t vocab_pad = whole(weight.n_rows, PM);
+    const int64_t vocab_pad = whole(weight.n_rows, P_MOST_SIDE);
     w.live.list = reinterpret_cast<int32_t*>(take(rows * 4));
     w.live.pos = reinterpret_cast<int32_t*>(take(rows * 4));
     w.live.count = reinterpret_cast<int32_t*>(take(4));
     w.term = reinterpret_cast<RowTerm*>(take(rows * (int64_t)sizeof(RowTerm)));
-    w.top = reinterpret_cast<int32_t*>(take((vocab_pad / PM + 1) * 4));
+    w.top = reinterpret_cast<int32_t*>(take((vocab_pad / P_MOST_SIDE + 1) * 4));
     const int64_t area = g_area(sh.rows_pad, vocab_pad);
     // (the weights laid out along the columns: at most HG_AREA elements too)
-    const int64_t width = std::min(area / sh.rows_pad, std::max<int64_t>(HG_AREA / whole(dim, PM), 8 * PM));
-    w.piece = (int32_t)std::min<int64_t>(vocab_pad, width / PM * PM);
+    const int64_t width = std::min(area / sh.rows_pad, std::max<int64_t>(HG_AREA / whole(dim, P_MOST_SIDE), 8 * P_MOST_SIDE));
+    w.piece = (int32_t)std::min<int64_t>(vocab_pad, width / P_MOST_SIDE * P_MOST_SIDE);
     w.pieces = (int32_t)((vocab_pad + w.piece - 1) / w.piece);
-    w.piece = (int32_t)whole((vocab_pad + w.pieces - 1) / w.pieces, PM);
+    w.piece = (int32_t)whole((vocab_pad + w.pieces - 1) / w.pieces, P_MOST_SIDE);
     w.pieces = (int32_t)((vocab_pad + w.piece - 1) / w.piece);
-    const int64_t widest = std::min(vocab_pad, std::max<int64_t>(HG_AREA / whole(dim, PM), 8 * PM));
+    const int64_t widest = std::min(vocab_pad, std::max<int64_t>(HG_AREA / whole(dim, P_MOST_SIDE), 8 * P_MOST_SIDE));
     w.hidden_plane = rows * sh.k_pad * 2;
     w.hidden = take(sh.copy_hidden ? planes * w.hidden_plane : 0);
     w.weight_plane = (int64_t)w.piece * sh.k_pad * 2;
@@ -398,9 +401,8 @@ static HeadGradWs carve_grad(void* base, const dc_matrix& hidden, const dc_matri
     w.g = take((f32 ? 3 : 1) * area * 2);
     w.gt = take(g_planes * area * 2);
     w.pitch = whole(dim, 4);
-    const int64_t row_tiles = sh.rows_pad / PN, col_tiles = (dim + PM - 1) / PM;
-    w.splits = (int32_t)std::max<int64_t>(1, std::min<int64_t>(HG_MOST_SPLITS, HG_SLOTS / (row_tiles * col_tiles)));
-    w.slab = reinterpret_cast<float*>(take(std::max(row_tiles, std::min<int64_t>(HG_MOST_SPLITS * row_tiles, HG_SLOTS / col_tiles)) * PN * w.pitch * 4));
+    w.cut_hidden = cut_product(rows, dim, w.piece / PK * parts_of(hidden.type, 0, 0).n, HG_MOST_SPLITS);
+    w.slab = reinterpret_cast<float*>(take(most_split_rows(sh.rows_pad, dim, HG_MOST_SPLITS) * w.pitch * 4));
     w.bytes = (size_t)at;
     return w;
 }
@@ -442,7 +444,6 @@ hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
     HeadPieceArgs p = {};
     p.steps = sh.k_pad / PK;
     p.parts = parts_of(type, w.weight_plane, w.hidden_plane);
-    p.row_tiles = (int32_t)(sh.rows_pad / PN);
     p.count = w.live.count;
     p.term = w.term;
     p.k = a.inv_t * LOG2E;
@@ -464,9 +465,10 @@ hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
     hh.wt = Operand{w.wt, w.piece * 2LL, nullptr};
     hh.g = Operand{w.g, w.piece * 2LL, nullptr};
     hh.parts = parts_of(type, w.wt_plane, w.g_plane);
-    hh.splits = w.splits;
-    hh.col_tiles = (dim + PM - 1) / PM;
-    hh.row_tiles = p.row_tiles;
+    hh.splits = w.cut_hidden.splits;
+    const auto tiles_of = [](int64_t n, bool small) { return (int32_t)((n + (small ? P_SIDE<4> : P_SIDE<8>) - 1) / (small ? P_SIDE<4> : P_SIDE<8>)); };
+    hh.col_tiles = tiles_of(dim, w.cut_hidden.small);
+    hh.row_tiles = tiles_of(rows, w.cut_hidden.small);
     hh.dim = dim;
     hh.count = w.live.count;
     hh.slab = w.slab;
@@ -478,7 +480,6 @@ hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
     hw.parts = parts_of(type, w.xt_plane, w.g_plane);
     const bool two = gw.d_data && !f32 && gw.type == DC_F32;
     if (two) hw.parts = Parts{2, 0, 1, 0, w.g_plane};        // the small one first
-    hw.col_tiles = hh.col_tiles;
     hw.dim = dim;
     hw.count = w.live.count;
     hw.top = top_x;
@@ -508,30 +509,50 @@ hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
         if (e != hipSuccess) break;
         p.v0 = v0;
         p.vocab_end = v0 + n;
-        p.tiles = (n + PM - 1) / PM;
-        const unsigned blocks = (unsigned)(p.row_tiles * p.tiles);
-        if (f32) head_piece_kernel<__bf16, __bf16, 3><<<blocks, P_THREADS, 0, st>>>(p);
-        else if (type == DC_BF16 && two) head_piece_kernel<__bf16, _Float16, 2><<<blocks, P_THREADS, 0, st>>>(p);
-        else if (type == DC_BF16) head_piece_kernel<__bf16, _Float16, 1><<<blocks, P_THREADS, 0, st>>>(p);
-        else if (two) head_piece_kernel<_Float16, _Float16, 2><<<blocks, P_THREADS, 0, st>>>(p);
-        else head_piece_kernel<_Float16, _Float16, 1><<<blocks, P_THREADS, 0, st>>>(p);
+        const bool small_piece = cut_product(rows, n, p.steps * p.parts.n, 1).small,
+                   small_weight = cut_product(n, dim, sh.rows_pad / PK * hw.parts.n, 1).small;
+        p.tiles = tiles_of(n, small_piece);
+        p.row_tiles = tiles_of(rows, small_piece);
+        const auto piece = [&](auto t, auto d, auto planes) {
+            using T = decltype(t);
+            using D = decltype(d);
+            constexpr int PLANES = decltype(planes)::value;
+            const unsigned blocks = (unsigned)(p.row_tiles * p.tiles);
+            if (small_piece) head_piece_kernel<T, D, PLANES, 4><<<blocks, P_THREADS, 0, st>>>(p);
+            else head_piece_kernel<T, D, PLANES, 8><<<blocks, P_THREADS, 0, st>>>(p);
+        };
+        using std::integral_constant;
+        if (f32) piece(__bf16{}, __bf16{}, integral_constant<int, 3>{});
+        else if (type == DC_BF16 && two) piece(__bf16{}, _Float16{}, integral_constant<int, 2>{});
+        else if (type == DC_BF16) piece(__bf16{}, _Float16{}, integral_constant<int, 1>{});
+        else if (two) piece(_Float16{}, _Float16{}, integral_constant<int, 2>{});
+        else piece(_Float16{}, _Float16{}, integral_constant<int, 1>{});
         if (gh.d_data) {
             hh.steps = (n + PK - 1) / PK;
             hh.top = top_w;
             hh.add = i > 0;
             const unsigned b = (unsigned)(hh.row_tiles * hh.col_tiles * hh.splits);
-            if (f32) head_hidden_kernel<__bf16><<<b, P_THREADS, 0, st>>>(hh);
-            else head_hidden_kernel<_Float16><<<b, P_THREADS, 0, st>>>(hh);
+            const auto go = [&](auto d) {
+                using D = decltype(d);
+                if (w.cut_hidden.small) head_hidden_kernel<D, 4><<<b, P_THREADS, 0, st>>>(hh);
+                else head_hidden_kernel<D, 8><<<b, P_THREADS, 0, st>>>(hh);
+            };
+            if (f32) go(__bf16{}); else go(_Float16{});
         }
         if (gw.d_data) {
             hw.n = n;
-            hw.row_tiles = (n + PN - 1) / PN;
+            hw.row_tiles = tiles_of(n, small_weight);
+            hw.col_tiles = tiles_of(dim, small_weight);
             hw.out = static_cast<char*>(gw.d_data) + v0 * gw.row_stride * out_bytes;
             const unsigned b = (unsigned)(hw.row_tiles * hw.col_tiles);
             e = with_type(gw.type, [&](auto el) {
                 using T = typename decltype(el)::type;
-                if (f32) head_weight_kernel<__bf16, T><<<b, P_THREADS, 0, st>>>(hw);
-                else head_weight_kernel<_Float16, T><<<b, P_THREADS, 0, st>>>(hw);
+                const auto go = [&](auto d) {
+                    using D = decltype(d);
+                    if (small_weight) head_weight_kernel<D, T, 4><<<b, P_THREADS, 0, st>>>(hw);
+                    else head_weight_kernel<D, T, 8><<<b, P_THREADS, 0, st>>>(hw);
+                };
+                if (f32) go(__bf16{}); else go(_Float16{});
                 return hipGetLastError();
             });
         }
@@ -541,7 +562,7 @@ hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
         e = with_type(gh.type, [&](auto el) {
             using T = typename decltype(el)::type;
             head_hidden_join_kernel<T><<<(unsigned)std::min<int64_t>((rows * (w.pitch / 4) + 255) / 256, 1 << 14), 256, 0, st>>>(
-                w.slab, w.splits, sh.rows_pad, w.pitch, w.live.pos, w.term, static_cast<T*>(gh.d_data), gh.row_stride, rows, dim);
+                w.slab, w.cut_hidden.splits, sh.rows_pad, w.pitch, w.live.pos, w.term, static_cast<T*>(gh.d_data), gh.row_stride, rows, dim);
             return hipGetLastError();
         });
     return e;

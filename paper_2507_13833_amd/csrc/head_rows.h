@@ -4,15 +4,23 @@
 
 namespace dc {
 
+constexpr int64_t align256(int64_t n) { return (n + 255) / 256 * 256; }
+constexpr int64_t whole(int64_t n, int64_t of) { return (n + of - 1) / of * of; }
+
 struct HeadShape {
-    int64_t rows_pad;               // rows, to whole tiles of B
+    int64_t rows_pad;               // rows, to whole tiles of either kind
     int32_t k_pad;                  // columns, to whole steps
     bool    copy_hidden, copy_weight;   // not as the product reads it: laid out in the workspace first
 };
-HeadShape head_shape(const dc_matrix& hidden, const dc_matrix& weight, bool listed);
+// How a product of m by n rows with that many steps is cut: tiles of Q = 4 (small) or 8, the steps shared by `splits` workgroups a tile.
+struct ProductCut { bool small; int32_t splits; };
+ProductCut cut_product(int64_t m, int64_t n, int64_t steps, int32_t most_splits);
+constexpr int64_t most_split_rows(int64_t rows, int64_t n, int32_t most_splits) {       // splits times rows (of whole tiles) of any cut of up to so many rows
+    const int64_t tiles = whole(n, P_SIDE<4>) / P_SIDE<4>, all = rows * most_splits, some = (1 << 18) / tiles;
+    return rows > (all < some ? all : some) ? rows : all < some ? all : some;
+}
 
-constexpr int64_t align256(int64_t n) { return (n + 255) / 256 * 256; }
-constexpr int64_t whole(int64_t n, int64_t of) { return (n + of - 1) / of * of; }
+HeadShape head_shape(const dc_matrix& hidden, const dc_matrix& weight, bool listed);
 
 // Rows `list` (or all) of src as PARTS planes of [rows][k_pad] 16-bit numbers, columns behind the last one 0.
 // *count (or n) rows, the planes `plane` bytes apart.
