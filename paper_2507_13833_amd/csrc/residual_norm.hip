@@ -10,42 +10,50 @@
 namespace dc {
 
 constexpr int NORM_WIDEST = 1024 * 8;            // columns that a workgroup's registers hold
-constexpr int64_t NORM_PARTS = 1024, NORM_WIDE_PARTS = 256;      // workgroups of the gradient: their sums are joined
+constexpr int64_t NORM_GRID = 1024, NORM_PARTS = 512, NORM_WIDE_PARTS = 256;      // workgroups of the gradient: their sums are joined
 
-// Eight columns of a thread: neighbours (WIDE: rows on multiples of 16 bytes, dim a multiple of 8), or P apart.
+// E columns of a thread.  WIDE (rows on multiples of 16 bytes and dim a multiple of 8): eight neighbours, and eight more 8 P further on;
+// else P apart (16 bytes at a time from wherever they lie: 131072 x 1365 bf16 559 us for 354).
 template <int P, bool WIDE>
-__device__ __forceinline__ int32_t norm_column(int t, int j) { return WIDE ? t * 8 + j : j * P + t; }
+__device__ __forceinline__ int32_t norm_column(int t, int j) { return WIDE ? j / 8 * (8 * P) + t * 8 + j % 8 : j * P + t; }
 
-template <int P, bool WIDE, typename T>
-__device__ __forceinline__ void norm_load(const T* row, int t, int32_t dim, Raw8<T>& r) {
-    if constexpr (WIDE) {
-        const u32x4* p = reinterpret_cast<const u32x4*>(row + min(t * 8, dim - 8));
+template <int P, bool WIDE, int G, typename T>
+__device__ __forceinline__ void norm_load(const T* row, int t, int32_t dim, Raw8<T> (&r)[G]) {
 #pragma unroll
-        for (int h = 0; h < (int)sizeof(T) / 2; ++h) r.q[h] = __builtin_nontemporal_load(p + h);
-    } else {
+    for (int g = 0; g < G; ++g) {
+        if constexpr (WIDE) {
+            const u32x4* p = reinterpret_cast<const u32x4*>(row + min(norm_column<P, WIDE>(t, 8 * g), dim - 8));
 #pragma unroll
-        for (int j = 0; j < 8; ++j) r.e[j] = row[min(j * P + t, dim - 1)];
+            for (int h = 0; h < (int)sizeof(T) / 2; ++h) r[g].q[h] = __builtin_nontemporal_load(p + h);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) r[g].e[j] = row[min(norm_column<P, WIDE>(t, 8 * g + j), dim - 1)];
+        }
     }
 }
 // (columns behind the last one: 0)
-template <int P, bool WIDE, typename T>
-__device__ __forceinline__ void norm_values(const Raw8<T>& r, int t, int32_t dim, float (&f)[8]) {
+template <int P, bool WIDE, int G, int E, typename T>
+__device__ __forceinline__ void norm_values(const Raw8<T> (&r)[G], int t, int32_t dim, float (&f)[E]) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = norm_column<P, WIDE>(t, j) < dim ? (float)r.e[j] : 0.0f;
+    for (int j = 0; j < E; ++j) f[j] = norm_column<P, WIDE>(t, j) < dim ? (float)r[j / 8].e[j % 8] : 0.0f;
 }
-template <int P, bool WIDE, typename T>
-__device__ __forceinline__ void norm_store(T* row, int t, int32_t dim, const float (&f)[8]) {
-    Raw8<T> r;
+template <int P, bool WIDE, int E, typename T>
+__device__ __forceinline__ void norm_store(T* row, int t, int32_t dim, const float (&f)[E]) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) r.e[j] = (T)f[j];
-    if constexpr (WIDE) {
-        if (t * 8 < dim)
+    for (int g = 0; g < E / 8; ++g) {
+        Raw8<T> r;
 #pragma unroll
-            for (int h = 0; h < (int)sizeof(T) / 2; ++h) store16(reinterpret_cast<u32x4*>(row + t * 8) + h, r.q[h]);
-    } else {
+        for (int j = 0; j < 8; ++j) r.e[j] = (T)f[8 * g + j];
+        if constexpr (WIDE) {
+            const int32_t c = norm_column<P, WIDE>(t, 8 * g);
+            if (c < dim)
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j * P + t < dim) row[j * P + t] = r.e[j];
+                for (int h = 0; h < (int)sizeof(T) / 2; ++h) store16(reinterpret_cast<u32x4*>(row + c) + h, r.q[h]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (norm_column<P, WIDE>(t, 8 * g + j) < dim) row[norm_column<P, WIDE>(t, 8 * g + j)] = r.e[j];
+        }
     }
 }
 __device__ __forceinline__ float factor_at(const NormFactor& f, int64_t r, int32_t c) {
@@ -54,13 +62,14 @@ __device__ __forceinline__ float factor_at(const NormFactor& f, int64_t r, int32
     return f.type == DC_F32 ? static_cast<const float*>(f.p)[at] : f.type == DC_BF16 ? (float)static_cast<const __bf16*>(f.p)[at]
                                                                                      : (float)static_cast<const _Float16*>(f.p)[at];
 }
-// The eight factors of a thread that all rows share.
-template <int P, bool WIDE>
-__device__ __forceinline__ void factors_of(const NormFactor& w, int t, int32_t dim, float (&f)[8]) {
+// A thread's factors that all rows share.
+template <int P, bool WIDE, int E>
+__device__ __forceinline__ void factors_of(const NormFactor& w, int t, int32_t dim, float (&f)[E]) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = factor_at(w, 0, min(norm_column<P, WIDE>(t, j), dim - 1));
+    for (int j = 0; j < E; ++j) f[j] = factor_at(w, 0, min(norm_column<P, WIDE>(t, j), dim - 1));
 }
 
+__device__ __forceinline__ float wave_read_lane_f(float v) { return __uint_as_float((uint32_t)__builtin_amdgcn_readfirstlane((int)__float_as_uint(v))); }
 // Sums over the P threads of a row; `tmp`: N floats per wave, of its own for every call between two barriers.
 template <int P, int N>
 __device__ __forceinline__ void row_sums(float (&v)[N], float* tmp) {
@@ -74,9 +83,10 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* tmp) {
         lds_barrier();
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            v[i] = 0.0f;
+            v[i] = lane_id() < WAVES ? tmp[i * WAVES + lane_id()] : 0.0f;
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) v[i] += tmp[i * WAVES + w];
+            for (int d = 1; d < WAVES; d <<= 1) v[i] += __shfl_xor(v[i], d);
+            v[i] = wave_read_lane_f(v[i]);
         }
     }
 }
@@ -101,15 +111,22 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void residual_norm_kernel(const 
     }
     const float each = 1.0f / (float)dim;
     int turn = 0;
-    for (int64_t r = blockIdx.x * (int64_t)ROWS + threadIdx.x / P; r < a.rows; r += gridDim.x * (int64_t)ROWS, turn ^= 1) {
-        Raw8<A> rb, rg;
-        Raw8<R> rr;
+    Raw8<A> rb[1], rg[1];
+    Raw8<R> rr[1];
+    const auto ask = [&](int64_t r) {
         norm_load<P, WIDE>(static_cast<const A*>(a.block.p) + r * a.block.stride, t, dim, rb);
         norm_load<P, WIDE>(static_cast<const R*>(a.residual.p) + r * a.residual.stride, t, dim, rr);
         if (gate_rows) norm_load<P, WIDE>(static_cast<const A*>(a.gate.p) + r * a.gate.stride, t, dim, rg);
+    };
+    const int64_t step = gridDim.x * (int64_t)ROWS;
+    int64_t r = blockIdx.x * (int64_t)ROWS + threadIdx.x / P;
+    if (r < a.rows) ask(r);
+    for (; r < a.rows; r += step, turn ^= 1) {
         float b[8], h[8];
         norm_values<P, WIDE>(rb, t, dim, b);
         norm_values<P, WIDE>(rr, t, dim, h);
+        if (gate_rows) norm_values<P, WIDE>(rg, t, dim, gate);
+        if (r + step < a.rows) ask(r + step);    // (the next row is on its way while this one is summed and stored)
         float r1 = 0.0f, r2 = 0.0f, s[1] = {0.0f};
         if (a.has_post) {
 #pragma unroll
@@ -119,11 +136,9 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void residual_norm_kernel(const 
 #pragma unroll
             for (int j = 0; j < 8; ++j) b[j] *= r1;
         }
-        if (gate_rows) {
-            norm_values<P, WIDE>(rg, t, dim, gate);
+        if (gate_rows)
 #pragma unroll
             for (int j = 0; j < 8; ++j) b[j] *= gate[j];
-        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) h[j] = fmaf(b[j], post[j], h[j] * a.residual_scale);
         norm_store<P, WIDE>(static_cast<R*>(a.residual_out.p) + r * a.residual_out.stride, t, dim, h);
@@ -180,17 +195,19 @@ __global__ __launch_bounds__(1024) void residual_norm_wide_kernel(const NormArgs
     }
 }
 
-// Threads to a row.  A single row of 2048: 256 threads, as many rows; short rows share a workgroup.
-static int norm_threads(int32_t dim) { return dim <= 512 ? 64 : dim <= 2048 ? 256 : dim <= 4096 ? 512 : 1024; }
-template <typename F>
+// Threads to a row, eight columns each; short rows share a workgroup.  The longest rows' gradient has half the threads and twice the
+// columns: 1024 threads have 128 registers each, of which it would spill 90 (32768 x 8192 bf16: 1641 us for 635).
+template <bool GRAD, typename F>
 static hipError_t with_threads(int32_t dim, bool wide, F&& f) {
-    const auto go = [&](auto p) { return wide ? f(p, std::true_type{}) : f(p, std::false_type{}); };
-    switch (norm_threads(dim)) {
-        case 64:  return go(std::integral_constant<int, 64>{});
-        case 256: return go(std::integral_constant<int, 256>{});
-        case 512: return go(std::integral_constant<int, 512>{});
-    }
-    return go(std::integral_constant<int, 1024>{});
+    using std::integral_constant;
+    const auto go = [&](auto p, auto e) { return wide ? f(p, e, std::true_type{}) : f(p, e, std::false_type{}); };
+    using Eight = integral_constant<int, 8>;
+    if (dim <= 512) return go(integral_constant<int, 64>{}, Eight{});
+    if (dim <= 2048) return go(integral_constant<int, 256>{}, Eight{});
+    if (dim <= 4096) return go(integral_constant<int, 512>{}, Eight{});
+    if constexpr (GRAD)
+        if (wide) return f(integral_constant<int, 512>{}, integral_constant<int, 16>{}, std::true_type{});
+    return go(integral_constant<int, 1024>{}, Eight{});
 }
 static bool lies_wide(const NormStream& s, int32_t type) {
     return reinterpret_cast<uintptr_t>(s.p) % 16 == 0 && s.stride * (type == DC_F32 ? 4 : 2) % 16 == 0;
@@ -208,9 +225,9 @@ hipError_t launch_residual_norm(const NormArgs& a, hipStream_t st) {
                 residual_norm_wide_kernel<A, R><<<(unsigned)std::min<int64_t>(a.rows, 2048), 1024, 0, st>>>(a);
                 return hipGetLastError();
             }
-            return with_threads(a.dim, wide, [&](auto p, auto w) {
+            return with_threads<false>(a.dim, wide, [&](auto p, auto, auto w) {
                 constexpr int P = decltype(p)::value, THREADS = P < 256 ? 256 : P, ROWS = THREADS / P;
-                const unsigned grid = (unsigned)std::min<int64_t>((a.rows + ROWS - 1) / ROWS, 2048 * 256 / THREADS);
+                const unsigned grid = (unsigned)std::min<int64_t>((a.rows + ROWS - 1) / ROWS, NORM_GRID * 256 / THREADS);
                 residual_norm_kernel<A, R, P, decltype(w)::value><<<grid, THREADS, 0, st>>>(a);
                 return hipGetLastError();
             });
@@ -222,45 +239,61 @@ hipError_t launch_residual_norm(const NormArgs& a, hipStream_t st) {
 
 // One round of sums to a row: with x = dy pre, n2 = h r2, n1 = b r1 (b without a norm), w = gate post n1 (0 without a norm),
 //   S1 = sum x n2,  Sa = sum (dh + r2 x) w,  Sb = sum n2 w:  sum dh' w = Sa - r2 S1 Sb / dim for dh' = dh + r2 (x - n2 S1 / dim).
-template <typename A, typename R, int P, bool WIDE>
+template <typename A, typename R, int P, int E, bool WIDE>
 __global__ __launch_bounds__(P < 256 ? 256 : P) void residual_norm_grad_kernel(const NormGradArgs a) {
     constexpr int THREADS = P < 256 ? 256 : P, ROWS = THREADS / P;
+    constexpr bool AHEAD = E == 8 && P < 1024;   // the next row is on its way while one is summed and stored (else: too many registers)
     __shared__ float tmp[2][3][THREADS / WAVE];
-    __shared__ float sums[ROWS > 1 ? ROWS * 3 * P * 8 : 1];
+    __shared__ float sums[ROWS > 1 ? ROWS * 3 * P * E : 1];
     const int t = threadIdx.x % P;
     const int32_t dim = a.dim;
     const bool gate_rows = a.gate.p && a.gate.rows;
-    float post[8], gate[8], pre[8], sum_post[8] = {}, sum_gate[8] = {}, sum_pre[8] = {};
+    float post[E], gate[E], pre[E], sum_post[E] = {}, sum_gate[E] = {}, sum_pre[E] = {};
     factors_of<P, WIDE>(a.post, t, dim, post);
     if (!gate_rows) factors_of<P, WIDE>(a.gate, t, dim, gate);
     factors_of<P, WIDE>(a.pre, t, dim, pre);
     const float each = 1.0f / (float)dim;
     int turn = 0;
-    for (int64_t r = blockIdx.x * (int64_t)ROWS + threadIdx.x / P; r < a.rows; r += gridDim.x * (int64_t)ROWS, turn ^= 1) {
-        Raw8<A> rb, rg, ry;
-        Raw8<R> rh, rd;
+    Raw8<A> rb[E / 8], rg[E / 8], ry[E / 8];
+    Raw8<R> rh[E / 8], rd[E / 8];
+    float next1 = 1.0f, next2 = 0.0f;
+    const auto ask = [&](int64_t r) {
         norm_load<P, WIDE>(static_cast<const A*>(a.block.p) + r * a.block.stride, t, dim, rb);
         if (a.grad_residual_out.p) norm_load<P, WIDE>(static_cast<const R*>(a.grad_residual_out.p) + r * a.grad_residual_out.stride, t, dim, rd);
         if (a.has_pre) {
             norm_load<P, WIDE>(static_cast<const R*>(a.residual_out.p) + r * a.residual_out.stride, t, dim, rh);
             norm_load<P, WIDE>(static_cast<const A*>(a.grad_out.p) + r * a.grad_out.stride, t, dim, ry);
+            next2 = a.stat[2 * r + 1];
         }
         if (gate_rows) norm_load<P, WIDE>(static_cast<const A*>(a.gate.p) + r * a.gate.stride, t, dim, rg);
-        const float r1 = a.has_post ? a.stat[2 * r] : 1.0f, r2 = a.has_pre ? a.stat[2 * r + 1] : 0.0f;
-        float n1[8], dh[8], n2[8], x[8];
+        if (a.has_post) next1 = a.stat[2 * r];
+    };
+    const int64_t step = gridDim.x * (int64_t)ROWS;
+    int64_t r = blockIdx.x * (int64_t)ROWS + threadIdx.x / P;
+    if (AHEAD && r < a.rows) ask(r);
+    for (; r < a.rows; r += step, turn ^= 1) {
+        if (!AHEAD) ask(r);
+        const float r1 = next1, r2 = next2;
+        float n1[E], dh[E], n2[E], x[E];
         norm_values<P, WIDE>(rb, t, dim, n1);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            n1[j] *= r1;
-            dh[j] = n2[j] = x[j] = 0.0f;
-        }
         if (a.grad_residual_out.p) norm_values<P, WIDE>(rd, t, dim, dh);
+        else
+#pragma unroll
+            for (int j = 0; j < E; ++j) dh[j] = 0.0f;
         if (gate_rows) norm_values<P, WIDE>(rg, t, dim, gate);
         if (a.has_pre) {
             norm_values<P, WIDE>(rh, t, dim, n2);
             norm_values<P, WIDE>(ry, t, dim, x);
+        } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < E; ++j) n2[j] = x[j] = 0.0f;
+        }
+        if (AHEAD && r + step < a.rows) ask(r + step);
+#pragma unroll
+        for (int j = 0; j < E; ++j) n1[j] *= r1;
+        if (a.has_pre) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
                 n2[j] *= r2;
                 sum_pre[j] = fmaf(x[j], n2[j], sum_pre[j]);
                 x[j] *= pre[j];
@@ -269,7 +302,7 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void residual_norm_grad_kernel(c
         }
         float s[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < E; ++j) {
             s[0] = fmaf(x[j], n2[j], s[0]);
             if (a.has_post) {
                 const float w = gate[j] * post[j] * n1[j];
@@ -279,15 +312,15 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void residual_norm_grad_kernel(c
         }
         row_sums<P>(s, tmp[turn][0]);
         const float along2 = r2 * s[0] * each, along1 = a.has_post ? (s[1] - along2 * s[2]) * each * a.block_scale : 0.0f;
-        float out[8];
+        float out[E];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < E; ++j) {
             dh[j] = fmaf(-along2, n2[j], dh[j]);
             out[j] = dh[j] * a.residual_scale;
         }
         if (a.grad_residual.p) norm_store<P, WIDE>(static_cast<R*>(a.grad_residual.p) + r * a.grad_residual.stride, t, dim, out);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < E; ++j) {
             const float du = dh[j] * a.block_scale, dg = du * n1[j] * post[j];
             sum_gate[j] += dg;
             out[j] = dg;
@@ -297,20 +330,20 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void residual_norm_grad_kernel(c
         if (a.grad_gate.p) norm_store<P, WIDE>(static_cast<A*>(a.grad_gate.p) + r * a.grad_gate.stride, t, dim, out);
         if (a.grad_block.p) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) out[j] = r1 * fmaf(-along1, n1[j], dh[j] * post[j]);
+            for (int j = 0; j < E; ++j) out[j] = r1 * fmaf(-along1, n1[j], dh[j] * post[j]);
             norm_store<P, WIDE>(static_cast<A*>(a.grad_block.p) + r * a.grad_block.stride, t, dim, out);
         }
     }
     float* part = a.part + (int64_t)blockIdx.x * 3 * dim;
-    const auto put = [&](int i, const float (&v)[8]) {
+    const auto put = [&](int i, const float (&v)[E]) {
         if (!a.sum[i].p) return;
         if constexpr (ROWS == 1) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
+            for (int j = 0; j < E; ++j)
                 if (norm_column<P, WIDE>(t, j) < dim) part[(int64_t)i * dim + norm_column<P, WIDE>(t, j)] = v[j];
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sums[(threadIdx.x / P * 3 + i) * P * 8 + norm_column<P, WIDE>(t, j)] = v[j];
+            for (int j = 0; j < E; ++j) sums[(threadIdx.x / P * 3 + i) * P * E + norm_column<P, WIDE>(t, j)] = v[j];
         }
     };
     put(0, sum_post);
@@ -322,7 +355,7 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void residual_norm_grad_kernel(c
             if (a.sum[i].p)
                 for (int32_t c = threadIdx.x; c < dim; c += THREADS) {
                     float v = 0.0f;
-                    for (int w = 0; w < ROWS; ++w) v += sums[(w * 3 + i) * P * 8 + c];
+                    for (int w = 0; w < ROWS; ++w) v += sums[(w * 3 + i) * P * E + c];
                     part[(int64_t)i * dim + c] = v;
                 }
     }
@@ -422,10 +455,10 @@ hipError_t launch_residual_norm_grad(const NormGradArgs& a, hipStream_t st) {
                     residual_norm_grad_wide_kernel<A, R><<<parts, 1024, 0, st>>>(a);
                     return hipGetLastError();
                 }
-                return with_threads(a.dim, wide, [&](auto p, auto w) {
+                return with_threads<true>(a.dim, wide, [&](auto p, auto e, auto w) {
                     constexpr int P = decltype(p)::value, THREADS = P < 256 ? 256 : P, ROWS = THREADS / P;
                     parts = (unsigned)std::min<int64_t>((a.rows + ROWS - 1) / ROWS, NORM_PARTS * 256 / THREADS);
-                    residual_norm_grad_kernel<A, R, P, decltype(w)::value><<<parts, THREADS, 0, st>>>(a);
+                    residual_norm_grad_kernel<A, R, P, decltype(e)::value, decltype(w)::value><<<parts, THREADS, 0, st>>>(a);
                     return hipGetLastError();
                 });
             });
