@@ -4,8 +4,9 @@
 // A workgroup keeps 128 rows and goes through its share of the vocabulary, 256 columns at a time.  A lane has four rows, and of
 // each tile 32 logits of every one, all in registers: their largest M, S = sum 2^(k (x - M)) and U = sum 2^(k (x - M)) k (x - M)
 // with k = log2(e) / T join what the lane has from the tiles before, and lanes and waves are joined at the end.  Products of
-// 16-bit floats are exact and summed in 32 bits.  Numbers of 32 bits are taken apart into three of bf16 (24 bits together), and
-// the six products of parts that reach 2^-24 are summed, the smallest first.
+// 16-bit floats are exact and summed in 32 bits.  Numbers of 32 bits, times powers of two that take a row's, or the weights', largest to
+// just below 2^15, are taken apart into two of f16 (22 bits together), and three of the four products are summed, the smallest first.
+// Up to 64 rows they are three of bf16 (24 bits) and six products: that is bound by memory.
 #include <algorithm>
 #include "head_rows.h"
 
@@ -19,6 +20,8 @@ struct HeadStatArgs {
     const int32_t* count;           // NULL: n_rows
     const int32_t* list;            // of the rows, for their tokens; NULL: as they lie
     const int32_t* token;
+    const int32_t* x_exp;           // numbers of 32 bits: of the rows, and of the weights, as launch_lay_rows has them; else NULL
+    const int32_t* w_exp;
     float          k;
     bool           add;             // to what an earlier piece of the vocabulary left
     RowSums*       sums;            // [row][segment]
@@ -46,14 +49,17 @@ __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_stat_kernel(co
     if (first >= n_rows) return;
     const int lane = lane_id(), wave = threadIdx.x / WAVE;
     const int32_t my_row = first + place_b<Q>();        // and the Q - 1 behind it
+    // sums of products of numbers of 32 bits are in units of the row's own: kr takes those to powers of two, as k does logits
     int32_t token[Q];
-    float m[Q], s[Q], u[Q];
+    float m[Q], s[Q], u[Q], kr[Q];
+    const auto unit_of = [&](int32_t r) { return h.x_exp ? h.x_exp[min(r, n_rows - 1)] + *h.w_exp - 30 : 0; };
 #pragma unroll
     for (int j = 0; j < Q; ++j) {
         const int32_t r = my_row + j;
         token[j] = -1;
         if (h.token && r < n_rows) token[j] = h.token[h.list ? h.list[r] : r];
         m[j] = -INFINITY;
+        kr[j] = ldexpf(h.k, unit_of(r));
         s[j] = u[j] = 0.0f;
     }
     Product<T, Q> product;
@@ -87,7 +93,7 @@ __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_stat_kernel(co
                 for (int i = 0; i < Q; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) own = off == (uint32_t)along_a(i, e) ? x[i][e] : own;
-                h.x_token[my_row + j] = own;
+                h.x_token[my_row + j] = ldexpf(own, unit_of(my_row + j));
             }
             if (!whole)
 #pragma unroll
@@ -99,9 +105,9 @@ __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_stat_kernel(co
             for (int i = 0; i < Q; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; e += 2) most = fmaxf(fmaxf(x[i][e], x[i][e + 1]), most);
-            const float base = most > -INFINITY ? most : 0.0f, base2 = base * h.k;
+            const float base = most > -INFINITY ? most : 0.0f, base2 = base * kr[j];
             const bool far = fabsf(base2) >= LOGIT_FAR;
-            const float d0 = fmaxf(less_reference(m[j], h.k, base, base2, far), -1e4f), f = __builtin_amdgcn_exp2f(d0);
+            const float d0 = fmaxf(less_reference(m[j], kr[j], base, base2, far), -1e4f), f = __builtin_amdgcn_exp2f(d0);
             if constexpr (ENTROPY) u[j] = f * (u[j] + d0 * s[j]);
             s[j] *= f;
             m[j] = most;
@@ -111,7 +117,7 @@ __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_stat_kernel(co
                 for (int i = 0; i < Q; ++i) {
                     float d[4], p[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) d[e] = !PLAIN && far ? (x[i][e] - base) * h.k : fmaf(x[i][e], h.k, -base2);
+                    for (int e = 0; e < 4; ++e) d[e] = !PLAIN && far ? (x[i][e] - base) * kr[j] : fmaf(x[i][e], kr[j], -base2);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(d[e]);
 #pragma unroll
@@ -130,10 +136,11 @@ __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_stat_kernel(co
     // (from here on relative to the largest logit itself)
 #pragma unroll
     for (int j = 0; j < Q; ++j) {
-        const float base = m[j] > -INFINITY ? m[j] : 0.0f, base2 = base * h.k;
-        const float d = fabsf(base2) >= LOGIT_FAR ? 0.0f : fmaf(-base, h.k, base2), f = __builtin_amdgcn_exp2f(d);
+        const float base = m[j] > -INFINITY ? m[j] : 0.0f, base2 = base * kr[j];
+        const float d = fabsf(base2) >= LOGIT_FAR ? 0.0f : fmaf(-base, kr[j], base2), f = __builtin_amdgcn_exp2f(d);
         u[j] = f * (u[j] + d * s[j]);
         s[j] *= f;
+        m[j] = ldexpf(m[j], unit_of(my_row + j));
     }
     const auto join = [&](RowSums p, RowSums q) {
         RowSums r = {fmaxf(p.m, q.m), 0.0f, 0.0f};
@@ -179,11 +186,19 @@ __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_logits_kernel(
     const int32_t v = h.v0 + t * SIDE + place_a<Q>(), row = first + place_b<Q>();
 #pragma unroll
     for (int j = 0; j < Q; ++j)
-        if (row + j < h.n_rows)
+        if (row + j < h.n_rows) {
+            const int unit = h.x_exp ? h.x_exp[row + j] + *h.w_exp - 30 : 0;
 #pragma unroll
             for (int i = 0; i < Q; ++i)
                 if (v + along_a(i, 0) < h.vocab_end)         // (the pitch is a multiple of 4)
-                    *reinterpret_cast<f32x4*>(logits + (row + j) * pitch + v + along_a(i, 0)) = acc[i][j];
+                    {
+                    f32x4 x = acc[i][j];
+                    if (h.x_exp)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[e] = ldexpf(x[e], unit);
+                    *reinterpret_cast<f32x4*>(logits + (row + j) * pitch + v + along_a(i, 0)) = x;
+                }
+        }
 }
 
 // ---- few rows: bound by reading the weights ----
@@ -492,7 +507,7 @@ constexpr int64_t HEAD_TOP_ROWS = 256;           // rows whose logits are held a
 constexpr int64_t HEAD_PIECE_BYTES = 256LL << 20;    // of weights laid out at once
 static int32_t weight_piece(const HeadShape& sh, const dc_matrix& w) {
     if (!sh.copy_weight) return (int32_t)w.n_rows;
-    const int64_t row = sh.k_pad * 2LL * (w.type == DC_F32 ? 3 : 1);
+    const int64_t row = sh.k_pad * 2LL * (w.type == DC_F32 ? 2 : 1);
     return (int32_t)std::min<int64_t>(whole(w.n_rows, P_MOST_SIDE), std::max<int64_t>(P_MOST_SIDE, HEAD_PIECE_BYTES / row / P_MOST_SIDE * P_MOST_SIDE));
 }
 
@@ -500,6 +515,7 @@ namespace {
 struct HeadWs {
     char*    hidden; int64_t hidden_plane;
     char*    weight; int64_t weight_plane; int32_t piece;
+    int32_t *x_exp, *w_exp;         // w_exp: one to a piece
     LiveRows live;
     float*   x_token;
     RowSums* sums;
@@ -518,13 +534,15 @@ static HeadWs carve(void* base, const dc_matrix& hidden, const dc_matrix& weight
         at += align256(bytes);
         return p;
     };
-    const int64_t rows = hidden.n_rows, planes = hidden.type == DC_F32 ? 3 : 1;
+    const int64_t rows = hidden.n_rows, planes = hidden.type == DC_F32 ? 2 : 1;
     const bool few = rows <= FEW_ROWS;
     w.hidden_plane = rows * sh.k_pad * 2;
-    w.hidden = take(sh.copy_hidden || few ? planes * w.hidden_plane : 0);
+    w.hidden = take(sh.copy_hidden || few ? (few && planes == 2 ? 3 : planes) * w.hidden_plane : 0);
     w.piece = weight_piece(sh, weight);
     w.weight_plane = (int64_t)w.piece * sh.k_pad * 2;
     w.weight = take(sh.copy_weight && !few ? planes * w.weight_plane : 0);
+    w.x_exp = reinterpret_cast<int32_t*>(take(planes == 2 ? rows * 4 : 0));
+    w.w_exp = reinterpret_cast<int32_t*>(take(planes == 2 && !few ? whole(weight.n_rows, w.piece) / w.piece * 4 : 0));
     w.pitch = whole(weight.n_rows, 4);
     if (few || n_top > 0) {
         w.logits = reinterpret_cast<float*>(take(std::min(rows, HEAD_TOP_ROWS) * w.pitch * 4));
@@ -569,7 +587,7 @@ hipError_t launch_head(const HeadArgs& a, void* d_ws, hipStream_t st) {
         FewArgs f = {a.weight.d_data, a.weight.row_stride, vocab, (int32_t)a.hidden.n_cols, static_cast<const char*>(a.hidden.d_data),
                      a.hidden.row_stride * (type == DC_F32 ? 4 : 2), 0, (int32_t)rows, w.logits, w.pitch};
         if (any) {
-            e = launch_lay_rows(a.hidden, 0, rows, nullptr, nullptr, sh.k_pad, w.hidden, w.hidden_plane, st);
+            e = launch_lay_rows(a.hidden, 0, rows, nullptr, nullptr, sh.k_pad, w.hidden, w.hidden_plane, BF16S, nullptr, nullptr, st);
             f.x = w.hidden;
             f.x_pitch = sh.k_pad * 2;
             f.x_plane = w.hidden_plane;
@@ -580,7 +598,10 @@ hipError_t launch_head(const HeadArgs& a, void* d_ws, hipStream_t st) {
     }
     const bool live = a.n_top == 0 && a.mask;
     if (live) e = launch_live_rows(a.mask, nullptr, nullptr, rows, w.live, st);
+    const bool f32 = type == DC_F32;
+    if (f32 && e == hipSuccess) e = launch_no_exponents(w.w_exp, (vocab + w.piece - 1) / w.piece, st);
     HeadStatArgs h = {};
+    h.x_exp = f32 ? w.x_exp : nullptr;
     h.steps = sh.k_pad / PK;
     h.parts = parts_of(type, w.weight_plane, w.hidden_plane);
     h.k = a.inv_t * LOG2E;
@@ -595,7 +616,8 @@ hipError_t launch_head(const HeadArgs& a, void* d_ws, hipStream_t st) {
     h.list = live ? w.live.list : nullptr;
     h.segments = segments_of(h.row_tiles, (std::min(w.piece, vocab) + side - 1) / side, small ? P_SLOTS<4> : P_SLOTS<8>);
     if (sh.copy_hidden) {
-        if (e == hipSuccess) e = launch_lay_rows(a.hidden, 0, rows, h.list, h.count, sh.k_pad, w.hidden, w.hidden_plane, st);
+        if (e == hipSuccess && f32) e = launch_row_exponents(a.hidden, rows, h.list, h.count, w.x_exp, st);
+        if (e == hipSuccess) e = launch_lay_rows(a.hidden, 0, rows, h.list, h.count, sh.k_pad, w.hidden, w.hidden_plane, F16S, w.x_exp, nullptr, st);
         h.x = Operand{w.hidden, sh.k_pad * 2, nullptr};
     } else {
         h.x = Operand{static_cast<const char*>(a.hidden.d_data), a.hidden.row_stride * 2, h.list};
@@ -608,7 +630,10 @@ hipError_t launch_head(const HeadArgs& a, void* d_ws, hipStream_t st) {
         for (int32_t v0 = 0; v0 < vocab && e == hipSuccess; v0 += w.piece) {
             const int32_t n = std::min(w.piece, vocab - v0);
             if (sh.copy_weight) {
-                e = launch_lay_rows(a.weight, v0, n, nullptr, nullptr, sh.k_pad, w.weight, w.weight_plane, st);
+                h.w_exp = w.w_exp + v0 / w.piece;
+                if (f32 && r0 == 0) e = launch_top_exponent(a.weight, v0, n, w.w_exp + v0 / w.piece, st);
+                if (e == hipSuccess)
+                    e = launch_lay_rows(a.weight, v0, n, nullptr, nullptr, sh.k_pad, w.weight, w.weight_plane, F16S, nullptr, h.w_exp, st);
                 h.w = Operand{w.weight, sh.k_pad * 2, nullptr};
             } else {
                 h.w = Operand{static_cast<const char*>(a.weight.d_data), a.weight.row_stride * 2, nullptr};
@@ -628,7 +653,7 @@ hipError_t launch_head(const HeadArgs& a, void* d_ws, hipStream_t st) {
             const auto with_q = [&](auto t) {
                 if (small) go(t, std::integral_constant<int, 4>{}); else go(t, std::integral_constant<int, 8>{});
             };
-            if (type == DC_F16) with_q(_Float16{}); else with_q(__bf16{});
+            if (type == DC_BF16) with_q(__bf16{}); else with_q(_Float16{});
             e = hipGetLastError();
         }
         if (a.n_top == 0) break;
@@ -645,6 +670,7 @@ hipError_t launch_head(const HeadArgs& a, void* d_ws, hipStream_t st) {
         o.top_logprob = from(a.top_logprob, a.n_top);
         if (e == hipSuccess) e = launch_logprob(o, DC_F32, w.logprob, st);
         h.x.p += HEAD_TOP_ROWS * h.x.pitch;
+        if (f32) h.x_exp += HEAD_TOP_ROWS;
     }
     if (e != hipSuccess || a.n_top > 0) return e;
     head_join_kernel<<<(unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 16), 256, 0, st>>>(out, live ? w.live.pos : nullptr, h.segments,

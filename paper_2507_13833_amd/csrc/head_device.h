@@ -59,8 +59,10 @@ struct Operand {
     const int32_t* list;            // which rows, by their numbers (the last one's end below 4 GB then); NULL: as they lie
 };
 constexpr int64_t P_MOST_PITCH = 1 << 23;
+// Second planes of f16 hold what the first leave off times so much: as exact down to 2^-28 of the largest value as near it.
+constexpr float SMALL_PART = 2048.0f;
 // The sum goes over n parts of `steps` times PK elements each: part i multiplies plane (a >> 2 i) % 4 of A, planes a_plane bytes apart,
-// by plane (b >> 2 i) % 4 of B.
+// by plane (b >> 2 i) % 4 of B.  All but the last hold one second plane.
 struct Parts { int32_t n; uint32_t a, b; int64_t a_plane, b_plane; };
 
 typedef const __attribute__((address_space(1))) void GlobalVoid;
@@ -194,31 +196,49 @@ struct Product {
 #pragma unroll
             for (int j = 0; j < Q; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
         settle_sums();
-        const int32_t all = steps * parts.n, first = stage - 2;
-        for (int32_t s = first; s < first + all; ++s) {
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int q = 0; q < 2 * Q; ++q) {    // half a row of places to a read
-#pragma unroll
-                for (int e = 0; e < Q / 2; ++e) Mfma<T>::add(fa[0][q / 2], fb[0][q % 2 * (Q / 2) + e], acc[q / 2][q % 2 * (Q / 2) + e]);
-                // (the first products of the next half want all of B and the first of A)
-                if (q < Q) read_b(s, 1, q); else read_a(s, 1, q - Q);
+        int32_t s = stage - 2;
+        const int32_t end = s + steps * parts.n;
+        const auto run = [&](int32_t to) {
+            for (; s < to; ++s) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 __builtin_amdgcn_sched_barrier(0);
-            }
-            wait_loads<0>();
-            bare_barrier();
-            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int q = 0; q < 2 * Q; ++q) {
+                for (int q = 0; q < 2 * Q; ++q) {    // half a row of places to a read
 #pragma unroll
-                for (int e = 0; e < Q / 2; ++e) Mfma<T>::add(fa[1][q / 2], fb[1][q % 2 * (Q / 2) + e], acc[q / 2][q % 2 * (Q / 2) + e]);
-                if (q < Q) ask_a(q); else ask_b(q - Q);
-                if (q < Q) read_b(s + 1, 0, q); else read_a(s + 1, 0, q - Q);
+                    for (int e = 0; e < Q / 2; ++e) Mfma<T>::add(fa[0][q / 2], fb[0][q % 2 * (Q / 2) + e], acc[q / 2][q % 2 * (Q / 2) + e]);
+                    // (the first products of the next half want all of B and the first of A)
+                    if (q < Q) read_b(s, 1, q); else read_a(s, 1, q - Q);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                wait_loads<0>();
+                bare_barrier();
                 __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int q = 0; q < 2 * Q; ++q) {
+#pragma unroll
+                    for (int e = 0; e < Q / 2; ++e) Mfma<T>::add(fa[1][q / 2], fb[1][q % 2 * (Q / 2) + e], acc[q / 2][q % 2 * (Q / 2) + e]);
+                    if (q < Q) ask_a(q); else ask_b(q - Q);
+                    if (q < Q) read_b(s + 1, 0, q); else read_a(s + 1, 0, q - Q);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                asked(next);
             }
-            asked(next);
+        };
+        if (parts.n > 1) {                       // the small parts' products are SMALL_PART times too large
+            run(end - steps);
+            settle_sums();
+#pragma unroll
+            for (int i = 0; i < Q; ++i)
+#pragma unroll
+                for (int j = 0; j < Q; ++j) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j][e] = sum_of(acc[i][j][e]) * (1.0f / SMALL_PART);
+                    asm volatile("" : "+a"(acc[i][j]));              // (back where they belong, four at a time)
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            settle_sums();
         }
+        run(end);
         settle_sums();
     }
 
@@ -264,7 +284,7 @@ __device__ __forceinline__ TilePair tile_pair(int32_t at, int32_t first, int32_t
 
 // ---- operands laid out for the product ----
 
-// The first of how many 16-bit numbers a value is taken apart into: together they are it, to 8 or 11 bits a number.
+// The first of how many 16-bit numbers a value is taken apart into, 11 (f16) or 8 (bf16) bits each; rest: what the next are made of.
 template <typename D>
 __device__ __forceinline__ D take_part(float& rest) {
     D d = (D)rest;
@@ -272,7 +292,53 @@ __device__ __forceinline__ D take_part(float& rest) {
     if constexpr (std::is_same_v<D, __bf16>)
         if (fabsf(rest) < INFINITY && fabsf((float)d) == INFINITY) d = __builtin_bit_cast(__bf16, (uint16_t)(__float_as_uint(rest) >> 16));
     rest = fabsf(rest) < INFINITY ? rest - (float)d : 0.0f;
+    if constexpr (std::is_same_v<D, _Float16>) rest *= SMALL_PART;
     return d;
+}
+
+// ---- powers of two of operands ----
+
+constexpr int NO_EXPONENT = -100000;
+__device__ __forceinline__ int exponent_above(float magnitude) { return (int)(__float_as_uint(magnitude) >> 23) - 126; }     // 2^it is above
+// A wave's largest finite magnitude of a row, as bits (those of a float without a sign sort like it).
+template <typename T>
+__device__ __forceinline__ uint32_t row_top(const T* row, int32_t cols) {
+    constexpr int N = 16 / sizeof(T);
+    const int lane = lane_id();
+    uint32_t big = 0;
+    const auto one = [&](T v) {
+        const uint32_t bits = __float_as_uint(fabsf((float)v));
+        big = max(big, bits < 0x7F800000u ? bits : 0u);
+    };
+    const int32_t head = min(cols, (int32_t)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int32_t)sizeof(T)), chunks = (cols - head) / N;
+    if (lane < head) one(row[lane]);
+    const u32x4* body = reinterpret_cast<const u32x4*>(row + head);
+    for (int32_t c = lane; c < chunks; c += 4 * WAVE) {
+        union { u32x4 q; T e[N]; } in[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) in[j].q = body[min(c + j * WAVE, chunks - 1)];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < N; ++i) one(in[j].e[i]);
+    }
+    if (head + chunks * N + lane < cols) one(row[head + chunks * N + lane]);
+    return big;
+}
+__device__ __forceinline__ uint32_t wave_top(uint32_t big) {
+#pragma unroll
+    for (int d = 1; d < WAVE; d <<= 1) big = max(big, (uint32_t)__shfl_xor((int)big, d));
+    return big;
+}
+// The largest of the four waves' exponents goes to *top: one atomic a workgroup, and few of those (8192 waves' own took 98 us).
+constexpr int64_t TOP_BLOCKS = 512;
+__device__ __forceinline__ void raise_top(int most, int* tmp, int32_t* top) {
+    if (lane_id() == 0) tmp[threadIdx.x / WAVE] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        most = max(max(tmp[0], tmp[1]), max(tmp[2], tmp[3]));
+        if (most != NO_EXPONENT) atomicMax(top, most);
+    }
 }
 
 }  // namespace dc

@@ -6,11 +6,11 @@
 // the workspace once along the rows and once along the vocabulary; two products of matrices read it there.  Rows that add nothing
 // (masked, or a = b = 0) take part in none of it: the live rows are numbered first.
 //
-// 16-bit operands: G, the weights and the hidden states are held in f16 (11 bits, three more than bf16's), each times a power of
-// two that takes its largest magnitude to just below 2^15: per row for G (from |a|, |b| and H, which bound it), undone in the row's
-// hidden gradient and in the row's hidden state, per piece for the weights.  G in one f16 is off by at most 2^-11 of each value,
-// before sums of 32 bits that are rounded to 16 bits themselves; a gradient of the weights in 32 bits takes G in two (2^-22).
-// Numbers of 32 bits are taken apart into three of bf16 everywhere, as in the forward direction.
+// G, the weights and the hidden states are held in f16 (11 bits, three more than bf16's), each times a power of two that takes its
+// largest magnitude to just below 2^15: per row for G (from |a|, |b| and H, which bound it), undone in the row's hidden gradient and in
+// the row's hidden state, per piece for the weights.  G in one f16 is off by at most 2^-11 of each value, before sums of 32 bits that are
+// rounded to 16 bits themselves; for a gradient of the weights in 32 bits it takes two (2^-22).  Operands of 32 bits are two f16 as
+// well, and three of the four products of their parts are summed (the fourth is 2^-22).
 #include <algorithm>
 #include "head_rows.h"
 
@@ -18,53 +18,10 @@ namespace dc {
 
 // ---- per row ----
 
-constexpr int NO_EXPONENT = -100000;
-__device__ __forceinline__ int exponent_above(float magnitude) {         // 2^it is above; infinities and NaN: 129
-    return (int)(__float_as_uint(magnitude) >> 23) - 126;
-}
-
-// A wave's largest magnitude of a row, as bits (those of a float without a sign sort like it).
-template <typename T>
-__device__ __forceinline__ uint32_t row_top(const T* row, int32_t cols) {
-    constexpr int N = 16 / sizeof(T);
-    const int lane = lane_id();
-    uint32_t big = 0;
-    const auto one = [&](T v) { big = max(big, __float_as_uint(fabsf((float)v))); };
-    const int32_t head = min(cols, (int32_t)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int32_t)sizeof(T)), chunks = (cols - head) / N;
-    if (lane < head) one(row[lane]);
-    const u32x4* body = reinterpret_cast<const u32x4*>(row + head);
-    for (int32_t c = lane; c < chunks; c += 4 * WAVE) {
-        union { u32x4 q; T e[N]; } in[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) in[j].q = body[min(c + j * WAVE, chunks - 1)];
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int i = 0; i < N; ++i) one(in[j].e[i]);
-    }
-    if (head + chunks * N + lane < cols) one(row[head + chunks * N + lane]);
-    return big;
-}
-__device__ __forceinline__ uint32_t wave_top(uint32_t big) {
-#pragma unroll
-    for (int d = 1; d < WAVE; d <<= 1) big = max(big, (uint32_t)__shfl_xor((int)big, d));
-    return big;
-}
-// The largest of the four waves' exponents goes to *top: one atomic a workgroup, and few of those (8192 waves' own took 98 us).
-constexpr int64_t TOP_BLOCKS = 512;
-__device__ __forceinline__ void raise_top(int most, int* tmp, int32_t* top) {
-    if (lane_id() == 0) tmp[threadIdx.x / WAVE] = most;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        most = max(max(tmp[0], tmp[1]), max(tmp[2], tmp[3]));
-        if (most != NO_EXPONENT) atomicMax(top, most);
-    }
-}
-
 struct TermArgs {
     const void*    x;
     int64_t        stride, n_rows;
-    int32_t        dim, vocab, scaled;           // scaled: operands have powers of two of their own
+    int32_t        dim, vocab;
     float          inv_t;
     const int32_t* token;
     const float*   stat;
@@ -73,13 +30,10 @@ struct TermArgs {
     const float*   b;
     const int32_t* pos;
     RowTerm*       term;
+    int32_t*       x_exp;
     int32_t*       top;             // [0]: of the hidden states, [1 ..]: of the pieces of the weights
     int32_t*       status;
 };
-
-__global__ __launch_bounds__(256) void no_exponents_kernel(int32_t* top, int32_t n) {
-    for (int32_t i = threadIdx.x; i < n; i += 256) top[i] = NO_EXPONENT;
-}
 
 // A wave per row.
 template <typename T>
@@ -91,16 +45,13 @@ __global__ __launch_bounds__(256) void head_terms_kernel(const TermArgs t) {
         const int32_t at = t.pos[r];
         if (at < 0) continue;
         const float a = t.a[r] * t.inv_t, b = t.b ? t.b[r] * t.inv_t : 0.0f, h = b != 0.0f ? t.entropy[r] : 0.0f;
-        int e = 0;
-        if (t.scaled) {
-            // |p (log p + H)| <= max(1 / e, H)
-            const float bound = fabsf(a) + fabsf(b) * (fabsf(h) + 1.0f);
-            e = max(-120, min(100, 14 - exponent_above(bound)));
-            if (!(bound < INFINITY)) e = 0;
-            const uint32_t big = wave_top(row_top(static_cast<const T*>(t.x) + r * t.stride, t.dim));
-            most = max(most, exponent_above(__uint_as_float(big)) - e);
-        }
+        // |p (log p + H)| <= max(1 / e, H)
+        const float bound = fabsf(a) + fabsf(b) * (fabsf(h) + 1.0f);
+        const int e = bound < INFINITY ? max(-120, min(100, 14 - exponent_above(bound))) : 0;
+        const int x_exp = exponent_above(__uint_as_float(wave_top(row_top(static_cast<const T*>(t.x) + r * t.stride, t.dim))));
+        most = max(most, x_exp - e);
         if (lane == 0) {
+            t.x_exp[at] = x_exp;
             int32_t token = -1;
             if (t.token) {
                 token = t.token[r];
@@ -110,19 +61,10 @@ __global__ __launch_bounds__(256) void head_terms_kernel(const TermArgs t) {
                 }
             }
             t.term[at] = RowTerm{t.stat[2 * r], t.stat[2 * r + 1] * LOG2E, ldexpf(b != 0.0f ? -fmaf(b, h, a) : -a, e), ldexpf(-b * LN2, e),
-                                 ldexpf(a, e), token, e, 0};
+                                 ldexpf(a, e), token, e, x_exp};
         }
     }
-    if (t.scaled) raise_top(most, tmp, t.top);
-}
-
-// The largest magnitude of a piece of the weights.
-template <typename T>
-__global__ __launch_bounds__(256) void head_top_kernel(const T* w, int64_t stride, int64_t rows, int32_t cols, int32_t* top) {
-    __shared__ int tmp[4];
-    uint32_t big = 0;
-    for (int64_t r = blockIdx.x * 4LL + threadIdx.x / WAVE; r < rows; r += gridDim.x * 4LL) big = max(big, row_top(w + r * stride, cols));
-    raise_top(exponent_above(__uint_as_float(wave_top(big))), tmp, top);
+    raise_top(most, tmp, t.top);
 }
 
 // ---- G of a piece ----
@@ -133,14 +75,15 @@ struct HeadPieceArgs {
     int32_t        steps, v0, vocab_end, tiles, row_tiles;
     const int32_t* count;
     const RowTerm* term;
+    const int32_t* w_top;           // numbers of 32 bits: of the weights; the rows' own are in their terms
     float          k;
     char*          g;               // [plane][row][width], NULL: not wanted
     char*          gt;              // [plane][vocabulary entry][rows_pad], NULL: not wanted
     int64_t        width, rows_pad;
 };
 
-// T: of the operands, D: of G; PLANES of it along the vocabulary (gt) and, for bf16, along the rows too (f16: one there).
-template <typename T, typename D, int PLANES, int Q>
+// T: of the operands.  PLANES of G along the vocabulary (gt), ROW_PLANES along the rows.
+template <typename T, int PLANES, int ROW_PLANES, int Q>
 __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_piece_kernel(const HeadPieceArgs h) {
     constexpr int SIDE = P_SIDE<Q>;
     __shared__ __attribute__((aligned(1024))) char lds[P_LDS<Q>];
@@ -156,7 +99,8 @@ __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_piece_kernel(c
         product<T, Q>(acc, a, b, h.parts, h.steps, lds);
     }
     const int32_t u = t * SIDE + place_a<Q>(), row = first + place_b<Q>();
-    constexpr int ROW_PLANES = std::is_same_v<D, _Float16> ? 1 : PLANES;
+    using D = _Float16;
+    const int w_exp = h.w_top ? *h.w_top - 30 : 0;
     const int64_t g_plane = h.width * h.rows_pad * 2;
     // whole: all of the tile's rows and entries are there
     const auto put = [&](auto whole) {
@@ -164,6 +108,9 @@ __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_piece_kernel(c
         RowTerm of[Q];
 #pragma unroll
         for (int j = 0; j < Q; ++j) of[j] = h.term[WHOLE ? row + j : min(row + j, n_rows - 1)];
+        float unit[Q];                               // of the row's sums
+#pragma unroll
+        for (int j = 0; j < Q; ++j) unit[j] = h.w_top ? ldexpf(1.0f, of[j].x_exp + w_exp) : 1.0f;
 #pragma unroll
         for (int i = 0; i < Q; i += 2) {
             // eight entries of Q rows
@@ -173,7 +120,7 @@ __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_piece_kernel(c
             for (int j = 0; j < Q; ++j) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float l2 = fmaf(acc[i + e / 4][j][e % 4] - of[j].m, h.k, -of[j].l2), p = __builtin_amdgcn_exp2f(l2);
+                    const float l2 = fmaf(fmaf(acc[i + e / 4][j][e % 4], unit[j], -of[j].m), h.k, -of[j].l2), p = __builtin_amdgcn_exp2f(l2);
                     f[e][j] = p * fmaf(of[j].c1, WHOLE ? l2 : fmaxf(l2, -1e4f), of[j].c0);
                 }
                 const uint32_t own = (uint32_t)(of[j].token - h.v0 - v);
@@ -223,7 +170,7 @@ struct HeadHiddenArgs {             // slab[split][row][col] (+)= sum over this 
     float*         slab;
     int64_t        rows_pad, pitch;
 };
-template <typename D, int Q>
+template <int Q>
 __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_hidden_kernel(const HeadHiddenArgs h) {
     constexpr int SIDE = P_SIDE<Q>;
     __shared__ __attribute__((aligned(1024))) char lds[P_LDS<Q>];
@@ -240,9 +187,9 @@ __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_hidden_kernel(
         place_tile(b, h.g, first, n_rows);
         a.base += from * (PK * 2LL);
         b.base += from * (PK * 2LL);
-        product<D, Q>(acc, a, b, h.parts, max(steps, 0), lds);
+        product<_Float16, Q>(acc, a, b, h.parts, max(steps, 0), lds);
     }
-    const int up = std::is_same_v<D, _Float16> ? *h.top - 15 : 0;
+    const int up = *h.top - 15;
     const int32_t col = tile * SIDE + place_a<Q>(), row = first + place_b<Q>();
 #pragma unroll
     for (int j = 0; j < Q; ++j)
@@ -291,7 +238,7 @@ struct HeadWeightArgs {             // grad_weight[v0 + row of gt][col] (+)= sum
     void*          out;             // of the piece's first entry
     int64_t        stride;
 };
-template <typename D, typename T, int Q>
+template <typename T, int Q>
 __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_weight_kernel(const HeadWeightArgs h) {
     constexpr int SIDE = P_SIDE<Q>;
     __shared__ __attribute__((aligned(1024))) char lds[P_LDS<Q>];
@@ -303,9 +250,9 @@ __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_weight_kernel(
         TileOfB<Q> b;
         place_tile(a, h.xt, tile * SIDE, h.dim);
         place_tile(b, h.gt, first, h.n);
-        product<D, Q>(acc, a, b, h.parts, (*h.count + PK - 1) / PK, lds);
+        product<_Float16, Q>(acc, a, b, h.parts, (*h.count + PK - 1) / PK, lds);
     }
-    const int up = std::is_same_v<D, _Float16> ? *h.top - 15 : 0;
+    const int up = *h.top - 15;
     const int32_t col = tile * SIDE + place_a<Q>(), row = first + place_b<Q>();
 #pragma unroll
     for (int j = 0; j < Q; ++j) {
@@ -348,6 +295,7 @@ namespace {
 struct HeadGradWs {
     LiveRows live;
     RowTerm* term;
+    int32_t* x_exp;
     int32_t* top;
     int32_t  pieces, piece;         // entries of the vocabulary to a piece, a multiple of P_MOST_SIDE
     char*    hidden; int64_t hidden_plane;
@@ -374,12 +322,13 @@ static HeadGradWs carve_grad(void* base, const dc_matrix& hidden, const dc_matri
         return p;
     };
     const bool f32 = hidden.type == DC_F32;
-    const int64_t rows = hidden.n_rows, dim = hidden.n_cols, planes = f32 ? 3 : 1, g_planes = f32 ? 3 : grad_weight_type == DC_F32 ? 2 : 1;
+    const int64_t rows = hidden.n_rows, dim = hidden.n_cols, planes = f32 ? 2 : 1, g_planes = grad_weight_type == DC_F32 ? 2 : 1;
     const int64_t vocab_pad = whole(weight.n_rows, P_MOST_SIDE);
     w.live.list = reinterpret_cast<int32_t*>(take(rows * 4));
     w.live.pos = reinterpret_cast<int32_t*>(take(rows * 4));
     w.live.count = reinterpret_cast<int32_t*>(take(4));
     w.term = reinterpret_cast<RowTerm*>(take(rows * (int64_t)sizeof(RowTerm)));
+    w.x_exp = reinterpret_cast<int32_t*>(take(rows * 4));
     w.top = reinterpret_cast<int32_t*>(take((vocab_pad / P_MOST_SIDE + 1) * 4));
     const int64_t area = g_area(sh.rows_pad, vocab_pad);
     // (the weights laid out along the columns: at most HG_AREA elements too)
@@ -398,7 +347,7 @@ static HeadGradWs carve_grad(void* base, const dc_matrix& hidden, const dc_matri
     w.wt_plane = dim * w.piece * 2;
     w.wt = take(planes * dim * widest * 2);
     w.g_plane = sh.rows_pad * w.piece * 2;
-    w.g = take((f32 ? 3 : 1) * area * 2);
+    w.g = take(planes * area * 2);
     w.gt = take(g_planes * area * 2);
     w.pitch = whole(dim, 4);
     w.cut_hidden = cut_product(rows, dim, w.piece / PK * parts_of(hidden.type, 0, 0).n, HG_MOST_SPLITS);
@@ -433,11 +382,11 @@ hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
     const bool f32 = type == DC_F32;
     hipError_t e = launch_live_rows(a.mask, a.grad_logprob, a.grad_entropy, rows, w.live, st);
     if (e != hipSuccess) return e;
-    no_exponents_kernel<<<1, 256, 0, st>>>(w.top, w.pieces + 1);
-    const TermArgs t = {a.hidden.d_data, a.hidden.row_stride, rows, dim, vocab, !f32, a.inv_t, a.token, a.stat, a.entropy,
-                        a.grad_logprob, a.grad_entropy, w.live.pos, w.term, w.top, a.status};
+    e = launch_no_exponents(w.top, w.pieces + 1, st);
+    const TermArgs t = {a.hidden.d_data, a.hidden.row_stride, rows, dim, vocab, a.inv_t, a.token, a.stat, a.entropy,
+                        a.grad_logprob, a.grad_entropy, w.live.pos, w.term, w.x_exp, w.top, a.status};
     const unsigned waves4 = (unsigned)std::min<int64_t>((rows + 3) / 4, TOP_BLOCKS);
-    e = with_type(type, [&](auto el) {
+    if (e == hipSuccess) e = with_type(type, [&](auto el) {
         head_terms_kernel<typename decltype(el)::type><<<waves4, 256, 0, st>>>(t);
         return hipGetLastError();
     });
@@ -452,15 +401,13 @@ hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
     p.width = w.piece;
     p.rows_pad = sh.rows_pad;
     if (sh.copy_hidden) {
-        if (e == hipSuccess) e = launch_lay_rows(a.hidden, 0, rows, w.live.list, w.live.count, sh.k_pad, w.hidden, w.hidden_plane, st);
+        if (e == hipSuccess) e = launch_lay_rows(a.hidden, 0, rows, w.live.list, w.live.count, sh.k_pad, w.hidden, w.hidden_plane, F16S, w.x_exp, nullptr, st);
         p.x = Operand{w.hidden, sh.k_pad * 2, nullptr};
     } else {
         p.x = Operand{static_cast<const char*>(a.hidden.d_data), a.hidden.row_stride * 2, w.live.list};
     }
-    const int32_t* const top_x = f32 ? nullptr : w.top;
     if (gw.d_data && e == hipSuccess)
-        e = launch_lay_columns(a.hidden, 0, rows, w.live.list, w.live.count, f32 ? 3 : 1, sh.rows_pad, top_x, f32 ? nullptr : w.term, w.xt,
-                               w.xt_plane, st);
+        e = launch_lay_columns(a.hidden, 0, rows, w.live.list, w.live.count, sh.rows_pad, w.top, w.term, w.xt, w.xt_plane, st);
     HeadHiddenArgs hh = {};
     hh.wt = Operand{w.wt, w.piece * 2LL, nullptr};
     hh.g = Operand{w.g, w.piece * 2LL, nullptr};
@@ -482,30 +429,22 @@ hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
     if (two) hw.parts = Parts{2, 0, 1, 0, w.g_plane};        // the small one first
     hw.dim = dim;
     hw.count = w.live.count;
-    hw.top = top_x;
+    hw.top = w.top;
     hw.add = a.accumulate;
     hw.stride = gw.row_stride;
     const int64_t out_bytes = gw.type == DC_F32 ? 4 : 2;
     for (int32_t i = 0; i < w.pieces && e == hipSuccess; ++i) {
         const int32_t v0 = i * w.piece, n = std::min(w.piece, vocab - v0);
-        const int32_t* const top_w = f32 ? nullptr : w.top + 1 + i;
-        if (gh.d_data) {
-            if (!f32)
-                e = with_type(type, [&](auto el) {
-                    using T = typename decltype(el)::type;
-                    head_top_kernel<T><<<(unsigned)std::min<int64_t>(TOP_BLOCKS, (n + 3) / 4), 256, 0, st>>>(
-                        static_cast<const T*>(a.weight.d_data) + v0 * a.weight.row_stride, a.weight.row_stride, n, dim, w.top + 1 + i);
-                    return hipGetLastError();
-                });
-            if (e == hipSuccess)
-                e = launch_lay_columns(a.weight, v0, n, nullptr, nullptr, f32 ? 3 : 1, w.piece, top_w, nullptr, w.wt, w.wt_plane, st);
-        }
+        int32_t* const top_w = w.top + 1 + i;
+        if (gh.d_data || f32) e = launch_top_exponent(a.weight, v0, n, top_w, st);
+        if (gh.d_data && e == hipSuccess) e = launch_lay_columns(a.weight, v0, n, nullptr, nullptr, w.piece, top_w, nullptr, w.wt, w.wt_plane, st);
         if (sh.copy_weight) {
-            if (e == hipSuccess) e = launch_lay_rows(a.weight, v0, n, nullptr, nullptr, sh.k_pad, w.weight, w.weight_plane, st);
+            if (e == hipSuccess) e = launch_lay_rows(a.weight, v0, n, nullptr, nullptr, sh.k_pad, w.weight, w.weight_plane, F16S, nullptr, top_w, st);
             p.w = Operand{w.weight, sh.k_pad * 2, nullptr};
         } else {
             p.w = Operand{static_cast<const char*>(a.weight.d_data) + v0 * a.weight.row_stride * 2, a.weight.row_stride * 2, nullptr};
         }
+        p.w_top = f32 ? top_w : nullptr;
         if (e != hipSuccess) break;
         p.v0 = v0;
         p.vocab_end = v0 + n;
@@ -513,31 +452,27 @@ hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
                    small_weight = cut_product(n, dim, sh.rows_pad / PK * hw.parts.n, 1).small;
         p.tiles = tiles_of(n, small_piece);
         p.row_tiles = tiles_of(rows, small_piece);
-        const auto piece = [&](auto t, auto d, auto planes) {
+        const auto piece = [&](auto t, auto planes, auto row_planes) {
             using T = decltype(t);
-            using D = decltype(d);
-            constexpr int PLANES = decltype(planes)::value;
+            constexpr int PLANES = decltype(planes)::value, ROW_PLANES = decltype(row_planes)::value;
             const unsigned blocks = (unsigned)(p.row_tiles * p.tiles);
-            if (small_piece) head_piece_kernel<T, D, PLANES, 4><<<blocks, P_THREADS, 0, st>>>(p);
-            else head_piece_kernel<T, D, PLANES, 8><<<blocks, P_THREADS, 0, st>>>(p);
+            if (small_piece) head_piece_kernel<T, PLANES, ROW_PLANES, 4><<<blocks, P_THREADS, 0, st>>>(p);
+            else head_piece_kernel<T, PLANES, ROW_PLANES, 8><<<blocks, P_THREADS, 0, st>>>(p);
         };
-        using std::integral_constant;
-        if (f32) piece(__bf16{}, __bf16{}, integral_constant<int, 3>{});
-        else if (type == DC_BF16 && two) piece(__bf16{}, _Float16{}, integral_constant<int, 2>{});
-        else if (type == DC_BF16) piece(__bf16{}, _Float16{}, integral_constant<int, 1>{});
-        else if (two) piece(_Float16{}, _Float16{}, integral_constant<int, 2>{});
-        else piece(_Float16{}, _Float16{}, integral_constant<int, 1>{});
+        using One = std::integral_constant<int, 1>;
+        using Two = std::integral_constant<int, 2>;
+        if (f32) piece(_Float16{}, Two{}, Two{});
+        else if (type == DC_BF16 && two) piece(__bf16{}, Two{}, One{});
+        else if (type == DC_BF16) piece(__bf16{}, One{}, One{});
+        else if (two) piece(_Float16{}, Two{}, One{});
+        else piece(_Float16{}, One{}, One{});
         if (gh.d_data) {
             hh.steps = (n + PK - 1) / PK;
             hh.top = top_w;
             hh.add = i > 0;
             const unsigned b = (unsigned)(hh.row_tiles * hh.col_tiles * hh.splits);
-            const auto go = [&](auto d) {
-                using D = decltype(d);
-                if (w.cut_hidden.small) head_hidden_kernel<D, 4><<<b, P_THREADS, 0, st>>>(hh);
-                else head_hidden_kernel<D, 8><<<b, P_THREADS, 0, st>>>(hh);
-            };
-            if (f32) go(__bf16{}); else go(_Float16{});
+            if (w.cut_hidden.small) head_hidden_kernel<4><<<b, P_THREADS, 0, st>>>(hh);
+            else head_hidden_kernel<8><<<b, P_THREADS, 0, st>>>(hh);
         }
         if (gw.d_data) {
             hw.n = n;
@@ -547,12 +482,8 @@ hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
             const unsigned b = (unsigned)(hw.row_tiles * hw.col_tiles);
             e = with_type(gw.type, [&](auto el) {
                 using T = typename decltype(el)::type;
-                const auto go = [&](auto d) {
-                    using D = decltype(d);
-                    if (small_weight) head_weight_kernel<D, T, 4><<<b, P_THREADS, 0, st>>>(hw);
-                    else head_weight_kernel<D, T, 8><<<b, P_THREADS, 0, st>>>(hw);
-                };
-                if (f32) go(__bf16{}); else go(_Float16{});
+                if (small_weight) head_weight_kernel<T, 4><<<b, P_THREADS, 0, st>>>(hw);
+                else head_weight_kernel<T, 8><<<b, P_THREADS, 0, st>>>(hw);
                 return hipGetLastError();
             });
         }

@@ -35,7 +35,8 @@ HeadShape head_shape(const dc_matrix& hidden, const dc_matrix& weight, bool list
 // A thread takes eight neighbouring columns.  Bound by the bytes; sources of any alignment are read an element at a time.
 template <typename S, typename D, int PARTS>
 __global__ __launch_bounds__(256) void lay_rows_kernel(const S* src, int64_t stride, int64_t first, int64_t n, int32_t cols,
-                                                       const int32_t* list, const int32_t* count, int32_t k_pad, char* dst, int64_t plane) {
+                                                       const int32_t* list, const int32_t* count, int32_t k_pad, char* dst, int64_t plane,
+                                                       const int32_t* row_exp, const int32_t* all_exp) {
     const int64_t rows = count ? *count : n;
     const int32_t each = k_pad / 8;
     for (int64_t q = blockIdx.x * 256LL + threadIdx.x; q < rows * each; q += gridDim.x * 256LL) {
@@ -53,6 +54,11 @@ __global__ __launch_bounds__(256) void lay_rows_kernel(const S* src, int64_t str
 #pragma unroll
             for (int j = 0; j < 8; ++j) f[j] = c + j < cols ? (float)from[j] : 0.0f;
         }
+        if constexpr (PARTS == 2) {
+            const int up = 15 - (row_exp ? row_exp[r] : *all_exp);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = ldexpf(f[j], up);
+        }
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
             Raw8<D> out;
@@ -67,23 +73,69 @@ __global__ __launch_bounds__(256) void lay_rows_kernel(const S* src, int64_t str
 }
 
 hipError_t launch_lay_rows(const dc_matrix& src, int64_t first, int64_t n, const int32_t* list, const int32_t* count, int32_t k_pad,
-                           char* dst, int64_t plane, hipStream_t st) {
+                           char* dst, int64_t plane, Apart apart, const int32_t* row_exp, const int32_t* all_exp, hipStream_t st) {
     const int64_t blocks = std::min<int64_t>((n * (k_pad / 8) + 255) / 256, 8192);
     if (blocks == 0) return hipSuccess;
     const auto go = [&](auto s, auto d, auto parts) {
         using S = decltype(s);
         lay_rows_kernel<S, decltype(d), decltype(parts)::value><<<(unsigned)blocks, 256, 0, st>>>(
-            static_cast<const S*>(src.d_data), src.row_stride, first, n, (int32_t)src.n_cols, list, count, k_pad, dst, plane);
+            static_cast<const S*>(src.d_data), src.row_stride, first, n, (int32_t)src.n_cols, list, count, k_pad, dst, plane, row_exp, all_exp);
     };
-    if (src.type == DC_F32) go(float{}, __bf16{}, std::integral_constant<int, 3>{});
+    if (src.type == DC_F32 && apart == F16S) go(float{}, _Float16{}, std::integral_constant<int, 2>{});
+    else if (src.type == DC_F32) go(float{}, __bf16{}, std::integral_constant<int, 3>{});
     else if (src.type == DC_BF16) go(__bf16{}, __bf16{}, std::integral_constant<int, 1>{});
     else go(_Float16{}, _Float16{}, std::integral_constant<int, 1>{});
     return hipGetLastError();
 }
 
+// ---- powers of two ----
+
+__global__ __launch_bounds__(256) void no_exponents_kernel(int32_t* top, int32_t n) {
+    for (int32_t i = threadIdx.x; i < n; i += 256) top[i] = NO_EXPONENT;
+}
+hipError_t launch_no_exponents(int32_t* top, int32_t n, hipStream_t st) {
+    no_exponents_kernel<<<1, 256, 0, st>>>(top, n);
+    return hipGetLastError();
+}
+
+// A wave per row.
+template <typename T>
+__global__ __launch_bounds__(256) void row_exponents_kernel(const T* x, int64_t stride, int64_t n, int32_t cols, const int32_t* list,
+                                                            const int32_t* count, int32_t* out) {
+    const int64_t rows = count ? *count : n;
+    for (int64_t r = blockIdx.x * 4LL + threadIdx.x / WAVE; r < rows; r += gridDim.x * 4LL) {
+        const uint32_t big = wave_top(row_top(x + (list ? list[r] : r) * stride, cols));
+        if (lane_id() == 0) out[r] = exponent_above(__uint_as_float(big));
+    }
+}
+hipError_t launch_row_exponents(const dc_matrix& src, int64_t n, const int32_t* list, const int32_t* count, int32_t* out, hipStream_t st) {
+    return with_type(src.type, [&](auto el) {
+        using T = typename decltype(el)::type;
+        row_exponents_kernel<T><<<(unsigned)std::min<int64_t>((n + 3) / 4, 1 << 14), 256, 0, st>>>(static_cast<const T*>(src.d_data), src.row_stride, n,
+                                                                                                 (int32_t)src.n_cols, list, count, out);
+        return hipGetLastError();
+    });
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void top_exponent_kernel(const T* w, int64_t stride, int64_t rows, int32_t cols, int32_t* top) {
+    __shared__ int tmp[4];
+    uint32_t big = 0;
+    for (int64_t r = blockIdx.x * 4LL + threadIdx.x / WAVE; r < rows; r += gridDim.x * 4LL) big = max(big, row_top(w + r * stride, cols));
+    raise_top(exponent_above(__uint_as_float(wave_top(big))), tmp, top);
+}
+hipError_t launch_top_exponent(const dc_matrix& src, int64_t first, int64_t n, int32_t* top, hipStream_t st) {
+    return with_type(src.type, [&](auto el) {
+        using T = typename decltype(el)::type;
+        top_exponent_kernel<T><<<(unsigned)std::min<int64_t>(TOP_BLOCKS, (n + 3) / 4), 256, 0, st>>>(
+            static_cast<const T*>(src.d_data) + first * src.row_stride, src.row_stride, n, (int32_t)src.n_cols, top);
+        return hipGetLastError();
+    });
+}
+
 // Tiles of 64 x 64 through the LDS: read along the rows, written along the columns.  WIDE: rows on multiples of 16 bytes.  Bound by the
 // bytes: 15360 x 2048 bf16 (126 MB in and out) in 19 us.
-template <typename S, typename D, int PARTS, bool WIDE>
+template <typename S, int PARTS, bool WIDE>
 __global__ __launch_bounds__(256) void lay_columns_kernel(const S* src, int64_t stride, int64_t first, int64_t n, int32_t cols,
                                                           const int32_t* list, const int32_t* count, int64_t rows_pad, const int32_t* top,
                                                           const RowTerm* term, char* dst, int64_t plane) {
@@ -91,7 +143,7 @@ __global__ __launch_bounds__(256) void lay_columns_kernel(const S* src, int64_t 
     const int64_t rows = count ? *count : n, r0 = blockIdx.x * 64LL;
     if (r0 >= rows) return;
     const int32_t c0 = blockIdx.y * 64, tid = threadIdx.x;
-    const int up = top ? 15 - *top : 0;
+    const int up = 15 - *top;
     if (WIDE && c0 + 64 <= cols) {
         constexpr int N = 16 / sizeof(S), LANES = 64 / N, ROWS = 256 / LANES;
         u32x4 q[64 / ROWS];
@@ -107,17 +159,14 @@ __global__ __launch_bounds__(256) void lay_columns_kernel(const S* src, int64_t 
             const int x = up - (term && r < rows ? term[r].exponent : 0);
             union { u32x4 q; S e[N]; } in = {q[h]};
 #pragma unroll
-            for (int j = 0; j < N; ++j) tile[i][tid % LANES * N + j] = r < rows ? top ? ldexpf((float)in.e[j], x) : (float)in.e[j] : 0.0f;
+            for (int j = 0; j < N; ++j) tile[i][tid % LANES * N + j] = r < rows ? ldexpf((float)in.e[j], x) : 0.0f;
         }
     } else {
         for (int i = tid / 64; i < 64; i += 4) {
             const int64_t r = r0 + i;
             const int32_t c = c0 + (tid & 63);
             float v = 0.0f;
-            if (r < rows && c < cols) {
-                v = (float)src[(list ? list[r] : first + r) * stride + c];
-                if (top) v = ldexpf(v, up - (term ? term[r].exponent : 0));
-            }
+            if (r < rows && c < cols) v = ldexpf((float)src[(list ? list[r] : first + r) * stride + c], up - (term ? term[r].exponent : 0));
             tile[i][tid & 63] = v;
         }
     }
@@ -132,33 +181,30 @@ __global__ __launch_bounds__(256) void lay_columns_kernel(const S* src, int64_t 
         for (int j = 0; j < 8; ++j) f[j] = tile[i + j][c];
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
-            Raw8<D> out;
+            Raw8<_Float16> out;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                if constexpr (PARTS == 1) out.e[j] = (D)f[j];
-                else out.e[j] = take_part<D>(f[j]);
+                if constexpr (PARTS == 1) out.e[j] = (_Float16)f[j];
+                else out.e[j] = take_part<_Float16>(f[j]);
             }
             *reinterpret_cast<u32x4*>(dst + p * plane + ((c0 + c) * rows_pad + r0 + i) * 2) = out.q[0];
         }
     }
 }
 
-hipError_t launch_lay_columns(const dc_matrix& src, int64_t first, int64_t n, const int32_t* list, const int32_t* count, int32_t planes,
-                              int64_t rows_pad, const int32_t* top, const RowTerm* term, char* dst, int64_t plane, hipStream_t st) {
+hipError_t launch_lay_columns(const dc_matrix& src, int64_t first, int64_t n, const int32_t* list, const int32_t* count, int64_t rows_pad,
+                              const int32_t* top, const RowTerm* term, char* dst, int64_t plane, hipStream_t st) {
     if (n == 0) return hipSuccess;
     const dim3 grid((unsigned)((n + 63) / 64), (unsigned)((src.n_cols + 63) / 64));
-    const auto go = [&](auto s, auto d, auto parts) {
-        using S = decltype(s);
+    return with_type(src.type, [&](auto el) {
+        using S = typename decltype(el)::type;
         const auto launch = [&](auto wide) {
-            lay_columns_kernel<S, decltype(d), decltype(parts)::value, decltype(wide)::value><<<grid, 256, 0, st>>>(
+            lay_columns_kernel<S, sizeof(S) == 4 ? 2 : 1, decltype(wide)::value><<<grid, 256, 0, st>>>(
                 static_cast<const S*>(src.d_data), src.row_stride, first, n, (int32_t)src.n_cols, list, count, rows_pad, top, term, dst, plane);
         };
         if (rows_aligned<S>(src.d_data, src.row_stride)) launch(std::true_type{}); else launch(std::false_type{});
-    };
-    if (src.type == DC_F32) go(float{}, __bf16{}, std::integral_constant<int, 3>{});
-    else if (src.type == DC_BF16) go(__bf16{}, _Float16{}, std::integral_constant<int, 1>{});
-    else go(_Float16{}, _Float16{}, std::integral_constant<int, 1>{});
-    return hipGetLastError();
+        return hipGetLastError();
+    });
 }
 
 constexpr int LIVE_THREADS = 1024;
@@ -184,8 +230,7 @@ hipError_t launch_live_rows(const uint8_t* mask, const float* a, const float* b,
 
 Parts parts_of(int32_t type, int64_t a_plane, int64_t b_plane) {
     if (type != DC_F32) return Parts{1, 0, 0, a_plane, b_plane};
-    // (0, 2) (2, 0) (1, 1) (0, 1) (1, 0) (0, 0)
-    return Parts{6, 0u | 2u << 2 | 1u << 4 | 0u << 6 | 1u << 8 | 0u << 10, 2u | 0u << 2 | 1u << 4 | 1u << 6 | 0u << 8 | 0u << 10, a_plane, b_plane};
+    return Parts{3, 0u | 1u << 2 | 0u << 4, 1u | 0u << 2 | 0u << 4, a_plane, b_plane};       // the small ones first
 }
 
 }  // namespace dc
