@@ -16,7 +16,7 @@ struct HeadStatArgs {
     Operand        w, x;
     Parts          parts;
     int32_t        steps, v0, vocab_end, tiles;      // vocabulary entries v0 .. vocab_end - 1 are rows 0 .. of w; tiles: of P_SIDE
-    int32_t        row_tiles, segments, n_rows;
+    int32_t        row_tiles, segments, n_rows, most_tiles;      // for all rows; most_tiles: of the first piece
     const int32_t* count;           // NULL: n_rows
     const int32_t* list;            // of the rows, for their tokens; NULL: as they lie
     const int32_t* token;
@@ -43,10 +43,11 @@ template <typename T, bool ENTROPY, int Q>
 __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_stat_kernel(const HeadStatArgs h) {
     constexpr int SIDE = P_SIDE<Q>;
     __shared__ __attribute__((aligned(1024))) char lds[P_LDS<Q>];
-    const int32_t blocks = h.row_tiles * h.segments;
-    const TilePair at = tile_pair(by_chiplet(blockIdx.x, blocks), h.row_tiles, h.segments);
-    const int32_t n_rows = h.count ? *h.count : h.n_rows, first = at.first * SIDE;
-    if (first >= n_rows) return;
+    const int32_t n_rows = h.count ? *h.count : h.n_rows, row_tiles = (n_rows + SIDE - 1) / SIDE;
+    const int32_t segments = live_share(h.row_tiles * h.segments, row_tiles, h.most_tiles);
+    if ((int32_t)blockIdx.x >= row_tiles * segments) return;
+    const TilePair at = tile_pair(by_chiplet(blockIdx.x, row_tiles * segments), row_tiles, segments);
+    const int32_t first = at.first * SIDE;
     const int lane = lane_id(), wave = threadIdx.x / WAVE;
     const int32_t my_row = first + place_b<Q>();        // and the Q - 1 behind it
     // sums of products of numbers of 32 bits are in units of the row's own: kr takes those to powers of two, as k does logits
@@ -67,14 +68,14 @@ __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_stat_kernel(co
     product.steps = h.steps;
     int32_t asked = at.second;                   // the tile whose numbers are on their way
     const auto next = [&] {
-        if (asked + h.segments < h.tiles) place_tile(product.a, h.w, (asked += h.segments) * SIDE, h.vocab_end - h.v0);
+        if (asked + segments < h.tiles) place_tile(product.a, h.w, (asked += segments) * SIDE, h.vocab_end - h.v0);
     };
     if (asked < h.tiles) {                       // (the last piece of a vocabulary may have fewer tiles than there are segments)
         place_tile(product.a, h.w, asked * SIDE, h.vocab_end - h.v0);
         place_tile(product.b, h.x, first, n_rows);
         product.begin(lds, next);
     }
-    for (int32_t t = at.second; t < h.tiles; t += h.segments) {
+    for (int32_t t = at.second; t < h.tiles; t += segments) {
         f32x4 acc[Q][Q];
         product.tile(acc, next);
         const int32_t v = h.v0 + t * SIDE + place_a<Q>();       // of acc[0][.][0]
@@ -164,7 +165,7 @@ __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_stat_kernel(co
     for (int32_t i = threadIdx.x; i < SIDE && first + i < n_rows; i += P_THREADS) {
         const int32_t row = first + i;
         RowSums r = join(tmp[i], tmp[SIDE + i]);
-        RowSums* to = h.sums + (int64_t)row * h.segments + at.second;
+        RowSums* to = h.sums + (int64_t)row * segments + at.second;
         if (h.add) r = join(*to, r);
         *to = r;
     }
@@ -223,11 +224,16 @@ __device__ __forceinline__ void take_apart(const Eight<W>& from, Raw8<typename F
     if constexpr (sizeof(W) == 2) {
         part[0].q[0] = from.q[0];
     } else {
+        // the upper 16 bits of a number, of what they leave, and of what those leave: 24 bits, cut and not rounded, so exactly all of it
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            float rest = from.e[e];
+        for (int e = 0; e < 8; e += 2) {
+            float x = from.e[e], y = from.e[e + 1];
 #pragma unroll
-            for (int p = 0; p < 3; ++p) part[p].e[e] = take_part<__bf16>(rest);
+            for (int p = 0; p < 3; ++p) {
+                part[p].q[0][e / 2] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+                x -= __uint_as_float(__float_as_uint(x) & 0xFFFF0000u);
+                y -= __uint_as_float(__float_as_uint(y) & 0xFFFF0000u);
+            }
         }
     }
 }
@@ -454,8 +460,9 @@ static hipError_t launch_few(const FewArgs& f, int32_t type, bool any, hipStream
 }
 
 // A wave per row: its segments' sums as one, and the results.
-__global__ __launch_bounds__(256) void head_join_kernel(const LogprobArgs a, const int32_t* pos, int32_t segments, const RowSums* sums,
-                                                        const float* x_token) {
+__global__ __launch_bounds__(256) void head_join_kernel(const LogprobArgs a, const int32_t* pos, const int32_t* count, int32_t side, int32_t blocks,
+                                                        int32_t most_tiles, const RowSums* sums, const float* x_token) {
+    const int32_t segments = live_share(blocks, (int32_t)(((count ? *count : a.n_rows) + side - 1) / side), most_tiles);
     const float k = a.inv_t * LOG2E;
     const int lane = lane_id();
     for (int64_t r = blockIdx.x * 4LL + threadIdx.x / WAVE; r < a.n_rows; r += gridDim.x * 4LL) {
@@ -614,7 +621,8 @@ hipError_t launch_head(const HeadArgs& a, void* d_ws, hipStream_t st) {
     h.n_rows = (int32_t)rows;
     h.count = live ? w.live.count : nullptr;
     h.list = live ? w.live.list : nullptr;
-    h.segments = segments_of(h.row_tiles, (std::min(w.piece, vocab) + side - 1) / side, small ? P_SLOTS<4> : P_SLOTS<8>);
+    h.most_tiles = (std::min(w.piece, vocab) + side - 1) / side;
+    h.segments = segments_of(h.row_tiles, h.most_tiles, small ? P_SLOTS<4> : P_SLOTS<8>);
     if (sh.copy_hidden) {
         if (e == hipSuccess && f32) e = launch_row_exponents(a.hidden, rows, h.list, h.count, w.x_exp, st);
         if (e == hipSuccess) e = launch_lay_rows(a.hidden, 0, rows, h.list, h.count, sh.k_pad, w.hidden, w.hidden_plane, F16S, w.x_exp, nullptr, st);
@@ -673,8 +681,8 @@ hipError_t launch_head(const HeadArgs& a, void* d_ws, hipStream_t st) {
         if (f32) h.x_exp += HEAD_TOP_ROWS;
     }
     if (e != hipSuccess || a.n_top > 0) return e;
-    head_join_kernel<<<(unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 16), 256, 0, st>>>(out, live ? w.live.pos : nullptr, h.segments,
-                                                                                          w.sums, w.x_token);
+    head_join_kernel<<<(unsigned)std::min<int64_t>((rows + 3) / 4, 1 << 16), 256, 0, st>>>(
+        out, live ? w.live.pos : nullptr, h.count, side, h.row_tiles * h.segments, h.most_tiles, w.sums, w.x_token);
     return hipGetLastError();
 }
 

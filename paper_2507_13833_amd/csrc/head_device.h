@@ -275,6 +275,10 @@ __device__ __forceinline__ int32_t by_chiplet(int32_t block, int32_t blocks) {
     const int32_t each = blocks / 8, more = blocks % 8, x = block % 8;
     return x * each + min(x, more) + block / 8;
 }
+// Of `blocks` workgroups that were launched for all rows, how many come to each tile of those that take part; at most `most`.
+__device__ __forceinline__ int32_t live_share(int32_t blocks, int32_t tiles, int32_t most) {
+    return tiles > 0 ? min(blocks / tiles, most) : 0;
+}
 // Of `first` times `second` tiles the at-th: eight firsts beside each other for each second, so that neighbours share both.
 struct TilePair { int32_t first, second; };
 __device__ __forceinline__ TilePair tile_pair(int32_t at, int32_t first, int32_t second) {

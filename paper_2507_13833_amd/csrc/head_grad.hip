@@ -160,6 +160,7 @@ __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_piece_kernel(c
 
 // ---- the two products ----
 
+constexpr int32_t HG_MOST_SPLITS = 32;
 struct HeadHiddenArgs {             // slab[split][row][col] (+)= sum over this split's share of the piece
     Operand        wt, g;
     Parts          parts;
@@ -168,17 +169,18 @@ struct HeadHiddenArgs {             // slab[split][row][col] (+)= sum over this 
     const int32_t* top;
     bool           add;
     float*         slab;
-    int64_t        rows_pad, pitch;
+    int64_t        pitch;
 };
 template <int Q>
 __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_hidden_kernel(const HeadHiddenArgs h) {
     constexpr int SIDE = P_SIDE<Q>;
     __shared__ __attribute__((aligned(1024))) char lds[P_LDS<Q>];
-    const int32_t others = h.col_tiles * h.splits;
-    const TilePair at = tile_pair(by_chiplet(blockIdx.x, h.row_tiles * others), h.row_tiles, others);
-    const int32_t n_rows = *h.count, first = at.first * SIDE, tile = at.second % h.col_tiles, split = at.second / h.col_tiles;
-    if (first >= n_rows) return;
-    const int32_t each = (h.steps + h.splits - 1) / h.splits, from = split * each, steps = min(each, h.steps - from);
+    const int32_t n_rows = *h.count, row_tiles = (n_rows + SIDE - 1) / SIDE;
+    const int32_t splits = live_share(h.row_tiles * h.splits, row_tiles, HG_MOST_SPLITS), others = h.col_tiles * splits;
+    if ((int32_t)blockIdx.x >= row_tiles * others) return;
+    const TilePair at = tile_pair(by_chiplet(blockIdx.x, row_tiles * others), row_tiles, others);
+    const int32_t first = at.first * SIDE, tile = at.second % h.col_tiles, split = at.second / h.col_tiles;
+    const int32_t each = (h.steps + splits - 1) / splits, from = split * each, steps = min(each, h.steps - from);
     f32x4 acc[Q][Q];
     {
         TileOfA<Q> a;
@@ -197,7 +199,7 @@ __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_hidden_kernel(
 #pragma unroll
             for (int i = 0; i < Q; ++i)
                 if (col + along_a(i, 0) < h.pitch) {         // (a multiple of 4)
-                    f32x4* to = reinterpret_cast<f32x4*>(h.slab + ((int64_t)split * h.rows_pad + row + j) * h.pitch + col + along_a(i, 0));
+                    f32x4* to = reinterpret_cast<f32x4*>(h.slab + ((int64_t)split * row_tiles * SIDE + row + j) * h.pitch + col + along_a(i, 0));
                     f32x4 v = acc[i][j];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) v[e] = ldexpf(v[e], up);
@@ -208,16 +210,17 @@ __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_hidden_kernel(
 
 // A row's hidden gradient: the slabs' sum, its own power of two undone, rounded once.  Rows that take no part: +0.
 template <typename T>
-__global__ __launch_bounds__(256) void head_hidden_join_kernel(const float* slab, int32_t splits, int64_t rows_pad, int64_t pitch,
+__global__ __launch_bounds__(256) void head_hidden_join_kernel(const float* slab, const int32_t* count, int32_t side, int32_t blocks, int64_t pitch,
                                                                const int32_t* pos, const RowTerm* term, T* out, int64_t stride, int64_t rows,
                                                                int32_t dim) {
-    const int64_t each = pitch / 4;
+    const int64_t each = pitch / 4, row_tiles = (*count + side - 1) / side;
+    const int32_t splits = live_share(blocks, (int32_t)row_tiles, HG_MOST_SPLITS);
     for (int64_t q = blockIdx.x * 256LL + threadIdx.x; q < rows * each; q += gridDim.x * 256LL) {
         const int64_t r = q / each;
         const int32_t c = (int32_t)(q - r * each) * 4, at = pos[r];
         f32x4 sum = {0, 0, 0, 0};
         if (at >= 0) {
-            for (int32_t s = 0; s < splits; ++s) sum += *reinterpret_cast<const f32x4*>(slab + (s * rows_pad + at) * pitch + c);
+            for (int32_t s = 0; s < splits; ++s) sum += *reinterpret_cast<const f32x4*>(slab + (s * row_tiles * side + at) * pitch + c);
             const int e = -term[at].exponent;
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum[i] = ldexpf(sum[i], e);
@@ -289,7 +292,6 @@ __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_weight_kernel(
 // ---- the workspace ----
 
 constexpr int64_t HG_AREA = 1 << 27;             // elements of G, or of the weights laid out, held at once
-constexpr int32_t HG_MOST_SPLITS = 32;
 
 namespace {
 struct HeadGradWs {
@@ -419,7 +421,6 @@ hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
     hh.dim = dim;
     hh.count = w.live.count;
     hh.slab = w.slab;
-    hh.rows_pad = sh.rows_pad;
     hh.pitch = w.pitch;
     HeadWeightArgs hw = {};
     hw.xt = Operand{w.xt, sh.rows_pad * 2, nullptr};
@@ -493,7 +494,7 @@ hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
         e = with_type(gh.type, [&](auto el) {
             using T = typename decltype(el)::type;
             head_hidden_join_kernel<T><<<(unsigned)std::min<int64_t>((rows * (w.pitch / 4) + 255) / 256, 1 << 14), 256, 0, st>>>(
-                w.slab, w.cut_hidden.splits, sh.rows_pad, w.pitch, w.live.pos, w.term, static_cast<T*>(gh.d_data), gh.row_stride, rows, dim);
+                w.slab, w.live.count, w.cut_hidden.small ? P_SIDE<4> : P_SIDE<8>, hh.row_tiles * hh.splits, w.pitch, w.live.pos, w.term, static_cast<T*>(gh.d_data), gh.row_stride, rows, dim);
             return hipGetLastError();
         });
     return e;

@@ -125,10 +125,20 @@ __global__ __launch_bounds__(256) void top_exponent_kernel(const T* w, int64_t s
     raise_top(exponent_above(__uint_as_float(wave_top(big))), tmp, top);
 }
 hipError_t launch_top_exponent(const dc_matrix& src, int64_t first, int64_t n, int32_t* top, hipStream_t st) {
+    // (rows that follow each other directly: as whole pieces of 8192 elements, and the rest as one)
+    const int64_t together = src.row_stride == src.n_cols ? n * src.n_cols / 8192 : 0, left = src.row_stride == src.n_cols ? n * src.n_cols % 8192 : 0;
     return with_type(src.type, [&](auto el) {
         using T = typename decltype(el)::type;
-        top_exponent_kernel<T><<<(unsigned)std::min<int64_t>(TOP_BLOCKS, (n + 3) / 4), 256, 0, st>>>(
-            static_cast<const T*>(src.d_data) + first * src.row_stride, src.row_stride, n, (int32_t)src.n_cols, top);
+        const T* from = static_cast<const T*>(src.d_data) + first * src.row_stride;
+        const auto go = [&](const T* x, int64_t stride, int64_t rows, int64_t cols) {
+            if (rows > 0 && cols > 0) top_exponent_kernel<T><<<(unsigned)std::min<int64_t>(TOP_BLOCKS, (rows + 3) / 4), 256, 0, st>>>(x, stride, rows, (int32_t)cols, top);
+        };
+        if (src.row_stride == src.n_cols) {
+            go(from, 8192, together, 8192);
+            go(from + together * 8192, left, 1, left);
+        } else {
+            go(from, src.row_stride, n, src.n_cols);
+        }
         return hipGetLastError();
     });
 }
