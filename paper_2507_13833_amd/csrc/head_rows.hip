@@ -10,7 +10,7 @@ static bool readable(const dc_matrix& m, bool listed) {
     return pitch % 16 == 0 && pitch <= P_MOST_PITCH && (!listed || pitch * m.n_rows < 1LL << 32);
 }
 
-// A round of tiles takes, in us, about 1.4 a step and 14 around them with Q = 8, 0.85 and 5 with Q = 4, and a split's sums 2.5 a MB.
+// A round of tiles takes, in us, about 1.4 a step and 14 around them with Q = 8, 0.85 and 5 with Q = 4, and a split's sums 0.6 a MB.
 // Measured, the two sides, us: 1000 x 32000, 16 steps, Q = 8 66, Q = 4 73; 2048 x 32000, 32 steps 207, 245; 300 x 32003, 8 steps
 // 31.7, 27.5; 100 x 152064, 32 steps 176, 144; 4096 x 10000, 8 steps 57, 52; 500 x 32000, 48 steps 111, 125.
 ProductCut cut_product(int64_t m, int64_t n, int64_t steps, int32_t most_splits) {
@@ -21,7 +21,7 @@ ProductCut cut_product(int64_t m, int64_t n, int64_t steps, int32_t most_splits)
         const int64_t tiles = whole(m, side) / side * (whole(n, side) / side);
         for (int32_t s = 1; s <= most_splits && (s == 1 || tiles * s <= 2 * slots); ++s) {
             const double round = (double)((steps + s - 1) / s) * (small ? 0.85 : 1.4) + (small ? 5 : 14);
-            const double all = (double)((tiles * s + slots - 1) / slots) * round + (s - 1) * (double)m * n * 1e-5;
+            const double all = (double)((tiles * s + slots - 1) / slots) * round + (s - 1) * (double)m * n * 2.5e-6;
             if (least < 0 || all < least) { least = all; best = ProductCut{small, s}; }
         }
     }
