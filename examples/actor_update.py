@@ -1,8 +1,9 @@
 """The actor's update on a repacked GRPO batch, from end to end on one GPU.
 
 A rollout batch goes through the reshard (balance, advantages, plan, gather); one data-parallel rank's micro-batches then
-go through a small actor: the embedding of their token ids, a linear head, the log-probabilities of the next tokens, the
-clipped policy objective with an entropy bonus, and back, and AdamW with 8-bit states steps on 32-bit master weights.
+go through a small actor: the embedding of their token ids, a linear block whose normed result joins the residual stream, the
+stream normed for the head, the log-probabilities of the next tokens without a matrix of logits, the clipped policy objective
+with an entropy bonus, and back, and AdamW with 8-bit states steps on 32-bit master weights.
 The actor is a bigram model (the next token's logits come from the current token's embedding alone): what it learns is not
 the point, what it calls is.
 
@@ -30,53 +31,72 @@ class Actor:
         gen = torch.Generator(device=device).manual_seed(seed)
         self.dim, self.scale = dim, dim ** 0.5
         self.items = []
-        for std in (0.3 / self.scale, 1.0 / self.scale):                       # embedding, head
-            master = torch.randn(vocab, dim, generator=gen, device=device) * std
-            n, blocks = vocab * dim, -(-vocab * dim // B.DC_STATE_BLOCK)
+
+        def item(rows, std, mean=0.0, decay=0.01):
+            master = mean + torch.randn(rows, dim, generator=gen, device=device) * std
+            n, blocks = rows * dim, -(-rows * dim // B.DC_STATE_BLOCK)
             state = lambda: torch.zeros(n, dtype=torch.float8_e4m3fn, device=device)  # noqa: E731
-            self.items.append(dict(param=master.bfloat16(), master=master, grad=torch.zeros(vocab, dim, device=device),
+            self.items.append(dict(param=master.bfloat16(), master=master, grad=torch.zeros(rows, dim, device=device),
                                    exp_avg=state(), exp_avg_sq=state(), exp_avg_scale=torch.zeros(blocks, device=device),
-                                   exp_avg_sq_scale=torch.zeros(blocks, device=device), weight_decay=0.01))
-        self.embed, self.head = self.items
+                                   exp_avg_sq_scale=torch.zeros(blocks, device=device), weight_decay=decay))
+            return self.items[-1]
+
+        self.embed, self.head = item(vocab, 0.3 / self.scale), item(vocab, 0.3 / self.scale)
+        self.block = item(dim, 1.0 / self.scale)
+        self.post, self.pre = item(1, 0.0, 1.0, 0.0), item(1, 0.0, 1.0, 0.0)   # the norms' weights
+        self.norm = B.make_norm(1e-6, 1.0, 0.5)
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
-        # what the calls need is laid out once: the optimizer's table, workspaces for the largest micro-batch
+        # what the calls need is laid out once: the optimizer's table, activations and workspaces for the largest micro-batch
         self.tensors = B.AdamwTensors(self.items)
         self.table_bytes = B.dc_adamw_table_bytes(self.tensors)
         self.table = torch.empty(self.table_bytes, dtype=torch.uint8, device=device)
         B.dc_adamw_table(self.tensors, self.table, self.table_bytes)
-        self.hidden = torch.empty(max_tokens, dim, dtype=torch.bfloat16, device=device)
-        self.grad_ws_bytes = B.dc_embedding_backward_workspace_bytes(B.make_matrix(self.hidden), B.make_matrix(self.embed["grad"]))
-        self.grad_ws = torch.empty(max(1, self.grad_ws_bytes), dtype=torch.uint8, device=device)
+        new = lambda dtype, cols=dim: torch.empty(max_tokens, cols, dtype=dtype, device=device)  # noqa: E731
+        self.act = {"embed": new(torch.bfloat16), "block": new(torch.bfloat16), "stream": new(torch.bfloat16),
+                    "normed": new(torch.bfloat16), "stat": new(torch.float32, 2)}
+        self.grad = {k: new(torch.bfloat16) for k in ("normed", "block", "stream")}
+        m = B.make_matrix
+        normed, head = m(self.act["normed"]), m(self.head["param"])
+        self.ws_bytes = max(B.dc_head_logprob_workspace_bytes(normed, head, 5),
+                            B.dc_head_logprob_backward_workspace_bytes(normed, head, m(self.head["grad"])),
+                            B.dc_residual_norm_backward_workspace_bytes(normed),
+                            B.dc_embedding_backward_workspace_bytes(normed, m(self.embed["grad"])))
+        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
         self.steps = 0
 
-    def logits(self, ids: torch.Tensor) -> torch.Tensor:
-        """Of the tokens behind ids[:-1]; row t is for ids[t + 1]."""
-        self.h = self.hidden[: ids.numel() - 1]
-        B.dc_embedding(B.make_matrix(self.embed["param"]), ids, self.scale, B.make_matrix(self.h), self.status)
-        return torch.mm(self.h, self.head["param"].t())
+    def hidden(self, ids: torch.Tensor) -> torch.Tensor:
+        """The normed residual stream of the tokens behind ids[:-1]; row t is for ids[t + 1]."""
+        n, m = ids.numel() - 1, B.make_matrix
+        a = self.a = {k: v[:n] for k, v in self.act.items()}
+        B.dc_embedding(m(self.embed["param"]), ids, self.scale, m(a["embed"]), self.status)
+        torch.mm(a["embed"], self.block["param"], out=a["block"])
+        B.dc_residual_norm(m(a["block"]), m(self.post["param"]), None, m(a["embed"]), m(self.pre["param"]), self.norm,
+                           m(a["stream"]), m(a["normed"]), a["stat"])
+        return a["normed"]
 
-    def score(self, logits, ids, mask, temperature: float):
+    def score(self, hidden, ids, mask, temperature: float):
         """log-probability and entropy of every next token whose mask byte is set (0 elsewhere), and what their gradient needs."""
-        n = logits.shape[0]
-        logprob, entropy = torch.empty(n, device=logits.device), torch.empty(n, device=logits.device)
-        stat = torch.empty(n, 2, device=logits.device)
-        mx = B.make_matrix(logits)
-        need = B.dc_token_logprob_workspace_bytes(mx, 0)
-        ws = torch.empty(need, dtype=torch.uint8, device=logits.device) if need else None
-        B.dc_token_logprob(mx, temperature, ids[1:], mask[1:], 0, logprob, stat, entropy, None, None, ws, need, self.status)
+        n = hidden.shape[0]
+        logprob, entropy = torch.empty(n, device=hidden.device), torch.empty(n, device=hidden.device)
+        stat = torch.empty(n, 2, device=hidden.device)
+        B.dc_head_logprob(B.make_matrix(hidden), B.make_matrix(self.head["param"]), temperature, ids[1:], mask[1:], 0, logprob, stat,
+                          entropy, None, None, self.ws, self.ws_bytes, self.status)
         return logprob, entropy, stat
 
-    def backward(self, logits, ids, mask, temperature, stat, entropy, grad_logprob, grad_entropy, first: bool) -> None:
-        """Gradients of both tables, added to those of the micro-batches before unless this is the first; the logits'
-        gradient takes the logits' place."""
-        mx = B.make_matrix(logits)
-        B.dc_token_logprob_backward(mx, temperature, ids[1:], mask[1:], stat, entropy, grad_logprob, grad_entropy, mx, self.status)
+    def backward(self, hidden, ids, mask, temperature, stat, entropy, grad_logprob, grad_entropy, first: bool) -> None:
+        """Gradients of all weights, added to those of the micro-batches before unless this is the first."""
+        n, m, a = hidden.shape[0], B.make_matrix, self.a
+        g = {k: v[:n] for k, v in self.grad.items()}
+        B.dc_head_logprob_backward(m(hidden), m(self.head["param"]), temperature, ids[1:], mask[1:], stat, entropy, grad_logprob,
+                                   grad_entropy, m(g["normed"]), not first, m(self.head["grad"]), self.ws, self.ws_bytes, self.status)
+        B.dc_residual_norm_backward(m(a["block"]), m(self.post["param"]), None, m(a["stream"]), m(self.pre["param"]), self.norm, a["stat"],
+                                    None, m(g["normed"]), m(g["block"]), m(g["stream"]), not first, m(self.post["grad"]), None,
+                                    m(self.pre["grad"]), self.ws, self.ws_bytes)
         if first:
-            self.head["grad"].zero_()
-        self.head["grad"] += torch.mm(logits.t(), self.h)
-        grad_h = torch.mm(logits, self.head["param"])
-        B.dc_embedding_backward(B.make_matrix(grad_h), ids, self.scale, not first, B.make_matrix(self.embed["grad"]),
-                                self.grad_ws, self.grad_ws_bytes, self.status)
+            self.block["grad"].zero_()
+        self.block["grad"] += torch.mm(a["embed"].t(), g["block"])
+        grad_embed = torch.addmm(g["stream"], g["block"], self.block["param"].t())
+        B.dc_embedding_backward(m(grad_embed), ids, self.scale, not first, m(self.embed["grad"]), self.ws, self.ws_bytes, self.status)
 
     def step(self, lr: float, max_norm: float = 1.0) -> None:
         """AdamW on gradients whose norm is cut to max_norm; the factor stays on the device."""
@@ -113,8 +133,8 @@ def main(prompts: int = 16, epochs: int = 4, dim: int = 64, lr: float = 3e-3, cl
         objective = entropy_sum = 0.0
         for m, (a, b) in enumerate(spans):
             t, k, adv_m = ids[a:b], mask[a:b], adv[a + 1:b]
-            logits = actor.logits(t)
-            logprob, entropy, stat = actor.score(logits, t, k, temperature)
+            hidden = actor.hidden(t)
+            logprob, entropy, stat = actor.score(hidden, t, k, temperature)
             if epoch == 0:
                 old[m] = logprob.clone()                                       # the policy that the batch is scored with
             ratio = torch.exp(logprob - old[m])
@@ -122,7 +142,7 @@ def main(prompts: int = 16, epochs: int = 4, dim: int = 64, lr: float = 3e-3, cl
             objective += float((torch.minimum(ratio * adv_m, ratio.clamp(1 - clip, 1 + clip) * adv_m) * (k[1:] != 0)).sum())
             entropy_sum += float(entropy.sum())
             # what is made smaller: -(objective + entropy_coef * entropy) / tokens
-            actor.backward(logits, t, k, temperature, stat, entropy, -ratio * adv_m * kept / n_loss,
+            actor.backward(hidden, t, k, temperature, stat, entropy, -ratio * adv_m * kept / n_loss,
                            torch.full_like(entropy, -entropy_coef / n_loss), first=m == 0)
         actor.step(lr)
         history.append((objective / n_loss, entropy_sum / n_loss))
@@ -132,12 +152,10 @@ def main(prompts: int = 16, epochs: int = 4, dim: int = 64, lr: float = 3e-3, cl
     assert d.read_status() == 0 and int(actor.status) == 0
     if verbose:
         # the serving form: the next token behind the last one, with its likeliest alternatives
-        logits = actor.logits(ids[spans[-1][1] - 2:spans[-1][1]])
-        top, top_lp = torch.empty(1, 5, dtype=torch.int32, device=logits.device), torch.empty(1, 5, device=logits.device)
-        mx = B.make_matrix(logits)
-        need = B.dc_token_logprob_workspace_bytes(mx, 5)
-        ws = torch.empty(max(1, need), dtype=torch.uint8, device=logits.device)
-        B.dc_token_logprob(mx, temperature, None, None, 5, None, None, None, top, top_lp, ws, need, actor.status)
+        hidden = actor.hidden(ids[spans[-1][1] - 2:spans[-1][1]])
+        top, top_lp = torch.empty(1, 5, dtype=torch.int32, device=hidden.device), torch.empty(1, 5, device=hidden.device)
+        B.dc_head_logprob(B.make_matrix(hidden), B.make_matrix(actor.head["param"]), temperature, None, None, 5, None, None, None, top,
+                          top_lp, actor.ws, actor.ws_bytes, actor.status)
         print("alternatives:", [(i, round(p, 4)) for i, p in zip(top[0].tolist(), top_lp[0].tolist())])
     return history
 

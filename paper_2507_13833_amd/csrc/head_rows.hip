@@ -217,18 +217,29 @@ hipError_t launch_lay_columns(const dc_matrix& src, int64_t first, int64_t n, co
     });
 }
 
-constexpr int LIVE_THREADS = 1024;
+// One workgroup, eight neighbouring rows to a thread: a chain of scans, 8192 rows each.
+constexpr int LIVE_THREADS = 1024, LIVE_EACH = 8;
 __global__ __launch_bounds__(LIVE_THREADS) void live_rows_kernel(const uint8_t* mask, const float* a, const float* b, int64_t n, LiveRows l) {
     __shared__ int32_t tmp[LIVE_THREADS / WAVE];
     int32_t before = 0;
-    for (int64_t r0 = 0; r0 < n; r0 += LIVE_THREADS) {
-        const int64_t r = r0 + threadIdx.x;
-        int32_t live = r < n && (!mask || mask[r] != 0);
-        if (live && a) live = a[r] != 0.0f || (b && b[r] != 0.0f);
+    for (int64_t r0 = 0; r0 < n; r0 += LIVE_THREADS * LIVE_EACH) {
+        const int64_t r = r0 + threadIdx.x * LIVE_EACH;
+        uint32_t live = 0;
+#pragma unroll
+        for (int e = 0; e < LIVE_EACH; ++e) {
+            bool is = r + e < n && (!mask || mask[r + e] != 0);
+            if (is && a) is = a[r + e] != 0.0f || (b && b[r + e] != 0.0f);
+            live |= (uint32_t)is << e;
+        }
         int32_t total;
-        const int32_t at = before + block_excl_scan_add(live, tmp, &total);
-        if (r < n) l.pos[r] = live ? at : -1;
-        if (live) l.list[at] = (int32_t)r;
+        int32_t at = before + block_excl_scan_add((int32_t)__popc(live), tmp, &total);
+#pragma unroll
+        for (int e = 0; e < LIVE_EACH; ++e) {
+            if (r + e >= n) break;
+            const bool is = live >> e & 1;
+            l.pos[r + e] = is ? at : -1;
+            if (is) l.list[at++] = (int32_t)(r + e);
+        }
         before += total;
     }
     if (threadIdx.x == 0) *l.count = before;
