@@ -13,8 +13,8 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // D[i, j] += sum_k A[i, k] B[j, k] for 16 x 16 places and 32 k.  Lane l brings A[l % 16, 8 (l / 16) ..] and B likewise, and holds
 // D[4 (l / 16) + 0..3, l % 16].  The sums stay in the accumulation registers, which the compiler would share out otherwise and copy
-// from and to in the loop (add; sum is the ordinary way); it does not know these instructions for what they are, so settle_sums() keeps their distance from
-// ordinary ones that write or read the sums.
+// from and to in the loop (add; sum is the ordinary way).  It does not know these instructions for what they are, so settle_sums() keeps
+// their distance from ordinary ones that write or read the sums.
 template <typename T> struct Mfma;
 template <> struct Mfma<__bf16> {
     using Frag = bf16x8;
@@ -194,7 +194,10 @@ struct Product {
 #pragma unroll
         for (int i = 0; i < Q; ++i)
 #pragma unroll
-            for (int j = 0; j < Q; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+            for (int j = 0; j < Q; ++j) {
+                acc[i][j] = f32x4{0, 0, 0, 0};
+                asm volatile("" : "+a"(acc[i][j]));  // (in their registers from here on)
+            }
         settle_sums();
         int32_t s = stage - 2;
         const int32_t end = s + steps * parts.n;

@@ -220,6 +220,7 @@ __global__ __launch_bounds__(256) void head_hidden_join_kernel(const float* slab
         const int32_t c = (int32_t)(q - r * each) * 4, at = pos[r];
         f32x4 sum = {0, 0, 0, 0};
         if (at >= 0) {
+#pragma unroll 8
             for (int32_t s = 0; s < splits; ++s) sum += *reinterpret_cast<const f32x4*>(slab + (s * row_tiles * side + at) * pitch + c);
             const int e = -term[at].exponent;
 #pragma unroll
