@@ -454,8 +454,9 @@ dc_status dc_token_logprob_backward(const dc_matrix* logits, double temperature,
 /*
  * dc_token_logprob without a matrix of logits: x = hidden weight^T is made in pieces on the chip, where a row's sums are taken.
  *   x_v = sum_c hidden[r, c] * weight[v, c]  for the n_rows of hidden and the vocabulary = weight->n_rows; then as above.
- * hidden and weight have the same type and n_cols.  Products of 16-bit numbers are exact, of 32-bit ones right to 2^-24 or so
- * of the two factors' magnitude, and sums are held in 32 bits.  Arguments, masks, rows without a distribution, top
+ * hidden and weight have the same type and n_cols.  Products of 16-bit numbers are exact, sums are held in 32 bits.  Numbers of 32 bits
+ * are taken with 24 bits up to 64 rows and with 22 above, there down to 2^-49 of their row's (for weight: the matrix's) largest
+ * magnitude, and a product leaves off about 2^-21 of itself.  Arguments, masks, rows without a distribution, top
  * alternatives (ties to the lowest token) and device errors are those of dc_token_logprob; hidden rows of masked tokens are not
  * looked at.  An infinity or a NaN in a row of hidden, or in weight, may make a row one without a distribution.
  * Up to 64 rows, and 256 at a time where n_top > 0, go through logits in the workspace.
@@ -478,9 +479,10 @@ dc_status dc_head_logprob(const dc_matrix* hidden, const dc_matrix* weight, doub
  * their hidden rows are not looked at.  grad_weight: weight's shape, weight's type or f32; accumulate == 0: written, != 0: added to
  * in 32 bits before it is rounded.  Neither may overlap another array of the call.
  * Sums are held in 32 bits, in an order that depends on the sizes and on which rows take part (identical inputs give identical bits),
- * and rounded once.  With 16-bit types G itself is rounded: to 11 bits for results of 16 bits, to 22 for a grad_weight
- * in f32; below 2^-38 of the row's largest possible value it becomes 0.  hidden rows of a row-wise gradient below 2^-38 of the batch's
- * largest (row's gradient times row's largest magnitude) add nothing to grad_weight.
+ * and rounded once.  The factors are rounded before they are multiplied, in types of 16 bits to 11 bits, G for a grad_weight in f32
+ * and everything in types of 32 bits to 22; of a row's largest possible G, and of the largest magnitude of weight, what is below
+ * 2^-38 (22 bits: 2^-49) becomes 0, and so does, for grad_weight, what is as far below the batch's largest product of a row's
+ * largest possible G and its largest magnitude in hidden.
  * A row without a distribution (NaN in d_row_stat) that takes part gets NaN in grad_hidden, and grad_weight is NaN.
  * d_ws: 256-byte aligned, dc_head_logprob_backward_workspace_bytes(hidden, weight, grad_weight) bytes (grad_weight NULL: for calls
  * without it), which also serve every call of fewer rows of these matrices; holds nothing the caller needs afterwards.

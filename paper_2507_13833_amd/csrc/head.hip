@@ -1,8 +1,8 @@
 // Log-probabilities of given tokens straight from hidden states and the head's weights: the logits x = hidden weight^T are made
 // tile by tile on the matrix cores and come down to a row's sums where they are.
 //
-// A workgroup keeps 128 rows and goes through its share of the vocabulary, 256 columns at a time.  A lane has four rows, and of
-// each tile 32 logits of every one, all in registers: their largest M, S = sum 2^(k (x - M)) and U = sum 2^(k (x - M)) k (x - M)
+// A workgroup keeps 256 (128) rows and goes through its share of the vocabulary, as many entries at a time.  A lane has Q rows, and of
+// each tile 4 Q logits of every one, all in registers: their largest M, S = sum 2^(k (x - M)) and U = sum 2^(k (x - M)) k (x - M)
 // with k = log2(e) / T join what the lane has from the tiles before, and lanes and waves are joined at the end.  Products of
 // 16-bit floats are exact and summed in 32 bits.  Numbers of 32 bits, times powers of two that take a row's, or the weights', largest to
 // just below 2^15, are taken apart into two of f16 (22 bits together), and three of the four products are summed, the smallest first.
@@ -39,6 +39,11 @@ __device__ __forceinline__ float less_reference(float m, float k, float base, fl
     return was_far ? fmaf(m, k, -base2) : m2 - base2;
 }
 
+// Bound by the matrix cores, and by the clock that the card holds under them (1.5 to 1.6 of 2.4 GHz): the next tile's first operands
+// come while a tile's sums are taken.  us a call, Q = 8: 8192 rows x 152064 x 2048 bf16 3660 to 3830 (1.33 to 1.39 PFLOP/s; a
+// library's product of these sizes alone 3580), 6144 of 8192 x 32000 x 1024 345 (1.17); Q = 4: 200 of 333 x 32003 x 515 f32 123.
+// Also measured on the large one: 128 rows by 256 entries, two workgroups to a compute unit, 5500; eight waves of 128 by 64 with four
+// shorter stages 4650; sums that the compiler places 12 700 (copied from and to their registers).
 template <typename T, bool ENTROPY, int Q>
 __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_stat_kernel(const HeadStatArgs h) {
     constexpr int SIDE = P_SIDE<Q>;
@@ -347,7 +352,8 @@ __global__ __launch_bounds__(256) void head_few_kernel(const FewArgs f) {
 
 // The same for weights and rows that lie anyhow: a wave per 16 MT entries and 16 NB rows, the weights straight into the places that the
 // matrix cores want, AHEAD steps of 32 elements before they are multiplied; the rows, laid out with k_pad columns, 0 behind the last
-// one, come out of the L2.
+// one, come out of the L2.  Bound by its loads, 16 bytes a lane across the lines' borders: 152064 x 2048 bf16 in rows of 2049, us, one row
+// 307 (2.0 TB/s), 64 rows 420; f32 304 (4.1 TB/s); 32003 x 515 bf16 23 and 31.
 template <typename W, int MT, int NB, int AHEAD>
 __global__ __launch_bounds__(256) void head_few_any_kernel(const FewArgs f) {
     using T = typename FewTypes<W>::T;
@@ -497,8 +503,8 @@ __global__ __launch_bounds__(256) void head_join_kernel(const LogprobArgs a, con
     }
 }
 
-// How the vocabulary is shared out over workgroups: `segments` to each tile of rows, so that two to a compute unit finish at
-// about the same time.
+// How the vocabulary is shared out over workgroups: `segments` to each tile of rows, as many as make the fewest tiles one after another
+// for `slots` workgroups at once.
 constexpr int32_t HEAD_MOST_BLOCKS = 2048;
 static int32_t segments_of(int64_t row_tiles, int32_t tiles, int32_t slots) {
     int32_t best = 1;

@@ -82,6 +82,11 @@ struct HeadPieceArgs {
     int64_t        width, rows_pad;
 };
 
+// A tile to a workgroup: neighbours that share its rows or its entries run beside each other on a chiplet, and nothing is kept from
+// one to the next.  Bound by the matrix cores for the product and then, while they wait, by the two writes.  8192 x 15360 x 2048 bf16
+// (0.52 TFLOP, and both of G's layouts, 0.5 GB): 424 to 510 us, of which the product takes about 400; 6144 x 16384 x 1024 with two
+// planes along the vocabulary (0.21 TFLOP, 0.6 GB) 350.
+// G along the vocabulary could be read for the weights' gradient from the one layout with transposing loads: not tried.
 // T: of the operands.  PLANES of G along the vocabulary (gt), ROW_PLANES along the rows.
 template <typename T, int PLANES, int ROW_PLANES, int Q>
 __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_piece_kernel(const HeadPieceArgs h) {
@@ -171,6 +176,9 @@ struct HeadHiddenArgs {             // slab[split][row][col] (+)= sum over this 
     float*         slab;
     int64_t        pitch;
 };
+// The summed axis, a piece of the vocabulary, is long and the tiles are few (6144 x 1024: 96): `splits` workgroups take a share of it
+// each, into slabs of their own that grow from piece to piece; atomics would make the order of sums change.  Bound by the matrix cores:
+// 8192 x 2048 over 15360 entries 400 to 430 us (1.2 to 1.3 PFLOP/s), 6144 x 1024 over 16384 in shares 249 (0.83).
 template <int Q>
 __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_hidden_kernel(const HeadHiddenArgs h) {
     constexpr int SIDE = P_SIDE<Q>;
@@ -208,7 +216,8 @@ __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_hidden_kernel(
                 }
 }
 
-// A row's hidden gradient: the slabs' sum, its own power of two undone, rounded once.  Rows that take no part: +0.
+// A row's hidden gradient: the slabs' sum, its own power of two undone, rounded once.  Rows that take no part: +0.  Bound by the slabs'
+// bytes, eight asked for at once (8192 x 1024 in 6 slabs: 5 us, one at a time 13).
 template <typename T>
 __global__ __launch_bounds__(256) void head_hidden_join_kernel(const float* slab, const int32_t* count, int32_t side, int32_t blocks, int64_t pitch,
                                                                const int32_t* pos, const RowTerm* term, T* out, int64_t stride, int64_t rows,
@@ -242,6 +251,8 @@ struct HeadWeightArgs {             // grad_weight[v0 + row of gt][col] (+)= sum
     void*          out;             // of the piece's first entry
     int64_t        stride;
 };
+// The sum goes over the rows, for all of them in one workgroup: there are many tiles (15360 x 2048: 480).  Bound by the matrix cores:
+// those over 8192 rows 390 to 418 us (1.2 to 1.3 PFLOP/s), 16384 x 1024 over 6144 with two planes of G 320 (1.3).
 template <typename T, int Q>
 __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_weight_kernel(const HeadWeightArgs h) {
     constexpr int SIDE = P_SIDE<Q>;

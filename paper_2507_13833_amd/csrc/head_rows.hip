@@ -217,7 +217,8 @@ hipError_t launch_lay_columns(const dc_matrix& src, int64_t first, int64_t n, co
     });
 }
 
-// One workgroup, eight neighbouring rows to a thread: a chain of scans, 8192 rows each.
+// One workgroup, eight neighbouring rows to a thread: a chain of scans, 8192 rows each, and as many trips to memory (8192 rows: 8 us;
+// more rows have products that take a hundred times as long).
 constexpr int LIVE_THREADS = 1024, LIVE_EACH = 8;
 __global__ __launch_bounds__(LIVE_THREADS) void live_rows_kernel(const uint8_t* mask, const float* a, const float* b, int64_t n, LiveRows l) {
     __shared__ int32_t tmp[LIVE_THREADS / WAVE];

@@ -93,6 +93,8 @@ __device__ __forceinline__ void row_sums(float (&v)[N], float* tmp) {
 // 1 / sqrt, rounded twice
 __device__ __forceinline__ float inverse_root(float x) { return 1.0f / sqrtf(x); }
 
+// us: 131072 x 2048, block and out bf16, the stream f32 (3.2 GB) 681 (4.7 TB/s; a large copy reaches 4.9); one row 11, mostly
+// the host's: the kernel takes 6.
 template <typename A, typename R, int P, bool WIDE>
 __global__ __launch_bounds__(P < 256 ? 256 : P) void residual_norm_kernel(const NormArgs a) {
     constexpr int THREADS = P < 256 ? 256 : P, ROWS = THREADS / P;
@@ -239,6 +241,7 @@ hipError_t launch_residual_norm(const NormArgs& a, hipStream_t st) {
 
 // One round of sums to a row: with x = dy pre, n2 = h r2, n1 = b r1 (b without a norm), w = gate post n1 (0 without a norm),
 //   S1 = sum x n2,  Sa = sum (dh + r2 x) w,  Sb = sum n2 w:  sum dh' w = Sa - r2 S1 Sb / dim for dh' = dh + r2 (x - n2 S1 / dim).
+// 131072 x 2048 bf16, all gradients (3.2 GB): 652 us (4.9 TB/s), 12 of them the join's; 777 x 1365 f32 23, two launches and the host.
 template <typename A, typename R, int P, int E, bool WIDE>
 __global__ __launch_bounds__(P < 256 ? 256 : P) void residual_norm_grad_kernel(const NormGradArgs a) {
     constexpr int THREADS = P < 256 ? 256 : P, ROWS = THREADS / P;
