@@ -108,6 +108,7 @@ dc_status dc_head_logprob_backward(const dc_matrix* hidden, const dc_matrix* wei
     if (grad_weight && grad_weight->type != weight->type && grad_weight->type != DC_F32) return DC_ERR_INVALID_ARG;
     for (const dc_matrix* out : {grad_hidden, grad_weight})
         if (out && out->d_data && (out->d_data == hidden->d_data || out->d_data == weight->d_data)) return DC_ERR_INVALID_ARG;
+    if (grad_hidden && grad_weight && hidden->n_rows > 0 && grad_hidden->d_data == grad_weight->d_data) return DC_ERR_INVALID_ARG;
     if (hidden->n_rows > 0 && (!d_row_stat || !d_grad_logprob || (d_grad_entropy && !d_entropy))) return DC_ERR_INVALID_ARG;
     for (const void* p : {(const void*)d_token, (const void*)d_row_stat, (const void*)d_entropy, (const void*)d_grad_logprob,
                           (const void*)d_grad_entropy})
@@ -178,6 +179,16 @@ dc_status dc_residual_norm_backward(const dc_matrix* block, const dc_matrix* pos
     for (const dc_matrix* in : {block, grad_out})
         if (!lies_apart(grad_block, in)) return DC_ERR_INVALID_ARG;
     if (!lies_apart(grad_residual, grad_residual_out)) return DC_ERR_INVALID_ARG;
+    // (as above)
+    if (rows > 0 && cols > 0) {
+        const auto same = [](const dc_matrix* x, const dc_matrix* y) { return x && y && x->d_data == y->d_data; };
+        for (const dc_matrix* m : {residual_out, grad_residual_out, grad_residual, gate, grad_gate})
+            if (same(grad_block, m)) return DC_ERR_INVALID_ARG;
+        for (const dc_matrix* m : {block, residual_out, grad_out, gate, grad_gate})
+            if (same(grad_residual, m)) return DC_ERR_INVALID_ARG;
+        for (const dc_matrix* m : {block, residual_out, grad_residual_out, grad_out, gate})
+            if (same(grad_gate, m)) return DC_ERR_INVALID_ARG;
+    }
     if (!grad_block && !grad_residual && !grad_post_weight && !grad_gate && !grad_pre_weight) return DC_ERR_INVALID_ARG;
     rc = check_workspace(residual_norm_workspace_bytes(rows, cols), d_ws, ws_bytes);
     if (rc != DC_OK) return rc;

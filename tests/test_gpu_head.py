@@ -151,6 +151,28 @@ def test_head(env, rows, vocab, dim, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("rows", [1, 16, 17, 32, 33, 48, 64])
+@pytest.mark.parametrize("vocab,dim", [(5, 256), (4099, 768), (33003, 128), (20011, 2048), (1037, 320)])
+def test_head_few_rows(env, rows, vocab, dim, dtype):
+    h, w, token, mask = draw(env[0], rows, vocab, dim, dtype)
+    check(env, h, w, 0.9, token, mask, 0)
+    check(env, h, w, 1.0, token, None, 3)
+
+
+# ---- rows that lie more than 4 GB apart ----
+
+@pytest.mark.parametrize("rows,pad,vocab,wpad", [(9, 0, 2500, (1 << 20) - 64), (300, 0, 2500, (1 << 20) - 64), (1500, (1 << 21) - 64, 520, 0),
+                                                 (300, (1 << 23) - 64, 600, (1 << 22) + 64)])
+def test_head_far_apart_rows(env, rows, pad, vocab, wpad):
+    h, w, token, mask = draw(env[0], rows, vocab, 64, "bf16")
+    h, w = rows_of(env[0], h, pad, 0), rows_of(env[0], w, wpad, 0)
+    for m in (None, mask):
+        check(env, h, w, 0.9, token, m, 0)
+        check_grad(env, h, w, 0.9, token, m, pads=(wpad, 0) if rows == 9 else None)
+    check(env, h, w, 0.9, token, mask, 4)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("pad,shift,wpad,wshift", [(1, 0, 0, 0), (0, 1, 8, 8), (8, 8, 3, 5), (8, 0, 16, 0), (0, 0, 1, 1), (32, 16, 32, 8)])
 def test_head_strides(env, pad, shift, wpad, wshift, dtype):
     torch, B = env
@@ -317,7 +339,9 @@ def call_grad(env, h, w, temperature, token, mask, stat, entropy, a, b, grad_w="
 def grad_reference(torch, h, w, temperature, token, mask, stat, entropy, a, b, before=None, f32_weight=False):
     """Values and tolerances.  p is off by the logit's error and the roundings of log2 p = (x - M) k - log2 S (|z| and log S are
     rounded, 2^ is good to 2), G by those of its two factors; G is rounded to 2^-11 of itself (16-bit types: f16's half step,
-    eps / 2 = 2^-11; two of them, where the weights' gradient is in 32 bits, 2^-22; 32-bit types: three of bf16, 2^-24) or 2^-38 of its bound; sums of n terms are off by 2 n U.  The last rounding is of
+    eps / 2 = 2^-11; two of them, where the weights' gradient is in 32 bits, 2^-22; 32-bit types: two for each factor, and the product of
+    the small parts is left off, 3 times 2^-22 < 2^-20, which the 2 (6 n + 8) U of their sums hold with room for 2^-23 more) or 2^-38 of
+    its bound; sums of n terms are off by 2 n U.  The last rounding is of
     what was computed, not of the exact value v: off by e before it, |round(v + e) - v| <= e + half_step (|v| + e)."""
     x, dx = logits_of(torch, h, w)
     n, vocab = x.shape

@@ -230,6 +230,12 @@ def test_norm_strides(env, act, res, pad, shift):
         check(env, 5, dim, act, res, gate="token", pad=pad, shift=shift)
 
 
+@pytest.mark.parametrize("rows,dim,pad", [(2100, 64, (1 << 20) - 64), (600, 9000, 1 << 22)])
+def test_norm_far_apart_rows(env, rows, dim, pad):
+    """Rows that lie more than 4 GB apart."""
+    check(env, rows, dim, gate="token", pad=pad, shift=0)
+
+
 @pytest.mark.parametrize("rows,dim", [(1025, 40), (4097, 520), (3001, 2048), (1030, 4100), (300, 8192), (520, 8195)])
 def test_norm_more_rows_than_workgroups(env, rows, dim):
     check(env, rows, dim)

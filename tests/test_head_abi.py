@@ -227,3 +227,17 @@ def test_norm_workspaces_grow_with_rows_and_columns():
             big = B.dc_residual_norm_backward_workspace_bytes(mat(rows=r1, cols=d1))
             assert big >= B.dc_residual_norm_backward_workspace_bytes(mat(rows=r0, cols=d1))
             assert big >= B.dc_residual_norm_backward_workspace_bytes(mat(rows=r1, cols=d0))
+
+
+def test_outputs_in_one_place():
+    bad = B.DC_ERR_INVALID_ARG
+    head_grad(bad, gh=mat(data=3 * A))                                        # both gradients of the head
+    for at in (2, 3, 6):                                                      # residual_out, its gradient, the residual's gradient
+        norm_grad(bad, gb=mat(data=at * A))
+    for at in (1, 2, 4):                                                      # block, residual_out, grad_out
+        norm_grad(bad, gr=mat(data=at * A))
+    rows = B.make_norm(gate_rows=True)
+    for at in (1, 2, 3, 4, 5, 6, 8):
+        norm_grad(bad, gate=mat(data=8 * A), g_gate=mat(data=at * A), prm=rows)
+    norm_grad(bad, gate=mat(data=8 * A), gb=mat(data=8 * A), prm=rows)
+    norm_grad(bad, gate=mat(data=8 * A), gr=mat(data=8 * A), prm=rows)
