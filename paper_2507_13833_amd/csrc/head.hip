@@ -610,9 +610,10 @@ hipError_t launch_head(const HeadArgs& a, void* d_ws, hipStream_t st) {
         return e == hipSuccess ? launch_logprob(out, DC_F32, w.logprob, st) : e;
     }
     const bool live = a.n_top == 0 && a.mask;
-    if (live) e = launch_live_rows(a.mask, nullptr, nullptr, rows, w.live, st);
     const bool f32 = type == DC_F32;
-    if (f32 && e == hipSuccess) e = launch_no_exponents(w.w_exp, (vocab + w.piece - 1) / w.piece, st);
+    const FirstExponents none = {w.w_exp, f32 ? (vocab + w.piece - 1) / w.piece : 0, false};
+    if (live) e = launch_live_rows(a.mask, nullptr, nullptr, rows, w.live, none, st);
+    else if (f32) e = launch_first_exponents(none, st);
     HeadStatArgs h = {};
     h.x_exp = f32 ? w.x_exp : nullptr;
     h.steps = sh.k_pad / PK;

@@ -8,7 +8,7 @@
 //
 // G, the weights and the hidden states are held in f16 (11 bits, three more than bf16's), each times a power of two that takes its
 // largest magnitude to just below 2^15: per row for G (from |a|, |b| and H, which bound it), undone in the row's hidden gradient and in
-// the row's hidden state, per piece for the weights.  G in one f16 is off by at most 2^-11 of each value, before sums of 32 bits that are
+// the row's hidden state, per piece for the weights (f16 ones stay as they are).  G in one f16 is off by at most 2^-11 of each value, before sums of 32 bits that are
 // rounded to 16 bits themselves; for a gradient of the weights in 32 bits it takes two (2^-22).  Operands of 32 bits are two f16 as
 // well, and three of the four products of their parts are summed (the fourth is 2^-22).
 #include <algorithm>
@@ -394,9 +394,7 @@ hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
     const HeadGradWs w = carve_grad(d_ws, a.hidden, a.weight, gw.d_data ? gw.type : type);
     const HeadShape sh = head_shape(a.hidden, a.weight, true);
     const bool f32 = type == DC_F32;
-    hipError_t e = launch_live_rows(a.mask, a.grad_logprob, a.grad_entropy, rows, w.live, st);
-    if (e != hipSuccess) return e;
-    e = launch_no_exponents(w.top, w.pieces + 1, st);
+    hipError_t e = launch_live_rows(a.mask, a.grad_logprob, a.grad_entropy, rows, w.live, {w.top, w.pieces + 1, type == DC_F16}, st);
     const TermArgs t = {a.hidden.d_data, a.hidden.row_stride, rows, dim, vocab, a.inv_t, a.token, a.stat, a.entropy,
                         a.grad_logprob, a.grad_entropy, w.live.pos, w.term, w.x_exp, w.top, a.status};
     const unsigned waves4 = (unsigned)std::min<int64_t>((rows + 3) / 4, TOP_BLOCKS);
@@ -449,7 +447,7 @@ hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
     for (int32_t i = 0; i < w.pieces && e == hipSuccess; ++i) {
         const int32_t v0 = i * w.piece, n = std::min(w.piece, vocab - v0);
         int32_t* const top_w = w.top + 1 + i;
-        if (gh.d_data || f32) e = launch_top_exponent(a.weight, v0, n, top_w, st);
+        if (f32 || (gh.d_data && type == DC_BF16)) e = launch_top_exponent(a.weight, v0, n, top_w, st);
         if (gh.d_data && e == hipSuccess) e = launch_lay_columns(a.weight, v0, n, nullptr, nullptr, w.piece, top_w, nullptr, w.wt, w.wt_plane, st);
         if (sh.copy_weight) {
             if (e == hipSuccess) e = launch_lay_rows(a.weight, v0, n, nullptr, nullptr, sh.k_pad, w.weight, w.weight_plane, F16S, nullptr, top_w, st);

@@ -32,7 +32,9 @@ hipError_t launch_lay_rows(const dc_matrix& src, int64_t first, int64_t n, const
 hipError_t launch_row_exponents(const dc_matrix& src, int64_t n, const int32_t* list, const int32_t* count, int32_t* out, hipStream_t st);
 // *top, raised to the same of rows first .. first + n - 1.
 hipError_t launch_top_exponent(const dc_matrix& src, int64_t first, int64_t n, int32_t* top, hipStream_t st);
-hipError_t launch_no_exponents(int32_t* top, int32_t n, hipStream_t st);
+// What raised exponents begin with.  exact: all but the first are 15 instead, which leaves numbers as they are (f16 wants no other).
+struct FirstExponents { int32_t* top; int32_t n; bool exact; };
+hipError_t launch_first_exponents(const FirstExponents& x, hipStream_t st);
 
 // The other way round: planes of [cols][rows_pad] f16, one for 16-bit numbers and two for others, rows behind the last one 0 to the next
 // multiple of 64.  Values become 2^(15 - *top - term's exponent) times as much (a row's own exponent where there are terms).
@@ -47,8 +49,9 @@ struct alignas(16) RowTerm { float m, l2, c0, c1, ga; int32_t token, exponent, x
 
 // The live rows of a batch, in order: list, their number, and where each row went (-1: nowhere).
 struct LiveRows { int32_t* list; int32_t* pos; int32_t* count; };
-// A row is live where its mask byte is not 0 (mask NULL: everywhere) and, where a is given, a or b is not 0.
-hipError_t launch_live_rows(const uint8_t* mask, const float* a, const float* b, int64_t n, const LiveRows& l, hipStream_t st);
+// A row is live where its mask byte is not 0 (mask NULL: everywhere) and, where a is given, a or b is not 0.  Writes x on the way.
+hipError_t launch_live_rows(const uint8_t* mask, const float* a, const float* b, int64_t n, const LiveRows& l, const FirstExponents& x,
+                            hipStream_t st);
 
 // Which of the planes of two operands are multiplied: of two f16 each, all pairs but the two small ones.
 Parts parts_of(int32_t type, int64_t a_plane, int64_t b_plane);

@@ -90,11 +90,12 @@ hipError_t launch_lay_rows(const dc_matrix& src, int64_t first, int64_t n, const
 
 // ---- powers of two ----
 
-__global__ __launch_bounds__(256) void no_exponents_kernel(int32_t* top, int32_t n) {
-    for (int32_t i = threadIdx.x; i < n; i += 256) top[i] = NO_EXPONENT;
+__device__ __forceinline__ void write_first(const FirstExponents& x) {
+    for (int32_t i = threadIdx.x; i < x.n; i += blockDim.x) x.top[i] = i > 0 && x.exact ? 15 : NO_EXPONENT;
 }
-hipError_t launch_no_exponents(int32_t* top, int32_t n, hipStream_t st) {
-    no_exponents_kernel<<<1, 256, 0, st>>>(top, n);
+__global__ __launch_bounds__(256) void first_exponents_kernel(const FirstExponents x) { write_first(x); }
+hipError_t launch_first_exponents(const FirstExponents& x, hipStream_t st) {
+    first_exponents_kernel<<<1, 256, 0, st>>>(x);
     return hipGetLastError();
 }
 
@@ -118,27 +119,21 @@ hipError_t launch_row_exponents(const dc_matrix& src, int64_t n, const int32_t* 
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void top_exponent_kernel(const T* w, int64_t stride, int64_t rows, int32_t cols, int32_t* top) {
+__global__ __launch_bounds__(256) void top_exponent_kernel(const T* w, int64_t stride, int64_t rows, int32_t cols, int32_t last_cols, int32_t* top) {
     __shared__ int tmp[4];
     uint32_t big = 0;
-    for (int64_t r = blockIdx.x * 4LL + threadIdx.x / WAVE; r < rows; r += gridDim.x * 4LL) big = max(big, row_top(w + r * stride, cols));
+    for (int64_t r = blockIdx.x * 4LL + threadIdx.x / WAVE; r < rows; r += gridDim.x * 4LL) big = max(big, row_top(w + r * stride, r + 1 < rows ? cols : last_cols));
     raise_top(exponent_above(__uint_as_float(wave_top(big))), tmp, top);
 }
 hipError_t launch_top_exponent(const dc_matrix& src, int64_t first, int64_t n, int32_t* top, hipStream_t st) {
-    // (rows that follow each other directly: as whole pieces of 8192 elements, and the rest as one)
-    const int64_t together = src.row_stride == src.n_cols ? n * src.n_cols / 8192 : 0, left = src.row_stride == src.n_cols ? n * src.n_cols % 8192 : 0;
+    // (rows that follow each other directly: as pieces of 8192 elements, the last one shorter)
+    const bool together = src.row_stride == src.n_cols;
+    const int64_t all = n * src.n_cols, rows = together ? (all + 8191) / 8192 : n, stride = together ? 8192 : src.row_stride;
+    const int32_t cols = together ? 8192 : (int32_t)src.n_cols, last = together ? (int32_t)(all - (rows - 1) * 8192) : cols;
     return with_type(src.type, [&](auto el) {
         using T = typename decltype(el)::type;
         const T* from = static_cast<const T*>(src.d_data) + first * src.row_stride;
-        const auto go = [&](const T* x, int64_t stride, int64_t rows, int64_t cols) {
-            if (rows > 0 && cols > 0) top_exponent_kernel<T><<<(unsigned)std::min<int64_t>(TOP_BLOCKS, (rows + 3) / 4), 256, 0, st>>>(x, stride, rows, (int32_t)cols, top);
-        };
-        if (src.row_stride == src.n_cols) {
-            go(from, 8192, together, 8192);
-            go(from + together * 8192, left, 1, left);
-        } else {
-            go(from, src.row_stride, n, src.n_cols);
-        }
+        top_exponent_kernel<T><<<(unsigned)std::min<int64_t>(TOP_BLOCKS, (rows + 3) / 4), 256, 0, st>>>(from, stride, rows, cols, last, top);
         return hipGetLastError();
     });
 }
@@ -172,12 +167,17 @@ __global__ __launch_bounds__(256) void lay_columns_kernel(const S* src, int64_t 
             for (int j = 0; j < N; ++j) tile[i][tid % LANES * N + j] = r < rows ? ldexpf((float)in.e[j], x) : 0.0f;
         }
     } else {
-        for (int i = tid / 64; i < 64; i += 4) {
-            const int64_t r = r0 + i;
-            const int32_t c = c0 + (tid & 63);
-            float v = 0.0f;
-            if (r < rows && c < cols) v = ldexpf((float)src[(list ? list[r] : first + r) * stride + c], up - (term ? term[r].exponent : 0));
-            tile[i][tid & 63] = v;
+        const int32_t c = c0 + (tid & 63);
+        S in[16];
+#pragma unroll
+        for (int h = 0; h < 16; ++h) {
+            const int64_t r = min(r0 + tid / 64 + 4 * h, rows - 1);
+            in[h] = src[(list ? list[r] : first + r) * stride + min(c, cols - 1)];
+        }
+#pragma unroll
+        for (int h = 0; h < 16; ++h) {
+            const int64_t r = r0 + tid / 64 + 4 * h;
+            tile[tid / 64 + 4 * h][tid & 63] = r < rows && c < cols ? ldexpf((float)in[h], up - (term ? term[r].exponent : 0)) : 0.0f;
         }
     }
     __syncthreads();
@@ -220,8 +220,10 @@ hipError_t launch_lay_columns(const dc_matrix& src, int64_t first, int64_t n, co
 // One workgroup, eight neighbouring rows to a thread: a chain of scans, 8192 rows each, and as many trips to memory (8192 rows: 8 us;
 // more rows have products that take a hundred times as long).
 constexpr int LIVE_THREADS = 1024, LIVE_EACH = 8;
-__global__ __launch_bounds__(LIVE_THREADS) void live_rows_kernel(const uint8_t* mask, const float* a, const float* b, int64_t n, LiveRows l) {
+__global__ __launch_bounds__(LIVE_THREADS) void live_rows_kernel(const uint8_t* mask, const float* a, const float* b, int64_t n, LiveRows l,
+                                                                 const FirstExponents x) {
     __shared__ int32_t tmp[LIVE_THREADS / WAVE];
+    write_first(x);
     int32_t before = 0;
     for (int64_t r0 = 0; r0 < n; r0 += LIVE_THREADS * LIVE_EACH) {
         const int64_t r = r0 + threadIdx.x * LIVE_EACH;
@@ -245,8 +247,8 @@ __global__ __launch_bounds__(LIVE_THREADS) void live_rows_kernel(const uint8_t* 
     }
     if (threadIdx.x == 0) *l.count = before;
 }
-hipError_t launch_live_rows(const uint8_t* mask, const float* a, const float* b, int64_t n, const LiveRows& l, hipStream_t st) {
-    live_rows_kernel<<<1, LIVE_THREADS, 0, st>>>(mask, a, b, n, l);
+hipError_t launch_live_rows(const uint8_t* mask, const float* a, const float* b, int64_t n, const LiveRows& l, const FirstExponents& x, hipStream_t st) {
+    live_rows_kernel<<<1, LIVE_THREADS, 0, st>>>(mask, a, b, n, l, x);
     return hipGetLastError();
 }
 

@@ -486,6 +486,17 @@ def test_head_backward_token_outside_and_rows_without_a_distribution(env):
     assert got["hidden"][5].isnan().all() and torch.equal(got["hidden"][rest], clean["hidden"][rest]) and got["weight"].isnan().all()
 
 
+@pytest.mark.parametrize("rows", [3, 200])
+@pytest.mark.parametrize("scale", [2.0 ** -19, 2.0 ** 13])
+def test_head_f16_at_the_ends_of_its_range(env, rows, scale):
+    """Weights among the type's subnormal numbers, and next to its largest."""
+    h, w, token, mask = draw(env[0], rows, 700, 96, "f16")
+    w = (w * scale).clamp(-6e4, 6e4)
+    h = h if scale < 1 else h / scale
+    check(env, h, w, 1.0, token, mask, 0)
+    check_grad(env, h, w, 1.0, token, mask)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_head_backward_rows_of_very_different_size(env, dtype):
     """Gradients from 2^-90 to 2^6 in one batch, and hidden rows of different sizes: each row's own gradient is as exact as if it were
