@@ -41,7 +41,8 @@ __device__ __forceinline__ float less_reference(float m, float k, float base, fl
 
 // Bound by the matrix cores, and by the clock that the card holds under them (1.5 to 1.6 of 2.4 GHz): the next tile's first operands
 // come while a tile's sums are taken.  us a call, Q = 8: 8192 rows x 152064 x 2048 bf16 3660 to 3830 (1.33 to 1.39 PFLOP/s; a
-// library's product of these sizes alone 3580), 6144 of 8192 x 32000 x 1024 345 (1.17); Q = 4: 200 of 333 x 32003 x 515 f32 123.
+// library's product of these sizes alone 3580), 6144 of 8192 x 32000 x 1024 345 (1.17); 200 of 333 x 32003 x 515 f32 115,
+// of which it takes 52.
 // Also measured on the large one: 128 rows by 256 entries, two workgroups to a compute unit, 5500; eight waves of 128 by 64 with four
 // shorter stages 4650; sums that the compiler places 12 700 (copied from and to their registers).
 template <typename T, bool ENTROPY, int Q>
