@@ -477,7 +477,8 @@ dc_status dc_head_logprob(const dc_matrix* hidden, const dc_matrix* weight, doub
  *   grad_hidden[r, :] = sum_v G[r, v] weight[v, :],   grad_weight[v, :] (+)= sum_r G[r, v] hidden[r, :].
  * Either may be NULL.  grad_hidden: hidden's type and shape; rows with mask byte 0, and those whose a and b are both zero, get +0 and
  * their hidden rows are not looked at.  grad_weight: weight's shape, weight's type or f32; accumulate == 0: written, != 0: added to
- * in 32 bits before it is rounded.  Neither may overlap another array of the call.
+ * in 32 bits before it is rounded.  Neither may overlap another array of the call (INVALID_ARG, but for the workspace and for
+ * matrices of several rows that overlap at different row_strides: not looked for).
  * Sums are held in 32 bits, in an order that depends on the sizes and on which rows take part (identical inputs give identical bits),
  * and rounded once.  The factors are rounded before they are multiplied, in types of 16 bits to 11 bits, G for a grad_weight in f32
  * and everything in types of 32 bits to 22; of a row's largest possible G, and of the largest magnitude of weight, what is below
@@ -515,7 +516,7 @@ typedef struct dc_norm_params {
  * post_weight, pre_weight: one row, any type.  gate: one row (any type) for all rows, or with
  * gate_rows n_rows of them in block's type.
  * residual_out may be residual's own memory (same d_data and row_stride), out may be block's; no output overlaps another array
- * otherwise.
+ * otherwise (INVALID_ARG, but for matrices of several rows that overlap at different row_strides: not looked for).
  * Host errors: INVALID_ARG, UNSUPPORTED_SIZE (n_cols above DC_MAX_DIM), HIP.
  */
 dc_status dc_residual_norm(const dc_matrix* block, const dc_matrix* post_weight, const dc_matrix* gate, const dc_matrix* residual,
@@ -534,7 +535,7 @@ dc_status dc_residual_norm(const dc_matrix* block, const dc_matrix* post_weight,
  * of one row, any type.  Any of the gradients that are written may be NULL: not wanted.  accumulate != 0: those others are added to
  * in 32 bits before they are rounded.  Sums over rows are held in 32 bits in an order that depends on the sizes alone.
  * grad_block may be block's or grad_out's own memory, grad_residual grad_residual_out's (same d_data and row_stride); no output
- * overlaps another array otherwise.
+ * overlaps another array otherwise (as above).
  * d_ws: 256-byte aligned, dc_residual_norm_backward_workspace_bytes(block) bytes, which also serve every call of fewer rows, fewer
  * columns or both; holds nothing the caller needs afterwards.
  * Host errors: INVALID_ARG, UNSUPPORTED_SIZE (n_cols above DC_MAX_DIM), WORKSPACE, HIP.

@@ -1,6 +1,7 @@
 // C-ABI entry points of the head's log-probabilities without logits and of the residual norm: host-side validation and launches,
 // nothing else.
 #include <cmath>
+#include <utility>
 #include "api_checks.h"
 #include "head_internal.h"
 
@@ -30,9 +31,32 @@ static dc_status check_shaped(const dc_matrix* m, int64_t rows, int64_t cols, in
     return m->n_rows != rows || m->n_cols != cols || (type >= 0 && m->type != type) ? DC_ERR_INVALID_ARG : DC_OK;
 }
 
-// An output may lie where an input does only row by row.
-static bool lies_apart(const dc_matrix* out, const dc_matrix* in) {
-    return !out || !in || out->d_data != in->d_data || out->n_rows <= 1 || out->row_stride == in->row_stride;
+// An array of a call: rows of so many bytes, `pitch` from one to the next.
+struct Place { uintptr_t p; int64_t rows, bytes, pitch; };
+static Place place_of(const dc_matrix* m) {
+    if (!m) return Place{};
+    const int64_t each = (int64_t)elem_bytes(m->type);
+    return Place{reinterpret_cast<uintptr_t>(m->d_data), m->n_rows, m->n_cols * each, m->row_stride * each};
+}
+static Place place_of(const void* p, int64_t bytes) { return Place{reinterpret_cast<uintptr_t>(p), 1, bytes, bytes}; }
+
+// Whether two arrays share a byte.  Rows that interleave, as columns of one matrix do, share none.  Not decided, and so not refused:
+// two of several rows with different distances that do not begin in one place.
+static bool overlap(Place a, Place b) {
+    if (!a.p || !b.p || a.rows < 1 || b.rows < 1 || a.bytes < 1 || b.bytes < 1) return false;
+    if (a.p > b.p) std::swap(a, b);
+    const int64_t d = (int64_t)(b.p - a.p);
+    if (d == 0) return true;
+    if (d >= (a.rows - 1) * a.pitch + a.bytes) return false;
+    if (a.rows == 1) return true;
+    if (b.rows > 1 && a.pitch != b.pitch) return false;
+    // b begins within a row of a, or between two and reaches the next
+    return d % a.pitch < a.bytes || d % a.pitch + b.bytes > a.pitch;
+}
+// The same, but for an output that may lie in an input's place (of the same type and shape) row by row.
+static bool overlap(const dc_matrix* out, const dc_matrix* in, bool in_place) {
+    if (in_place && out && in && out->d_data == in->d_data && (out->n_rows <= 1 || out->row_stride == in->row_stride)) return false;
+    return overlap(place_of(out), place_of(in));
 }
 
 static dc_status check_norm(const dc_matrix* block, const dc_matrix* post, const dc_matrix* gate, const dc_matrix* pre,
@@ -106,13 +130,16 @@ dc_status dc_head_logprob_backward(const dc_matrix* hidden, const dc_matrix* wei
     if (grad_hidden && (rc = check_shaped(grad_hidden, hidden->n_rows, hidden->n_cols, hidden->type)) != DC_OK) return rc;
     if (grad_weight && (rc = check_shaped(grad_weight, weight->n_rows, weight->n_cols, -1)) != DC_OK) return rc;
     if (grad_weight && grad_weight->type != weight->type && grad_weight->type != DC_F32) return DC_ERR_INVALID_ARG;
-    for (const dc_matrix* out : {grad_hidden, grad_weight})
-        if (out && out->d_data && (out->d_data == hidden->d_data || out->d_data == weight->d_data)) return DC_ERR_INVALID_ARG;
-    if (grad_hidden && grad_weight && hidden->n_rows > 0 && grad_hidden->d_data == grad_weight->d_data) return DC_ERR_INVALID_ARG;
     if (hidden->n_rows > 0 && (!d_row_stat || !d_grad_logprob || (d_grad_entropy && !d_entropy))) return DC_ERR_INVALID_ARG;
     for (const void* p : {(const void*)d_token, (const void*)d_row_stat, (const void*)d_entropy, (const void*)d_grad_logprob,
                           (const void*)d_grad_entropy})
         if (!aligned_to(p, 4)) return DC_ERR_INVALID_ARG;
+    const int64_t n = hidden->n_rows;
+    const Place ins[] = {place_of(hidden), place_of(weight), place_of(d_token, n * 4), place_of(d_mask, n), place_of(d_row_stat, n * 8),
+                         place_of(d_entropy, n * 4), place_of(d_grad_logprob, n * 4), place_of(d_grad_entropy, n * 4)};
+    for (const Place& in : ins)
+        if (overlap(place_of(grad_hidden), in) || overlap(place_of(grad_weight), in)) return DC_ERR_INVALID_ARG;
+    if (overlap(place_of(grad_hidden), place_of(grad_weight))) return DC_ERR_INVALID_ARG;
     const int32_t type = grad_weight ? grad_weight->type : hidden->type;
     rc = check_workspace(head_grad_workspace_bytes(*hidden, *weight, type), d_ws, ws_bytes);
     if (rc != DC_OK) return rc;
@@ -132,13 +159,15 @@ dc_status dc_residual_norm(const dc_matrix* block, const dc_matrix* post_weight,
         return residual_out ? rc : DC_ERR_INVALID_ARG;
     if ((pre_weight == nullptr) != (out == nullptr)) return DC_ERR_INVALID_ARG;
     if (out && (rc = check_shaped(out, block->n_rows, block->n_cols, block->type)) != DC_OK) return rc;
-    if (!lies_apart(residual_out, residual) || !lies_apart(out, block) || !aligned_to(d_row_stat, 4)) return DC_ERR_INVALID_ARG;
-    // (elsewhere than on their own inputs the outputs overlap nothing)
-    if (block->n_rows > 0 && block->n_cols > 0) {
-        if (out && (out->d_data == residual_out->d_data || out->d_data == residual->d_data)) return DC_ERR_INVALID_ARG;
-        if (residual_out->d_data == block->d_data || (gate && (residual_out->d_data == gate->d_data || (out && out->d_data == gate->d_data))))
-            return DC_ERR_INVALID_ARG;
-    }
+    if (!aligned_to(d_row_stat, 4)) return DC_ERR_INVALID_ARG;
+    const Place stat = place_of(d_row_stat, block->n_rows * 8);
+    for (const dc_matrix* in : {block, post_weight, gate, residual, pre_weight, residual_out, out})
+        if (overlap(stat, place_of(in))) return DC_ERR_INVALID_ARG;
+    for (const dc_matrix* in : {post_weight, gate, pre_weight})
+        if (overlap(residual_out, in, false) || overlap(out, in, false)) return DC_ERR_INVALID_ARG;
+    if (overlap(residual_out, residual, true) || overlap(residual_out, block, false) || overlap(out, residual, false) ||
+        overlap(out, block, true) || overlap(residual_out, out, false))
+        return DC_ERR_INVALID_ARG;
     const NormArgs a = {block->n_rows, (int32_t)block->n_cols, block->type, residual->type, (float)prm->eps, (float)prm->residual_scale,
                         (float)prm->block_scale, factor_of(post_weight), factor_of(gate, prm->gate_rows), factor_of(pre_weight), post_weight != nullptr,
                         pre_weight != nullptr, stream_of(block), stream_of(residual), stream_of(residual_out), stream_of(out), d_row_stat};
@@ -176,18 +205,15 @@ dc_status dc_residual_norm_backward(const dc_matrix* block, const dc_matrix* pos
     if (grad_gate && (rc = check_shaped(grad_gate, gate->n_rows, cols, gate_rows ? block->type : -1)) != DC_OK) return rc;
     if (rows > 0 && (post_weight || pre_weight) && !d_row_stat) return DC_ERR_INVALID_ARG;
     if (!aligned_to(d_row_stat, 4)) return DC_ERR_INVALID_ARG;
-    for (const dc_matrix* in : {block, grad_out})
-        if (!lies_apart(grad_block, in)) return DC_ERR_INVALID_ARG;
-    if (!lies_apart(grad_residual, grad_residual_out)) return DC_ERR_INVALID_ARG;
-    // (as above)
-    if (rows > 0 && cols > 0) {
-        const auto same = [](const dc_matrix* x, const dc_matrix* y) { return x && y && x->d_data == y->d_data; };
-        for (const dc_matrix* m : {residual_out, grad_residual_out, grad_residual, gate, grad_gate})
-            if (same(grad_block, m)) return DC_ERR_INVALID_ARG;
-        for (const dc_matrix* m : {block, residual_out, grad_out, gate, grad_gate})
-            if (same(grad_residual, m)) return DC_ERR_INVALID_ARG;
-        for (const dc_matrix* m : {block, residual_out, grad_residual_out, grad_out, gate})
-            if (same(grad_gate, m)) return DC_ERR_INVALID_ARG;
+    const Place stat = place_of(d_row_stat, rows * 8);
+    const dc_matrix* const outs[] = {grad_block, grad_residual, grad_post_weight, grad_gate, grad_pre_weight};
+    for (int o = 0; o < 5; ++o) {
+        if (overlap(place_of(outs[o]), stat)) return DC_ERR_INVALID_ARG;
+        for (const dc_matrix* in : {post_weight, gate, residual_out, pre_weight})
+            if (overlap(outs[o], in, false)) return DC_ERR_INVALID_ARG;
+        if (overlap(outs[o], block, o == 0) || overlap(outs[o], grad_out, o == 0) || overlap(outs[o], grad_residual_out, o == 1)) return DC_ERR_INVALID_ARG;
+        for (int other = 0; other < o; ++other)
+            if (overlap(outs[o], outs[other], false)) return DC_ERR_INVALID_ARG;
     }
     if (!grad_block && !grad_residual && !grad_post_weight && !grad_gate && !grad_pre_weight) return DC_ERR_INVALID_ARG;
     rc = check_workspace(residual_norm_workspace_bytes(rows, cols), d_ws, ws_bytes);

@@ -241,3 +241,78 @@ def test_outputs_in_one_place():
         norm_grad(bad, gate=mat(data=8 * A), g_gate=mat(data=at * A), prm=rows)
     norm_grad(bad, gate=mat(data=8 * A), gb=mat(data=8 * A), prm=rows)
     norm_grad(bad, gate=mat(data=8 * A), gr=mat(data=8 * A), prm=rows)
+
+
+def norm_grad_places(**at):
+    """A call of every gradient whose arrays lie apart, but for those named: place, and rows' distance or columns where these are given too."""
+    spec = dict(block=(4, 1), post=(1, 2), gate=(1, 3), res_out=(4, 4), pre=(1, 5), stat=6, dh=(4, 7), dy=(4, 8), gb=(4, 9), gr=(4, 10),
+                g_post=(1, 11), g_gate=(1, 12), g_pre=(1, 13))
+    gate_rows = at.pop("gate_rows", False)
+    for name in ("gate", "g_gate") if gate_rows else ():
+        spec[name] = (4, spec[name][1])
+    m = {}
+    for name, where in spec.items():
+        if name == "stat":
+            m[name] = at.get(name, where * A)
+            continue
+        place = at.get(name, where[1] * A)
+        m[name] = mat(rows=where[0], data=place[0], stride=place[1]) if isinstance(place, tuple) else mat(rows=where[0], data=place)
+    return [m["block"], m["post"], m["gate"], m["res_out"], m["pre"], B.make_norm(gate_rows=gate_rows), m["stat"], m["dh"], m["dy"], m["gb"],
+            m["gr"], False, m["g_post"], m["g_gate"], m["g_pre"], A * 64]
+
+
+def test_no_output_of_the_norm_in_another_arrays_place():
+    """Every output against every other array, but for the places that the contract names: the same place, and a row's end or begin within."""
+    accepted = lambda **at: refuses(B.DC_ERR_WORKSPACE, B.dc_residual_norm_backward, *norm_grad_places(**at), 0)  # noqa: E731
+    refused = lambda **at: refuses(B.DC_ERR_INVALID_ARG, B.dc_residual_norm_backward, *norm_grad_places(**at), 0)  # noqa: E731
+    accepted()
+    accepted(gate_rows=True)
+    place = dict(block=1, post=2, gate=3, res_out=4, pre=5, stat=6, dh=7, dy=8, gb=9, gr=10, g_post=11, g_gate=12, g_pre=13)
+    for out in ("gb", "gr", "g_post", "g_gate", "g_pre"):
+        for other, at in place.items():
+            if other == out:
+                continue
+            for rows in (False, True):
+                if (out, other) in (("gb", "block"), ("gb", "dy"), ("gr", "dh")):
+                    accepted(**{out: at * A}, gate_rows=rows)
+                    refused(**{out: (at * A, 72)}, gate_rows=rows)
+                    accepted(**{out: (at * A, 72), other: (at * A, 72)}, gate_rows=rows)
+                else:
+                    refused(**{out: at * A}, gate_rows=rows)
+            if other != "stat":
+                refused(**{out: at * A + 2})                  # one element further on
+                refused(**{out: at * A - 2})
+            accepted(**{out: at * A - 4 * 64 * 2 if out in ("gb", "gr") else at * A - 64 * 2})        # ends where the other begins
+    # columns of one matrix: rows that interleave, beside each other and one element into each other
+    accepted(gb=(9 * A, 128), gr=(9 * A + 128, 128))
+    refused(gb=(9 * A, 128), gr=(9 * A + 126, 128))
+    refused(gb=(9 * A, 127), gr=(9 * A + 128, 127))
+    accepted(gb=(9 * A, 128), g_pre=9 * A + 128, g_post=9 * A + 256 + 128)                            # a row in a gap
+    refused(gb=(9 * A, 128), g_pre=9 * A + 130)
+    # the forward call
+    call = lambda res_out, out, stat: refuses(  # noqa: E731
+        B.DC_ERR_INVALID_ARG, B.dc_residual_norm, mat(), mat(rows=1, data=2 * A), mat(rows=1, data=3 * A), mat(data=4 * A), mat(rows=1, data=5 * A),
+        B.make_norm(), mat(data=res_out), mat(data=out), stat)
+    for at in (1, 2, 3, 5, 7):
+        call(at * A, 7 * A, 8 * A)
+    for at in (2, 3, 4, 5, 6):
+        call(6 * A, at * A, 8 * A)
+    for at in (1, 2, 3, 4, 5, 6, 7):
+        call(6 * A, 7 * A, at * A)
+    call(4 * A + 2, 7 * A, 8 * A)
+    call(6 * A, A - 2, 8 * A)
+    call(6 * A, 7 * A, 6 * A + 508)                           # statistics at the end of an output
+
+
+def test_no_gradient_of_the_head_in_another_arrays_place():
+    def grad(code, gh, gw):
+        refuses(code, B.dc_head_logprob_backward, mat(), mat(rows=100, data=2 * A), 1.0, 3 * A, 4 * A, 5 * A, 6 * A, 7 * A, 8 * A,
+                mat(data=gh), 0, mat(rows=100, data=gw), A * 64, 0, A)
+
+    grad(B.DC_ERR_WORKSPACE, 10 * A, 11 * A)
+    for at in range(1, 9):                                    # hidden, weight, token, mask, stat, entropy, both gradients
+        grad(B.DC_ERR_INVALID_ARG, at * A, 11 * A)
+        grad(B.DC_ERR_INVALID_ARG, 10 * A, at * A)
+        grad(B.DC_ERR_INVALID_ARG, 10 * A, at * A - 99 * 64 * 2)
+    grad(B.DC_ERR_INVALID_ARG, 11 * A + 50 * 128, 11 * A)
+    grad(B.DC_ERR_WORKSPACE, 11 * A - 4 * 128, 11 * A)
