@@ -307,6 +307,7 @@ __device__ __forceinline__ D take_part(float& rest) {
 
 constexpr int NO_EXPONENT = -100000;
 __device__ __forceinline__ int exponent_above(float magnitude) { return (int)(__float_as_uint(magnitude) >> 23) - 126; }     // 2^it is above
+__device__ __forceinline__ int exponent_above(double magnitude) { return (int)((uint64_t)__double_as_longlong(magnitude) >> 52) - 1022; }
 // A wave's largest finite magnitude of a row, as bits (those of a float without a sign sort like it).
 template <typename T>
 __device__ __forceinline__ uint32_t row_top(const T* row, int32_t cols) {

@@ -44,10 +44,11 @@ __global__ __launch_bounds__(256) void head_terms_kernel(const TermArgs t) {
     for (int64_t r = blockIdx.x * 4LL + threadIdx.x / WAVE; r < t.n_rows; r += gridDim.x * 4LL) {
         const int32_t at = t.pos[r];
         if (at < 0) continue;
-        const float a = t.a[r] * t.inv_t, b = t.b ? t.b[r] * t.inv_t : 0.0f, h = b != 0.0f ? t.entropy[r] : 0.0f;
+        // (in 64 bits: a / T may be subnormal in 32 or beyond them, and what it is multiplied with takes it back)
+        const double a = (double)t.a[r] * t.inv_t, b = t.b ? (double)t.b[r] * t.inv_t : 0.0, h = b != 0.0 ? (double)t.entropy[r] : 0.0;
         // |p (log p + H)| <= max(1 / e, H)
-        const float bound = fabsf(a) + fabsf(b) * (fabsf(h) + 1.0f);
-        const int e = bound < INFINITY ? max(-120, min(100, 14 - exponent_above(bound))) : 0;
+        const double bound = fabs(a) + fabs(b) * (fabs(h) + 1.0);
+        const int e = bound < INFINITY ? 14 - exponent_above(bound) : 0;
         const int x_exp = exponent_above(__uint_as_float(wave_top(row_top(static_cast<const T*>(t.x) + r * t.stride, t.dim))));
         most = max(most, x_exp - e);
         if (lane == 0) {
@@ -60,8 +61,8 @@ __global__ __launch_bounds__(256) void head_terms_kernel(const TermArgs t) {
                     token = -1;
                 }
             }
-            t.term[at] = RowTerm{t.stat[2 * r], t.stat[2 * r + 1] * LOG2E, ldexpf(b != 0.0f ? -fmaf(b, h, a) : -a, e), ldexpf(-b * LN2, e),
-                                 ldexpf(a, e), token, e, x_exp};
+            t.term[at] = RowTerm{t.stat[2 * r], t.stat[2 * r + 1] * LOG2E, (float)ldexp(b != 0.0 ? -fma(b, h, a) : -a, e),
+                                 (float)(ldexp(-b, e) * (double)LN2), (float)ldexp(a, e), token, e, x_exp};
         }
     }
     raise_top(most, tmp, t.top);

@@ -510,6 +510,26 @@ def test_head_backward_rows_of_very_different_size(env, dtype):
     check_grad(env, h, w, 1.0, token, None, a=a * scale, b=b * scale, grad_w="f32")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("size,temperature,scale", [(-60, 1.0, 20), (-105, 0.7, 20), (-115, 1.0, 30), (-118, 1.0, 40), (-118, 2.0 ** 24, 60), (-145, 1.0, 60),
+                                                    (118, 2.0 ** -20, -40)])
+def test_head_backward_gradients_at_the_ends_of_the_range(env, dtype, size, temperature, scale):
+    """Gradients of the logits that are subnormal in 32 bits, or beyond their range, with weights (then hidden rows) that take a result
+    back into it: as exact as any other."""
+    torch, B = env
+    h, w, token, mask = draw(torch, 60, 500, 64, dtype)
+    a, b = gradients(torch, 60)
+    # (a subnormal a has few bits of its own, and is given as it is)
+    a, b = (torch.ldexp(x.double(), torch.tensor(float(size), device="cuda").double()).float() for x in (a, b))
+    # (the other gradient goes further out of the range by as much: below 2^-149, or to 2^158 and more)
+    for k in (scale, -scale):
+        hk, wk = (torch.ldexp(x.float(), torch.tensor(float(e), device="cuda")).to(x.dtype) for x, e in ((h, -k), (w, k)))
+        hk = torch.ldexp(hk.float(), torch.tensor(math.log2(temperature), device="cuda").round()).to(h.dtype)
+        check_grad(env, hk, wk, temperature, token, mask, a=a, b=b, **(dict(grad_w=None) if k == scale else dict(hidden=False)))
+        if k != scale:
+            check_grad(env, hk, wk, temperature, token, None, a=a, b=b, hidden=False, grad_w="f32")
+
+
 def test_head_backward_parts_alone(env):
     """Either gradient without the other is the same bits."""
     torch, B = env
