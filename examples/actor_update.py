@@ -2,12 +2,13 @@
 
 A rollout batch goes through the reshard (balance, advantages, plan, gather); one data-parallel rank's micro-batches then
 go through a small actor: the embedding of their token ids, a linear block whose normed result joins the residual stream, the
-stream normed for the head, the log-probabilities of the next tokens without a matrix of logits, the clipped policy objective
+stream normed for the head, the log-probabilities of the next tokens without a matrix of logits (or, with --keep-logits, from a
+matrix of them, which a program that does more with its logits has anyway), the clipped policy objective
 with an entropy bonus, and back, and AdamW with 8-bit states steps on 32-bit master weights.
 The actor is a bigram model (the next token's logits come from the current token's embedding alone): what it learns is not
 the point, what it calls is.
 
-    python examples/actor_update.py
+    python examples/actor_update.py [--keep-logits]
 """
 from __future__ import annotations
 
@@ -27,7 +28,7 @@ from paper_2507_13833_amd import runner, workloads
 class Actor:
     """Weights, gradients and optimizer states of the model, and the calls of its forward and backward pass."""
 
-    def __init__(self, vocab: int, dim: int, max_tokens: int, device: str = "cuda:0", seed: int = 0):
+    def __init__(self, vocab: int, dim: int, max_tokens: int, device: str = "cuda:0", seed: int = 0, keep_logits: bool = False):
         gen = torch.Generator(device=device).manual_seed(seed)
         self.dim, self.scale = dim, dim ** 0.5
         self.items = []
@@ -57,9 +58,11 @@ class Actor:
         self.grad = {k: new(torch.bfloat16) for k in ("normed", "block", "stream")}
         m = B.make_matrix
         normed, head = m(self.act["normed"]), m(self.head["param"])
-        self.ws_bytes = max(B.dc_head_logprob_workspace_bytes(normed, head, 5),
-                            B.dc_head_logprob_backward_workspace_bytes(normed, head, m(self.head["grad"])),
-                            B.dc_residual_norm_backward_workspace_bytes(normed),
+        self.logits = new(torch.bfloat16, vocab) if keep_logits else None
+        of_head = [B.dc_token_logprob_workspace_bytes(m(self.logits), 5)] if keep_logits else \
+            [B.dc_head_logprob_workspace_bytes(normed, head, 5),
+             B.dc_head_logprob_backward_workspace_bytes(normed, head, m(self.head["grad"]))]
+        self.ws_bytes = max(*of_head, B.dc_residual_norm_backward_workspace_bytes(normed),
                             B.dc_embedding_backward_workspace_bytes(normed, m(self.embed["grad"])))
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device)
         self.steps = 0
@@ -74,21 +77,40 @@ class Actor:
                            m(a["stream"]), m(a["normed"]), a["stat"])
         return a["normed"]
 
+    def logprob(self, hidden, temperature, *rest) -> None:
+        """The head's log-probabilities of rows of hidden states: what follows is dc_token_logprob's."""
+        m = B.make_matrix
+        if self.logits is None:
+            B.dc_head_logprob(m(hidden), m(self.head["param"]), temperature, *rest, self.ws, self.ws_bytes, self.status)
+        else:
+            logits = self.logits[:hidden.shape[0]]
+            torch.mm(hidden, self.head["param"].t(), out=logits)
+            B.dc_token_logprob(m(logits), temperature, *rest, self.ws, self.ws_bytes, self.status)
+
     def score(self, hidden, ids, mask, temperature: float):
         """log-probability and entropy of every next token whose mask byte is set (0 elsewhere), and what their gradient needs."""
         n = hidden.shape[0]
         logprob, entropy = torch.empty(n, device=hidden.device), torch.empty(n, device=hidden.device)
         stat = torch.empty(n, 2, device=hidden.device)
-        B.dc_head_logprob(B.make_matrix(hidden), B.make_matrix(self.head["param"]), temperature, ids[1:], mask[1:], 0, logprob, stat,
-                          entropy, None, None, self.ws, self.ws_bytes, self.status)
+        self.logprob(hidden, temperature, ids[1:], mask[1:], 0, logprob, stat, entropy, None, None)
         return logprob, entropy, stat
 
     def backward(self, hidden, ids, mask, temperature, stat, entropy, grad_logprob, grad_entropy, first: bool) -> None:
         """Gradients of all weights, added to those of the micro-batches before unless this is the first."""
         n, m, a = hidden.shape[0], B.make_matrix, self.a
         g = {k: v[:n] for k, v in self.grad.items()}
-        B.dc_head_logprob_backward(m(hidden), m(self.head["param"]), temperature, ids[1:], mask[1:], stat, entropy, grad_logprob,
-                                   grad_entropy, m(g["normed"]), not first, m(self.head["grad"]), self.ws, self.ws_bytes, self.status)
+        if self.logits is None:
+            B.dc_head_logprob_backward(m(hidden), m(self.head["param"]), temperature, ids[1:], mask[1:], stat, entropy, grad_logprob,
+                                       grad_entropy, m(g["normed"]), not first, m(self.head["grad"]), self.ws, self.ws_bytes,
+                                       self.status)
+        else:                                                                  # the logits' gradient takes their place
+            logits = self.logits[:n]
+            B.dc_token_logprob_backward(m(logits), temperature, ids[1:], mask[1:], stat, entropy, grad_logprob, grad_entropy,
+                                        m(logits), self.status)
+            torch.mm(logits, self.head["param"], out=g["normed"])
+            if first:
+                self.head["grad"].zero_()
+            self.head["grad"] += torch.mm(logits.t(), hidden)
         B.dc_residual_norm_backward(m(a["block"]), m(self.post["param"]), None, m(a["stream"]), m(self.pre["param"]), self.norm, a["stat"],
                                     None, m(g["normed"]), m(g["block"]), m(g["stream"]), not first, m(self.post["grad"]), None,
                                     m(self.pre["grad"]), self.ws, self.ws_bytes)
@@ -118,7 +140,7 @@ def micro_batches(d: runner.DeviceBatch, shard: int):
 
 
 def main(prompts: int = 16, epochs: int = 4, dim: int = 64, lr: float = 3e-3, clip: float = 0.2, entropy_coef: float = 1e-3,
-         temperature: float = 1.0, verbose: bool = True):
+         temperature: float = 1.0, verbose: bool = True, keep_logits: bool = False):
     vocab = 32000                                                              # workload 1's
     w = workloads.make_workload(1, prompts=prompts)
     d = runner.DeviceBatch(w)
@@ -126,7 +148,7 @@ def main(prompts: int = 16, epochs: int = 4, dim: int = 64, lr: float = 3e-3, cl
     spans = micro_batches(d, 0)
     ids, mask = d.dst_fields["token_id"], d.dst_fields["mask"]
     adv = d.dst_fields["adv_tok"].view(torch.float32)
-    actor = Actor(vocab, dim, max(b - a for a, b in spans))
+    actor = Actor(vocab, dim, max(b - a for a, b in spans), keep_logits=keep_logits)
     n_loss = max(1, sum(int(mask[a + 1:b].ne(0).sum()) for a, b in spans))
     old, history = {}, []
     for epoch in range(epochs):
@@ -154,11 +176,10 @@ def main(prompts: int = 16, epochs: int = 4, dim: int = 64, lr: float = 3e-3, cl
         # the serving form: the next token behind the last one, with its likeliest alternatives
         hidden = actor.hidden(ids[spans[-1][1] - 2:spans[-1][1]])
         top, top_lp = torch.empty(1, 5, dtype=torch.int32, device=hidden.device), torch.empty(1, 5, device=hidden.device)
-        B.dc_head_logprob(B.make_matrix(hidden), B.make_matrix(actor.head["param"]), temperature, None, None, 5, None, None, None, top,
-                          top_lp, actor.ws, actor.ws_bytes, actor.status)
+        actor.logprob(hidden, temperature, None, None, 5, None, None, None, top, top_lp)
         print("alternatives:", [(i, round(p, 4)) for i, p in zip(top[0].tolist(), top_lp[0].tolist())])
     return history
 
 
 if __name__ == "__main__":
-    main()
+    main(keep_logits="--keep-logits" in sys.argv[1:])

@@ -41,3 +41,39 @@ def test_actor_update_gradients():
         # a value on the way is rounded to 16 bits (2^-8 of it at most) no more than eight times: embedding, block, stream, its norm,
         # three gradients and their sum
         assert float((it["grad"].double() - ref).norm() / ref.norm()) < 8 * 2.0 ** -8
+
+
+def example():
+    spec = importlib.util.spec_from_file_location("actor_update", os.path.join(ROOT, "examples", "actor_update.py"))
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    return m
+
+
+@pytest.mark.gpu
+def test_actor_update_gradients_with_logits_kept():
+    """As without: a matrix of logits and one of their gradient are two roundings to 16 bits more than the eight of the test above."""
+    import torch
+    m = example()
+    vocab, dim, n = 700, 64, 201
+    actors = [m.Actor(vocab, dim, 400, keep_logits=k) for k in (False, True)]
+    g = torch.Generator(device="cuda").manual_seed(4)
+    for k in range(2):
+        ids = torch.randint(0, vocab, (n,), generator=g, device="cuda").to(torch.int32)
+        mask = (torch.rand(n, generator=g, device="cuda") < 0.7).to(torch.uint8)
+        a, b = torch.randn(n - 1, generator=g, device="cuda") * 0.3, torch.randn(n - 1, generator=g, device="cuda") * 0.1
+        for actor in actors:
+            hidden = actor.hidden(ids)
+            logprob, entropy, stat = actor.score(hidden, ids, mask, 0.9)
+            actor.backward(hidden, ids, mask, 0.9, stat, entropy, a, b, first=k == 0)
+    torch.cuda.synchronize()
+    for x, y in zip(*(actor.items for actor in actors)):
+        assert float((x["grad"] - y["grad"]).norm() / x["grad"].norm()) < (8 + 10) * 2.0 ** -8
+    assert all(int(actor.status) == 0 for actor in actors)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("keep_logits", [False, True])
+def test_actor_update_runs(keep_logits):
+    history = example().main(prompts=2, epochs=2, keep_logits=keep_logits)
+    assert len(history) == 2 and all(abs(x) < float("inf") for step in history for x in step)
