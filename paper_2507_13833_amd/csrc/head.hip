@@ -455,8 +455,12 @@ static hipError_t launch_few(const FewArgs& f, int32_t type, bool any, hipStream
                     constexpr int GROUPS = decltype(groups)::value;
                     head_few_kernel<W, NB, decltype(bytes)::value, decltype(stage)::value, GROUPS><<<(unsigned)std::min((f.vocab + 15) / 16, GROUPS), 256, 0, st>>>(f);
                 };
-                if (NB < 4 && f.dim * sizeof(W) % 512 == 0) launch_with<512, 32768, 256>(launch);
-                else launch_with<128, 16384, 512>(launch);
+                if constexpr (NB < 4)
+                    if (f.dim * sizeof(W) % 512 == 0) {
+                        launch_with<512, 32768, 256>(launch);
+                        return;
+                    }
+                launch_with<128, 16384, 512>(launch);
             }
         };
         if (f.n_rows <= 16) go(integral_constant<int, 1>{}, integral_constant<int, 1>{}, integral_constant<int, F32 ? 2 : 8>{});

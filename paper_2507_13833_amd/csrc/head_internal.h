@@ -4,8 +4,6 @@
 
 namespace dc {
 
-constexpr int64_t HEAD_MAX_ROWS = 1 << 22;
-
 struct HeadArgs {
     dc_matrix      hidden, weight;
     float          inv_t;           // 1 / temperature

@@ -28,9 +28,9 @@ HeadShape head_shape(const dc_matrix& hidden, const dc_matrix& weight, bool list
 enum Apart { F16S, BF16S };
 hipError_t launch_lay_rows(const dc_matrix& src, int64_t first, int64_t n, const int32_t* list, const int32_t* count, int32_t k_pad,
                            char* dst, int64_t plane, Apart apart, const int32_t* row_exp, const int32_t* all_exp, hipStream_t st);
-// out[i]: of the largest finite magnitude of row list[i] (or i), the power of two above it.
+// out[i]: of the largest finite magnitude of row list[i] (or i) of 32 bits, the power of two above it.
 hipError_t launch_row_exponents(const dc_matrix& src, int64_t n, const int32_t* list, const int32_t* count, int32_t* out, hipStream_t st);
-// *top, raised to the same of rows first .. first + n - 1.
+// *top, raised to the same of rows first .. first + n - 1, f32 or bf16 (f16 wants none).
 hipError_t launch_top_exponent(const dc_matrix& src, int64_t first, int64_t n, int32_t* top, hipStream_t st);
 // What raised exponents begin with.  exact: all but the first are 15 instead, which leaves numbers as they are (f16 wants no other).
 struct FirstExponents { int32_t* top; int32_t n; bool exact; };

@@ -100,8 +100,7 @@ hipError_t launch_first_exponents(const FirstExponents& x, hipStream_t st) {
 }
 
 // A wave per row.
-template <typename T>
-__global__ __launch_bounds__(256) void row_exponents_kernel(const T* x, int64_t stride, int64_t n, int32_t cols, const int32_t* list,
+__global__ __launch_bounds__(256) void row_exponents_kernel(const float* x, int64_t stride, int64_t n, int32_t cols, const int32_t* list,
                                                             const int32_t* count, int32_t* out) {
     const int64_t rows = count ? *count : n;
     for (int64_t r = blockIdx.x * 4LL + threadIdx.x / WAVE; r < rows; r += gridDim.x * 4LL) {
@@ -110,12 +109,9 @@ __global__ __launch_bounds__(256) void row_exponents_kernel(const T* x, int64_t 
     }
 }
 hipError_t launch_row_exponents(const dc_matrix& src, int64_t n, const int32_t* list, const int32_t* count, int32_t* out, hipStream_t st) {
-    return with_type(src.type, [&](auto el) {
-        using T = typename decltype(el)::type;
-        row_exponents_kernel<T><<<(unsigned)std::min<int64_t>((n + 3) / 4, 1 << 14), 256, 0, st>>>(static_cast<const T*>(src.d_data), src.row_stride, n,
-                                                                                                 (int32_t)src.n_cols, list, count, out);
-        return hipGetLastError();
-    });
+    row_exponents_kernel<<<(unsigned)std::min<int64_t>((n + 3) / 4, 1 << 14), 256, 0, st>>>(static_cast<const float*>(src.d_data), src.row_stride, n,
+                                                                                           (int32_t)src.n_cols, list, count, out);
+    return hipGetLastError();
 }
 
 template <typename T>
@@ -130,12 +126,13 @@ hipError_t launch_top_exponent(const dc_matrix& src, int64_t first, int64_t n, i
     const bool together = src.row_stride == src.n_cols;
     const int64_t all = n * src.n_cols, rows = together ? (all + 8191) / 8192 : n, stride = together ? 8192 : src.row_stride;
     const int32_t cols = together ? 8192 : (int32_t)src.n_cols, last = together ? (int32_t)(all - (rows - 1) * 8192) : cols;
-    return with_type(src.type, [&](auto el) {
-        using T = typename decltype(el)::type;
+    const auto launch = [&](auto el) {
+        using T = decltype(el);
         const T* from = static_cast<const T*>(src.d_data) + first * src.row_stride;
         top_exponent_kernel<T><<<(unsigned)std::min<int64_t>(TOP_BLOCKS, (rows + 3) / 4), 256, 0, st>>>(from, stride, rows, cols, last, top);
-        return hipGetLastError();
-    });
+    };
+    if (src.type == DC_F32) launch(float{}); else launch(__bf16{});
+    return hipGetLastError();
 }
 
 // Tiles of 64 x 64 through the LDS: read along the rows, written along the columns.  WIDE: rows on multiples of 16 bytes.  Bound by the

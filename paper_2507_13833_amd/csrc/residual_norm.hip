@@ -208,8 +208,10 @@ static hipError_t with_threads(int32_t dim, bool wide, F&& f) {
     if (dim <= 2048) return go(integral_constant<int, 256>{}, Eight{});
     if (dim <= 4096) return go(integral_constant<int, 512>{}, Eight{});
     if constexpr (GRAD)
-        if (wide) return f(integral_constant<int, 512>{}, integral_constant<int, 16>{}, std::true_type{});
-    return go(integral_constant<int, 1024>{}, Eight{});
+        return wide ? f(integral_constant<int, 512>{}, integral_constant<int, 16>{}, std::true_type{})
+                    : f(integral_constant<int, 1024>{}, Eight{}, std::false_type{});
+    else
+        return go(integral_constant<int, 1024>{}, Eight{});
 }
 static bool lies_wide(const NormStream& s, int32_t type) {
     return reinterpret_cast<uintptr_t>(s.p) % 16 == 0 && s.stride * (type == DC_F32 ? 4 : 2) % 16 == 0;
