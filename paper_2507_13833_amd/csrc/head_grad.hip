@@ -172,6 +172,7 @@ struct HeadHiddenArgs {             // slab[split][row][col] (+)= sum over this 
     Parts          parts;
     int32_t        steps, splits, col_tiles, row_tiles, dim;
     const int32_t* count;
+    const RowTerm* term;
     const int32_t* top;
     bool           add;
     float*         slab;
@@ -200,11 +201,12 @@ __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_hidden_kernel(
         b.base += from * (PK * 2LL);
         product<_Float16, Q>(acc, a, b, h.parts, max(steps, 0), lds);
     }
-    const int up = *h.top - 15;
     const int32_t col = tile * SIDE + place_a<Q>(), row = first + place_b<Q>();
 #pragma unroll
     for (int j = 0; j < Q; ++j)
-        if (row + j < n_rows)
+        if (row + j < n_rows) {
+            // (the slabs hold the gradient itself: a sum of pieces with the row's own power of two might leave the range)
+            const int up = *h.top - 15 - h.term[row + j].exponent;
 #pragma unroll
             for (int i = 0; i < Q; ++i)
                 if (col + along_a(i, 0) < h.pitch) {         // (a multiple of 4)
@@ -215,14 +217,14 @@ __global__ __launch_bounds__(P_THREADS, Q == 8 ? 1 : 2) void head_hidden_kernel(
                     if (h.add) v += *to;
                     *to = v;
                 }
+        }
 }
 
-// A row's hidden gradient: the slabs' sum, its own power of two undone, rounded once.  Rows that take no part: +0.  Bound by the slabs'
+// A row's hidden gradient: the slabs' sum, rounded once.  Rows that take no part: +0.  Bound by the slabs'
 // bytes, eight asked for at once (8192 x 1024 in 6 slabs: 5 us, one at a time 13).
 template <typename T>
 __global__ __launch_bounds__(256) void head_hidden_join_kernel(const float* slab, const int32_t* count, int32_t side, int32_t blocks, int64_t pitch,
-                                                               const int32_t* pos, const RowTerm* term, T* out, int64_t stride, int64_t rows,
-                                                               int32_t dim) {
+                                                               const int32_t* pos, T* out, int64_t stride, int64_t rows, int32_t dim) {
     const int64_t each = pitch / 4, row_tiles = (*count + side - 1) / side;
     const int32_t splits = live_share(blocks, (int32_t)row_tiles, HG_MOST_SPLITS);
     for (int64_t q = blockIdx.x * 256LL + threadIdx.x; q < rows * each; q += gridDim.x * 256LL) {
@@ -232,9 +234,6 @@ __global__ __launch_bounds__(256) void head_hidden_join_kernel(const float* slab
         if (at >= 0) {
 #pragma unroll 8
             for (int32_t s = 0; s < splits; ++s) sum += *reinterpret_cast<const f32x4*>(slab + (s * row_tiles * side + at) * pitch + c);
-            const int e = -term[at].exponent;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sum[i] = ldexpf(sum[i], e);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -431,6 +430,7 @@ hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
     hh.row_tiles = tiles_of(rows, w.cut_hidden.small);
     hh.dim = dim;
     hh.count = w.live.count;
+    hh.term = w.term;
     hh.slab = w.slab;
     hh.pitch = w.pitch;
     HeadWeightArgs hw = {};
@@ -505,7 +505,7 @@ hipError_t launch_head_grad(const HeadGradArgs& a, void* d_ws, hipStream_t st) {
         e = with_type(gh.type, [&](auto el) {
             using T = typename decltype(el)::type;
             head_hidden_join_kernel<T><<<(unsigned)std::min<int64_t>((rows * (w.pitch / 4) + 255) / 256, 1 << 14), 256, 0, st>>>(
-                w.slab, w.live.count, w.cut_hidden.small ? P_SIDE<4> : P_SIDE<8>, hh.row_tiles * hh.splits, w.pitch, w.live.pos, w.term, static_cast<T*>(gh.d_data), gh.row_stride, rows, dim);
+                w.slab, w.live.count, w.cut_hidden.small ? P_SIDE<4> : P_SIDE<8>, hh.row_tiles * hh.splits, w.pitch, w.live.pos, static_cast<T*>(gh.d_data), gh.row_stride, rows, dim);
             return hipGetLastError();
         });
     return e;

@@ -530,6 +530,19 @@ def test_head_backward_gradients_at_the_ends_of_the_range(env, dtype, size, temp
             check_grad(env, hk, wk, temperature, token, None, a=a, b=b, hidden=False, grad_w="f32")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("scale", [100, 114, 120, 124, -100, -114, -120])
+def test_head_backward_weights_at_the_ends_of_the_range(env, dtype, scale):
+    """Weights next to the largest and the smallest numbers, hidden states that take the logits back: gradients that 32 bits hold are
+    finite and as exact as any other."""
+    torch, B = env
+    for rows, vocab, dim in ((9, 700, 64), (300, 1000, 96)):
+        h, w, token, mask = draw(torch, rows, vocab, dim, dtype)
+        h, w = (torch.ldexp(x.float(), torch.tensor(float(e), device="cuda")).to(x.dtype) for x, e in ((h, -scale), (w, scale)))
+        check_grad(env, h, w, 1.0, token, mask)
+        check_grad(env, h, w, 0.7, token, None, grad_w="f32")
+
+
 def test_head_backward_parts_alone(env):
     """Either gradient without the other is the same bits."""
     torch, B = env
