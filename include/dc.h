@@ -455,11 +455,12 @@ dc_status dc_token_logprob_backward(const dc_matrix* logits, double temperature,
  * dc_token_logprob without a matrix of logits: x = hidden weight^T is made in pieces on the chip, where a row's sums are taken.
  *   x_v = sum_c hidden[r, c] * weight[v, c]  for the n_rows of hidden and the vocabulary = weight->n_rows; then as above.
  * hidden and weight have the same type and n_cols.  Products of 16-bit numbers are exact, sums are held in 32 bits.  Numbers of 32 bits
- * are taken with 24 bits up to 64 rows and with 22 above, there down to 2^-49 of their row's (for weight: the matrix's) largest
- * magnitude, and a product leaves off about 2^-21 of itself.  Arguments, masks, rows without a distribution, top
+ * are taken with 24 bits up to 64 rows (their bits below 2^-133 are left off) and with 22 above, there down to 2^-49 of their row's
+ * (for weight: the matrix's) largest magnitude, and a product leaves off about 2^-21 of itself.  Arguments, masks, rows without a distribution, top
  * alternatives (ties to the lowest token) and device errors are those of dc_token_logprob; hidden rows of masked tokens are not
  * looked at.  An infinity or a NaN in a row of hidden, or in weight, may make a row one without a distribution.
- * Up to 64 rows, and 256 at a time where n_top > 0, go through logits in the workspace.
+ * Up to 64 rows, and 256 at a time where n_top > 0, go through logits in the workspace; weights of 32 bits, or whose rows do not lie
+ * in whole steps of 128 bytes, are then laid out anew for every 256 rows.
  * d_ws: 256-byte aligned, dc_head_logprob_workspace_bytes(hidden, weight, n_top) bytes, which also serve every call of fewer rows
  * of these matrices, fewer alternatives or both; holds nothing the caller needs afterwards.
  * Host errors: INVALID_ARG, UNSUPPORTED_SIZE (vocabulary above DC_MAX_VOCAB, n_cols above DC_MAX_DIM, more than DC_MAX_HEAD_ROWS
@@ -511,7 +512,7 @@ typedef struct dc_norm_params {
  *   h = residual_scale * residual + block_scale * gate * u                 (gate NULL: 1)
  *   out = h * r2 * pre_weight,     r2 = 1 / sqrt(mean(h^2) + eps)          (pre_weight and out NULL: no norm)
  *   residual_out = h;  d_row_stat[2r], [2r+1] = r1, r2 (0 where there is no norm; d_row_stat may be NULL).
- * All in 32 bits, each output rounded once, out and r2 from h before it is rounded.
+ * All in 32 bits (a row whose sum of squares passes 2^128 has r = 0), each output rounded once, out and r2 from h before it is rounded.
  * block, residual, residual_out, out: n_rows x n_cols; out has block's type and residual_out residual's, the two types may differ.
  * post_weight, pre_weight: one row, any type.  gate: one row (any type) for all rows, or with
  * gate_rows n_rows of them in block's type.

@@ -42,7 +42,7 @@ __device__ __forceinline__ float less_reference(float m, float k, float base, fl
 // Bound by the matrix cores, and by the clock that the card holds under them (1.5 to 1.6 of 2.4 GHz): the next tile's first operands
 // come while a tile's sums are taken.  us a call, Q = 8: 8192 rows x 152064 x 2048 bf16 3660 to 3830 (1.33 to 1.39 PFLOP/s; a
 // library's product of these sizes alone 3580), 6144 of 8192 x 32000 x 1024 345 (1.17); 200 of 333 x 32003 x 515 f32 115,
-// of which it takes 52.
+// of which it takes 52.  With entropies and Q = 8 the compiler spills 6 registers, outside the products.
 // Also measured on the large one: 128 rows by 256 entries, two workgroups to a compute unit, 5500; eight waves of 128 by 64 with four
 // shorter stages 4650; sums that the compiler places 12 700 (copied from and to their registers).
 template <typename T, bool ENTROPY, int Q>
@@ -259,7 +259,8 @@ __device__ __forceinline__ void multiply_parts(const Raw8<typename FewTypes<W>::
 // rows.  Numbers of 32 bits lie in the LDS as they are and are taken apart on the way to the matrix cores.
 // 152064 x 2048 bf16 (622 MB), us, one row: 512 bytes of 64 entries and one workgroup to a compute unit 99 (6.3 TB/s), 256 of 64 and two
 // 106, 128 of 128 and two 120; without the loads' hint not to keep the weights 119 instead of 106.  64 rows, which come out of the L2
-// once per stage: 128 bytes of 128 entries and two workgroups 151, 256 bytes of 64 entries 159; a wave of its own that asks 170.
+// once per stage: 128 bytes of 128 entries and two workgroups 151, 256 bytes of 64 entries 159; a wave of its own that asks 170.  f32
+// (1.25 GB), the whole call: 4 rows 250 (5.0 TB/s), 32 rows 343, 64 rows 386.
 template <typename W, int NB, int BYTES, int W_STAGE, int GROUPS>
 __global__ __launch_bounds__(256) void head_few_kernel(const FewArgs f) {
     constexpr int TILE = W_STAGE / BYTES, MT = TILE / 64, LANES = BYTES / 16, AT_ONCE = 256 / LANES;     // rows of BYTES that a load of all threads fills
@@ -643,7 +644,8 @@ hipError_t launch_head(const HeadArgs& a, void* d_ws, hipStream_t st) {
         h.x = Operand{static_cast<const char*>(a.hidden.d_data), a.hidden.row_stride * 2, h.list};
     }
     for (int64_t r0 = 0; r0 < rows && e == hipSuccess; r0 += HEAD_TOP_ROWS) {
-        if (a.n_top > 0) {                       // so many rows at a time
+        // so many rows at a time (copied weights are copied for each: 4096 x 32003 x 515 f32 1295 us, without alternatives 427)
+        if (a.n_top > 0) {
             h.n_rows = (int32_t)std::min(HEAD_TOP_ROWS, rows - r0);
             h.row_tiles = (h.n_rows + side - 1) / side;
         }

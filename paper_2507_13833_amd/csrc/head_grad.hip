@@ -86,7 +86,7 @@ struct HeadPieceArgs {
 // A tile to a workgroup: neighbours that share its rows or its entries run beside each other on a chiplet, and nothing is kept from
 // one to the next.  Bound by the matrix cores for the product and then, while they wait, by the two writes.  8192 x 15360 x 2048 bf16
 // (0.52 TFLOP, and both of G's layouts, 0.5 GB): 424 to 510 us, of which the product takes about 400; 6144 x 16384 x 1024 with two
-// planes along the vocabulary (0.21 TFLOP, 0.6 GB) 350.
+// planes along the vocabulary (0.21 TFLOP, 0.6 GB) 350.  With one plane and Q = 8 the compiler spills 4 registers behind the product.
 // G along the vocabulary could be read for the weights' gradient from the one layout with transposing loads: not tried.
 // T: of the operands.  PLANES of G along the vocabulary (gt), ROW_PLANES along the rows.
 template <typename T, int PLANES, int ROW_PLANES, int Q>

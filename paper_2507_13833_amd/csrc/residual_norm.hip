@@ -161,7 +161,8 @@ __global__ __launch_bounds__(P < 256 ? 256 : P) void residual_norm_kernel(const 
     }
 }
 
-// Rows longer than a workgroup's registers: read again from the caches for each sum and for the stores.
+// Rows longer than a workgroup's registers: read again from the caches for each sum and for the stores, an element at a time, which is
+// what bounds it (16384 x 16384 bf16, 2.1 GB: 2766 us, 0.8 TB/s; the gradient, whose sums over rows go through memory, 4747, 0.7).
 template <typename A, typename R>
 __global__ __launch_bounds__(1024) void residual_norm_wide_kernel(const NormArgs a) {
     __shared__ float tmp[2][16];
@@ -198,7 +199,9 @@ __global__ __launch_bounds__(1024) void residual_norm_wide_kernel(const NormArgs
 }
 
 // Threads to a row, eight columns each; short rows share a workgroup.  The longest rows' gradient has half the threads and twice the
-// columns: 1024 threads have 128 registers each, of which it would spill 90 (32768 x 8192 bf16: 1641 us for 635).
+// columns: 1024 threads have 128 registers each, of which it would spill 90 (32768 x 8192 bf16: 1641 us for 639, 5.0 TB/s).  Where one of
+// the streams has 32 bits 36 to 65 registers are spilled all the same (stream in f32 1094 us, 4.4 TB/s; both 1512, 4.3), and where rows
+// are odd, on 1024 threads, 50 to 65 (32768 x 5001 bf16: 1383 us, 1.4 TB/s; stream in f32 3292, 0.9).
 template <bool GRAD, typename F>
 static hipError_t with_threads(int32_t dim, bool wide, F&& f) {
     using std::integral_constant;
