@@ -456,9 +456,9 @@ dc_status dc_token_logprob_backward(const dc_matrix* logits, double temperature,
  *   x_v = sum_c hidden[r, c] * weight[v, c]  for the n_rows of hidden and the vocabulary = weight->n_rows; then as above.
  * hidden and weight have the same type and n_cols.  Products of 16-bit numbers are exact, sums are held in 32 bits.  Numbers of 32 bits
  * are taken with 24 bits up to 64 rows (their bits below 2^-133 are left off) and with 22 above, there down to 2^-49 of their row's
- * (for weight: the matrix's) largest magnitude, and a product leaves off about 2^-21 of itself.  Arguments, masks, rows without a distribution, top
- * alternatives (ties to the lowest token) and device errors are those of dc_token_logprob; hidden rows of masked tokens are not
- * looked at.  An infinity or a NaN in a row of hidden, or in weight, may make a row one without a distribution.
+ * (for weight: the matrix's) largest magnitude, and a product leaves off about 2^-21 of itself.  Arguments, masks, rows without a
+ * distribution, top alternatives (ties to the lowest token) and device errors are those of dc_token_logprob; hidden rows of masked
+ * tokens are not looked at.  An infinity or a NaN in a row of hidden, or in weight, may make a row one without a distribution.
  * Up to 64 rows, and 256 at a time where n_top > 0, go through logits in the workspace; weights of 32 bits, or whose rows do not lie
  * in whole steps of 128 bytes, are then laid out anew for every 256 rows.
  * d_ws: 256-byte aligned, dc_head_logprob_workspace_bytes(hidden, weight, n_top) bytes, which also serve every call of fewer rows
